@@ -305,10 +305,122 @@ obf_status_t evict_only_static(const obf_params_t *params, const obf_cache_t *ca
                                void *stream);
 obf_status_t obf_static_scratch_status(void *stream, uint32_t *device_status);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators on a relayed cache: what a user does with the cache after the hand-off.  (The paper relays through its host
+ * framework's attention; these entry points are the library's own.)
+ *
+ * The next agent attends over the relayed cache and appends to it (obf_attend), several agents read one relay
+ * (obf_attend_shared), and a cache that has grown is brought down again by the attention mass that its positions have
+ * received since (obf_evict_by_mass).  One call is one layer of a batch of sequences: keys and values
+ * [batch, kv_heads, capacity, head_dim], queries [batch, q_heads, n_q, head_dim], q head = kv_head * G + g.  Lengths are
+ * read on the device, so a captured call can be replayed while the caches grow.
+ * ---------------------------------------------------------------------------------------------------------------- */
+
+/*
+ * Attention of n_q queries per sequence and query head over a cache.  Sequence b holds lens[b] keys (rows 0 .. lens[b] - 1)
+ * and q_lens[b] queries; query i is the token at position t = lens[b] - q_lens[b] + i and sees key j <= t when
+ *
+ *     window == 0   or   j > t - window   or   j < sinks
+ *
+ * (a sliding window, its own position included, and the first tokens, which stay visible).  With x_j = scale q . k_j over
+ * the visible keys:  out = sum_j softmax_j(x) v_j,  lse = ln sum_j exp(x_j),  and, when mass_out is given, for every KV head
+ * and key j < lens[b]
+ *
+ *     mass_out_j = decay * mass_in_j + sum over the head's G q_lens[b] query rows of softmax_j(x)          (Eq. 1, kept up
+ *                                                                                                    while decoding)
+ *
+ * A query that sees no key (t < 0, when q_lens[b] > lens[b]) has out = 0 and lse = -infinity.  What lies behind a
+ * length - queries and outputs from q_lens[b] on, keys, values and masses from lens[b] on - is not read into any result
+ * and left as it was; so are values that no query of the sequence sees, whatever they hold.  (A value that is not finite
+ * and that some query sees may also spoil queries of the same head that do not see it, as 0 * inf does in a matrix product.)
+ * lens outside [0, capacity] and q_lens outside [0, n_q] are clamped and set OBF_DEV_INTERNAL in the status word.
+ * obf_cache_t.lse_extra of a later compression is the lse of its observation queries over the keys outside the prompt.
+ *
+ * Numerics: products of the inputs accumulated in fp32, softmax in fp32; on the tensor cores the weights of a row, at most
+ * one, are rounded to bf16 before they multiply the values (their sum is not), out is rounded once.  The result does not
+ * depend on what else the batch holds except through the batch's sizes, and is the same in every run.
+ */
+typedef struct {
+    int32_t batch, kv_heads, q_heads;   /* q_heads % kv_heads == 0                                               */
+    int32_t head_dim;                   /* 64 or 128                                                             */
+    int32_t n_q;                        /* query rows per sequence and query head, 1 <= n_q <= OBF_MAX_T         */
+    int32_t capacity;                   /* rows of k and v per sequence and KV head, 1 <= capacity <= OBF_MAX_T  */
+    int32_t window;                     /* >= 0; 0: every key up to the query's own                              */
+    int32_t sinks;                      /* >= 0; has no effect without a window                                  */
+    int32_t dtype;                      /* obf_dtype_t of q, k, v, out                                           */
+    float scale;                        /* factor of the logits, > 0; 0: 1 / sqrt(head_dim)                      */
+    float decay;                        /* >= 0; factor of mass_in                                               */
+    uint32_t flags;                     /* 0 or OBF_FLAG_GENERIC_PATH (CUDA-core kernels where the tensor cores apply) */
+    const void *q, *k, *v;              /* device, 16-byte aligned                                               */
+    void *out;                          /* [batch, q_heads, n_q, head_dim], must not overlap the inputs          */
+    int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
+                                        /* elements from one sequence, head and row to the next; channels are
+                                           contiguous.  Multiples of 16 bytes, at least head_dim where there is more
+                                           than one of them, in any order ([batch, n_q, q_heads, head_dim] is one)   */
+    const int32_t *lens;                /* device [batch], or NULL: capacity                                     */
+    const int32_t *q_lens;              /* device [batch], or NULL: n_q                                          */
+    float *lse_out;                     /* device [batch, q_heads, n_q], or NULL                                 */
+    const float *mass_in;               /* device [batch, kv_heads, capacity], or NULL: zeros                    */
+    float *mass_out;                    /* the same, or NULL; may be mass_in.  Needs G * n_q <= 64, else
+                                           OBF_ERR_UNSUPPORTED (a prompt's masses are obf_compress's scores_out)  */
+} obf_attend_t;
+
+/* Keys and values that every sequence of a batch sees before its own. */
+typedef struct {
+    const void *k, *v;                  /* device, 16-byte aligned, [kv_heads, rows, head_dim]                   */
+    int64_t k_stride[2], v_stride[2];   /* elements from one head and row to the next, as above                  */
+    int32_t rows;                       /* 1 <= rows <= OBF_MAX_T                                                */
+} obf_prefix_t;
+
+/* Device scratch for obf_attend (prefix NULL) or obf_attend_shared.  Host-only; pointers are not inspected, but whether
+   mass_out is NULL counts. */
+obf_status_t obf_attend_workspace_bytes(const obf_attend_t *args, const obf_prefix_t *prefix, size_t *bytes);
+
+/*
+ * Enqueues the attention on `stream`; allocates nothing and never synchronises, can be captured into a graph.  `workspace`:
+ * at least obf_attend_workspace_bytes(), 256-byte aligned, private to the call until its work is done (two captured graphs
+ * that share one must not overlap); nothing in it is kept from call to call except the status word that
+ * obf_last_device_status reads.  Device-side waits are bounded, as in obf_compress.
+ */
+obf_status_t obf_attend(const obf_attend_t *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The same over a prefix that all sequences share and each sequence's own keys behind it: every query sees all rows of the
+ * prefix and the keys of its own sequence up to its own position (t counts own keys; with t < 0 the prefix alone).  The
+ * prefix is read once for the queries of all sequences together.  window, sinks, mass_in and mass_out must be 0 / NULL.
+ */
+obf_status_t obf_attend_shared(const obf_attend_t *args, const obf_prefix_t *prefix, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/*
+ * Eviction by accumulated mass: of the lens[b] rows of every (sequence, KV head) the first `sinks`, the last `recent` and,
+ * of the others, those of largest mass are kept, min(keep, lens[b]) in all; equal masses are resolved towards the lower
+ * position, a mass that is not a number counts as the lowest.  Kept rows are copied in ascending order to rows
+ * 0 .. min(keep, lens[b]) - 1 of the outputs; what lies behind them is left as it was.  With lens[b] <= keep every row is
+ * kept.  Inputs must not overlap outputs.  lens outside [0, capacity] are clamped.
+ */
+typedef struct {
+    int32_t batch, kv_heads, head_dim, capacity, dtype;   /* as above                                            */
+    int32_t keep;                       /* 1 <= keep <= OBF_MAX_T, keep >= sinks + recent                        */
+    int32_t sinks, recent;              /* >= 0                                                                  */
+    const void *k, *v;
+    void *k_out, *v_out;                /* [batch, kv_heads, >= keep, head_dim]                                  */
+    int64_t k_stride[3], v_stride[3], k_out_stride[3], v_out_stride[3];
+    const float *mass;                  /* device [batch, kv_heads, capacity]                                    */
+    const int32_t *lens;                /* device [batch], or NULL: capacity                                     */
+    int32_t *idx_out;                   /* device [batch, kv_heads, keep] kept positions, or NULL                */
+    float *mass_out;                    /* device [batch, kv_heads, mass_out_rows] masses of the kept rows, or NULL */
+    int32_t mass_out_rows;              /* >= keep (the capacity of the cache that the outputs go on as)         */
+    int32_t *lens_out;                  /* device [batch], or NULL: min(keep, lens[b])                           */
+} obf_evict_t;
+
+/* Enqueues the eviction on `stream`; needs no workspace, allocates nothing and never synchronises. */
+obf_status_t obf_evict_by_mass(const obf_evict_t *args, void *stream);
+
 /* Static, never NULL. */
 const char *obf_status_string(obf_status_t status);
 
-/* Number of kernels the last obf_compress / evict_only call of this thread enqueued. */
+/* Number of kernels the last call of this thread that enqueues work enqueued. */
 int32_t obf_last_launch_count(void);
 
 #ifdef __cplusplus

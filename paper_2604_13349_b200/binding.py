@@ -55,7 +55,8 @@ OBF_MAX_CACHES = 32
 EXPORTS = ("obf_workspace_bytes", "obf_compress", "evict_only", "obf_host_arena_bytes",
            "obf_compress_host", "obf_last_device_status", "obf_status_string",
            "obf_last_launch_count", "obf_compress_profiled", "obf_phase_name",
-           "evict_only_static", "obf_static_scratch_status")
+           "evict_only_static", "obf_static_scratch_status",
+           "obf_attend_workspace_bytes", "obf_attend", "obf_attend_shared", "obf_evict_by_mass")
 OBF_STATIC_SCRATCH_BYTES = 8 << 20
 OBF_MAX_PHASES = 16
 
@@ -85,6 +86,26 @@ class ObfCache(ctypes.Structure):
                 ("diag_out", ctypes.c_void_p), ("scores_out", ctypes.c_void_p), ("delta_out", ctypes.c_void_p),
                 ("lse_extra", ctypes.c_void_p), ("k_q8_out", ctypes.c_void_p), ("v_q8_out", ctypes.c_void_p),
                 ("k_scale_out", ctypes.c_void_p), ("v_scale_out", ctypes.c_void_p), ("assign_out", ctypes.c_void_p)]
+
+
+class ObfAttend(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "kv_heads", "q_heads", "head_dim", "n_q", "capacity", "window", "sinks", "dtype")] + [
+        ("scale", ctypes.c_float), ("decay", ctypes.c_float), ("flags", ctypes.c_uint32)] + [
+        (n, ctypes.c_void_p) for n in ("q", "k", "v", "out")] + [
+        (n, ctypes.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride", "out_stride")] + [
+        (n, ctypes.c_void_p) for n in ("lens", "q_lens", "lse_out", "mass_in", "mass_out")]
+
+
+class ObfPrefix(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2),
+                ("rows", ctypes.c_int32)]
+
+
+class ObfEvict(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "kv_heads", "head_dim", "capacity", "dtype", "keep", "sinks", "recent")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_out", "v_out")] + [
+        (n, ctypes.c_int64 * 3) for n in ("k_stride", "v_stride", "k_out_stride", "v_out_stride")] + [
+        (n, ctypes.c_void_p) for n in ("mass", "lens", "idx_out", "mass_out")] + [("mass_out_rows", ctypes.c_int32), ("lens_out", ctypes.c_void_p)]
 
 
 class ObfError(RuntimeError):
@@ -133,6 +154,13 @@ def load() -> ctypes.CDLL:
         lib.evict_only_static.restype = ctypes.c_int
         lib.obf_static_scratch_status.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_uint32)]
         lib.obf_static_scratch_status.restype = ctypes.c_int
+        pa, px = ctypes.POINTER(ObfAttend), ctypes.POINTER(ObfPrefix)
+        lib.obf_attend_workspace_bytes.argtypes = [pa, px, ctypes.POINTER(ctypes.c_size_t)]
+        lib.obf_attend.argtypes = [pa, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        lib.obf_attend_shared.argtypes = [pa, px, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        lib.obf_evict_by_mass.argtypes = [ctypes.POINTER(ObfEvict), ctypes.c_void_p]
+        for name in ("obf_attend_workspace_bytes", "obf_attend", "obf_attend_shared", "obf_evict_by_mass"):
+            getattr(lib, name).restype = ctypes.c_int
         lib.obf_last_launch_count.argtypes = []
         lib.obf_last_launch_count.restype = ctypes.c_int32
         _lib = lib
@@ -326,3 +354,166 @@ def compress_caches(params: ObfParams, caches_in: Sequence[Dict[str, object]], *
         o["workspace"] = workspace
         o["cache_structs"] = cs                 # for a repeated call on the same buffers (profiling)
     return outs
+
+
+# ---------------------------------------------------------------------------
+# operators on a relayed cache
+# ---------------------------------------------------------------------------
+_DTYPES = {torch.float32: OBF_F32, torch.bfloat16: OBF_BF16}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(t: torch.Tensor, shape, like: torch.Tensor, name: str):
+    """A tensor of rows of contiguous channels, as the C structs take it: checked shape, type and device, and its strides."""
+    _need(tuple(t.shape) == tuple(shape), "%s: shape %s expected, got %s" % (name, tuple(shape), tuple(t.shape)))
+    _need(t.dtype == like.dtype and t.device == like.device, "%s: %s on %s expected" % (name, like.dtype, like.device))
+    st = t.stride()
+    _need(st[-1] == 1, "%s: channels must be contiguous" % name)
+    return st[:-1]
+
+
+def _dense(t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.device == like.device and t.is_contiguous(),
+          "%s: contiguous %s %s on %s expected" % (name, tuple(shape), dtype, like.device))
+    return t.data_ptr()
+
+
+def _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags) -> ObfAttend:
+    _need(q.dim() == 4 and k.dim() == 4 and q.is_cuda, "q and k: device tensors [batch, heads, rows, head_dim] expected")
+    B, hq, n_q, d = q.shape
+    kv, cap = k.shape[1], k.shape[2]
+    _need(q.dtype in _DTYPES, "q: float32 or bfloat16 expected")
+    return ObfAttend(
+        B, kv, hq, d, n_q, cap, window, sinks, _DTYPES[q.dtype], scale, decay, flags, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+        _rows(q, (B, hq, n_q, d), q, "q"), _rows(k, (B, kv, cap, d), q, "k"), _rows(v, (B, kv, cap, d), q, "v"), _rows(out, (B, hq, n_q, d), q, "out"),
+        _dense(lens, (B,), torch.int32, q, "lens"), _dense(q_lens, (B,), torch.int32, q, "q_lens"),
+        _dense(lse_out, (B, hq, n_q), torch.float32, q, "lse_out"), _dense(mass_in, (B, kv, cap), torch.float32, q, "mass_in"),
+        _dense(mass_out, (B, kv, cap), torch.float32, q, "mass_out"))
+
+
+def _enqueue(name: str, device: torch.device, call, stream) -> None:
+    """call(stream handle) with the tensors' device current, on its current stream unless another is given."""
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            rc = call(_stream_handle(stream))
+    else:
+        rc = call(_stream_handle(stream))
+    if rc != OBF_OK:
+        raise ObfError(rc, name)
+
+
+def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, stream):
+    lib = load()
+    nb = ctypes.c_size_t(0)
+    px = ctypes.byref(prefix) if prefix is not None else None
+    rc = lib.obf_attend_workspace_bytes(ctypes.byref(args), px, ctypes.byref(nb))
+    if rc != OBF_OK:
+        raise ObfError(rc, name)
+    if workspace is None:
+        workspace = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+        if stream is not None:                   # the allocator gives the memory on once the given stream is done with it
+            workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream, device=q.device))
+    size = workspace.numel() * workspace.element_size()
+    if prefix is None:
+        _enqueue(name, q.device, lambda st: lib.obf_attend(ctypes.byref(args), workspace.data_ptr(), size, st), stream)
+    else:
+        _enqueue(name, q.device, lambda st: lib.obf_attend_shared(ctypes.byref(args), px, workspace.data_ptr(), size, st), stream)
+    got = {"out": out, "workspace": workspace}
+    if lse_out is not None:
+        got["lse"] = lse_out
+    if mass_out is not None:
+        got["mass"] = mass_out
+    return got
+
+
+def _attend_outputs(q, q_lens, out, lse_out, want_lse):
+    make = torch.empty if q_lens is None else torch.zeros        # what lies behind a sequence's queries is not written
+    if out is None:
+        out = make(q.shape, dtype=q.dtype, device=q.device)
+    if lse_out is None and want_lse:
+        lse_out = make(q.shape[:3], dtype=torch.float32, device=q.device)
+    return out, lse_out
+
+
+def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, lens: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None,
+           window: int = 0, sinks: int = 0, scale: float = 0.0, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
+           want_lse: bool = False, mass_in: Optional[torch.Tensor] = None, mass_out: Optional[torch.Tensor] = None, decay: float = 1.0,
+           flags: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Causal attention of ``q [batch, q_heads, n_q, d]`` over caches ``k, v [batch, kv_heads, capacity, d]`` with an optional sliding
+    window whose first ``sinks`` keys stay visible (``obf_attend`` in include/obf.h).
+
+    ``lens``, ``q_lens``: int32 device tensors ``[batch]``, the rows of a sequence's cache and its queries that count (None: all);
+    the queries are the last tokens of the cache.  Any strides with contiguous channels.  ``mass_out [batch, kv_heads, capacity]``
+    (fp32) receives ``decay * mass_in`` plus the attention mass of every key; it may be ``mass_in``.  ``workspace``: a uint8
+    device tensor of ``obf_attend_workspace_bytes``, else one is allocated; its status word is read with
+    ``obf_last_device_status``.  Returns ``out``, ``workspace`` and, where asked for, ``lse [batch, q_heads, n_q]`` (natural log)
+    and ``mass``.
+    """
+    out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse)
+    args = _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags)
+    return _attend_call("obf_attend", args, None, q, out, lse_out, mass_out, workspace, stream)
+
+
+def attend_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *,
+                  lens: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None, scale: float = 0.0,
+                  out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, want_lse: bool = False, flags: int = 0,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """The same for a batch whose sequences all see ``k_prefix, v_prefix [kv_heads, rows, d]`` before their own keys
+    (``obf_attend_shared``): the prefix is read once for all of them."""
+    out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse)
+    args = _attend_args(q, k, v, lens, q_lens, 0, 0, scale, out, lse_out, None, None, 1.0, flags)
+    _need(k_prefix.dim() == 3, "k_prefix: [kv_heads, rows, head_dim] expected")
+    rows = k_prefix.shape[1]
+    shape = (k.shape[1], rows, q.shape[3])
+    prefix = ObfPrefix(k_prefix.data_ptr(), v_prefix.data_ptr(), _rows(k_prefix, shape, q, "k_prefix"), _rows(v_prefix, shape, q, "v_prefix"), rows)
+    return _attend_call("obf_attend_shared", args, prefix, q, out, lse_out, None, workspace, stream)
+
+
+def obf_attend_workspace_bytes(args: ObfAttend, prefix: Optional[ObfPrefix] = None) -> int:
+    out = ctypes.c_size_t(0)
+    rc = load().obf_attend_workspace_bytes(ctypes.byref(args), ctypes.byref(prefix) if prefix is not None else None, ctypes.byref(out))
+    if rc != OBF_OK:
+        raise ObfError(rc, "obf_attend_workspace_bytes")
+    return int(out.value)
+
+
+def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: int, *, lens: Optional[torch.Tensor] = None, sinks: int = 0,
+                  recent: int = 0, k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+                  idx_out: Optional[torch.Tensor] = None, mass_out: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+                  stream=None) -> Dict[str, torch.Tensor]:
+    """Brings caches ``k, v [batch, kv_heads, capacity, d]`` down to ``keep`` rows per head by their accumulated masses
+    ``[batch, kv_heads, capacity]``: the first ``sinks``, the last ``recent`` and the heaviest others, in ascending order
+    (``obf_evict_by_mass`` in include/obf.h).  ``k_out, v_out`` and ``mass_out`` may have more rows than ``keep``: the cache goes on
+    there.  Returns ``K_out, V_out, idx, mass, lens``."""
+    _need(k.dim() == 4 and k.is_cuda and k.dtype in _DTYPES, "k: a float32 or bfloat16 device tensor [batch, kv_heads, capacity, head_dim] expected")
+    B, kv, cap, d = k.shape
+    dev = k.device
+    short = lens is not None or keep > cap                       # rows may stay behind a sequence's last one: not written
+    make = torch.zeros if short else torch.empty
+    if k_out is None:
+        k_out = make((B, kv, keep, d), dtype=k.dtype, device=dev)
+    if v_out is None:
+        v_out = make((B, kv, keep, d), dtype=k.dtype, device=dev)
+    if idx_out is None:
+        idx_out = make((B, kv, keep), dtype=torch.int32, device=dev)
+    if mass_out is None:
+        mass_out = make((B, kv, keep), dtype=torch.float32, device=dev)
+    if lens_out is None:
+        lens_out = torch.empty((B,), dtype=torch.int32, device=dev)
+    ko, vo, mo = k_out.shape[2], v_out.shape[2], mass_out.shape[2]
+    _need(min(ko, vo, mo) >= keep, "k_out, v_out and mass_out: at least `keep` rows expected")
+    args = ObfEvict(
+        B, kv, d, cap, _DTYPES[k.dtype], keep, sinks, recent, k.data_ptr(), v.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+        _rows(k, (B, kv, cap, d), k, "k"), _rows(v, (B, kv, cap, d), k, "v"), _rows(k_out, (B, kv, ko, d), k, "k_out"), _rows(v_out, (B, kv, vo, d), k, "v_out"),
+        _dense(mass, (B, kv, cap), torch.float32, k, "mass"), _dense(lens, (B,), torch.int32, k, "lens"),
+        _dense(idx_out, (B, kv, keep), torch.int32, k, "idx_out"), _dense(mass_out, (B, kv, mo), torch.float32, k, "mass_out"), mo,
+        _dense(lens_out, (B,), torch.int32, k, "lens_out"))
+    lib = load()
+    _enqueue("obf_evict_by_mass", dev, lambda st: lib.obf_evict_by_mass(ctypes.byref(args), st), stream)
+    return {"K_out": k_out, "V_out": v_out, "idx": idx_out, "mass": mass_out, "lens": lens_out}

@@ -8,13 +8,13 @@
 #include "common.cuh"
 #include "generic.cuh"
 #include "gram_tc.cuh"
+#include "host.cuh"
 #include "merge.cuh"
 #include "score_tc.cuh"
 #include "span_test.cuh"
 
 namespace obf {
 
-static thread_local int32_t g_last_launches = 0;
 static thread_local bool g_keep_status = false;
 
 // Optional per-launch timing (obf_compress_profiled): an event after every launch.
@@ -80,8 +80,6 @@ static inline void mark(cudaStream_t st, const char *name)
     }
 }
 
-static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
 struct Layout {
     size_t off_status, off_scores, off_keep, off_stats, off_sums, off_lscores, clear_end;
     size_t off_gram_d, off_gram_k, off_uvec, off_delta, off_hflag, off_svec, off_assign, off_rows_y, off_rows_m;
@@ -106,23 +104,6 @@ struct Layout {
     size_t sc_part_512;             // as many pairs as chunks of 512 keys would have (evict_only_static)
     size_t off_sc_part;
 };
-
-// Streaming multiprocessors of the current device (148 on a B200 when no device can be asked).
-static int sm_count()
-{
-    static int cached[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 148; }
-    if (cached[dev] == 0) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-            cudaGetLastError();
-            n = 148;
-        }
-        cached[dev] = n;
-    }
-    return cached[dev];
-}
 
 // The tensor-core kernels cover bf16 caches with at least one full 128-token tile.
 static bool tuned_path_applies(const obf_params_t *p, const obf_cache_t *caches, int32_t n)
@@ -287,73 +268,6 @@ static void make_layout(const obf_params_t *p, const obf_cache_t *caches, int32_
     L.off_assign = o;
     if (p->flags & OBF_FLAG_MERGE) o = align_up(o + tok * sizeof(int32_t), 256);
     L.total = o;
-}
-
-static bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
-#define OBF_CUDA_TRY(expr)                                                        \
-    do {                                                                          \
-        cudaError_t e_ = (expr);                                                  \
-        if (e_ != cudaSuccess) {                                                  \
-            std::fprintf(stderr, "obf: %s failed: %s\n", #expr, cudaGetErrorString(e_)); \
-            (void)cudaGetLastError();      /* reported here: not the next call's */       \
-            return OBF_ERR_CUDA;                                                  \
-        }                                                                         \
-    } while (0)
-
-// The limit belongs to the kernel, not to the launch, and host threads share it: a kernel whose use of shared memory varies
-// is given the most it can ever need, the same in every call, so that no call lowers it between another's limit and launch.
-template <typename K>
-static obf_status_t set_smem(K kernel, size_t bytes)
-{
-    OBF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    OBF_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared));
-    return OBF_OK;
-}
-
-#define OBF_TRY(expr)                        \
-    do {                                     \
-        const obf_status_t s_ = (expr);      \
-        if (s_ != OBF_OK) return s_;         \
-    } while (0)
-
-// Launch that may be set up while the stream's kernel before it still runs: every kernel launched so begins with
-// pdl_wait().  Between two kernels of a call that is about a microsecond less.
-template <typename... P, typename... A>
-static obf_status_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args)
-{
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    OBF_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
-    return OBF_OK;
-}
-
-// cuTensorMapEncodeTiled, looked up through the runtime so that the library does not link the driver.
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn tensor_map_encoder()
-{
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void *ptr = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) != cudaSuccess || !ptr) {
-            cudaGetLastError();
-            return nullptr;
-        }
-        fn = reinterpret_cast<EncodeTiledFn>(ptr);
-    }
-    return fn;
 }
 
 // Tensor map of a bf16 array [heads, rows, d] as [heads][64-column blocks][rows][64]: a box is GT_TILE rows of all

@@ -1,0 +1,253 @@
+// Host side of the operators on a relayed cache (include/obf.h): argument validation, workspace layout, kernel dispatch.
+#include <cmath>
+
+#include "attend_common.cuh"
+#include "attend_generic.cuh"
+#include "evict_mass.cuh"
+#include "host.cuh"
+
+namespace obf {
+
+static obf_status_t check_stride(const int64_t *st, const int64_t *n, int dims, int head_dim, int esize)
+{
+    for (int i = 0; i < dims; ++i) {
+        if (n[i] < 2) continue;                           // never stepped over
+        if (st[i] < head_dim || st[i] > (int64_t)1 << 40 || st[i] * esize % 16 != 0) return OBF_ERR_INVALID_ARG;
+    }
+    return OBF_OK;
+}
+
+static obf_status_t validate_attend(const obf_attend_t *a, const obf_prefix_t *x)
+{
+    if (!a) return OBF_ERR_INVALID_ARG;
+    if (a->batch < 1 || a->kv_heads < 1 || a->q_heads < 1 || a->q_heads % a->kv_heads != 0) return OBF_ERR_INVALID_ARG;
+    if (a->n_q < 1 || a->n_q > OBF_MAX_T || a->capacity < 1 || a->capacity > OBF_MAX_T) return OBF_ERR_INVALID_ARG;
+    if (a->window < 0 || a->sinks < 0) return OBF_ERR_INVALID_ARG;
+    if (!(a->scale >= 0.f) || !std::isfinite(a->scale) || !(a->decay >= 0.f) || !std::isfinite(a->decay)) return OBF_ERR_INVALID_ARG;
+    if (a->flags & ~(uint32_t)OBF_FLAG_GENERIC_PATH) return OBF_ERR_INVALID_ARG;
+    if (a->head_dim != 64 && a->head_dim != 128) return OBF_ERR_UNSUPPORTED;
+    if (a->dtype != OBF_F32 && a->dtype != OBF_BF16) return OBF_ERR_UNSUPPORTED;
+    if ((long long)a->batch * a->q_heads > (1 << 24) || (long long)a->batch * a->q_heads * a->n_q > 1ll << 30) return OBF_ERR_UNSUPPORTED;
+    if (x) {
+        if (x->rows < 1 || x->rows > OBF_MAX_T) return OBF_ERR_INVALID_ARG;
+        if (a->window || a->sinks || a->mass_in || a->mass_out) return OBF_ERR_INVALID_ARG;
+    }
+    if (a->mass_in && !a->mass_out) return OBF_ERR_INVALID_ARG;
+    if (a->mass_out && (long long)(a->q_heads / a->kv_heads) * a->n_q > 64) return OBF_ERR_UNSUPPORTED;
+    return OBF_OK;
+}
+
+static obf_status_t validate_attend_pointers(const obf_attend_t *a, const obf_prefix_t *x)
+{
+    const int es = a->dtype == OBF_F32 ? 4 : 2;
+    if (!a->q || !a->k || !a->v || !a->out || misaligned(a->q) || misaligned(a->k) || misaligned(a->v) || misaligned(a->out)) return OBF_ERR_INVALID_ARG;
+    const int64_t nq[3] = {a->batch, a->q_heads, a->n_q}, nk[3] = {a->batch, a->kv_heads, a->capacity};
+    OBF_TRY(check_stride(a->q_stride, nq, 3, a->head_dim, es));
+    OBF_TRY(check_stride(a->out_stride, nq, 3, a->head_dim, es));
+    OBF_TRY(check_stride(a->k_stride, nk, 3, a->head_dim, es));
+    OBF_TRY(check_stride(a->v_stride, nk, 3, a->head_dim, es));
+    if (x) {
+        if (!x->k || !x->v || misaligned(x->k) || misaligned(x->v)) return OBF_ERR_INVALID_ARG;
+        const int64_t np[2] = {a->kv_heads, x->rows};
+        OBF_TRY(check_stride(x->k_stride, np, 2, a->head_dim, es));
+        OBF_TRY(check_stride(x->v_stride, np, 2, a->head_dim, es));
+    }
+    const void *words[] = {a->lens, a->q_lens, a->lse_out, a->mass_in, a->mass_out};
+    for (const void *w : words)
+        if (reinterpret_cast<uintptr_t>(w) & 3u) return OBF_ERR_INVALID_ARG;
+    return OBF_OK;
+}
+
+struct AttendLayout {
+    int p_slots, own_slots;          // parts of the prefix and of a sequence's own keys
+    size_t off_part_o, off_part_lse, off_logits, total;
+};
+
+// Parts of `keys` keys for `tiles` tiles of query rows: about two blocks per multiprocessor, at least four key tiles each.
+static int parts_for(long long tiles, long long keys)
+{
+    long long s = (2 * 148 + tiles - 1) / tiles, most = (keys + 4 * AG_TILE - 1) / (4 * AG_TILE);
+    if (s > most) s = most;
+    if (s > 64) s = 64;
+    return (int)(s < 1 ? 1 : s);
+}
+
+// Keys that a query row can see at most.
+static long long most_keys(const obf_attend_t *a, int rows_of_queries)
+{
+    if (a->window == 0) return a->capacity;
+    const long long n = (long long)a->window + rows_of_queries + a->sinks;
+    return n < a->capacity ? n : a->capacity;
+}
+
+static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
+{
+    AttendLayout L;
+    const long long rows_seq = (long long)(a->q_heads / a->kv_heads) * a->n_q, heads = (long long)a->batch * a->kv_heads, rows = heads * rows_seq;
+    const long long own_tiles = heads * ((rows_seq + AG_TILE - 1) / AG_TILE);
+    L.own_slots = parts_for(own_tiles, most_keys(a, AG_TILE));
+    L.p_slots = 0;
+    if (x) L.p_slots = parts_for((long long)a->kv_heads * ((a->batch * rows_seq + AG_TILE - 1) / AG_TILE), x->rows);
+    const int slots = L.own_slots + L.p_slots;
+    size_t o = 256;
+    const bool join = slots > 1 || a->mass_out;
+    L.off_part_o = o;
+    if (join) o = align_up(o + (size_t)slots * rows * a->head_dim * sizeof(float), 256);
+    L.off_part_lse = o;
+    if (join) o = align_up(o + (size_t)slots * rows * sizeof(float), 256);
+    L.off_logits = o;
+    if (a->mass_out) o = align_up(o + (size_t)rows * a->capacity * sizeof(float), 256);
+    L.total = o;
+    return L;
+}
+
+// Raises a kernel's shared-memory limit the first time it is used on a device.
+template <typename K>
+static obf_status_t set_smem_once(K kernel, size_t bytes, bool (&done)[64])
+{
+    int dev = 0;
+    OBF_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev >= 0 && dev < 64 && done[dev]) return OBF_OK;
+    OBF_TRY(set_smem(kernel, bytes));
+    if (dev >= 0 && dev < 64) done[dev] = true;
+    return OBF_OK;
+}
+
+template <typename TIN, int D, bool PREFIX>
+static obf_status_t launch_attend_generic(const AttendDev &p, int first, cudaStream_t st)
+{
+    static bool done[64];
+    OBF_TRY(set_smem_once(k_attend_generic<TIN, D, PREFIX>, attend_generic_smem<D>(), done));
+    const long long rows = (PREFIX ? (long long)p.batch : 1) * p.n_q * p.G, tiles = (rows + AG_TILE - 1) / AG_TILE;
+    const long long blocks = (PREFIX ? p.p_slots : p.slots - p.p_slots) * tiles * p.kv_heads * (PREFIX ? 1 : p.batch);
+    if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
+    OBF_TRY(launch(k_attend_generic<TIN, D, PREFIX>, dim3((unsigned)blocks), AG_NT, attend_generic_smem<D>(), st, p, first));
+    ++g_last_launches;
+    return OBF_OK;
+}
+
+template <typename TIN, int D>
+static obf_status_t run_attend(const AttendDev &p, cudaStream_t st)
+{
+    if (p.prefix) OBF_TRY((launch_attend_generic<TIN, D, true>(p, 1, st)));
+    OBF_TRY((launch_attend_generic<TIN, D, false>(p, p.prefix == 0, st)));
+    if (p.slots > 1 || p.mass_out) {
+        long long blocks = p.rows_total;
+        if (p.mass_out) blocks += (long long)p.batch * p.kv_heads * ((p.capacity + AJ_KEYS - 1) / AJ_KEYS);
+        if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
+        OBF_TRY(launch(k_attend_join<TIN, D>, dim3((unsigned)blocks), AJ_NT, 0, st, p));
+        ++g_last_launches;
+    }
+    return OBF_OK;
+}
+
+static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *workspace, size_t bytes, void *stream)
+{
+    g_last_launches = 0;
+    OBF_TRY(validate_attend(a, x));
+    OBF_TRY(validate_attend_pointers(a, x));
+    const AttendLayout L = attend_layout(a, x);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < L.total) return OBF_ERR_WORKSPACE;
+    AttendDev p = {};
+    p.q = a->q; p.k = a->k; p.v = a->v; p.out = a->out;
+    for (int i = 0; i < 3; ++i) { p.qs[i] = a->q_stride[i]; p.ks[i] = a->k_stride[i]; p.vs[i] = a->v_stride[i]; p.os[i] = a->out_stride[i]; }
+    if (x) {
+        p.pk = x->k; p.pv = x->v; p.prefix = x->rows;
+        for (int i = 0; i < 2; ++i) { p.pks[i] = x->k_stride[i]; p.pvs[i] = x->v_stride[i]; }
+    }
+    p.lens = a->lens; p.q_lens = a->q_lens; p.lse_out = a->lse_out; p.mass_in = a->mass_in; p.mass_out = a->mass_out;
+    p.decay = a->decay;
+    p.c = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f;
+    p.batch = a->batch; p.kv_heads = a->kv_heads; p.G = a->q_heads / a->kv_heads; p.n_q = a->n_q; p.capacity = a->capacity;
+    // beyond any position a window or a number of first tokens changes nothing; clamped, positions minus windows cannot overflow
+    p.window = a->window < 2 * OBF_MAX_T ? a->window : 2 * OBF_MAX_T;
+    p.sinks = a->sinks < 2 * OBF_MAX_T ? a->sinks : 2 * OBF_MAX_T;
+    p.p_slots = L.p_slots; p.slots = L.p_slots + L.own_slots;
+    p.rows_total = (long long)p.batch * p.kv_heads * p.n_q * p.G;
+    char *ws = static_cast<char *>(workspace);
+    p.status = reinterpret_cast<uint32_t *>(ws);
+    p.part_o = reinterpret_cast<float *>(ws + L.off_part_o);
+    p.part_lse = reinterpret_cast<float *>(ws + L.off_part_lse);
+    p.logits = reinterpret_cast<float *>(ws + L.off_logits);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a->dtype == OBF_F32) return a->head_dim == 64 ? run_attend<float, 64>(p, st) : run_attend<float, 128>(p, st);
+    return a->head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, st) : run_attend<__nv_bfloat16, 128>(p, st);
+}
+
+template <int ROW_BYTES>
+static obf_status_t launch_evict(const EvictDev &p, cudaStream_t st)
+{
+    static bool done[64];
+    OBF_TRY(set_smem_once(k_evict_mass<ROW_BYTES>, evict_smem(EM_CACHE), done));
+    OBF_TRY(launch(k_evict_mass<ROW_BYTES>, dim3((unsigned)(p.batch * p.kv_heads * p.parts)), EM_NT, evict_smem(p.capacity), st, p));
+    ++g_last_launches;
+    return OBF_OK;
+}
+
+}  // namespace obf
+
+using namespace obf;
+
+extern "C" {
+
+obf_status_t obf_attend_workspace_bytes(const obf_attend_t *args, const obf_prefix_t *prefix, size_t *bytes)
+{
+    if (!bytes) return OBF_ERR_INVALID_ARG;
+    OBF_TRY(validate_attend(args, prefix));
+    *bytes = attend_layout(args, prefix).total;
+    return OBF_OK;
+}
+
+obf_status_t obf_attend(const obf_attend_t *args, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return attend(args, nullptr, workspace, workspace_bytes, stream);
+}
+
+obf_status_t obf_attend_shared(const obf_attend_t *args, const obf_prefix_t *prefix, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!prefix) return OBF_ERR_INVALID_ARG;
+    return attend(args, prefix, workspace, workspace_bytes, stream);
+}
+
+obf_status_t obf_evict_by_mass(const obf_evict_t *a, void *stream)
+{
+    g_last_launches = 0;
+    if (!a) return OBF_ERR_INVALID_ARG;
+    if (a->batch < 1 || a->kv_heads < 1 || a->capacity < 1 || a->capacity > OBF_MAX_T) return OBF_ERR_INVALID_ARG;
+    if (a->keep < 1 || a->keep > OBF_MAX_T || a->sinks < 0 || a->recent < 0 || (long long)a->sinks + a->recent > a->keep) return OBF_ERR_INVALID_ARG;
+    if (a->head_dim != 64 && a->head_dim != 128) return OBF_ERR_UNSUPPORTED;
+    if (a->dtype != OBF_F32 && a->dtype != OBF_BF16) return OBF_ERR_UNSUPPORTED;
+    const long long heads = (long long)a->batch * a->kv_heads;
+    if (heads > 1 << 24) return OBF_ERR_UNSUPPORTED;
+    if (!a->k || !a->v || !a->k_out || !a->v_out || !a->mass || misaligned(a->k) || misaligned(a->v) || misaligned(a->k_out) || misaligned(a->v_out))
+        return OBF_ERR_INVALID_ARG;
+    const void *words[] = {a->mass, a->lens, a->idx_out, a->mass_out, a->lens_out};
+    for (const void *w : words)
+        if (reinterpret_cast<uintptr_t>(w) & 3u) return OBF_ERR_INVALID_ARG;
+    if (a->mass_out && a->mass_out_rows < a->keep) return OBF_ERR_INVALID_ARG;
+    const int es = a->dtype == OBF_F32 ? 4 : 2;
+    const int64_t ni[3] = {a->batch, a->kv_heads, a->capacity}, no[3] = {a->batch, a->kv_heads, a->keep};
+    OBF_TRY(check_stride(a->k_stride, ni, 3, a->head_dim, es));
+    OBF_TRY(check_stride(a->v_stride, ni, 3, a->head_dim, es));
+    OBF_TRY(check_stride(a->k_out_stride, no, 3, a->head_dim, es));
+    OBF_TRY(check_stride(a->v_out_stride, no, 3, a->head_dim, es));
+    EvictDev p = {};
+    p.k = a->k; p.v = a->v; p.k_out = a->k_out; p.v_out = a->v_out;
+    for (int i = 0; i < 3; ++i) { p.ks[i] = a->k_stride[i] * es; p.vs[i] = a->v_stride[i] * es; p.kos[i] = a->k_out_stride[i] * es; p.vos[i] = a->v_out_stride[i] * es; }
+    p.mass = a->mass; p.lens = a->lens; p.idx_out = a->idx_out; p.mass_out = a->mass_out; p.lens_out = a->lens_out;
+    p.batch = a->batch; p.kv_heads = a->kv_heads; p.capacity = a->capacity; p.keep = a->keep; p.sinks = a->sinks; p.recent = a->recent;
+    p.mass_out_rows = a->mass_out_rows;
+    // about four blocks per multiprocessor, at least 64 rows each
+    const int kept = a->keep < a->capacity ? a->keep : a->capacity;
+    long long parts = (4 * 148 + heads - 1) / heads;
+    if (parts > (kept + 63) / 64) parts = (kept + 63) / 64;
+    p.parts = (int)parts;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    switch (a->head_dim * es) {
+    case 128: return launch_evict<128>(p, st);
+    case 256: return launch_evict<256>(p, st);
+    default: return launch_evict<512>(p, st);
+    }
+}
+
+}  // extern "C"

@@ -1,0 +1,310 @@
+"""Operators on a relayed cache: attention with a window and sinks, over a shared prefix, masses, eviction by mass."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2604_13349_b200 as P
+from paper_2604_13349_b200 import binding, build
+from tests import _attend_ref as ref
+
+GENERIC = binding.OBF_FLAG_GENERIC_PATH
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+# ---- refusals: decided on the host, nothing reaches a device ------------------------------------------------------
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return binding.load()
+
+
+def _args(**kw):
+    d = dict(batch=2, kv_heads=2, q_heads=8, head_dim=64, n_q=3, capacity=100, window=0, sinks=0, dtype=P.OBF_BF16, scale=0.0, decay=1.0, flags=0,
+             q=0x1000, k=0x1000, v=0x1000, out=0x1000)
+    d.update(kw)
+    a = P.ObfAttend(**{n: x for n, x in d.items() if not n.endswith("stride")})
+    D = a.head_dim
+    strides = dict(q_stride=(a.q_heads * a.n_q * D, a.n_q * D, D), out_stride=(a.q_heads * a.n_q * D, a.n_q * D, D),
+                   k_stride=(a.kv_heads * a.capacity * D, a.capacity * D, D), v_stride=(a.kv_heads * a.capacity * D, a.capacity * D, D))
+    strides.update({n: x for n, x in d.items() if n.endswith("stride")})
+    for n, x in strides.items():
+        setattr(a, n, (ctypes.c_int64 * 3)(*x))
+    return a
+
+
+def _prefix(rows=50, D=64, k=0x1000, **kw):
+    x = P.ObfPrefix(k, 0x1000, (ctypes.c_int64 * 2)(rows * D, D), (ctypes.c_int64 * 2)(rows * D, D), rows)
+    for n, y in kw.items():
+        setattr(x, n, y)
+    return x
+
+
+INVALID, UNSUPPORTED, WORKSPACE = binding.OBF_ERR_INVALID_ARG, binding.OBF_ERR_UNSUPPORTED, binding.OBF_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=0), INVALID), (dict(kv_heads=0), INVALID), (dict(q_heads=7), INVALID), (dict(q_heads=0), INVALID), (dict(n_q=0), INVALID),
+    (dict(n_q=(1 << 20) + 1), INVALID), (dict(capacity=0), INVALID), (dict(capacity=(1 << 20) + 1), INVALID), (dict(window=-1), INVALID),
+    (dict(sinks=-1), INVALID), (dict(scale=-0.5), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID),
+    (dict(decay=-1.0), INVALID), (dict(decay=math.nan), INVALID), (dict(flags=2), INVALID), (dict(head_dim=96), UNSUPPORTED),
+    (dict(dtype=5), UNSUPPORTED), (dict(mass_in=0x1000), INVALID), (dict(mass_out=0x1000, n_q=17), UNSUPPORTED),
+    (dict(batch=1 << 20, n_q=1 << 10), UNSUPPORTED),
+])
+def test_attend_refuses_bad_shapes(lib, kw, code):
+    with pytest.raises(P.ObfError) as e:
+        P.obf_attend_workspace_bytes(_args(**kw))
+    assert e.value.code == code
+    assert lib.obf_attend(ctypes.byref(_args(**kw)), 0x100, 1 << 50, None) == code
+    assert lib.obf_last_launch_count() == 0
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=0), dict(k=0), dict(v=0), dict(out=0), dict(q=0x1008), dict(k=0x1002), dict(v=0x1004), dict(out=0x1008), dict(lens=0x1002), dict(q_lens=0x1001),
+    dict(lse_out=0x1002), dict(mass_out=0x1002), dict(q_stride=(1536, 192, 63)), dict(k_stride=(12800, 6400, 68)), dict(v_stride=(12800, -6400, 64)),
+    dict(out_stride=(1536, 0, 64)), dict(k_stride=(1 << 41, 6400, 64)),
+])
+def test_attend_refuses_bad_pointers_and_strides(lib, kw):
+    assert lib.obf_attend(ctypes.byref(_args(**kw)), 0x100, 1 << 50, None) == INVALID
+    assert lib.obf_last_launch_count() == 0
+
+
+def test_a_stride_that_is_never_stepped_over_may_be_anything():
+    a = _args(batch=1, n_q=1, q_stride=(0, 64, 3), out_stride=(5, 64, 0))
+    need = P.obf_attend_workspace_bytes(a)
+    assert binding.load().obf_attend(ctypes.byref(a), 0x100, need - 1, None) == WORKSPACE        # past the checks of strides
+
+
+def test_attend_refuses_a_small_or_misaligned_workspace(lib):
+    a = _args()
+    need = P.obf_attend_workspace_bytes(a)
+    assert need >= 256 and need % 256 == 0
+    for ws, n in ((None, need), (0x110, need), (0x100, need - 1)):
+        assert lib.obf_attend(ctypes.byref(a), ws, n, None) == WORKSPACE
+    assert P.obf_attend_workspace_bytes(_args(mass_out=0x1000)) > need
+    x = _prefix()
+    need = P.obf_attend_workspace_bytes(a, x)
+    assert lib.obf_attend_shared(ctypes.byref(a), ctypes.byref(x), 0x100, need - 1, None) == WORKSPACE
+
+
+@pytest.mark.parametrize("kw,px", [
+    (dict(window=5), {}), (dict(sinks=1), {}), (dict(mass_out=0x1000), {}), (dict(), dict(rows=0)), (dict(), dict(rows=(1 << 20) + 1)),
+    (dict(), dict(k=0)), (dict(), dict(v=0x1008)), (dict(), dict(k_stride=(ctypes.c_int64 * 2)(3200, 60))),
+])
+def test_attend_shared_refuses(lib, kw, px):
+    rows = px.pop("rows", 50)
+    a, x = _args(**kw), _prefix(**px)
+    x.rows = rows
+    assert lib.obf_attend_shared(ctypes.byref(a), ctypes.byref(x), 0x100, 1 << 50, None) == INVALID
+    assert lib.obf_attend_shared(ctypes.byref(_args()), None, 0x100, 1 << 50, None) == INVALID
+
+
+def _evict_args(**kw):
+    d = dict(batch=2, kv_heads=2, head_dim=64, capacity=100, dtype=P.OBF_BF16, keep=10, sinks=2, recent=3, k=0x1000, v=0x1000, k_out=0x1000, v_out=0x1000,
+             mass=0x1000, mass_out_rows=10)
+    strides = dict(k_stride=(12800, 6400, 64), v_stride=(12800, 6400, 64), k_out_stride=(1280, 640, 64), v_out_stride=(1280, 640, 64))
+    for n, x in kw.items():
+        (strides if n in strides else d)[n] = x
+    a = P.ObfEvict(**d)
+    for n, x in strides.items():
+        setattr(a, n, (ctypes.c_int64 * 3)(*x))
+    return a
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=0), INVALID), (dict(kv_heads=0), INVALID), (dict(capacity=0), INVALID), (dict(keep=0), INVALID), (dict(keep=4), INVALID),
+    (dict(sinks=-1), INVALID), (dict(recent=-1), INVALID), (dict(sinks=(1 << 31) - 1, recent=(1 << 31) - 1), INVALID), (dict(head_dim=80), UNSUPPORTED),
+    (dict(dtype=3), UNSUPPORTED), (dict(k=0), INVALID), (dict(mass=0), INVALID), (dict(v_out=0x1008), INVALID), (dict(lens=0x1001), INVALID),
+    (dict(idx_out=0x1002), INVALID), (dict(mass_out=0x1000, mass_out_rows=9), INVALID), (dict(k_stride=(12800, 6400, 65)), INVALID),
+    (dict(v_out_stride=(1280, 0, 64)), INVALID), (dict(batch=1 << 20, kv_heads=32), UNSUPPORTED),
+])
+def test_evict_by_mass_refuses(lib, kw, code):
+    assert lib.obf_evict_by_mass(ctypes.byref(_evict_args(**kw)), None) == code
+    assert lib.obf_last_launch_count() == 0
+    assert lib.obf_evict_by_mass(None, None) == INVALID
+
+
+def test_struct_sizes_match_the_header():
+    assert (ctypes.sizeof(binding.ObfAttend), ctypes.sizeof(binding.ObfPrefix), ctypes.sizeof(binding.ObfEvict)) == (216, 56, 208)
+
+
+def test_python_wrappers_refuse_host_tensors():
+    with pytest.raises(ValueError):
+        P.attend(torch.zeros(1, 4, 1, 64), torch.zeros(1, 2, 8, 64), torch.zeros(1, 2, 8, 64))
+    with pytest.raises(ValueError):
+        P.evict_by_mass(torch.zeros(1, 2, 8, 64), torch.zeros(1, 2, 8, 64), torch.zeros(1, 2, 8), 4)
+
+
+# ---- on the device --------------------------------------------------------------------------------------------------
+SENTINEL = -77.0
+
+
+def _data(gen, B, kv, G, d, n_q, cap, dtype):
+    q = torch.randn(B, kv * G, n_q, d, generator=gen).to(dtype)
+    k = torch.randn(B, kv, cap, d, generator=gen).to(dtype)
+    v = (torch.randn(B, kv, cap, d, generator=gen) + 0.5).to(dtype)
+    return q, k, v
+
+
+def _check(got, want, tol, what):
+    got = got.double().cpu()
+    assert torch.equal(torch.isinf(got), torch.isinf(want)), what
+    fine = ~torch.isinf(want)
+    assert torch.equal(got[~fine], want[~fine]), what
+    off = torch.where(fine, got - want, 0.0).abs()
+    bad = ~(off <= tol)
+    assert not bad.any(), "%s: %d values off, worst %.3g against %.3g" % (what, int(bad.sum()), float(off[bad].max()), float(tol[bad][off[bad].argmax()]))
+
+
+def _spoil_unseen(k, v, lens, q_lens, window, sinks):
+    """NaN and infinities wherever no query of the sequence looks."""
+    cap = k.shape[2]
+    for b, (n, ql) in enumerate(zip(lens, q_lens)):
+        j = torch.arange(cap)
+        seen = torch.zeros(cap, dtype=torch.bool)
+        for i in range(ql):
+            t = n - ql + i
+            seen |= (j <= t) & (j < n) & ((j > t - window) | (j < sinks) if window else torch.ones(cap, dtype=torch.bool))
+        k[b, :, ~seen] = math.nan
+        v[b, :, ~seen] = math.inf
+        v[b, :, ~seen, 1] = math.nan
+
+
+def _attend_case(B, kv, G, d, n_q, cap, lens, q_lens, dtype, window=0, sinks=0, scale=0.0, mass=False, decay=1.0, prefix_rows=0, flags=0, seed=0,
+                 token_major=False):
+    gen = torch.Generator().manual_seed(seed)
+    q, k, v = _data(gen, B, kv, G, d, n_q, cap, dtype)
+    px = None
+    if prefix_rows:
+        px = (torch.randn(kv, prefix_rows, d, generator=gen).to(dtype), torch.randn(kv, prefix_rows, d, generator=gen).to(dtype))
+    mass_in = torch.rand(B, kv, cap, generator=gen) if mass else None
+    want = ref.attend(q, k, v, lens, q_lens, window, sinks, scale, px, mass_in, decay, mass)
+    _spoil_unseen(k, v, lens, q_lens, window, sinks)
+    dev = lambda x: x.cuda()                                                       # noqa: E731
+    for b in range(B):
+        q[b, :, q_lens[b]:] = math.nan
+    if token_major:
+        qd = dev(q.transpose(1, 2).contiguous()).transpose(1, 2)
+        out = torch.full((B, n_q, kv * G, d), SENTINEL, dtype=dtype, device="cuda").transpose(1, 2)
+    else:
+        qd, out = dev(q), torch.full((B, kv * G, n_q, d), SENTINEL, dtype=dtype, device="cuda")
+    lse = torch.full((B, kv * G, n_q), SENTINEL, device="cuda")
+    ln, ql = torch.tensor(lens, dtype=torch.int32, device="cuda"), torch.tensor(q_lens, dtype=torch.int32, device="cuda")
+    if prefix_rows:
+        r = P.attend_shared(qd, dev(px[0]), dev(px[1]), dev(k), dev(v), lens=ln, q_lens=ql, scale=scale, out=out, lse_out=lse, flags=flags)
+    else:
+        m_out = torch.full((B, kv, cap), SENTINEL, device="cuda") if mass else None
+        r = P.attend(qd, dev(k), dev(v), lens=ln, q_lens=ql, window=window, sinks=sinks, scale=scale, out=out, lse_out=lse,
+                     mass_in=dev(mass_in) if mass else None, mass_out=m_out, decay=decay, flags=flags)
+    assert P.obf_last_device_status(r["workspace"]) == 0
+    for b in range(B):
+        assert (out[b, :, q_lens[b]:] == SENTINEL).all() and (lse[b, :, q_lens[b]:] == SENTINEL).all(), "written behind the queries"
+        out[b, :, q_lens[b]:] = 0
+        lse[b, :, q_lens[b]:] = 0
+        if mass:
+            assert (m_out[b, :, lens[b]:] == SENTINEL).all(), "masses written behind the keys"
+            m_out[b, :, lens[b]:] = 0
+    _check(out, want[0], want[1], "out")
+    _check(lse, want[2], want[3], "lse")
+    if mass:
+        _check(m_out, want[4], want[5], "mass")
+
+
+PATHS = [pytest.param(BF16, 0, id="bf16"), pytest.param(BF16, GENERIC, id="bf16-generic"), pytest.param(F32, 0, id="f32")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,flags", PATHS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n_q,cap,lens,window,sinks", [
+    (1, 1, 1, [1, 0], 0, 0),                  # one key, and none
+    (4, 1, 64, [64, 63], 0, 0),
+    (4, 1, 700, [700, 513], 0, 0),
+    (4, 1, 700, [700, 3], 100, 4),            # decoding with a window; a sequence shorter than its sinks
+    (4, 1, 300, [300, 129], 1, 0),            # the query's own key alone
+    (3, 1, 1300, [1300, 1025], 1000, 77),
+    (8, 2, 257, [257, 255], 50, 51),
+    (7, 5, 400, [399, 5], 16, 1),
+    (16, 1, 130, [130, 17], 0, 0),
+    (40, 1, 130, [130, 17], 90, 2),           # more heads in a group than a tile of 16 rows holds
+])
+def test_attend_few_queries(dtype, flags, d, G, n_q, cap, lens, window, sinks):
+    q_lens = [min(n_q, n) for n in lens]
+    _attend_case(2, 2, G, d, n_q, cap, lens, q_lens, dtype, window, sinks, flags=flags, mass=n_q * G <= 64, decay=0.75, seed=cap)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,flags", PATHS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n_q,cap,lens,q_lens,window,sinks", [
+    (1, 300, 300, [300, 257], [300, 257], 0, 0),              # whole prompts, ragged
+    (4, 200, 200, [200, 1], [200, 1], 0, 0),
+    (2, 513, 513, [513, 129], [513, 129], 128, 4),            # window of a tile
+    (1, 400, 400, [400, 399], [400, 399], 127, 130),          # more sinks than the window
+    (3, 150, 400, [400, 151], [150, 149], 33, 2),             # a chunk of queries at the end of a longer cache; a group that divides no tile
+    (5, 64, 1500, [1500, 700], [64, 3], 0, 0),                # few rows over many keys
+    (4, 70, 64, [64, 0], [70, 5], 20, 3),                     # more queries than keys: rows that see nothing
+    (8, 40, 300, [300, 40], [40, 0], 7, 0),                   # a sequence without queries
+    (130, 2, 90, [90, 61], [2, 1], 0, 0),                     # a group larger than a tile of rows
+    (1, 129, 385, [385, 384], [129, 128], 256, 17),
+])
+def test_attend_many_queries(dtype, flags, d, G, n_q, cap, lens, q_lens, window, sinks):
+    _attend_case(2, 1 if G > 64 else 2, G, d, n_q, cap, lens, q_lens, dtype, window, sinks, flags=flags, token_major=cap % 2 == 0, seed=cap)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,flags", PATHS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,G,n_q,cap,lens,q_lens,rows", [
+    (1, 4, 1, 8, [8], [1], 1),
+    (3, 4, 1, 40, [40, 1, 17], [1, 1, 1], 129),
+    (5, 2, 1, 70, [70, 0, 64, 65, 1], [1, 1, 1, 0, 1], 1012),    # a sequence without own keys, one without a query
+    (33, 4, 1, 16, [16 - i % 16 for i in range(33)], [1] * 33, 300),
+    (3, 3, 40, 90, [90, 40, 41], [40, 40, 17], 257),
+    (2, 1, 200, 300, [300, 250], [200, 199], 64),
+    (4, 8, 9, 20, [20, 9, 10, 3], [9, 9, 2, 9], 700),            # more queries than own keys
+    (300, 1, 1, 3, [1 + i % 3 for i in range(300)], [1] * 300, 130),
+])
+def test_attend_shared(dtype, flags, d, B, G, n_q, cap, lens, q_lens, rows):
+    _attend_case(B, 2, G, d, n_q, cap, lens, q_lens, dtype, prefix_rows=rows, flags=flags, token_major=B % 2 == 0, seed=rows)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,flags", PATHS)
+def test_attend_scale_and_large_logits(dtype, flags):
+    _attend_case(1, 2, 4, 64, 1, 500, [500], [1], dtype, scale=3.0, flags=flags)           # logits of hundreds: one weight near one
+    _attend_case(1, 2, 4, 128, 90, 200, [200], [90], dtype, scale=2.5, flags=flags, window=50, sinks=3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dtype", [(64, BF16), (128, BF16), (128, F32)])
+@pytest.mark.parametrize("cap,lens,keep,sinks,recent", [
+    (1, [1, 0], 1, 0, 0), (64, [64, 10], 16, 4, 4), (300, [300, 299], 299, 0, 0), (1000, [1000, 512], 101, 4, 16), (700, [700, 650], 64, 60, 4),
+    (500, [500, 3], 700, 5, 5), (2100, [2100, 2049], 1500, 0, 1), (20000, [20000, 17000], 300, 4, 100),
+])
+def test_evict_by_mass(d, dtype, cap, lens, keep, sinks, recent):
+    gen = torch.Generator().manual_seed(cap)
+    k, v = (torch.randn(2, 2, cap, d, generator=gen).to(dtype) for _ in range(2))
+    mass = torch.exp(3 * torch.randn(2, 2, cap, generator=gen))
+    mass[:, :, ::3] = torch.round(mass[:, :, ::3])                                         # many equal ones
+    mass[:, 1, 1::11], mass[:, 1, 2::13] = math.nan, math.inf
+    mass[0, 0, 5::17], mass[0, 0, 6::17] = 0.0, -0.0
+    mass[:, 1, 3::29] = -math.inf
+    extra = 3
+    k_out, v_out = (torch.full((2, 2, keep + extra, d), SENTINEL, dtype=dtype, device="cuda") for _ in range(2))
+    idx = torch.full((2, 2, keep), -1, dtype=torch.int32, device="cuda")
+    m_out = torch.full((2, 2, keep + extra), SENTINEL, device="cuda")
+    r = P.evict_by_mass(k.cuda(), v.cuda(), mass.cuda(), keep, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"), sinks=sinks, recent=recent,
+                        k_out=k_out, v_out=v_out, idx_out=idx, mass_out=m_out)
+    want = ref.evict(mass, lens, keep, sinks, recent)
+    assert r["lens"].tolist() == [min(n, keep) for n in lens]
+    for b in range(2):
+        for h in range(2):
+            w = want[b][h]
+            n = len(w)
+            assert idx[b, h, :n].tolist() == w, (b, h)
+            assert (idx[b, h, n:] == -1).all() and (m_out[b, h, n:] == SENTINEL).all()
+            assert torch.equal(k_out[b, h, :n].cpu(), k[b, h, w]) and torch.equal(v_out[b, h, :n].cpu(), v[b, h, w])
+            assert (k_out[b, h, n:] == SENTINEL).all() and (v_out[b, h, n:] == SENTINEL).all()
+            assert torch.equal(m_out[b, h, :n].cpu().nan_to_num(nan=-5.0), mass[b, h, w].nan_to_num(nan=-5.0))
