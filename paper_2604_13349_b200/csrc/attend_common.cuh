@@ -89,7 +89,22 @@ __device__ __forceinline__ bool attend_sees(const AttendDev &p, int t, int j)
 // Final result of a row: out rounded to its type and lse in the natural log.
 __device__ __forceinline__ float natural_lse(float lse2) { return lse2 * 0.6931471805599453f; }
 
-// One value of a row of `out` pairs: 4 channels.
+// 2^x by the special-function unit (2 ulp; results below 2^-126 become zero).
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Four neighbouring channels of a row, rounded to its type.
 template <typename T>
 __device__ __forceinline__ void store4(T *dst, float4 v)
 {

@@ -2,6 +2,7 @@
 #include <cmath>
 
 #include "attend_common.cuh"
+#include "attend_few.cuh"
 #include "attend_generic.cuh"
 #include "evict_mass.cuh"
 #include "host.cuh"
@@ -58,17 +59,21 @@ static obf_status_t validate_attend_pointers(const obf_attend_t *a, const obf_pr
     return OBF_OK;
 }
 
+// Kernels that a set of keys (a sequence's own ones, the shared prefix) is worked on by.
+enum AttendPath { ATTEND_GENERIC, ATTEND_FEW };
+
 struct AttendLayout {
+    AttendPath own_path, p_path;
     int p_slots, own_slots;          // parts of the prefix and of a sequence's own keys
     size_t off_part_o, off_part_lse, off_logits, total;
 };
 
-// Parts of `keys` keys for `tiles` tiles of query rows: about two blocks per multiprocessor, at least four key tiles each.
-static int parts_for(long long tiles, long long keys)
+// Parts of `keys` keys for `tiles` tiles of query rows: about `blocks` blocks in all, at least `least` keys each.
+static int parts_for(long long tiles, long long keys, long long blocks, int least)
 {
-    long long s = (2 * 148 + tiles - 1) / tiles, most = (keys + 4 * AG_TILE - 1) / (4 * AG_TILE);
+    long long s = (blocks + tiles - 1) / tiles, most = (keys + least - 1) / least;
     if (s > most) s = most;
-    if (s > 64) s = 64;
+    if (s > 128) s = 128;
     return (int)(s < 1 ? 1 : s);
 }
 
@@ -80,14 +85,35 @@ static long long most_keys(const obf_attend_t *a, int rows_of_queries)
     return n < a->capacity ? n : a->capacity;
 }
 
+// Up to 16 query rows (and a mass call's at most 64) go where the tensor cores' 128-row tiles would stay empty.
+static AttendPath path_for(const obf_attend_t *a, long long rows)
+{
+    if (a->dtype != OBF_BF16 || (a->flags & OBF_FLAG_GENERIC_PATH)) return ATTEND_GENERIC;
+    if (rows <= 16 || a->mass_out) return ATTEND_FEW;
+    return ATTEND_GENERIC;
+}
+
+static int few_rows(long long rows) { return rows <= 8 ? 8 : 16; }
+
 static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
 {
     AttendLayout L;
     const long long rows_seq = (long long)(a->q_heads / a->kv_heads) * a->n_q, heads = (long long)a->batch * a->kv_heads, rows = heads * rows_seq;
-    const long long own_tiles = heads * ((rows_seq + AG_TILE - 1) / AG_TILE);
-    L.own_slots = parts_for(own_tiles, most_keys(a, AG_TILE));
+    const auto parts = [&](AttendPath path, long long runs, long long rows_run, long long keys) {
+        if (path == ATTEND_FEW) {
+            const int t = few_rows(rows_run);
+            return parts_for(runs * ((rows_run + t - 1) / t), keys, 6 * 148, 256);
+        }
+        return parts_for(runs * ((rows_run + AG_TILE - 1) / AG_TILE), keys, 2 * 148, 4 * AG_TILE);
+    };
+    L.own_path = path_for(a, rows_seq);
+    L.own_slots = parts(L.own_path, heads, rows_seq, most_keys(a, AG_TILE));
+    L.p_path = ATTEND_GENERIC;
     L.p_slots = 0;
-    if (x) L.p_slots = parts_for((long long)a->kv_heads * ((a->batch * rows_seq + AG_TILE - 1) / AG_TILE), x->rows);
+    if (x) {
+        L.p_path = path_for(a, a->batch * rows_seq);
+        L.p_slots = parts(L.p_path, a->kv_heads, a->batch * rows_seq, x->rows);
+    }
     const int slots = L.own_slots + L.p_slots;
     size_t o = 256;
     const bool join = slots > 1 || a->mass_out;
@@ -126,11 +152,39 @@ static obf_status_t launch_attend_generic(const AttendDev &p, int first, cudaStr
     return OBF_OK;
 }
 
-template <typename TIN, int D>
-static obf_status_t run_attend(const AttendDev &p, cudaStream_t st)
+template <int D, int NT, bool PREFIX>
+static obf_status_t launch_attend_few_nt(const AttendDev &p, int first, cudaStream_t st)
 {
-    if (p.prefix) OBF_TRY((launch_attend_generic<TIN, D, true>(p, 1, st)));
-    OBF_TRY((launch_attend_generic<TIN, D, false>(p, p.prefix == 0, st)));
+    static bool done[64];
+    OBF_TRY(set_smem_once(k_attend_few<D, NT, PREFIX>, attend_few_smem<D>(), done));
+    const long long rows = (PREFIX ? (long long)p.batch : 1) * p.n_q * p.G, tiles = (rows + 8 * NT - 1) / (8 * NT);
+    const long long blocks = (PREFIX ? p.p_slots : p.slots - p.p_slots) * tiles * p.kv_heads * (PREFIX ? 1 : p.batch);
+    if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
+    OBF_TRY(launch(k_attend_few<D, NT, PREFIX>, dim3((unsigned)blocks), AF_NT, attend_few_smem<D>(), st, p, first));
+    ++g_last_launches;
+    return OBF_OK;
+}
+
+template <int D, bool PREFIX>
+static obf_status_t launch_attend_few(const AttendDev &p, int first, cudaStream_t st)
+{
+    const long long rows = (PREFIX ? (long long)p.batch : 1) * p.n_q * p.G;
+    return few_rows(rows) == 8 ? launch_attend_few_nt<D, 1, PREFIX>(p, first, st) : launch_attend_few_nt<D, 2, PREFIX>(p, first, st);
+}
+
+template <typename TIN, int D, bool PREFIX>
+static obf_status_t launch_attend(AttendPath path, const AttendDev &p, int first, cudaStream_t st)
+{
+    if constexpr (sizeof(TIN) == 2)
+        if (path == ATTEND_FEW) return launch_attend_few<D, PREFIX>(p, first, st);
+    return launch_attend_generic<TIN, D, PREFIX>(p, first, st);
+}
+
+template <typename TIN, int D>
+static obf_status_t run_attend(const AttendLayout &L, const AttendDev &p, cudaStream_t st)
+{
+    if (p.prefix) OBF_TRY((launch_attend<TIN, D, true>(L.p_path, p, 1, st)));
+    OBF_TRY((launch_attend<TIN, D, false>(L.own_path, p, p.prefix == 0, st)));
     if (p.slots > 1 || p.mass_out) {
         long long blocks = p.rows_total;
         if (p.mass_out) blocks += (long long)p.batch * p.kv_heads * ((p.capacity + AJ_KEYS - 1) / AJ_KEYS);
@@ -170,8 +224,8 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *w
     p.part_lse = reinterpret_cast<float *>(ws + L.off_part_lse);
     p.logits = reinterpret_cast<float *>(ws + L.off_logits);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (a->dtype == OBF_F32) return a->head_dim == 64 ? run_attend<float, 64>(p, st) : run_attend<float, 128>(p, st);
-    return a->head_dim == 64 ? run_attend<__nv_bfloat16, 64>(p, st) : run_attend<__nv_bfloat16, 128>(p, st);
+    if (a->dtype == OBF_F32) return a->head_dim == 64 ? run_attend<float, 64>(L, p, st) : run_attend<float, 128>(L, p, st);
+    return a->head_dim == 64 ? run_attend<__nv_bfloat16, 64>(L, p, st) : run_attend<__nv_bfloat16, 128>(L, p, st);
 }
 
 template <int ROW_BYTES>
