@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import torch
@@ -361,69 +362,104 @@ def compress_caches(params: ObfParams, caches_in: Sequence[Dict[str, object]], *
 # ---------------------------------------------------------------------------
 _DTYPES = {torch.float32: OBF_F32, torch.bfloat16: OBF_BF16}
 
+# A single token's attention takes some microseconds on the device, so these wrappers hand the structs over as packed bytes
+# (building a ctypes structure field by field takes longer than the kernels).
+_ATTEND = struct.Struct("@9i2fI4P12q5P")
+_PREFIX = struct.Struct("@2P4qi4x")
+_EVICT = struct.Struct("@8i4P12q4Pi4xP")
+assert (_ATTEND.size, _PREFIX.size, _EVICT.size) == (ctypes.sizeof(ObfAttend), ctypes.sizeof(ObfPrefix), ctypes.sizeof(ObfEvict))
+_packed_calls: Dict[str, object] = {}
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+
+def _packed(name: str):
+    """An entry point taking its structs as bytes."""
+    fn = _packed_calls.get(name)
+    if fn is None:
+        bytes_, ptr, size = ctypes.c_char_p, ctypes.c_void_p, ctypes.c_size_t
+        args = {"obf_attend_workspace_bytes": (bytes_, bytes_, ptr), "obf_attend": (bytes_, ptr, size, ptr),
+                "obf_attend_shared": (bytes_, bytes_, ptr, size, ptr), "obf_evict_by_mass": (bytes_, ptr)}[name]
+        fn = _packed_calls[name] = ctypes.CFUNCTYPE(ctypes.c_int, *args)((name, load()))
+    return fn
 
 
-def _rows(t: torch.Tensor, shape, like: torch.Tensor, name: str):
-    """A tensor of rows of contiguous channels, as the C structs take it: checked shape, type and device, and its strides."""
-    _need(tuple(t.shape) == tuple(shape), "%s: shape %s expected, got %s" % (name, tuple(shape), tuple(t.shape)))
-    _need(t.dtype == like.dtype and t.device == like.device, "%s: %s on %s expected" % (name, like.dtype, like.device))
+def _refuse(name: str, t, shape, dtype, device) -> None:
+    raise ValueError("%s: %s %s on %s expected, got %s" % (
+        name, dtype, tuple(shape), device, "%s %s on %s" % (t.dtype, tuple(t.shape), t.device) if isinstance(t, torch.Tensor) else type(t).__name__))
+
+
+def _rows(t: torch.Tensor, shape, dtype, device, name: str):
+    """Checks a tensor of rows of contiguous channels and gives its strides."""
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        _refuse(name, t, shape, dtype, device)
     st = t.stride()
-    _need(st[-1] == 1, "%s: channels must be contiguous" % name)
-    return st[:-1]
+    if st[-1] != 1:
+        raise ValueError("%s: channels must be contiguous" % name)
+    return st
 
 
-def _dense(t: Optional[torch.Tensor], shape, dtype, like: torch.Tensor, name: str) -> Optional[int]:
+def _dense(t: Optional[torch.Tensor], shape, dtype, device, name: str) -> int:
     if t is None:
-        return None
-    _need(tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.device == like.device and t.is_contiguous(),
-          "%s: contiguous %s %s on %s expected" % (name, tuple(shape), dtype, like.device))
+        return 0
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        _refuse(name + " (contiguous)", t, shape, dtype, device)
     return t.data_ptr()
 
 
-def _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags) -> ObfAttend:
-    _need(q.dim() == 4 and k.dim() == 4 and q.is_cuda, "q and k: device tensors [batch, heads, rows, head_dim] expected")
-    B, hq, n_q, d = q.shape
+def _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags) -> bytes:
+    dt, dev = q.dtype, q.device
+    if dt not in _DTYPES or dev.type != "cuda" or q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k: float32 or bfloat16 device tensors [batch, heads, rows, head_dim] expected")
+    B, hq, n_q, d = shape_q = q.shape
     kv, cap = k.shape[1], k.shape[2]
-    _need(q.dtype in _DTYPES, "q: float32 or bfloat16 expected")
-    return ObfAttend(
-        B, kv, hq, d, n_q, cap, window, sinks, _DTYPES[q.dtype], scale, decay, flags, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-        _rows(q, (B, hq, n_q, d), q, "q"), _rows(k, (B, kv, cap, d), q, "k"), _rows(v, (B, kv, cap, d), q, "v"), _rows(out, (B, hq, n_q, d), q, "out"),
-        _dense(lens, (B,), torch.int32, q, "lens"), _dense(q_lens, (B,), torch.int32, q, "q_lens"),
-        _dense(lse_out, (B, hq, n_q), torch.float32, q, "lse_out"), _dense(mass_in, (B, kv, cap), torch.float32, q, "mass_in"),
-        _dense(mass_out, (B, kv, cap), torch.float32, q, "mass_out"))
+    shape_k = (B, kv, cap, d)
+    sq, so = _rows(q, shape_q, dt, dev, "q"), _rows(out, shape_q, dt, dev, "out")
+    sk, sv = _rows(k, shape_k, dt, dev, "k"), _rows(v, shape_k, dt, dev, "v")
+    return _ATTEND.pack(
+        B, kv, hq, d, n_q, cap, window, sinks, _DTYPES[dt], scale, decay, flags, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+        sq[0], sq[1], sq[2], sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], so[0], so[1], so[2],
+        _dense(lens, (B,), torch.int32, dev, "lens"), _dense(q_lens, (B,), torch.int32, dev, "q_lens"),
+        _dense(lse_out, (B, hq, n_q), torch.float32, dev, "lse_out"), _dense(mass_in, (B, kv, cap), torch.float32, dev, "mass_in"),
+        _dense(mass_out, (B, kv, cap), torch.float32, dev, "mass_out"))
 
 
-def _enqueue(name: str, device: torch.device, call, stream) -> None:
-    """call(stream handle) with the tensors' device current, on its current stream unless another is given."""
+def _handle(stream, device: torch.device) -> int:
+    """The given stream's handle, else that of the device's current stream."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _enqueue(name: str, device: torch.device, *args) -> None:
+    """The call, with the tensors' device current."""
+    fn = _packed(name)
     if device.index != torch.cuda.current_device():
         with torch.cuda.device(device):
-            rc = call(_stream_handle(stream))
+            rc = fn(*args)
     else:
-        rc = call(_stream_handle(stream))
+        rc = fn(*args)
     if rc != OBF_OK:
         raise ObfError(rc, name)
 
 
 def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, stream):
-    lib = load()
-    nb = ctypes.c_size_t(0)
-    px = ctypes.byref(prefix) if prefix is not None else None
-    rc = lib.obf_attend_workspace_bytes(ctypes.byref(args), px, ctypes.byref(nb))
-    if rc != OBF_OK:
-        raise ObfError(rc, name)
+    dev = q.device
     if workspace is None:
-        workspace = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+        nb = ctypes.c_size_t(0)
+        rc = _packed("obf_attend_workspace_bytes")(args, prefix, ctypes.addressof(nb))
+        if rc != OBF_OK:
+            raise ObfError(rc, name)
+        size = nb.value
+        workspace = torch.empty(size, dtype=torch.uint8, device=dev)
         if stream is not None:                   # the allocator gives the memory on once the given stream is done with it
-            workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream, device=q.device))
-    size = workspace.numel() * workspace.element_size()
-    if prefix is None:
-        _enqueue(name, q.device, lambda st: lib.obf_attend(ctypes.byref(args), workspace.data_ptr(), size, st), stream)
+            workspace.record_stream(torch.cuda.ExternalStream(stream, device=dev) if isinstance(stream, int) else stream)
     else:
-        _enqueue(name, q.device, lambda st: lib.obf_attend_shared(ctypes.byref(args), px, workspace.data_ptr(), size, st), stream)
+        if workspace.device != dev:
+            raise ValueError("workspace: on %s expected" % dev)
+        size = workspace.numel() * workspace.element_size()
+    if prefix is None:
+        _enqueue(name, dev, args, workspace.data_ptr(), size, _handle(stream, dev))
+    else:
+        _enqueue(name, dev, args, prefix, workspace.data_ptr(), size, _handle(stream, dev))
     got = {"out": out, "workspace": workspace}
     if lse_out is not None:
         got["lse"] = lse_out
@@ -468,10 +504,12 @@ def attend_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tenso
     (``obf_attend_shared``): the prefix is read once for all of them."""
     out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse)
     args = _attend_args(q, k, v, lens, q_lens, 0, 0, scale, out, lse_out, None, None, 1.0, flags)
-    _need(k_prefix.dim() == 3, "k_prefix: [kv_heads, rows, head_dim] expected")
+    if k_prefix.dim() != 3:
+        raise ValueError("k_prefix: [kv_heads, rows, head_dim] expected")
     rows = k_prefix.shape[1]
     shape = (k.shape[1], rows, q.shape[3])
-    prefix = ObfPrefix(k_prefix.data_ptr(), v_prefix.data_ptr(), _rows(k_prefix, shape, q, "k_prefix"), _rows(v_prefix, shape, q, "v_prefix"), rows)
+    sk, sv = _rows(k_prefix, shape, q.dtype, q.device, "k_prefix"), _rows(v_prefix, shape, q.dtype, q.device, "v_prefix")
+    prefix = _PREFIX.pack(k_prefix.data_ptr(), v_prefix.data_ptr(), sk[0], sk[1], sv[0], sv[1], rows)
     return _attend_call("obf_attend_shared", args, prefix, q, out, lse_out, None, workspace, stream)
 
 
@@ -491,15 +529,15 @@ def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: in
     ``[batch, kv_heads, capacity]``: the first ``sinks``, the last ``recent`` and the heaviest others, in ascending order
     (``obf_evict_by_mass`` in include/obf.h).  ``k_out, v_out`` and ``mass_out`` may have more rows than ``keep``: the cache goes on
     there.  Returns ``K_out, V_out, idx, mass, lens``."""
-    _need(k.dim() == 4 and k.is_cuda and k.dtype in _DTYPES, "k: a float32 or bfloat16 device tensor [batch, kv_heads, capacity, head_dim] expected")
-    B, kv, cap, d = k.shape
-    dev = k.device
-    short = lens is not None or keep > cap                       # rows may stay behind a sequence's last one: not written
-    make = torch.zeros if short else torch.empty
+    dt, dev = k.dtype, k.device
+    if dt not in _DTYPES or dev.type != "cuda" or k.dim() != 4:
+        raise ValueError("k: a float32 or bfloat16 device tensor [batch, kv_heads, capacity, head_dim] expected")
+    B, kv, cap, d = shape = k.shape
+    make = torch.zeros if lens is not None or keep > cap else torch.empty        # rows behind a sequence's last one are not written
     if k_out is None:
-        k_out = make((B, kv, keep, d), dtype=k.dtype, device=dev)
+        k_out = make((B, kv, keep, d), dtype=dt, device=dev)
     if v_out is None:
-        v_out = make((B, kv, keep, d), dtype=k.dtype, device=dev)
+        v_out = make((B, kv, keep, d), dtype=dt, device=dev)
     if idx_out is None:
         idx_out = make((B, kv, keep), dtype=torch.int32, device=dev)
     if mass_out is None:
@@ -507,13 +545,15 @@ def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: in
     if lens_out is None:
         lens_out = torch.empty((B,), dtype=torch.int32, device=dev)
     ko, vo, mo = k_out.shape[2], v_out.shape[2], mass_out.shape[2]
-    _need(min(ko, vo, mo) >= keep, "k_out, v_out and mass_out: at least `keep` rows expected")
-    args = ObfEvict(
-        B, kv, d, cap, _DTYPES[k.dtype], keep, sinks, recent, k.data_ptr(), v.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
-        _rows(k, (B, kv, cap, d), k, "k"), _rows(v, (B, kv, cap, d), k, "v"), _rows(k_out, (B, kv, ko, d), k, "k_out"), _rows(v_out, (B, kv, vo, d), k, "v_out"),
-        _dense(mass, (B, kv, cap), torch.float32, k, "mass"), _dense(lens, (B,), torch.int32, k, "lens"),
-        _dense(idx_out, (B, kv, keep), torch.int32, k, "idx_out"), _dense(mass_out, (B, kv, mo), torch.float32, k, "mass_out"), mo,
-        _dense(lens_out, (B,), torch.int32, k, "lens_out"))
-    lib = load()
-    _enqueue("obf_evict_by_mass", dev, lambda st: lib.obf_evict_by_mass(ctypes.byref(args), st), stream)
+    if min(ko, vo, mo) < keep:
+        raise ValueError("k_out, v_out and mass_out: at least `keep` rows expected")
+    sk, sv = _rows(k, shape, dt, dev, "k"), _rows(v, shape, dt, dev, "v")
+    s1, s2 = _rows(k_out, (B, kv, ko, d), dt, dev, "k_out"), _rows(v_out, (B, kv, vo, d), dt, dev, "v_out")
+    args = _EVICT.pack(
+        B, kv, d, cap, _DTYPES[dt], keep, sinks, recent, k.data_ptr(), v.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+        sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], s1[0], s1[1], s1[2], s2[0], s2[1], s2[2],
+        _dense(mass, (B, kv, cap), torch.float32, dev, "mass"), _dense(lens, (B,), torch.int32, dev, "lens"),
+        _dense(idx_out, (B, kv, keep), torch.int32, dev, "idx_out"), _dense(mass_out, (B, kv, mo), torch.float32, dev, "mass_out"), mo,
+        _dense(lens_out, (B,), torch.int32, dev, "lens_out"))
+    _enqueue("obf_evict_by_mass", dev, args, _handle(stream, dev))
     return {"K_out": k_out, "V_out": v_out, "idx": idx_out, "mass": mass_out, "lens": lens_out}
