@@ -1,0 +1,501 @@
+// Attention of many query rows per KV head on the tensor cores (bf16): prompts, chunks of queries, a batch over a shared prefix.
+//
+// A block (one per multiprocessor, persistent) works on items: two tiles of up to 128 query rows of a KV head and a part of the
+// keys that they see.  A tile is `ti` queries x the G heads of the group (so its rows see nearly the same keys and a window
+// wastes little), over a shared prefix also `nb` sequences.  Keys come in tiles of 128: first the sinks, in a tile of their own
+// that is only as wide as needed, then the window's range.
+//   warp 9, a thread    Q, K and V tiles by TMA (128-byte swizzle) into a ring of K and V slots
+//   warp 8, a thread    S = Q K^T into tensor memory, O += P V with P from tensor memory; the two query tiles take turns, so the
+//                       products of one run while the softmax of the other does
+//   warps 0-3, 4-7      softmax of the first and the second query tile, a row per thread, weights to bf16 over the logits'
+//                       columns, their fp32 sum; after the last tile O / sum to memory
+//
+// Softmax: fp32 and bf16 have the same exponents, so a row's reference need not be its maximum, only within 2^64 of it: the
+// maximum of the first tile of keys that the row sees serves, the logits are read once, and their maximum is formed beside the
+// exponentials instead of before them.  Only when it exceeds the reference by more than 64 in the log2 domain (never for most
+// rows) are the tile's weights formed again against the new one and O and the sum rescaled - in place: the products before
+// have completed, since they were issued before the logits that the thread has waited for.
+// Tensor memory: S (P) and O of the two tiles, 512 columns.  Every wait is bounded.
+//
+// Rows of V past the last key may hold anything, and 0 * NaN is not 0: the product over a short tile runs over its keys rounded
+// up to 16, and warp 8 clears the rows in between.
+//
+// Bound by the exponentials (16 per cycle and multiprocessor: 1024 cycles a tile of 128 x 128) and the two products (512 cycles
+// each) alike.
+#pragma once
+
+#include "attend_common.cuh"
+#include "tc_common.cuh"
+
+namespace obf {
+
+constexpr int AT_TILE = 128;
+constexpr int AT_THREADS = 320;
+constexpr float AT_RAISE = 64.f;
+
+template <int D>
+struct AttendTcShape {
+    static constexpr int SLOT_BYTES = AT_TILE * D * 2;                    // a tile of Q, K or V
+    static constexpr int SLOTS = D == 128 ? 5 : 8;
+    static constexpr int SMEM_BYTES = (2 + SLOTS) * SLOT_BYTES + 1024;
+};
+
+// Tensor maps and tile shape of the kernel.
+struct AttendTcMaps {
+    CUtensorMap q, k, v;
+    int32_t ti, nb;                                                       // queries and sequences of a tile of rows
+};
+
+// Of two values, without an array that is indexed at run time.
+template <typename T>
+__device__ __forceinline__ T pick(const T (&a)[2], int x) { return x ? a[1] : a[0]; }
+
+// What every role of a block knows about an item.
+template <bool PREFIX>
+struct AttendTcItem {
+    int h, b, part;                  // KV head, first sequence, part of the keys
+    int i0, ti, nb;                  // first query of the first tile, queries and sequences of a tile
+    int s, lo, hi, nsink;            // keys of the pair: s sinks in nsink tiles, then lo .. hi - 1
+    int jb, je;                      // the part's tiles
+    int t0[2], t1[2], lo_s[2], hi_s[2];
+    bool valid[2], any;
+    int len, ql;
+
+    bool seqs;                       // the pair's tiles are of different sequences (all their queries fit a tile)
+
+    __device__ __forceinline__ int first_i(int x) const { return seqs ? 0 : i0 + x * ti; }
+    __device__ __forceinline__ int first_b(int x) const { return seqs ? b + x * nb : b; }
+
+    __device__ __forceinline__ void init(const AttendDev &p, const AttendTcMaps &tm, int item)
+    {
+        ti = tm.ti;
+        nb = tm.nb;
+        const int parts = PREFIX ? p.p_slots : p.slots - p.p_slots;
+        part = item % parts;
+        item /= parts;
+        seqs = PREFIX && ti >= p.n_q;
+        h = item % p.kv_heads;
+        item /= p.kv_heads;
+        if (seqs) {
+            b = item * 2 * nb;
+            i0 = 0;
+        } else {
+            b = item % p.batch;
+            item /= p.batch;
+            const int pairs = (p.n_q + 2 * ti - 1) / (2 * ti);
+            i0 = (pairs - 1 - item) * 2 * ti;                             // the longest key ranges first
+        }
+        any = false;
+        if (PREFIX) {
+            s = lo = 0;
+            hi = p.prefix;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                valid[x] = first_b(x) < p.batch && first_i(x) < p.n_q;
+                any = any || valid[x];
+            }
+        } else {
+            len = attend_len(p, b);
+            ql = attend_q_len(p, b);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int a = first_i(x), e = min(a + ti, ql) - 1;
+                valid[x] = a <= e;
+                t0[x] = len - ql + a;
+                t1[x] = len - ql + e;
+                const KeyRange r = attend_range(p, t0[x], max(t0[x], t1[x]), len);
+                lo_s[x] = r.lo;
+                hi_s[x] = valid[x] ? r.hi : 0;
+                any = any || valid[x];
+            }
+            const KeyRange r = attend_range(p, t0[0], valid[1] ? t1[1] : max(t0[0], t1[0]), len);
+            s = r.s;
+            lo = r.lo;
+            hi = any ? r.hi : r.lo;
+            if (!any) s = 0;
+        }
+        nsink = (s + AT_TILE - 1) / AT_TILE;
+        const int tiles = nsink + (hi - lo + AT_TILE - 1) / AT_TILE, per = (tiles + parts - 1) / parts;
+        jb = min(part * per, tiles);
+        je = min(jb + per, tiles);
+    }
+
+    __device__ __forceinline__ void tile(int j, int &j0, int &width) const
+    {
+        if (j < nsink) {
+            j0 = j * AT_TILE;
+            width = min(AT_TILE, s - j0);
+        } else {
+            j0 = lo + (j - nsink) * AT_TILE;
+            width = min(AT_TILE, hi - j0);
+        }
+    }
+
+    // Whether some row of query tile x sees a key of the tile.
+    __device__ __forceinline__ bool active(const AttendDev &p, int x, int j, int j0, int width) const
+    {
+        if (PREFIX) return pick(valid, x);
+        return pick(valid, x) && (j < nsink || (j0 < pick(hi_s, x) && (j0 + width > pick(lo_s, x) || j0 < p.sinks)));
+    }
+
+    // Whether all rows of query tile x see all keys of the tile.
+    __device__ __forceinline__ bool full(const AttendDev &p, int x, int j0, int width) const
+    {
+        if (width & 31) return false;
+        if (PREFIX) return true;
+        return j0 + width - 1 <= pick(t0, x) && (p.window == 0 || j0 > pick(t1, x) - p.window || j0 + width <= p.sinks);
+    }
+};
+
+// D[tmem] (+)= A[tmem] * B, K = 16 per instruction: A holds two bf16 of a row per column.
+__device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int c0, int c1, int c2, int c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+
+// Bits of columns a .. b - 1 of 32.
+__device__ __forceinline__ uint32_t column_bits(int a, int b)
+{
+    a = max(a, 0);
+    b = min(b, 32);
+    if (a >= b) return 0u;
+    return (0xFFFFFFFFu >> (32 - b)) & (0xFFFFFFFFu << a);
+}
+
+template <int D, bool PREFIX>
+__global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_constant__ AttendDev p, const __grid_constant__ AttendTcMaps tm, const int items,
+                                                           const int first)
+{
+    constexpr int SLOTS = AttendTcShape<D>::SLOTS, SLOT_BYTES = AttendTcShape<D>::SLOT_BYTES, BLOCK = AT_TILE * 128, NB = D / 64;
+    extern __shared__ uint8_t at_smem_raw[];
+    uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *q_sm = base, *ring = base + 2 * SLOT_BYTES;
+    __shared__ uint64_t bar_full[SLOTS], bar_empty[SLOTS], bar_q_full, bar_q_empty, bar_drain;
+    __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2];
+    __shared__ uint32_t s_tmem, s_abort;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    tc::WaitCtx wc{&s_abort, p.status, p.wait_limit_ns};
+    if (tid == 0) {
+        s_abort = 0u;
+        for (int i = 0; i < SLOTS; ++i) { tc::mbar_init(&bar_full[i], 1); tc::mbar_init(&bar_empty[i], 1); }
+        tc::mbar_init(&bar_q_full, 1);
+        tc::mbar_init(&bar_q_empty, 1);
+        tc::mbar_init(&bar_drain, 1);
+        for (int x = 0; x < 2; ++x) {
+            tc::mbar_init(&bar_s[x], 1);
+            tc::mbar_init(&bar_p[x], 4);
+            tc::mbar_init(&bar_o[x], 1);
+            tc::mbar_init(&bar_o_read[x], 4);
+        }
+        tc::mbar_init_fence();
+    }
+    if (warp == 8) tc::tmem_alloc(&s_tmem, 512);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    pdl_wait();
+    if (first && blockIdx.x == 0) attend_status(p);
+
+    AttendTcItem<PREFIX> it;
+    if (warp == 9) {
+        // ---------------- copies ----------------
+        if (lane == 0) {
+            uint32_t n = 0, nq = 0;
+            bool dead = false;
+            for (int item = blockIdx.x; item < items && !dead; item += gridDim.x) {
+                it.init(p, tm, item);
+                if (it.jb >= it.je) continue;
+                if (!tc::mbar_wait(&bar_q_empty, (nq & 1u) ^ 1u, wc)) break;
+                const int rows = p.G * it.ti * it.nb, loads = (it.valid[0] ? NB : 0) + (it.valid[1] ? NB : 0);
+                tc::mbar_expect_tx(&bar_q_full, (uint32_t)(loads * rows * 128));
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (it.valid[x])
+                        for (int c = 0; c < NB; ++c)
+                            tma_load_4d(tc::smem_u32(q_sm + x * SLOT_BYTES + c * BLOCK), &tm.q, &bar_q_full, 64 * c, it.h * p.G, it.first_i(x), it.first_b(x));
+                ++nq;
+                for (int j = it.jb; j < it.je && !dead; ++j) {
+                    int j0, width;
+                    it.tile(j, j0, width);
+                    for (int kv = 0; kv < 2; ++kv, ++n) {
+                        const uint32_t sl = n % SLOTS;
+                        if (!tc::mbar_wait(&bar_empty[sl], ((n / SLOTS) & 1u) ^ 1u, wc)) { dead = true; break; }
+                        tc::mbar_expect_tx(&bar_full[sl], SLOT_BYTES);
+                        asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %3, %5, %6}], [%2];"
+                                     ::"r"(tc::smem_u32(ring + sl * SLOT_BYTES)), "l"(kv ? &tm.v : &tm.k), "r"(tc::smem_u32(&bar_full[sl])), "r"(0), "r"(j0), "r"(it.h),
+                                       "r"(PREFIX ? 0 : it.b) : "memory");
+                    }
+                }
+            }
+            // nothing that this thread started may be in flight when the block exits
+            for (uint32_t j = n > (uint32_t)SLOTS ? n - SLOTS : 0u; j < n; ++j) tc::mbar_drain(&bar_full[j % SLOTS], (j / SLOTS) & 1u, wc);
+            if (nq) tc::mbar_drain(&bar_q_full, (nq - 1) & 1u, wc);
+        }
+    } else if (warp == 8) {
+        // ---------------- products ----------------
+        constexpr uint32_t idesc_o = tc::idesc_bf16(128, D, 0, 1);
+        uint32_t n = 0, nq = 0, ns[2] = {0, 0}, no[2] = {0, 0};
+        bool dead = false;
+        for (int item = blockIdx.x; item < items && !dead; item += gridDim.x) {
+            it.init(p, tm, item);
+            if (it.jb >= it.je) continue;
+            if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_q_full, nq & 1u, wc))) break;
+            ++nq;
+            bool pending[2] = {false, false}, started[2] = {false, false};
+            int width_prev = 0;
+            // ring positions: K of tile j at n + 2 (j - jb), V behind it
+            for (int j = it.jb; j <= it.je && !dead; ++j) {
+                int j0 = 0, width = 0;
+                const uint32_t nk = n + 2 * (j - it.jb), nv = nk - 1;
+                if (j < it.je) {
+                    it.tile(j, j0, width);
+                    if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_full[nk % SLOTS], (nk / SLOTS) & 1u, wc))) { dead = true; break; }
+                }
+                const int w16 = (width + 15) & ~15, w16_prev = (width_prev + 15) & ~15;
+                const uint32_t vs = tc::smem_u32(ring + (nv % SLOTS) * SLOT_BYTES), ks = tc::smem_u32(ring + (nk % SLOTS) * SLOT_BYTES);
+                if (j > it.jb) {
+                    if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_full[nv % SLOTS], (nv / SLOTS) & 1u, wc))) { dead = true; break; }
+                    if (w16_prev != width_prev) {
+                        // rows behind the last key: they may hold anything
+                        uint8_t *v = ring + (nv % SLOTS) * SLOT_BYTES;
+                        for (int i = lane; i < (w16_prev - width_prev) * 8 * NB; i += 32) {
+                            const int r = width_prev + i / (8 * NB), c = i % (8 * NB);
+                            *reinterpret_cast<uint4 *>(v + (c >> 3) * BLOCK + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        tc::fence_async_smem();
+                        __syncwarp();
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t s_t = tmem + 128 * x, o_t = tmem + 256 + 128 * x;
+                    if (pending[x]) {
+                        if (!started[x] && !__all_sync(0xffffffffu, tc::mbar_wait(&bar_o_read[x], (no[x] & 1u) ^ 1u, wc))) { dead = true; break; }
+                        if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_p[x], (ns[x] - 1) & 1u, wc))) { dead = true; break; }
+                        tc::tc_fence_after();
+                        if (lane == 0)
+                            for (int k = 0; k < w16_prev / 16; ++k)
+                                umma_bf16_ta(o_t, s_t + 8 * k, tc::smem_desc_sw128(vs + k * 2048, BLOCK, 1024), idesc_o, (started[x] || k > 0) ? 1u : 0u);
+                        started[x] = true;
+                        pending[x] = false;
+                    }
+                    if (j < it.je && it.active(p, x, j, j0, width)) {
+                        tc::tc_fence_after();
+                        if (lane == 0) {
+                            const uint32_t qs = tc::smem_u32(q_sm + x * SLOT_BYTES), idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k) {
+                                const uint32_t off = (k >> 2) * BLOCK + (k & 3) * 32;
+                                tc::umma_bf16(s_t, tc::smem_desc_sw128(qs + off, 16, 1024), tc::smem_desc_sw128(ks + off, 16, 1024), idesc_s, k > 0);
+                            }
+                            tc::umma_commit(&bar_s[x]);
+                        }
+                        ++ns[x];
+                        pending[x] = true;
+                    }
+                }
+                if (dead) break;
+                if (lane == 0) {
+                    if (j > it.jb) tc::umma_commit(&bar_empty[nv % SLOTS]);
+                    if (j < it.je) tc::umma_commit(&bar_empty[nk % SLOTS]);
+                    if (j == it.je - 1) tc::umma_commit(&bar_q_empty);
+                    if (j == it.je)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+                            if (started[x]) tc::umma_commit(&bar_o[x]);
+                }
+                width_prev = width;
+                __syncwarp();
+            }
+            n += 2 * (it.je - it.jb);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) no[x] += started[x] ? 1 : 0;
+        }
+        // nor may a product
+        if (lane == 0) {
+            tc::umma_commit(&bar_drain);
+            tc::mbar_drain(&bar_drain, 0, wc);
+        }
+        __syncwarp();
+    } else {
+        // ---------------- softmax ----------------
+        const int x = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_t = tmem + 128 * x + lanes, o_t = tmem + 256 + 128 * x + lanes;
+        const f32x2 c2 = pk(p.c, p.c);
+        uint32_t ns = 0, no = 0;
+        bool dead = false;
+        for (int item = blockIdx.x; item < items && !dead; item += gridDim.x) {
+            it.init(p, tm, item);
+            // the row
+            const int g = row % p.G, iq = row / p.G, bi = iq / it.ti, i = it.first_i(x) + iq - bi * it.ti, b = it.first_b(x) + bi;
+            bool real = pick(it.valid, x) && bi < it.nb && b < p.batch;
+            if (PREFIX) real = real && i < attend_q_len(p, b);
+            else real = real && i < it.ql;
+            const int t = PREFIX || !real ? 0 : it.len - it.ql + i;
+            float m = -INFINITY;
+            f32x2 l2 = 0ull;
+            bool started = false;
+            for (int j = it.jb; j < it.je; ++j) {
+                int j0, width;
+                it.tile(j, j0, width);
+                if (!it.active(p, x, j, j0, width)) continue;
+                if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_s[x], ns & 1u, wc))) { dead = true; break; }
+                ++ns;
+                tc::tc_fence_after();
+                const int nch = (width + 31) >> 5;
+                const bool full = it.full(p, x, j0, width);
+                // columns of chunk c that the row sees
+                auto seen = [&](int c) {
+                    uint32_t bits = column_bits(0, width - 32 * c);
+                    if (!PREFIX) {
+                        // up to the row's position, and behind its window's lower end or among the first tokens
+                        const int a = j0 + 32 * c;
+                        const uint32_t in = p.window ? column_bits(t - p.window + 1 - a, 32) | column_bits(0, p.sinks - a) : 0xFFFFFFFFu;
+                        bits &= real ? in & column_bits(0, t + 1 - a) : 0u;
+                    }
+                    return bits;
+                };
+                auto hide = [&](uint32_t (&r)[32], int c) {
+                    const uint32_t bits = seen(c);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
+                };
+                bool known = started;                     // the rows have references
+                uint32_t w[4][16];
+                f32x2 z;
+                for (;;) {
+                    if (!known) {
+                        float mx = -INFINITY;
+#pragma unroll 1
+                        for (int c = 0; c < nch; ++c) {
+                            uint32_t r[32];
+                            tc::tmem_ld32(s_t + 32 * c, r);
+                            tc::tmem_ld_wait32(r);
+                            if (!full) hide(r, c);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(r[e]), __uint_as_float(r[e + 1])));
+                        }
+                        mx *= p.c;
+                        const float f = mx > m ? ex2(m - mx) : 1.f;
+                        m = fmaxf(m, mx);
+                        l2 = mul2(l2, pk(f, f));
+                        if (started) {
+#pragma unroll 1
+                            for (int c = 0; c < D / 32; ++c) {
+                                uint32_t o[32];
+                                tc::tmem_ld32(o_t + 32 * c, o);
+                                tc::tmem_ld_wait32(o);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tc::tmem_st32(o_t + 32 * c, o);
+                            }
+                        }
+                    }
+                    const float ref = m == -INFINITY ? 0.f : -m;
+                    const f32x2 r2 = pk(ref, ref);
+                    float mx = -INFINITY;
+                    z = 0ull;
+                    uint32_t r[2][32];
+                    tc::tmem_ld32(s_t, r[0]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (c < nch) {
+                            tc::tmem_ld_wait32(r[c & 1]);
+                            if (c + 1 < nch) tc::tmem_ld32(s_t + 32 * (c + 1), r[(c + 1) & 1]);
+                            if (!full) hide(r[c & 1], c);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const float s0 = __uint_as_float(r[c & 1][2 * e]), s1 = __uint_as_float(r[c & 1][2 * e + 1]);
+                                mx = fmaxf(mx, fmaxf(s0, s1));
+                                float a, b2;
+                                upk(fma2(pk(s0, s1), c2, r2), a, b2);
+                                a = ex2(a);
+                                b2 = ex2(b2);
+                                z = add2(z, pk(a, b2));
+                                w[c][e] = pack_bf16(a, b2);
+                            }
+                        }
+                    }
+                    if (!known || !__any_sync(0xffffffffu, mx * p.c > m + AT_RAISE)) break;
+                    known = false;
+                }
+                started = true;
+                l2 = add2(l2, z);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (c < nch) tmem_st16(s_t + 16 * c, w[c]);
+                tc::tmem_st_wait();
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&bar_p[x]);
+            }
+            if (dead) break;
+            const float l = sum2(l2);
+            if (started) {
+                if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_o[x], no & 1u, wc))) break;
+                ++no;
+                tc::tc_fence_after();
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+            const long long R = (((long long)b * p.kv_heads + it.h) * p.n_q + i) * p.G + g;
+            const bool last = p.slots == 1;
+            const long long at = (long long)(PREFIX ? it.part : p.p_slots + it.part) * p.rows_total + R;
+            __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.out) + b * p.os[0] + (long long)(it.h * p.G + g) * p.os[1] + (long long)i * p.os[2];
+            float *part = p.part_o + at * D;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                if (started) {
+                    tc::tmem_ld32(o_t + 32 * c, o);
+                    tc::tmem_ld_wait32(o);
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
+                if (real && last) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 w;
+                        w.x = pack_bf16(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
+                        w.y = pack_bf16(__uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+                        w.z = pack_bf16(__uint_as_float(o[e + 4]), __uint_as_float(o[e + 5]));
+                        w.w = pack_bf16(__uint_as_float(o[e + 6]), __uint_as_float(o[e + 7]));
+                        *reinterpret_cast<uint4 *>(dst + 32 * c + e) = w;
+                    }
+                } else if (real && l != 0.f) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<uint4 *>(part + 32 * c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+            }
+            if (started) {
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&bar_o_read[x]);
+            }
+            if (real) {
+                if (!last) p.part_lse[at] = lse2;
+                else if (p.lse_out) p.lse_out[((long long)b * p.kv_heads * p.G + it.h * p.G + g) * p.n_q + i] = natural_lse(lse2);
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (warp == 8) tc::tmem_dealloc(tmem, 512);
+}
+
+}  // namespace obf

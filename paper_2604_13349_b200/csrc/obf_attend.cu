@@ -4,6 +4,7 @@
 #include "attend_common.cuh"
 #include "attend_few.cuh"
 #include "attend_generic.cuh"
+#include "attend_tc.cuh"
 #include "evict_mass.cuh"
 #include "host.cuh"
 
@@ -60,7 +61,7 @@ static obf_status_t validate_attend_pointers(const obf_attend_t *a, const obf_pr
 }
 
 // Kernels that a set of keys (a sequence's own ones, the shared prefix) is worked on by.
-enum AttendPath { ATTEND_GENERIC, ATTEND_FEW };
+enum AttendPath { ATTEND_GENERIC, ATTEND_FEW, ATTEND_TC };
 
 struct AttendLayout {
     AttendPath own_path, p_path;
@@ -90,10 +91,45 @@ static AttendPath path_for(const obf_attend_t *a, long long rows)
 {
     if (a->dtype != OBF_BF16 || (a->flags & OBF_FLAG_GENERIC_PATH)) return ATTEND_GENERIC;
     if (rows <= 16 || a->mass_out) return ATTEND_FEW;
-    return ATTEND_GENERIC;
+    return a->q_heads / a->kv_heads <= AT_TILE ? ATTEND_TC : ATTEND_GENERIC;
 }
 
 static int few_rows(long long rows) { return rows <= 8 ? 8 : 16; }
+
+// Tiles of query rows on the tensor cores: `ti` queries of `nb` sequences with the G heads of the group.
+struct TcTiles {
+    int ti, nb;
+    long long pairs;                 // pairs of tiles over the call
+};
+
+static TcTiles tc_tiles(int G, int n_q, int batch, int kv_heads, bool prefix)
+{
+    TcTiles t;
+    t.ti = AT_TILE / G < n_q ? AT_TILE / G : n_q;
+    t.nb = 1;
+    if (prefix && t.ti == n_q) {
+        t.nb = AT_TILE / (G * n_q) < batch ? AT_TILE / (G * n_q) : batch;
+        t.pairs = (long long)kv_heads * ((batch + 2 * t.nb - 1) / (2 * t.nb));
+    } else {
+        t.pairs = (long long)kv_heads * batch * ((n_q + 2 * t.ti - 1) / (2 * t.ti));
+    }
+    return t;
+}
+
+// Parts of the keys for the persistent kernel: as many as make its last round of items (one per multiprocessor) fullest,
+// counting an item's fixed cost as that of one tile of keys.
+static int tc_parts(long long pairs, long long keys)
+{
+    const long long tiles = (keys + AT_TILE - 1) / AT_TILE;
+    int best = 1;
+    double cost = 1e300;
+    for (int s = 1; s <= 128 && s <= (tiles + 1) / 2; ++s) {
+        const double c = (double)((pairs * s + 147) / 148) * ((double)((tiles + s - 1) / s) + 1.0 + (s > 1 ? 0.5 : 0.0));
+        if (c < cost * 0.97) { cost = c; best = s; }
+        if (pairs * s > 148 * 4) break;
+    }
+    return best;
+}
 
 static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
 {
@@ -104,6 +140,7 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
             const int t = few_rows(rows_run);
             return parts_for(runs * ((rows_run + t - 1) / t), keys, 6 * 148, 256);
         }
+        if (path == ATTEND_TC) return tc_parts(tc_tiles((int)(a->q_heads / a->kv_heads), a->n_q, a->batch, a->kv_heads, rows_run != rows_seq).pairs, keys);
         return parts_for(runs * ((rows_run + AG_TILE - 1) / AG_TILE), keys, 2 * 148, 4 * AG_TILE);
     };
     L.own_path = path_for(a, rows_seq);
@@ -172,11 +209,61 @@ static obf_status_t launch_attend_few(const AttendDev &p, int first, cudaStream_
     return few_rows(rows) == 8 ? launch_attend_few_nt<D, 1, PREFIX>(p, first, st) : launch_attend_few_nt<D, 2, PREFIX>(p, first, st);
 }
 
+// Strides of dimensions that are never stepped over may be anything for the caller, not for a tensor map.
+static cuuint64_t map_stride(long long elements, uint64_t n) { return n > 1 ? (cuuint64_t)elements * 2 : 16; }
+
+static obf_status_t encode_map(CUtensorMap *m, const void *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box)
+{
+    EncodeTiledFn enc = tensor_map_encoder();
+    if (!enc) return OBF_ERR_CUDA;
+    const cuuint32_t es[5] = {1, 1, 1, 1, 1};
+    const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        std::fprintf(stderr, "obf: cuTensorMapEncodeTiled failed with %d\n", (int)r);
+        return OBF_ERR_CUDA;
+    }
+    return OBF_OK;
+}
+
+template <int D, bool PREFIX>
+static obf_status_t launch_attend_tc(const AttendDev &p, int first, cudaStream_t st)
+{
+    static bool done[64];
+    OBF_TRY(set_smem_once(k_attend_tc<D, PREFIX>, AttendTcShape<D>::SMEM_BYTES, done));
+    const TcTiles t = tc_tiles(p.G, p.n_q, p.batch, p.kv_heads, PREFIX);
+    AttendTcMaps m;
+    m.ti = t.ti;
+    m.nb = t.nb;
+    const cuuint64_t hq = (cuuint64_t)p.kv_heads * p.G, nq = p.n_q, nb = p.batch, kv = p.kv_heads;
+    {
+        const cuuint64_t dims[4] = {D, hq, nq, nb}, strides[3] = {map_stride(p.qs[1], hq), map_stride(p.qs[2], nq), map_stride(p.qs[0], nb)};
+        const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)t.ti, (cuuint32_t)t.nb};
+        OBF_TRY(encode_map(&m.q, p.q, 4, dims, strides, box));
+    }
+    for (int i = 0; i < 2; ++i) {
+        const long long *s3 = i ? p.vs : p.ks, *s2 = i ? p.pvs : p.pks;
+        const cuuint64_t rows = PREFIX ? p.prefix : p.capacity, n = PREFIX ? 1 : nb;
+        const cuuint64_t dims[5] = {64, rows, D / 64, kv, n};
+        const cuuint64_t strides[4] = {map_stride(PREFIX ? s2[1] : s3[2], rows), 128, map_stride(PREFIX ? s2[0] : s3[1], kv), PREFIX ? 16 : map_stride(s3[0], n)};
+        const cuuint32_t box[5] = {64, AT_TILE, D / 64, 1, 1};
+        OBF_TRY(encode_map(i ? &m.v : &m.k, PREFIX ? (i ? p.pv : p.pk) : (i ? p.v : p.k), 5, dims, strides, box));
+    }
+    const long long items = t.pairs * (PREFIX ? p.p_slots : p.slots - p.p_slots);
+    if (items > INT_MAX / 2) return OBF_ERR_UNSUPPORTED;
+    const int blocks = items < sm_count() ? (int)items : sm_count();
+    OBF_TRY(launch(k_attend_tc<D, PREFIX>, dim3(blocks), AT_THREADS, AttendTcShape<D>::SMEM_BYTES, st, p, m, (int)items, first));
+    ++g_last_launches;
+    return OBF_OK;
+}
+
 template <typename TIN, int D, bool PREFIX>
 static obf_status_t launch_attend(AttendPath path, const AttendDev &p, int first, cudaStream_t st)
 {
-    if constexpr (sizeof(TIN) == 2)
+    if constexpr (sizeof(TIN) == 2) {
         if (path == ATTEND_FEW) return launch_attend_few<D, PREFIX>(p, first, st);
+        if (path == ATTEND_TC) return launch_attend_tc<D, PREFIX>(p, first, st);
+    }
     return launch_attend_generic<TIN, D, PREFIX>(p, first, st);
 }
 
@@ -211,6 +298,7 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *w
     }
     p.lens = a->lens; p.q_lens = a->q_lens; p.lse_out = a->lse_out; p.mass_in = a->mass_in; p.mass_out = a->mass_out;
     p.decay = a->decay;
+    p.wait_limit_ns = tc::WAIT_LIMIT_NS;
     p.c = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f;
     p.batch = a->batch; p.kv_heads = a->kv_heads; p.G = a->q_heads / a->kv_heads; p.n_q = a->n_q; p.capacity = a->capacity;
     // beyond any position a window or a number of first tokens changes nothing; clamped, positions minus windows cannot overflow
