@@ -57,10 +57,11 @@ struct AttendTcItem {
     int i0, ti, nb;                  // first query of the first tile, queries and sequences of a tile
     int s, lo, hi, nsink;            // keys of the pair: s sinks in nsink tiles, then lo .. hi - 1
     int jb, je;                      // the part's tiles
-    int t0[2], t1[2], lo_s[2], hi_s[2];
-    bool valid[2], any;
-    int len, ql;
-
+    // per tile of rows: some row sees tile j of the keys when j < sk or ja <= j < jz, every row sees all of it when fa <= j < fz
+    int sk[2], ja[2], jz[2], fa[2], fz[2];
+    bool valid[2];
+    int t;                           // position of a sequence's first query
+    int ql;
     bool seqs;                       // the pair's tiles are of different sequences (all their queries fit a tile)
 
     __device__ __forceinline__ int first_i(int x) const { return seqs ? 0 : i0 + x * ti; }
@@ -85,36 +86,44 @@ struct AttendTcItem {
             const int pairs = (p.n_q + 2 * ti - 1) / (2 * ti);
             i0 = (pairs - 1 - item) * 2 * ti;                             // the longest key ranges first
         }
-        any = false;
         if (PREFIX) {
-            s = lo = 0;
+            s = lo = t = ql = nsink = 0;
             hi = p.prefix;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 valid[x] = first_b(x) < p.batch && first_i(x) < p.n_q;
-                any = any || valid[x];
+                sk[x] = ja[x] = fa[x] = 0;
+                jz[x] = valid[x] ? (hi + AT_TILE - 1) / AT_TILE : 0;
+                fz[x] = hi / AT_TILE;
             }
         } else {
-            len = attend_len(p, b);
+            const int len = attend_len(p, b);
             ql = attend_q_len(p, b);
+            t = len - ql;
+            s = lo = hi = nsink = 0;
+            valid[0] = i0 < ql;
+            valid[1] = i0 + ti < ql;
+            if (valid[0]) {
+                const KeyRange r = attend_range(p, t + i0, t + min(i0 + 2 * ti, ql) - 1, len);
+                s = r.s;
+                lo = r.lo;
+                hi = r.hi;
+                nsink = (s + AT_TILE - 1) / AT_TILE;
+            }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int a = first_i(x), e = min(a + ti, ql) - 1;
-                valid[x] = a <= e;
-                t0[x] = len - ql + a;
-                t1[x] = len - ql + e;
-                const KeyRange r = attend_range(p, t0[x], max(t0[x], t1[x]), len);
-                lo_s[x] = r.lo;
-                hi_s[x] = valid[x] ? r.hi : 0;
-                any = any || valid[x];
+                sk[x] = ja[x] = jz[x] = fa[x] = fz[x] = 0;
+                if (valid[x]) {
+                    const int ta = t + i0 + x * ti, tb = t + min(i0 + (x + 1) * ti, ql) - 1;      // positions of its first and last query
+                    const KeyRange r = attend_range(p, ta, tb, len);
+                    sk[x] = nsink;
+                    ja[x] = nsink + (p.sinks > lo ? 0 : (r.lo - lo) / AT_TILE);
+                    jz[x] = nsink + (r.hi - lo + AT_TILE - 1) / AT_TILE;
+                    fa[x] = nsink + (p.window ? max(tb - p.window + 1 - lo + AT_TILE - 1, 0) / AT_TILE : 0);
+                    fz[x] = nsink + max(ta + 1 - lo, 0) / AT_TILE;
+                }
             }
-            const KeyRange r = attend_range(p, t0[0], valid[1] ? t1[1] : max(t0[0], t1[0]), len);
-            s = r.s;
-            lo = r.lo;
-            hi = any ? r.hi : r.lo;
-            if (!any) s = 0;
         }
-        nsink = (s + AT_TILE - 1) / AT_TILE;
         const int tiles = nsink + (hi - lo + AT_TILE - 1) / AT_TILE, per = (tiles + parts - 1) / parts;
         jb = min(part * per, tiles);
         je = min(jb + per, tiles);
@@ -131,20 +140,7 @@ struct AttendTcItem {
         }
     }
 
-    // Whether some row of query tile x sees a key of the tile.
-    __device__ __forceinline__ bool active(const AttendDev &p, int x, int j, int j0, int width) const
-    {
-        if (PREFIX) return pick(valid, x);
-        return pick(valid, x) && (j < nsink || (j0 < pick(hi_s, x) && (j0 + width > pick(lo_s, x) || j0 < p.sinks)));
-    }
-
-    // Whether all rows of query tile x see all keys of the tile.
-    __device__ __forceinline__ bool full(const AttendDev &p, int x, int j0, int width) const
-    {
-        if (width & 31) return false;
-        if (PREFIX) return true;
-        return j0 + width - 1 <= pick(t0, x) && (p.window == 0 || j0 > pick(t1, x) - p.window || j0 + width <= p.sinks);
-    }
+    __device__ __forceinline__ bool active(int x, int j) const { return j < pick(sk, x) || (j >= pick(ja, x) && j < pick(jz, x)); }
 };
 
 // D[tmem] (+)= A[tmem] * B, K = 16 per instruction: A holds two bf16 of a row per column.
@@ -287,20 +283,30 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         if (!started[x] && !__all_sync(0xffffffffu, tc::mbar_wait(&bar_o_read[x], (no[x] & 1u) ^ 1u, wc))) { dead = true; break; }
                         if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_p[x], (ns[x] - 1) & 1u, wc))) { dead = true; break; }
                         tc::tc_fence_after();
-                        if (lane == 0)
-                            for (int k = 0; k < w16_prev / 16; ++k)
-                                umma_bf16_ta(o_t, s_t + 8 * k, tc::smem_desc_sw128(vs + k * 2048, BLOCK, 1024), idesc_o, (started[x] || k > 0) ? 1u : 0u);
+                        if (lane == 0) {
+                            // 16 keys on: 2048 bytes, 128 in the descriptor
+                            const uint64_t vd = tc::smem_desc_sw128(vs, BLOCK, 1024);
+                            if (w16_prev == AT_TILE) {
+#pragma unroll
+                                for (int k = 0; k < AT_TILE / 16; ++k) umma_bf16_ta(o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started[x] || k > 0) ? 1u : 0u);
+                            } else {
+                                for (int k = 0; k < w16_prev / 16; ++k) umma_bf16_ta(o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started[x] || k > 0) ? 1u : 0u);
+                            }
+                        }
                         started[x] = true;
                         pending[x] = false;
                     }
-                    if (j < it.je && it.active(p, x, j, j0, width)) {
+                    if (j < it.je && it.active(x, j)) {
                         tc::tc_fence_after();
                         if (lane == 0) {
-                            const uint32_t qs = tc::smem_u32(q_sm + x * SLOT_BYTES), idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
+                            const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
+                            const uint64_t qd = tc::smem_desc_sw128(tc::smem_u32(q_sm + x * SLOT_BYTES), 16, 1024), kd = tc::smem_desc_sw128(ks, 16, 1024);
 #pragma unroll
                             for (int k = 0; k < D / 16; ++k) {
-                                const uint32_t off = (k >> 2) * BLOCK + (k & 3) * 32;
-                                tc::umma_bf16(s_t, tc::smem_desc_sw128(qs + off, 16, 1024), tc::smem_desc_sw128(ks + off, 16, 1024), idesc_s, k > 0);
+                                // 16 channels on: 32 bytes, every 64 the next column block
+                                constexpr uint32_t unit = 16;
+                                const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / unit;
+                                tc::umma_bf16(s_t, qd + off, kd + off, idesc_s, k > 0);
                             }
                             tc::umma_commit(&bar_s[x]);
                         }
@@ -345,52 +351,76 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             bool real = pick(it.valid, x) && bi < it.nb && b < p.batch;
             if (PREFIX) real = real && i < attend_q_len(p, b);
             else real = real && i < it.ql;
-            const int t = PREFIX || !real ? 0 : it.len - it.ql + i;
+            const int t = PREFIX || !real ? 0 : it.t + i, sk = pick(it.sk, x), ja = pick(it.ja, x), jz = pick(it.jz, x), fa = pick(it.fa, x), fz = pick(it.fz, x);
             float m = -INFINITY;
             f32x2 l2 = 0ull;
             bool started = false;
             for (int j = it.jb; j < it.je; ++j) {
-                int j0, width;
-                it.tile(j, j0, width);
-                if (!it.active(p, x, j, j0, width)) continue;
+                if (!(j < sk || (j >= ja && j < jz))) continue;
                 if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_s[x], ns & 1u, wc))) { dead = true; break; }
                 ++ns;
                 tc::tc_fence_after();
-                const int nch = (width + 31) >> 5;
-                const bool full = it.full(p, x, j0, width);
-                // columns of chunk c that the row sees
-                auto seen = [&](int c) {
-                    uint32_t bits = column_bits(0, width - 32 * c);
-                    if (!PREFIX) {
-                        // up to the row's position, and behind its window's lower end or among the first tokens
-                        const int a = j0 + 32 * c;
-                        const uint32_t in = p.window ? column_bits(t - p.window + 1 - a, 32) | column_bits(0, p.sinks - a) : 0xFFFFFFFFu;
-                        bits &= real ? in & column_bits(0, t + 1 - a) : 0u;
-                    }
-                    return bits;
-                };
-                auto hide = [&](uint32_t (&r)[32], int c) {
-                    const uint32_t bits = seen(c);
+                bool formed = false;                      // the tile's weights
+                if (started && j >= fa && j < fz) {
+                    // every row sees all 128 keys and has a reference
+                    const float ref = m == -INFINITY ? 0.f : -m;
+                    const f32x2 r2 = pk(ref, ref);
+                    float mx = -INFINITY;
+                    f32x2 z = 0ull;
+                    uint32_t w[4][16], r[2][32];
+                    tc::tmem_ld32(s_t, r[0]);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
-                };
-                bool known = started;                     // the rows have references
-                uint32_t w[4][16];
-                f32x2 z;
-                for (;;) {
-                    if (!known) {
-                        float mx = -INFINITY;
-#pragma unroll 1
-                        for (int c = 0; c < nch; ++c) {
-                            uint32_t r[32];
-                            tc::tmem_ld32(s_t + 32 * c, r);
-                            tc::tmem_ld_wait32(r);
-                            if (!full) hide(r, c);
+                    for (int c = 0; c < 4; ++c) {
+                        tc::tmem_ld_wait32(r[c & 1]);
+                        if (c < 3) tc::tmem_ld32(s_t + 32 * (c + 1), r[(c + 1) & 1]);
 #pragma unroll
-                            for (int e = 0; e < 32; e += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(r[e]), __uint_as_float(r[e + 1])));
+                        for (int e = 0; e < 16; ++e) {
+                            const float s0 = __uint_as_float(r[c & 1][2 * e]), s1 = __uint_as_float(r[c & 1][2 * e + 1]);
+                            mx = fmaxf(mx, fmaxf(s0, s1));
+                            float a, b2;
+                            upk(fma2(pk(s0, s1), c2, r2), a, b2);
+                            a = ex2(a);
+                            b2 = ex2(b2);
+                            z = add2(z, pk(a, b2));
+                            w[c][e] = pack_bf16(a, b2);
                         }
-                        mx *= p.c;
+                    }
+                    if (!__any_sync(0xffffffffu, mx * p.c > m + AT_RAISE)) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tmem_st16(s_t + 16 * c, w[c]);
+                        l2 = add2(l2, z);
+                        formed = true;
+                    }
+                }
+                if (!formed) {
+                    int j0, width;
+                    it.tile(j, j0, width);
+                    const int nch = (width + 31) >> 5;
+                    auto load = [&](uint32_t (&r)[32], int c) {
+                        tc::tmem_ld32(s_t + 32 * c, r);
+                        uint32_t bits = column_bits(0, width - 32 * c);
+                        if (!PREFIX) {
+                            // keys up to the row's position, and behind its window's lower end or among the first tokens
+                            const int a = j0 + 32 * c;
+                            const uint32_t in = p.window ? column_bits(t - p.window + 1 - a, 32) | column_bits(0, p.sinks - a) : 0xFFFFFFFFu;
+                            bits &= real ? in & column_bits(0, t + 1 - a) : 0u;
+                        }
+                        tc::tmem_ld_wait32(r);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
+                    };
+                    float mx = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < nch; ++c) {
+                        uint32_t r[32];
+                        load(r, c);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(r[e]), __uint_as_float(r[e + 1])));
+                    }
+                    mx *= p.c;
+                    // (a maximum below the reference changes nothing)
+                    if (__any_sync(0xffffffffu, started ? mx > m + AT_RAISE : true)) {
                         const float f = mx > m ? ex2(m - mx) : 1.f;
                         m = fmaxf(m, mx);
                         l2 = mul2(l2, pk(f, f));
@@ -408,37 +438,23 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     }
                     const float ref = m == -INFINITY ? 0.f : -m;
                     const f32x2 r2 = pk(ref, ref);
-                    float mx = -INFINITY;
-                    z = 0ull;
-                    uint32_t r[2][32];
-                    tc::tmem_ld32(s_t, r[0]);
+#pragma unroll 1
+                    for (int c = 0; c < nch; ++c) {
+                        uint32_t r[32], w[16];
+                        load(r, c);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if (c < nch) {
-                            tc::tmem_ld_wait32(r[c & 1]);
-                            if (c + 1 < nch) tc::tmem_ld32(s_t + 32 * (c + 1), r[(c + 1) & 1]);
-                            if (!full) hide(r[c & 1], c);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const float s0 = __uint_as_float(r[c & 1][2 * e]), s1 = __uint_as_float(r[c & 1][2 * e + 1]);
-                                mx = fmaxf(mx, fmaxf(s0, s1));
-                                float a, b2;
-                                upk(fma2(pk(s0, s1), c2, r2), a, b2);
-                                a = ex2(a);
-                                b2 = ex2(b2);
-                                z = add2(z, pk(a, b2));
-                                w[c][e] = pack_bf16(a, b2);
-                            }
+                        for (int e = 0; e < 16; ++e) {
+                            float a, b2;
+                            upk(fma2(pk(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, r2), a, b2);
+                            a = ex2(a);
+                            b2 = ex2(b2);
+                            l2 = add2(l2, pk(a, b2));
+                            w[e] = pack_bf16(a, b2);
                         }
+                        tmem_st16(s_t + 16 * c, w);
                     }
-                    if (!known || !__any_sync(0xffffffffu, mx * p.c > m + AT_RAISE)) break;
-                    known = false;
                 }
                 started = true;
-                l2 = add2(l2, z);
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (c < nch) tmem_st16(s_t + 16 * c, w[c]);
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
                 __syncwarp();
