@@ -4,7 +4,8 @@
 // keys that they see.  A tile is `ti` queries x the G heads of the group (so its rows see nearly the same keys and a window
 // wastes little), over a shared prefix also `nb` sequences.  Keys come in tiles of 128: first the sinks, in a tile of their own
 // that is only as wide as needed, then the window's range.
-//   warp 9, a thread    Q, K and V tiles by TMA (128-byte swizzle) into a ring of K and V slots
+//   warp 9, a thread    works out the items (ahead of the others, who read them from shared memory); Q, K and V tiles by TMA
+//                       (128-byte swizzle) into a ring of K and V slots
 //   warp 8, a thread    S = Q K^T into tensor memory, O += P V with P from tensor memory; the two query tiles take turns, so the
 //                       products of one run while the softmax of the other does
 //   warps 0-3, 4-7      softmax of the first and the second query tile, a row per thread, weights to bf16 over the logits'
@@ -18,7 +19,7 @@
 // Tensor memory: S (P) and O of the two tiles, 512 columns.  Every wait is bounded.
 //
 // Rows of V past the last key may hold anything, and 0 * NaN is not 0: the product over a short tile runs over its keys rounded
-// up to 16, and warp 8 clears the rows in between.
+// up to 16, and the softmax warps clear the rows in between.
 //
 // Bound by the exponentials (16 per cycle and multiprocessor: 1024 cycles a tile of 128 x 128) and the two products (512 cycles
 // each) alike.
@@ -180,7 +181,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *q_sm = base, *ring = base + 2 * SLOT_BYTES;
     __shared__ uint64_t bar_full[SLOTS], bar_empty[SLOTS], bar_q_full, bar_q_empty, bar_drain;
-    __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2];
+    __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2], bar_item[2], bar_item_read[2];
+    __shared__ AttendTcItem<PREFIX> sm_item[2];
     __shared__ uint32_t s_tmem, s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     tc::WaitCtx wc{&s_abort, p.status, p.wait_limit_ns};
@@ -195,6 +197,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             tc::mbar_init(&bar_p[x], 4);
             tc::mbar_init(&bar_o[x], 1);
             tc::mbar_init(&bar_o_read[x], 4);
+            tc::mbar_init(&bar_item[x], 1);
+            tc::mbar_init(&bar_item_read[x], 9);
         }
         tc::mbar_init_fence();
     }
@@ -210,10 +214,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     if (warp == 9) {
         // ---------------- copies ----------------
         if (lane == 0) {
-            uint32_t n = 0, nq = 0;
+            uint32_t n = 0, nq = 0, ni = 0;
             bool dead = false;
-            for (int item = blockIdx.x; item < items && !dead; item += gridDim.x) {
+            for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
                 it.init(p, tm, item);
+                if (!tc::mbar_wait(&bar_item_read[ni & 1u], ((ni >> 1) & 1u) ^ 1u, wc)) break;
+                sm_item[ni & 1u] = it;
+                tc::mbar_arrive(&bar_item[ni & 1u]);
                 if (it.jb >= it.je) continue;
                 if (!tc::mbar_wait(&bar_q_empty, (nq & 1u) ^ 1u, wc)) break;
                 const int rows = p.G * it.ti * it.nb, loads = (it.valid[0] ? NB : 0) + (it.valid[1] ? NB : 0);
@@ -243,96 +250,78 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         }
     } else if (warp == 8) {
         // ---------------- products ----------------
-        constexpr uint32_t idesc_o = tc::idesc_bf16(128, D, 0, 1);
-        uint32_t n = 0, nq = 0, ns[2] = {0, 0}, no[2] = {0, 0};
-        bool dead = false;
-        for (int item = blockIdx.x; item < items && !dead; item += gridDim.x) {
-            it.init(p, tm, item);
-            if (it.jb >= it.je) continue;
-            if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_q_full, nq & 1u, wc))) break;
-            ++nq;
-            bool pending[2] = {false, false}, started[2] = {false, false};
-            int width_prev = 0;
-            // ring positions: K of tile j at n + 2 (j - jb), V behind it
-            for (int j = it.jb; j <= it.je && !dead; ++j) {
-                int j0 = 0, width = 0;
-                const uint32_t nk = n + 2 * (j - it.jb), nv = nk - 1;
-                if (j < it.je) {
-                    it.tile(j, j0, width);
-                    if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_full[nk % SLOTS], (nk / SLOTS) & 1u, wc))) { dead = true; break; }
-                }
-                const int w16 = (width + 15) & ~15, w16_prev = (width_prev + 15) & ~15;
-                const uint32_t vs = tc::smem_u32(ring + (nv % SLOTS) * SLOT_BYTES), ks = tc::smem_u32(ring + (nk % SLOTS) * SLOT_BYTES);
-                if (j > it.jb) {
-                    if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_full[nv % SLOTS], (nv / SLOTS) & 1u, wc))) { dead = true; break; }
-                    if (w16_prev != width_prev) {
-                        // rows behind the last key: they may hold anything
-                        uint8_t *v = ring + (nv % SLOTS) * SLOT_BYTES;
-                        for (int i = lane; i < (w16_prev - width_prev) * 8 * NB; i += 32) {
-                            const int r = width_prev + i / (8 * NB), c = i % (8 * NB);
-                            *reinterpret_cast<uint4 *>(v + (c >> 3) * BLOCK + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                        }
-                        tc::fence_async_smem();
-                        __syncwarp();
+        if (lane == 0) {
+            constexpr uint32_t idesc_o = tc::idesc_bf16(128, D, 0, 1);
+            uint32_t n = 0, nq = 0, ni = 0, ns[2] = {0, 0}, no[2] = {0, 0};
+            bool dead = false;
+            for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
+                if (!tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc)) break;
+                it = sm_item[ni & 1u];
+                tc::mbar_arrive(&bar_item_read[ni & 1u]);
+                if (it.jb >= it.je) continue;
+                if (!tc::mbar_wait(&bar_q_full, nq & 1u, wc)) break;
+                ++nq;
+                bool pending[2] = {false, false}, started[2] = {false, false};
+                int w16_prev = 0;
+                // ring positions: K of tile j at n + 2 (j - jb), V behind it
+                for (int j = it.jb; j <= it.je && !dead; ++j) {
+                    int w16 = 0;
+                    const uint32_t nk = n + 2 * (j - it.jb), nv = nk - 1, slot_k = nk % SLOTS, slot_v = nv % SLOTS;
+                    if (j < it.je) {
+                        int j0, width;
+                        it.tile(j, j0, width);
+                        w16 = (width + 15) & ~15;
+                        if (!tc::mbar_wait(&bar_full[slot_k], (nk / SLOTS) & 1u, wc)) { dead = true; break; }
                     }
-                }
+                    if (j > it.jb && !tc::mbar_wait(&bar_full[slot_v], (nv / SLOTS) & 1u, wc)) { dead = true; break; }
+                    // 16 keys of V on: 2048 bytes, 128 in the descriptor
+                    const uint64_t vd = tc::smem_desc_sw128(tc::smem_u32(ring + slot_v * SLOT_BYTES), BLOCK, 1024);
+                    const uint64_t kd = tc::smem_desc_sw128(tc::smem_u32(ring + slot_k * SLOT_BYTES), 16, 1024);
+                    const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const uint32_t s_t = tmem + 128 * x, o_t = tmem + 256 + 128 * x;
-                    if (pending[x]) {
-                        if (!started[x] && !__all_sync(0xffffffffu, tc::mbar_wait(&bar_o_read[x], (no[x] & 1u) ^ 1u, wc))) { dead = true; break; }
-                        if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_p[x], (ns[x] - 1) & 1u, wc))) { dead = true; break; }
-                        tc::tc_fence_after();
-                        if (lane == 0) {
-                            // 16 keys on: 2048 bytes, 128 in the descriptor
-                            const uint64_t vd = tc::smem_desc_sw128(vs, BLOCK, 1024);
+                    for (int x = 0; x < 2; ++x) {
+                        const uint32_t s_t = tmem + 128 * x, o_t = tmem + 256 + 128 * x;
+                        if (pending[x]) {
+                            if (!started[x] && !tc::mbar_wait(&bar_o_read[x], (no[x] & 1u) ^ 1u, wc)) { dead = true; break; }
+                            if (!tc::mbar_wait(&bar_p[x], (ns[x] - 1) & 1u, wc)) { dead = true; break; }
+                            tc::tc_fence_after();
                             if (w16_prev == AT_TILE) {
 #pragma unroll
                                 for (int k = 0; k < AT_TILE / 16; ++k) umma_bf16_ta(o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started[x] || k > 0) ? 1u : 0u);
                             } else {
                                 for (int k = 0; k < w16_prev / 16; ++k) umma_bf16_ta(o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started[x] || k > 0) ? 1u : 0u);
                             }
+                            started[x] = true;
+                            pending[x] = false;
+                            if (j == it.je) tc::umma_commit(&bar_o[x]);
+                        } else if (j == it.je && started[x]) {
+                            tc::umma_commit(&bar_o[x]);
                         }
-                        started[x] = true;
-                        pending[x] = false;
-                    }
-                    if (j < it.je && it.active(x, j)) {
-                        tc::tc_fence_after();
-                        if (lane == 0) {
-                            const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
-                            const uint64_t qd = tc::smem_desc_sw128(tc::smem_u32(q_sm + x * SLOT_BYTES), 16, 1024), kd = tc::smem_desc_sw128(ks, 16, 1024);
+                        if (j < it.je && it.active(x, j)) {
+                            tc::tc_fence_after();
+                            const uint64_t qd = tc::smem_desc_sw128(tc::smem_u32(q_sm + x * SLOT_BYTES), 16, 1024);
 #pragma unroll
                             for (int k = 0; k < D / 16; ++k) {
-                                // 16 channels on: 32 bytes, every 64 the next column block
-                                constexpr uint32_t unit = 16;
-                                const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / unit;
+                                // 16 channels on: 32 bytes, every 64 the next column block; descriptors count 16 bytes
+                                const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / 16;
                                 tc::umma_bf16(s_t, qd + off, kd + off, idesc_s, k > 0);
                             }
                             tc::umma_commit(&bar_s[x]);
+                            ++ns[x];
+                            pending[x] = true;
                         }
-                        ++ns[x];
-                        pending[x] = true;
                     }
-                }
-                if (dead) break;
-                if (lane == 0) {
-                    if (j > it.jb) tc::umma_commit(&bar_empty[nv % SLOTS]);
-                    if (j < it.je) tc::umma_commit(&bar_empty[nk % SLOTS]);
+                    if (dead) break;
+                    if (j > it.jb) tc::umma_commit(&bar_empty[slot_v]);
+                    if (j < it.je) tc::umma_commit(&bar_empty[slot_k]);
                     if (j == it.je - 1) tc::umma_commit(&bar_q_empty);
-                    if (j == it.je)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-                            if (started[x]) tc::umma_commit(&bar_o[x]);
+                    w16_prev = w16;
                 }
-                width_prev = width;
-                __syncwarp();
-            }
-            n += 2 * (it.je - it.jb);
+                n += 2 * (it.je - it.jb);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) no[x] += started[x] ? 1 : 0;
-        }
-        // nor may a product
-        if (lane == 0) {
+                for (int x = 0; x < 2; ++x) no[x] += started[x] ? 1 : 0;
+            }
+            // no product may be in flight when the block exits
             tc::umma_commit(&bar_drain);
             tc::mbar_drain(&bar_drain, 0, wc);
         }
@@ -342,10 +331,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         const int x = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_t = tmem + 128 * x + lanes, o_t = tmem + 256 + 128 * x + lanes;
         const f32x2 c2 = pk(p.c, p.c);
-        uint32_t ns = 0, no = 0;
+        uint32_t n = 0, ni = 0, ns = 0, no = 0;
         bool dead = false;
-        for (int item = blockIdx.x; item < items && !dead; item += gridDim.x) {
-            it.init(p, tm, item);
+        for (int item = blockIdx.x; item < items && !dead; n += 2 * (it.je - it.jb), item += gridDim.x, ++ni) {
+            if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc))) break;
+            it = sm_item[ni & 1u];
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&bar_item_read[ni & 1u]);
             // the row
             const int g = row % p.G, iq = row / p.G, bi = iq / it.ti, i = it.first_i(x) + iq - bi * it.ti, b = it.first_b(x) + bi;
             bool real = pick(it.valid, x) && bi < it.nb && b < p.batch;
@@ -453,6 +445,18 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         }
                         tmem_st16(s_t + 16 * c, w);
                     }
+                    if (width & 15) {
+                        // rows of V behind the last key, up to the next multiple of 16, may hold anything: cleared (by the warps of
+                        // both query tiles, each before its own product)
+                        const uint32_t nv = n + 2 * (j - it.jb) + 1;
+                        if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_full[nv % SLOTS], (nv / SLOTS) & 1u, wc))) { dead = true; break; }
+                        uint8_t *v = ring + (nv % SLOTS) * SLOT_BYTES;
+                        for (int e = (warp & 3) * 32 + lane; e < ((width + 15) / 16 * 16 - width) * 8 * NB; e += 128) {
+                            const int vr = width + e / (8 * NB), vc = e % (8 * NB);
+                            *reinterpret_cast<uint4 *>(v + (vc >> 3) * BLOCK + vr * 128 + (vc & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        tc::fence_async_smem();
+                    }
                 }
                 started = true;
                 tc::tmem_st_wait();
@@ -471,31 +475,66 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             const long long R = (((long long)b * p.kv_heads + it.h) * p.n_q + i) * p.G + g;
             const bool last = p.slots == 1;
             const long long at = (long long)(PREFIX ? it.part : p.p_slots + it.part) * p.rows_total + R;
-            __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.out) + b * p.os[0] + (long long)(it.h * p.G + g) * p.os[1] + (long long)i * p.os[2];
-            float *part = p.part_o + at * D;
+            // O is read as matrix fragments: of eight columns 8 b .. a lane has 2 (lane mod 4), + 1 of rows lane / 4 and lane / 4 + 8.
+            // The four lanes of a row then trade pieces so that each has 8 neighbouring channels of the four blocks: their stores
+            // are whole sectors, eight rows at a time, where a row per thread would touch 32 lines with every store.
+            const int quad = lane & 3;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                if (started) {
-                    tc::tmem_ld32(o_t + 32 * c, o);
-                    tc::tmem_ld_wait32(o);
+            for (int hrow = 0; hrow < 32; hrow += 16) {
+                float scale[2];
+                bool there[2];
+                long long to[2];
+                const long long to_own = last ? b * p.os[0] + (long long)(it.h * p.G + g) * p.os[1] + (long long)i * p.os[2] : at * D;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int from = hrow + 8 * u + lane / 4;
+                    scale[u] = __shfl_sync(0xffffffffu, inv, from);
+                    there[u] = __shfl_sync(0xffffffffu, (int)(real && (last || l != 0.f)), from) != 0;
+                    to[u] = __shfl_sync(0xffffffffu, to_own, from);
                 }
+#pragma unroll 1
+                for (int c = 0; c < D / 64; ++c) {
+                    uint32_t o[32];
+                    if (started) {
+                        tc::tmem_ld_frag(o_t + ((uint32_t)hrow << 16) + 64 * c, o);
+                        tc::tmem_ld_wait32(o);
+                    } else {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
-                if (real && last) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint4 w;
-                        w.x = pack_bf16(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
-                        w.y = pack_bf16(__uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
-                        w.z = pack_bf16(__uint_as_float(o[e + 4]), __uint_as_float(o[e + 5]));
-                        w.w = pack_bf16(__uint_as_float(o[e + 6]), __uint_as_float(o[e + 7]));
-                        *reinterpret_cast<uint4 *>(dst + 32 * c + e) = w;
+                        for (int e = 0; e < 32; ++e) o[e] = 0u;
                     }
-                } else if (real && l != 0.f) {
+                    if (last) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4 *>(part + 32 * c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int q4 = 0; q4 < 2; ++q4) {
+                                // blocks 4 q4 .. + 3: this lane's pair of columns of each, two at a time traded with the lane two, then one, on
+                                uint32_t a[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const int k = 4 * (4 * q4 + e) + 2 * u;
+                                    a[e] = scale[u] == 0.f ? 0u : pack_bf16(__uint_as_float(o[k]) * scale[u], __uint_as_float(o[k + 1]) * scale[u]);
+                                }
+                                const bool hi2 = quad & 2, hi1 = quad & 1;
+                                const uint32_t s0 = __shfl_xor_sync(0xffffffffu, hi2 ? a[0] : a[2], 2), s1 = __shfl_xor_sync(0xffffffffu, hi2 ? a[1] : a[3], 2);
+                                // now rows of a 2 x 2 of 2 x 2 blocks: c0, c1 from lanes quad and quad ^ 2 of blocks 2 (quad / 2), + 1
+                                const uint32_t c0 = hi2 ? s0 : a[0], c1 = hi2 ? s1 : a[1], c2_ = hi2 ? a[2] : s0, c3 = hi2 ? a[3] : s1;
+                                const uint32_t t0 = __shfl_xor_sync(0xffffffffu, hi1 ? c0 : c1, 1), t1 = __shfl_xor_sync(0xffffffffu, hi1 ? c2_ : c3, 1);
+                                uint4 w;
+                                w.x = hi1 ? t0 : c0;
+                                w.y = hi1 ? c1 : t0;
+                                w.z = hi1 ? t1 : c2_;
+                                w.w = hi1 ? c3 : t1;
+                                if (there[u]) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + to[u] + 64 * c + 32 * q4 + 8 * quad) = w;
+                            }
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (there[u])
+                                    *reinterpret_cast<float2 *>(p.part_o + to[u] + 64 * c + 8 * k + 2 * quad) =
+                                        make_float2(__uint_as_float(o[4 * k + 2 * u]) * scale[u], __uint_as_float(o[4 * k + 2 * u + 1]) * scale[u]);
+                    }
                 }
             }
             if (started) {
