@@ -4,10 +4,10 @@
 // keys that they see.  A tile is `ti` queries x the G heads of the group (so its rows see nearly the same keys and a window
 // wastes little), over a shared prefix also `nb` sequences.  Keys come in tiles of 128: first the sinks, in a tile of their own
 // that is only as wide as needed, then the window's range.
-//   warp 9, a thread    works out the items (ahead of the others, who read them from shared memory); Q, K and V tiles by TMA
+//   warp 10, a thread   works out the items (ahead of the others, who read them from shared memory); Q, K and V tiles by TMA
 //                       (128-byte swizzle) into a ring of K and V slots
-//   warp 8, a thread    S = Q K^T into tensor memory, O += P V with P from tensor memory; the two query tiles take turns, so the
-//                       products of one run while the softmax of the other does
+//   warps 8, 9          products of the first and the second query tile: S = Q K^T into tensor memory, O += P V with P from
+//                       tensor memory; those of one tile run while the softmax of the other does
 //   warps 0-3, 4-7      softmax of the first and the second query tile, a row per thread, weights to bf16 over the logits'
 //                       columns, their fp32 sum; after the last tile O / sum to memory
 //
@@ -31,8 +31,9 @@
 namespace obf {
 
 constexpr int AT_TILE = 128;
-constexpr int AT_THREADS = 320;
+constexpr int AT_THREADS = 352;
 constexpr float AT_RAISE = 64.f;
+constexpr int AT_POLY = 3;                                // of every three pairs of weights one by exp2_poly
 
 template <int D>
 struct AttendTcShape {
@@ -140,15 +141,35 @@ struct AttendTcItem {
             width = min(AT_TILE, hi - j0);
         }
     }
-
-    __device__ __forceinline__ bool active(int x, int j) const { return j < pick(sk, x) || (j >= pick(ja, x) && j < pick(jz, x)); }
 };
 
-// D[tmem] (+)= A[tmem] * B, K = 16 per instruction: A holds two bf16 of a row per column.
-__device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+// The warp that issues the products runs as a whole, one lane of it issuing: with operands that the compiler knows to be the
+// same in all lanes they stay in uniform registers, and a product costs a handful of instructions.  (A single thread in a branch
+// of its own cost 110 cycles of issue per product, more than the 64 that the product takes.)
+__device__ __forceinline__ void umma_ss(bool leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+    asm volatile("{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %5, 0;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"((int)leader) : "memory");
+}
+
+// The same with A in tensor memory, two bf16 of a row per column.
+__device__ __forceinline__ void umma_ts(bool leader, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %5, 0;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"((int)leader) : "memory");
+}
+
+__device__ __forceinline__ void umma_done(bool leader, uint64_t *bar)
+{
+    asm volatile("{\n .reg .pred e;\n setp.ne.b32 e, %1, 0;\n @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}"
+                 ::"r"(tc::smem_u32(bar)), "r"((int)leader) : "memory");
+}
+
+// tc::mbar_wait by a whole warp, which goes on as one.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, const tc::WaitCtx &w)
+{
+    if (__all_sync(0xffffffffu, tc::mbar_try(bar, parity))) return true;
+    return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, w));
 }
 
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
@@ -161,6 +182,35 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map
 {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                  ::"r"(dst), "l"(map), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+
+// The larger of three, NaN if one is.
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// 2^x of a pair on the multiply-add units, for a share of the weights: the special-function unit's 16 results per cycle would
+// otherwise be the narrowest place.  x = n + f with |f| <= 1/2 (n by adding and subtracting 1.5 * 2^23), a polynomial of degree
+// four in f whose relative error is evenly spread (exchange algorithm; 2.7e-6 at most in fp32, 4e-8 on average), n added to the
+// exponent.  For x < 127; below -126 the result is 2^-126 (bf16 weights and an fp32 sum whose other terms are near one); not for NaN.
+__device__ __forceinline__ void exp2_poly(f32x2 x, float &a, float &b)
+{
+    float x0, x1;
+    upk(x, x0, x1);
+    x = pk(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+    const f32x2 y = add2(x, pk(12582912.f, 12582912.f)), f = fma2(add2(y, pk(-12582912.f, -12582912.f)), pk(-1.f, -1.f), x);
+    f32x2 q = fma2(f, pk(0.009570102207362652f, 0.009570102207362652f), pk(0.05591785907745361f, 0.05591785907745361f));
+    q = fma2(q, f, pk(0.240247443318367f, 0.240247443318367f));
+    q = fma2(q, f, pk(0.6931217908859253f, 0.6931217908859253f));
+    q = fma2(q, f, pk(0.9999992847442627f, 0.9999992847442627f));
+    float q0, q1, y0, y1;
+    upk(q, q0, q1);
+    upk(y, y0, y1);
+    a = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(y0) << 23));
+    b = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(y1) << 23));
 }
 
 // Bits of columns a .. b - 1 of 32.
@@ -180,7 +230,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     extern __shared__ uint8_t at_smem_raw[];
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *q_sm = base, *ring = base + 2 * SLOT_BYTES;
-    __shared__ uint64_t bar_full[SLOTS], bar_empty[SLOTS], bar_q_full, bar_q_empty, bar_drain;
+    __shared__ uint64_t bar_full[SLOTS], bar_empty[SLOTS], bar_q_full, bar_q_empty, bar_drain[2];
     __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2], bar_item[2], bar_item_read[2];
     __shared__ AttendTcItem<PREFIX> sm_item[2];
     __shared__ uint32_t s_tmem, s_abort;
@@ -188,17 +238,17 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     tc::WaitCtx wc{&s_abort, p.status, p.wait_limit_ns};
     if (tid == 0) {
         s_abort = 0u;
-        for (int i = 0; i < SLOTS; ++i) { tc::mbar_init(&bar_full[i], 1); tc::mbar_init(&bar_empty[i], 1); }
+        for (int i = 0; i < SLOTS; ++i) { tc::mbar_init(&bar_full[i], 1); tc::mbar_init(&bar_empty[i], 2); }
         tc::mbar_init(&bar_q_full, 1);
-        tc::mbar_init(&bar_q_empty, 1);
-        tc::mbar_init(&bar_drain, 1);
+        tc::mbar_init(&bar_q_empty, 2);
         for (int x = 0; x < 2; ++x) {
             tc::mbar_init(&bar_s[x], 1);
             tc::mbar_init(&bar_p[x], 4);
             tc::mbar_init(&bar_o[x], 1);
             tc::mbar_init(&bar_o_read[x], 4);
             tc::mbar_init(&bar_item[x], 1);
-            tc::mbar_init(&bar_item_read[x], 9);
+            tc::mbar_init(&bar_item_read[x], 10);
+            tc::mbar_init(&bar_drain[x], 1);
         }
         tc::mbar_init_fence();
     }
@@ -211,7 +261,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     if (first && blockIdx.x == 0) attend_status(p);
 
     AttendTcItem<PREFIX> it;
-    if (warp == 9) {
+    if (warp == 10) {
         // ---------------- copies ----------------
         if (lane == 0) {
             uint32_t n = 0, nq = 0, ni = 0;
@@ -222,15 +272,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 sm_item[ni & 1u] = it;
                 tc::mbar_arrive(&bar_item[ni & 1u]);
                 if (it.jb >= it.je) continue;
-                if (!tc::mbar_wait(&bar_q_empty, (nq & 1u) ^ 1u, wc)) break;
-                const int rows = p.G * it.ti * it.nb, loads = (it.valid[0] ? NB : 0) + (it.valid[1] ? NB : 0);
-                tc::mbar_expect_tx(&bar_q_full, (uint32_t)(loads * rows * 128));
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (it.valid[x])
-                        for (int c = 0; c < NB; ++c)
-                            tma_load_4d(tc::smem_u32(q_sm + x * SLOT_BYTES + c * BLOCK), &tm.q, &bar_q_full, 64 * c, it.h * p.G, it.first_i(x), it.first_b(x));
-                ++nq;
                 for (int j = it.jb; j < it.je && !dead; ++j) {
                     int j0, width;
                     it.tile(j, j0, width);
@@ -242,89 +283,109 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                                      ::"r"(tc::smem_u32(ring + sl * SLOT_BYTES)), "l"(kv ? &tm.v : &tm.k), "r"(tc::smem_u32(&bar_full[sl])), "r"(0), "r"(j0), "r"(it.h),
                                        "r"(PREFIX ? 0 : it.b) : "memory");
                     }
+                    if (j > it.jb || dead) continue;
+                    // the queries behind the first tile of keys, which need not wait until the last item's are done with
+                    if (!tc::mbar_wait(&bar_q_empty, (nq & 1u) ^ 1u, wc)) { dead = true; break; }
+                    const int rows = p.G * it.ti * it.nb, loads = (it.valid[0] ? NB : 0) + (it.valid[1] ? NB : 0);
+                    tc::mbar_expect_tx(&bar_q_full, (uint32_t)(loads * rows * 128));
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (it.valid[x])
+                            for (int c = 0; c < NB; ++c)
+                                tma_load_4d(tc::smem_u32(q_sm + x * SLOT_BYTES + c * BLOCK), &tm.q, &bar_q_full, 64 * c, it.h * p.G, it.first_i(x), it.first_b(x));
+                    ++nq;
                 }
             }
             // nothing that this thread started may be in flight when the block exits
             for (uint32_t j = n > (uint32_t)SLOTS ? n - SLOTS : 0u; j < n; ++j) tc::mbar_drain(&bar_full[j % SLOTS], (j / SLOTS) & 1u, wc);
             if (nq) tc::mbar_drain(&bar_q_full, (nq - 1) & 1u, wc);
         }
-    } else if (warp == 8) {
+    } else if (warp >= 8) {
         // ---------------- products ----------------
-        if (lane == 0) {
-            constexpr uint32_t idesc_o = tc::idesc_bf16(128, D, 0, 1);
-            uint32_t n = 0, nq = 0, ni = 0, ns[2] = {0, 0}, no[2] = {0, 0};
-            bool dead = false;
-            for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
-                if (!tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc)) break;
-                it = sm_item[ni & 1u];
-                tc::mbar_arrive(&bar_item_read[ni & 1u]);
-                if (it.jb >= it.je) continue;
-                if (!tc::mbar_wait(&bar_q_full, nq & 1u, wc)) break;
-                ++nq;
-                bool pending[2] = {false, false}, started[2] = {false, false};
-                int w16_prev = 0;
-                // ring positions: K of tile j at n + 2 (j - jb), V behind it
-                for (int j = it.jb; j <= it.je && !dead; ++j) {
-                    int w16 = 0;
-                    const uint32_t nk = n + 2 * (j - it.jb), nv = nk - 1, slot_k = nk % SLOTS, slot_v = nv % SLOTS;
-                    if (j < it.je) {
+        const bool leader = lane == 0;
+        const int x = warp_uniform(warp - 8);
+        const uint32_t tm_u = warp_uniform((int)tmem), q_u = warp_uniform((int)tc::smem_u32(q_sm)), ring_u = warp_uniform((int)tc::smem_u32(ring));
+        const uint32_t s_t = tm_u + 128 * x, o_t = tm_u + 256 + 128 * x;
+        const uint64_t qd = tc::smem_desc_sw128(q_u + x * SLOT_BYTES, 16, 1024);
+        constexpr uint32_t idesc_o = tc::idesc_bf16(128, D, 0, 1);
+        uint32_t n = 0, nq = 0, ni = 0, ns = 0, no = 0;
+        bool dead = false;
+        for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
+            if (!mbar_wait_warp(&bar_item[ni & 1u], (ni >> 1) & 1u, wc)) break;
+            const AttendTcItem<PREFIX> &im = sm_item[ni & 1u];
+            it.jb = warp_uniform(im.jb);
+            it.je = warp_uniform(im.je);
+            it.s = warp_uniform(im.s);
+            it.lo = warp_uniform(im.lo);
+            it.hi = warp_uniform(im.hi);
+            it.nsink = warp_uniform(im.nsink);
+            const int sk = warp_uniform(im.sk[x]), ja = warp_uniform(im.ja[x]), jz = warp_uniform(im.jz[x]);
+            if (leader) tc::mbar_arrive(&bar_item_read[ni & 1u]);
+            __syncwarp();
+            if (it.jb >= it.je) continue;
+            if (!mbar_wait_warp(&bar_q_full, nq & 1u, wc)) break;
+            ++nq;
+            bool pending = false, started = false;
+            int w16_prev = 0;
+            // ring positions: K of tile j at n + 2 (j - jb), V behind it
+            for (int j = it.jb; j <= it.je; ++j) {
+                int w16 = 0;
+                const uint32_t nk = n + 2 * (j - it.jb), nv = nk - 1, slot_k = nk % SLOTS, slot_v = nv % SLOTS;
+                if (j > it.jb) {
+                    if (!mbar_wait_warp(&bar_full[slot_v], (nv / SLOTS) & 1u, wc)) { dead = true; break; }
+                    if (pending) {
+                        // 16 keys of V on: 2048 bytes, 128 in the descriptor
+                        const uint64_t vd = tc::smem_desc_sw128(ring_u + slot_v * SLOT_BYTES, BLOCK, 1024);
+                        if (!started && !mbar_wait_warp(&bar_o_read[x], (no & 1u) ^ 1u, wc)) { dead = true; break; }
+                        if (!mbar_wait_warp(&bar_p[x], (ns - 1) & 1u, wc)) { dead = true; break; }
+                        tc::tc_fence_after();
+                        if (w16_prev == AT_TILE) {
+#pragma unroll
+                            for (int k = 0; k < AT_TILE / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
+                        } else {
+                            for (int k = 0; k < w16_prev / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
+                        }
+                        started = true;
+                        pending = false;
+                        umma_done(leader, &bar_empty[slot_v]);
+                    } else if (leader) {
+                        tc::mbar_arrive(&bar_empty[slot_v]);
+                    }
+                }
+                if (j < it.je) {
+                    if (!mbar_wait_warp(&bar_full[slot_k], (nk / SLOTS) & 1u, wc)) { dead = true; break; }
+                    if (j < sk || (j >= ja && j < jz)) {
                         int j0, width;
                         it.tile(j, j0, width);
                         w16 = (width + 15) & ~15;
-                        if (!tc::mbar_wait(&bar_full[slot_k], (nk / SLOTS) & 1u, wc)) { dead = true; break; }
-                    }
-                    if (j > it.jb && !tc::mbar_wait(&bar_full[slot_v], (nv / SLOTS) & 1u, wc)) { dead = true; break; }
-                    // 16 keys of V on: 2048 bytes, 128 in the descriptor
-                    const uint64_t vd = tc::smem_desc_sw128(tc::smem_u32(ring + slot_v * SLOT_BYTES), BLOCK, 1024);
-                    const uint64_t kd = tc::smem_desc_sw128(tc::smem_u32(ring + slot_k * SLOT_BYTES), 16, 1024);
-                    const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
+                        const uint64_t kd = tc::smem_desc_sw128(ring_u + slot_k * SLOT_BYTES, 16, 1024);
+                        const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const uint32_t s_t = tmem + 128 * x, o_t = tmem + 256 + 128 * x;
-                        if (pending[x]) {
-                            if (!started[x] && !tc::mbar_wait(&bar_o_read[x], (no[x] & 1u) ^ 1u, wc)) { dead = true; break; }
-                            if (!tc::mbar_wait(&bar_p[x], (ns[x] - 1) & 1u, wc)) { dead = true; break; }
-                            tc::tc_fence_after();
-                            if (w16_prev == AT_TILE) {
-#pragma unroll
-                                for (int k = 0; k < AT_TILE / 16; ++k) umma_bf16_ta(o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started[x] || k > 0) ? 1u : 0u);
-                            } else {
-                                for (int k = 0; k < w16_prev / 16; ++k) umma_bf16_ta(o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started[x] || k > 0) ? 1u : 0u);
-                            }
-                            started[x] = true;
-                            pending[x] = false;
-                            if (j == it.je) tc::umma_commit(&bar_o[x]);
-                        } else if (j == it.je && started[x]) {
-                            tc::umma_commit(&bar_o[x]);
+                        for (int k = 0; k < D / 16; ++k) {
+                            // 16 channels on: 32 bytes, every 64 the next column block; descriptors count 16 bytes
+                            const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / 16;
+                            umma_ss(leader, s_t, qd + off, kd + off, idesc_s, k > 0);
                         }
-                        if (j < it.je && it.active(x, j)) {
-                            tc::tc_fence_after();
-                            const uint64_t qd = tc::smem_desc_sw128(tc::smem_u32(q_sm + x * SLOT_BYTES), 16, 1024);
-#pragma unroll
-                            for (int k = 0; k < D / 16; ++k) {
-                                // 16 channels on: 32 bytes, every 64 the next column block; descriptors count 16 bytes
-                                const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / 16;
-                                tc::umma_bf16(s_t, qd + off, kd + off, idesc_s, k > 0);
-                            }
-                            tc::umma_commit(&bar_s[x]);
-                            ++ns[x];
-                            pending[x] = true;
-                        }
+                        umma_done(leader, &bar_s[x]);
+                        umma_done(leader, &bar_empty[slot_k]);
+                        ++ns;
+                        pending = true;
+                    } else if (leader) {
+                        tc::mbar_arrive(&bar_empty[slot_k]);
                     }
-                    if (dead) break;
-                    if (j > it.jb) tc::umma_commit(&bar_empty[slot_v]);
-                    if (j < it.je) tc::umma_commit(&bar_empty[slot_k]);
-                    if (j == it.je - 1) tc::umma_commit(&bar_q_empty);
-                    w16_prev = w16;
+                    if (j == it.je - 1) umma_done(leader, &bar_q_empty);
+                } else if (started) {
+                    umma_done(leader, &bar_o[x]);
                 }
-                n += 2 * (it.je - it.jb);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) no[x] += started[x] ? 1 : 0;
+                w16_prev = w16;
+                __syncwarp();
             }
-            // no product may be in flight when the block exits
-            tc::umma_commit(&bar_drain);
-            tc::mbar_drain(&bar_drain, 0, wc);
+            n += 2 * (it.je - it.jb);
+            no += started ? 1 : 0;
         }
+        // no product may be in flight when the block exits
+        umma_done(leader, &bar_drain[x]);
+        tc::mbar_drain(&bar_drain[x], 0, wc);
         __syncwarp();
     } else {
         // ---------------- softmax ----------------
@@ -344,7 +405,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             if (PREFIX) real = real && i < attend_q_len(p, b);
             else real = real && i < it.ql;
             const int t = PREFIX || !real ? 0 : it.t + i, sk = pick(it.sk, x), ja = pick(it.ja, x), jz = pick(it.jz, x), fa = pick(it.fa, x), fz = pick(it.fz, x);
-            float m = -INFINITY;
+            float m = real ? -INFINITY : 0.f;            // (rows that are none have a reference from the start)
             f32x2 l2 = 0ull;
             bool started = false;
             for (int j = it.jb; j < it.je; ++j) {
@@ -352,11 +413,24 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_s[x], ns & 1u, wc))) { dead = true; break; }
                 ++ns;
                 tc::tc_fence_after();
+                int j0, width;
+                it.tile(j, j0, width);
+                // columns of chunk c (32 of them) that the row sees
+                auto seen = [&](int c) {
+                    uint32_t bits = column_bits(0, width - 32 * c);
+                    if (!PREFIX) {
+                        // keys up to the row's position, and behind its window's lower end or among the first tokens
+                        const int a = j0 + 32 * c;
+                        const uint32_t in = p.window ? column_bits(t - p.window + 1 - a, 32) | column_bits(0, p.sinks - a) : 0xFFFFFFFFu;
+                        bits &= real ? in & column_bits(0, t + 1 - a) : 0u;
+                    }
+                    return bits;
+                };
                 bool formed = false;                      // the tile's weights
-                if (started && j >= fa && j < fz) {
-                    // every row sees all 128 keys and has a reference
-                    const float ref = m == -INFINITY ? 0.f : -m;
-                    const f32x2 r2 = pk(ref, ref);
+                if (width == AT_TILE && __all_sync(0xffffffffu, m > -INFINITY)) {
+                    // every row has a reference, and a sum that the 2^-126 of exp2_poly for a hidden key does not show in
+                    const bool full = j >= fa && j < fz;
+                    const f32x2 r2 = pk(-m, -m);
                     float mx = -INFINITY;
                     f32x2 z = 0ull;
                     uint32_t w[4][16], r[2][32];
@@ -365,19 +439,31 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     for (int c = 0; c < 4; ++c) {
                         tc::tmem_ld_wait32(r[c & 1]);
                         if (c < 3) tc::tmem_ld32(s_t + 32 * (c + 1), r[(c + 1) & 1]);
+                        if (!full) {
+                            const uint32_t bits = seen(c);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(bits >> e & 1u)) r[c & 1][e] = 0xFF800000u;
+                        }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const float s0 = __uint_as_float(r[c & 1][2 * e]), s1 = __uint_as_float(r[c & 1][2 * e + 1]);
-                            mx = fmaxf(mx, fmaxf(s0, s1));
+                            mx = max3_nan(mx, s0, s1);
+                            const f32x2 y = fma2(pk(s0, s1), c2, r2);
                             float a, b2;
-                            upk(fma2(pk(s0, s1), c2, r2), a, b2);
-                            a = ex2(a);
-                            b2 = ex2(b2);
+                            if (e % AT_POLY == 1) {
+                                exp2_poly(y, a, b2);
+                            } else {
+                                upk(y, a, b2);
+                                a = ex2(a);
+                                b2 = ex2(b2);
+                            }
                             z = add2(z, pk(a, b2));
                             w[c][e] = pack_bf16(a, b2);
                         }
                     }
-                    if (!__any_sync(0xffffffffu, mx * p.c > m + AT_RAISE)) {
+                    // (a maximum that is not a number sends the tile the other way, too, where it spreads)
+                    if (__all_sync(0xffffffffu, mx * p.c <= m + AT_RAISE || mx == -INFINITY)) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c) tmem_st16(s_t + 16 * c, w[c]);
                         l2 = add2(l2, z);
@@ -385,18 +471,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     }
                 }
                 if (!formed) {
-                    int j0, width;
-                    it.tile(j, j0, width);
                     const int nch = (width + 31) >> 5;
                     auto load = [&](uint32_t (&r)[32], int c) {
                         tc::tmem_ld32(s_t + 32 * c, r);
-                        uint32_t bits = column_bits(0, width - 32 * c);
-                        if (!PREFIX) {
-                            // keys up to the row's position, and behind its window's lower end or among the first tokens
-                            const int a = j0 + 32 * c;
-                            const uint32_t in = p.window ? column_bits(t - p.window + 1 - a, 32) | column_bits(0, p.sinks - a) : 0xFFFFFFFFu;
-                            bits &= real ? in & column_bits(0, t + 1 - a) : 0u;
-                        }
+                        const uint32_t bits = seen(c);
                         tc::tmem_ld_wait32(r);
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
