@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *q_sm = base, *ring = base + 2 * SLOT_BYTES;
     __shared__ uint64_t bar_full[SLOTS], bar_empty[SLOTS], bar_q_full, bar_q_empty, bar_drain[2];
-    __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2], bar_item[2], bar_item_read[2];
+    __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2], bar_item[2], bar_item_read[2], bar_turn[2];
     __shared__ AttendTcItem<PREFIX> sm_item[2];
     __shared__ uint32_t s_tmem, s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -249,6 +249,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             tc::mbar_init(&bar_item[x], 1);
             tc::mbar_init(&bar_item_read[x], 10);
             tc::mbar_init(&bar_drain[x], 1);
+            tc::mbar_init(&bar_turn[x], 1);
         }
         tc::mbar_init_fence();
     }
@@ -308,7 +309,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         const uint32_t s_t = tm_u + 128 * x, o_t = tm_u + 256 + 128 * x;
         const uint64_t qd = tc::smem_desc_sw128(q_u + x * SLOT_BYTES, 16, 1024);
         constexpr uint32_t idesc_o = tc::idesc_bf16(128, D, 0, 1);
-        uint32_t n = 0, nq = 0, ni = 0, ns = 0, no = 0;
+        uint32_t n = 0, nq = 0, ni = 0, ns = 0, no = 0, nt = 0;
         bool dead = false;
         for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
             if (!mbar_wait_warp(&bar_item[ni & 1u], (ni >> 1) & 1u, wc)) break;
@@ -333,50 +334,50 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 const uint32_t nk = n + 2 * (j - it.jb), nv = nk - 1, slot_k = nk % SLOTS, slot_v = nv % SLOTS;
                 if (j > it.jb) {
                     if (!mbar_wait_warp(&bar_full[slot_v], (nv / SLOTS) & 1u, wc)) { dead = true; break; }
-                    if (pending) {
-                        // 16 keys of V on: 2048 bytes, 128 in the descriptor
-                        const uint64_t vd = tc::smem_desc_sw128(ring_u + slot_v * SLOT_BYTES, BLOCK, 1024);
-                        if (!started && !mbar_wait_warp(&bar_o_read[x], (no & 1u) ^ 1u, wc)) { dead = true; break; }
-                        if (!mbar_wait_warp(&bar_p[x], (ns - 1) & 1u, wc)) { dead = true; break; }
-                        tc::tc_fence_after();
-                        if (w16_prev == AT_TILE) {
-#pragma unroll
-                            for (int k = 0; k < AT_TILE / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
-                        } else {
-                            for (int k = 0; k < w16_prev / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
-                        }
-                        started = true;
-                        pending = false;
-                        umma_done(leader, &bar_empty[slot_v]);
-                    } else if (leader) {
-                        tc::mbar_arrive(&bar_empty[slot_v]);
-                    }
+                    if (pending && !started && !mbar_wait_warp(&bar_o_read[x], (no & 1u) ^ 1u, wc)) { dead = true; break; }
                 }
-                if (j < it.je) {
-                    if (!mbar_wait_warp(&bar_full[slot_k], (nk / SLOTS) & 1u, wc)) { dead = true; break; }
-                    if (j < sk || (j >= ja && j < jz)) {
-                        int j0, width;
-                        it.tile(j, j0, width);
-                        w16 = (width + 15) & ~15;
-                        const uint64_t kd = tc::smem_desc_sw128(ring_u + slot_k * SLOT_BYTES, 16, 1024);
-                        const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
+                if (j < it.je && !mbar_wait_warp(&bar_full[slot_k], (nk / SLOTS) & 1u, wc)) { dead = true; break; }
+                if (pending && !mbar_wait_warp(&bar_p[x], (ns - 1) & 1u, wc)) { dead = true; break; }
+                // The two warps take turns: left alone they fall into step, both tiles in their softmax, then both in their products.
+                if (!mbar_wait_warp(&bar_turn[x], (nt & 1u) ^ (uint32_t)(x ^ 1), wc)) { dead = true; break; }
+                ++nt;
+                tc::tc_fence_after();
+                if (pending) {
+                    // 16 keys of V on: 2048 bytes, 128 in the descriptor
+                    const uint64_t vd = tc::smem_desc_sw128(ring_u + slot_v * SLOT_BYTES, BLOCK, 1024);
+                    if (w16_prev == AT_TILE) {
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k) {
-                            // 16 channels on: 32 bytes, every 64 the next column block; descriptors count 16 bytes
-                            const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / 16;
-                            umma_ss(leader, s_t, qd + off, kd + off, idesc_s, k > 0);
-                        }
-                        umma_done(leader, &bar_s[x]);
-                        umma_done(leader, &bar_empty[slot_k]);
-                        ++ns;
-                        pending = true;
-                    } else if (leader) {
-                        tc::mbar_arrive(&bar_empty[slot_k]);
+                        for (int k = 0; k < AT_TILE / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
+                    } else {
+                        for (int k = 0; k < w16_prev / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
                     }
-                    if (j == it.je - 1) umma_done(leader, &bar_q_empty);
-                } else if (started) {
-                    umma_done(leader, &bar_o[x]);
+                    started = true;
+                    umma_done(leader, &bar_empty[slot_v]);
+                } else if (j > it.jb && leader) {
+                    tc::mbar_arrive(&bar_empty[slot_v]);
                 }
+                pending = j < it.je && (j < sk || (j >= ja && j < jz));
+                if (pending) {
+                    int j0, width;
+                    it.tile(j, j0, width);
+                    w16 = (width + 15) & ~15;
+                    const uint64_t kd = tc::smem_desc_sw128(ring_u + slot_k * SLOT_BYTES, 16, 1024);
+                    const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        // 16 channels on: 32 bytes, every 64 the next column block; descriptors count 16 bytes
+                        const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / 16;
+                        umma_ss(leader, s_t, qd + off, kd + off, idesc_s, k > 0);
+                    }
+                    umma_done(leader, &bar_s[x]);
+                    umma_done(leader, &bar_empty[slot_k]);
+                    ++ns;
+                } else if (j < it.je && leader) {
+                    tc::mbar_arrive(&bar_empty[slot_k]);
+                }
+                if (leader) tc::mbar_arrive(&bar_turn[x ^ 1]);
+                if (j == it.je - 1) umma_done(leader, &bar_q_empty);
+                if (j == it.je && started) umma_done(leader, &bar_o[x]);
                 w16_prev = w16;
                 __syncwarp();
             }
