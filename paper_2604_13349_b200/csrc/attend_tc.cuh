@@ -4,12 +4,13 @@
 // keys that they see.  A tile is `ti` queries x the G heads of the group (so its rows see nearly the same keys and a window
 // wastes little), over a shared prefix also `nb` sequences.  Keys come in tiles of 128: first the sinks, in a tile of their own
 // that is only as wide as needed, then the window's range.
-//   warp 10, a thread   works out the items (ahead of the others, who read them from shared memory); Q, K and V tiles by TMA
+//   warp 18, a thread   works out the items (ahead of the others, who read them from shared memory); Q, K and V tiles by TMA
 //                       (128-byte swizzle) into a ring of K and V slots
-//   warps 8, 9          products of the first and the second query tile: S = Q K^T into tensor memory, O += P V with P from
+//   warps 16, 17        products of the first and the second query tile: S = Q K^T into tensor memory, O += P V with P from
 //                       tensor memory; those of one tile run while the softmax of the other does
-//   warps 0-3, 4-7      softmax of the first and the second query tile, a row per thread, weights to bf16 over the logits'
-//                       columns, their fp32 sum; after the last tile O / sum to memory
+//   warps 0-7, 8-15     softmax of the first and the second query tile, two threads per row with 64 keys each (one would take
+//                       twice as long for its tile, and the products wait for it), weights to bf16 over the logits' columns,
+//                       their fp32 sum; after the last tile O / sum to memory
 //
 // Softmax: fp32 and bf16 have the same exponents, so a row's reference need not be its maximum, only within 2^64 of it: the
 // maximum of the first tile of keys that the row sees serves, the logits are read once, and their maximum is formed beside the
@@ -31,7 +32,7 @@
 namespace obf {
 
 constexpr int AT_TILE = 128;
-constexpr int AT_THREADS = 352;
+constexpr int AT_THREADS = 608;
 constexpr float AT_RAISE = 64.f;
 constexpr int AT_POLY = 3;                                // of every three pairs of weights one by exp2_poly
 
@@ -172,6 +173,19 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, c
     return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, w));
 }
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
+
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
@@ -233,6 +247,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     __shared__ uint64_t bar_full[SLOTS], bar_empty[SLOTS], bar_q_full, bar_q_empty, bar_drain[2];
     __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2], bar_item[2], bar_item_read[2], bar_turn[2];
     __shared__ AttendTcItem<PREFIX> sm_item[2];
+    __shared__ float sm_row[2][AT_TILE];                  // a row's two threads trade their maxima and sums
     __shared__ uint32_t s_tmem, s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     tc::WaitCtx wc{&s_abort, p.status, p.wait_limit_ns};
@@ -243,17 +258,17 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         tc::mbar_init(&bar_q_empty, 2);
         for (int x = 0; x < 2; ++x) {
             tc::mbar_init(&bar_s[x], 1);
-            tc::mbar_init(&bar_p[x], 4);
+            tc::mbar_init(&bar_p[x], 8);
             tc::mbar_init(&bar_o[x], 1);
-            tc::mbar_init(&bar_o_read[x], 4);
+            tc::mbar_init(&bar_o_read[x], 8);
             tc::mbar_init(&bar_item[x], 1);
-            tc::mbar_init(&bar_item_read[x], 10);
+            tc::mbar_init(&bar_item_read[x], 18);
             tc::mbar_init(&bar_drain[x], 1);
             tc::mbar_init(&bar_turn[x], 1);
         }
         tc::mbar_init_fence();
     }
-    if (warp == 8) tc::tmem_alloc(&s_tmem, 512);
+    if (warp == 16) tc::tmem_alloc(&s_tmem, 512);
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -262,7 +277,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     if (first && blockIdx.x == 0) attend_status(p);
 
     AttendTcItem<PREFIX> it;
-    if (warp == 10) {
+    if (warp == 18) {
         // ---------------- copies ----------------
         if (lane == 0) {
             uint32_t n = 0, nq = 0, ni = 0;
@@ -301,10 +316,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             for (uint32_t j = n > (uint32_t)SLOTS ? n - SLOTS : 0u; j < n; ++j) tc::mbar_drain(&bar_full[j % SLOTS], (j / SLOTS) & 1u, wc);
             if (nq) tc::mbar_drain(&bar_q_full, (nq - 1) & 1u, wc);
         }
-    } else if (warp >= 8) {
+    } else if (warp >= 16) {
         // ---------------- products ----------------
         const bool leader = lane == 0;
-        const int x = warp_uniform(warp - 8);
+        const int x = warp_uniform(warp - 16);
         const uint32_t tm_u = warp_uniform((int)tmem), q_u = warp_uniform((int)tc::smem_u32(q_sm)), ring_u = warp_uniform((int)tc::smem_u32(ring));
         const uint32_t s_t = tm_u + 128 * x, o_t = tm_u + 256 + 128 * x;
         const uint64_t qd = tc::smem_desc_sw128(q_u + x * SLOT_BYTES, 16, 1024);
@@ -390,13 +405,35 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         __syncwarp();
     } else {
         // ---------------- softmax ----------------
-        const int x = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const int x = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, col0 = half * 64;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_t = tmem + 128 * x + lanes, o_t = tmem + 256 + 128 * x + lanes;
         const f32x2 c2 = pk(p.c, p.c);
+        // Whether the condition holds for some thread of the query tile; all 256 of them come here the same number of times,
+        // those whose wait ran out too, so that they leave together.
+        auto any = [&](bool c) {
+            uint32_t r;
+            tc::tc_fence_before();
+            __syncwarp();
+            asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %2, 0;\n barrier.cta.red.or.pred.aligned q, %1, 256, p;\n selp.u32 %0, 1, 0, q;\n}"
+                         : "=r"(r) : "r"(1 + x), "r"((int)c) : "memory");
+            tc::tc_fence_after();
+            return r != 0;
+        };
+        // The larger, or the sum, of a value of the row's two threads.
+        auto trade = [&](float v, bool sum) {
+            if (half) sm_row[x][row] = v;
+            any(false);
+            if (!half) {
+                v = sum ? v + sm_row[x][row] : fmaxf(v, sm_row[x][row]);
+                sm_row[x][row] = v;
+            }
+            any(false);
+            return sm_row[x][row];
+        };
         uint32_t n = 0, ni = 0, ns = 0, no = 0;
         bool dead = false;
         for (int item = blockIdx.x; item < items && !dead; n += 2 * (it.je - it.jb), item += gridDim.x, ++ni) {
-            if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc))) break;
+            if (any(!tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc))) break;
             it = sm_item[ni & 1u];
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&bar_item_read[ni & 1u]);
@@ -408,51 +445,53 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             const int t = PREFIX || !real ? 0 : it.t + i, sk = pick(it.sk, x), ja = pick(it.ja, x), jz = pick(it.jz, x), fa = pick(it.fa, x), fz = pick(it.fz, x);
             float m = real ? -INFINITY : 0.f;            // (rows that are none have a reference from the start)
             f32x2 l2 = 0ull;
-            bool started = false;
+            bool started = false, known = false;          // known: all rows have references
             for (int j = it.jb; j < it.je; ++j) {
                 if (!(j < sk || (j >= ja && j < jz))) continue;
-                if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_s[x], ns & 1u, wc))) { dead = true; break; }
+                const bool late = !tc::mbar_wait(&bar_s[x], ns & 1u, wc);
                 ++ns;
+                __syncwarp();
                 tc::tc_fence_after();
                 int j0, width;
                 it.tile(j, j0, width);
-                // columns of chunk c (32 of them) that the row sees
+                // of 32 columns from col0 + 32 c on, those that the row sees
                 auto seen = [&](int c) {
-                    uint32_t bits = column_bits(0, width - 32 * c);
+                    uint32_t bits = column_bits(0, width - col0 - 32 * c);
                     if (!PREFIX) {
                         // keys up to the row's position, and behind its window's lower end or among the first tokens
-                        const int a = j0 + 32 * c;
+                        const int a = j0 + col0 + 32 * c;
                         const uint32_t in = p.window ? column_bits(t - p.window + 1 - a, 32) | column_bits(0, p.sinks - a) : 0xFFFFFFFFu;
                         bits &= real ? in & column_bits(0, t + 1 - a) : 0u;
                     }
                     return bits;
                 };
                 bool formed = false;                      // the tile's weights
-                if (width == AT_TILE && __all_sync(0xffffffffu, m > -INFINITY)) {
+                uint32_t w[32];
+                if (known && width == AT_TILE) {
                     // every row has a reference, and a sum that the 2^-126 of exp2_poly for a hidden key does not show in
                     const bool full = j >= fa && j < fz;
                     const f32x2 r2 = pk(-m, -m);
                     float mx = -INFINITY;
                     f32x2 z = 0ull;
-                    uint32_t w[4][16], r[2][32];
-                    tc::tmem_ld32(s_t, r[0]);
+                    uint32_t r[2][16];
+                    tmem_ld16(s_t + col0, r[0]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        tc::tmem_ld_wait32(r[c & 1]);
-                        if (c < 3) tc::tmem_ld32(s_t + 32 * (c + 1), r[(c + 1) & 1]);
+                        tmem_ld_wait16(r[c & 1]);
+                        if (c < 3) tmem_ld16(s_t + col0 + 16 * (c + 1), r[(c + 1) & 1]);
                         if (!full) {
-                            const uint32_t bits = seen(c);
+                            const uint32_t bits = seen(c >> 1) >> (c & 1) * 16;
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
+                            for (int e = 0; e < 16; ++e)
                                 if (!(bits >> e & 1u)) r[c & 1][e] = 0xFF800000u;
                         }
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
+                        for (int e = 0; e < 8; ++e) {
                             const float s0 = __uint_as_float(r[c & 1][2 * e]), s1 = __uint_as_float(r[c & 1][2 * e + 1]);
                             mx = max3_nan(mx, s0, s1);
                             const f32x2 y = fma2(pk(s0, s1), c2, r2);
                             float a, b2;
-                            if (e % AT_POLY == 1) {
+                            if ((8 * c + e) % AT_POLY == 1) {
                                 exp2_poly(y, a, b2);
                             } else {
                                 upk(y, a, b2);
@@ -460,21 +499,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                                 b2 = ex2(b2);
                             }
                             z = add2(z, pk(a, b2));
-                            w[c][e] = pack_bf16(a, b2);
+                            w[8 * c + e] = pack_bf16(a, b2);
                         }
                     }
                     // (a maximum that is not a number sends the tile the other way, too, where it spreads)
-                    if (__all_sync(0xffffffffu, mx * p.c <= m + AT_RAISE || mx == -INFINITY)) {
+                    if (!any(late || !(mx * p.c <= m + AT_RAISE || mx == -INFINITY))) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) tmem_st16(s_t + 16 * c, w[c]);
+                        for (int c = 0; c < 2; ++c) tmem_st16(s_t + 32 * half + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                         l2 = add2(l2, z);
                         formed = true;
                     }
                 }
                 if (!formed) {
-                    const int nch = (width + 31) >> 5;
+                    if (any(late)) { dead = true; break; }
+                    const int nch = min(2, max(0, width - col0 + 31) >> 5);
                     auto load = [&](uint32_t (&r)[32], int c) {
-                        tc::tmem_ld32(s_t + 32 * c, r);
+                        tc::tmem_ld32(s_t + col0 + 32 * c, r);
                         const uint32_t bits = seen(c);
                         tc::tmem_ld_wait32(r);
 #pragma unroll
@@ -489,29 +529,31 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(r[e]), __uint_as_float(r[e + 1])));
                     }
-                    mx *= p.c;
+                    mx = trade(mx, false) * p.c;
                     // (a maximum below the reference changes nothing)
-                    if (__any_sync(0xffffffffu, started ? mx > m + AT_RAISE : true)) {
+                    if (any(started ? mx > m + AT_RAISE : true)) {
                         const float f = mx > m ? ex2(m - mx) : 1.f;
                         m = fmaxf(m, mx);
                         l2 = mul2(l2, pk(f, f));
                         if (started) {
 #pragma unroll 1
-                            for (int c = 0; c < D / 32; ++c) {
+                            for (int c = 0; c < D / 64; ++c) {
                                 uint32_t o[32];
-                                tc::tmem_ld32(o_t + 32 * c, o);
+                                const uint32_t at = o_t + half * (D / 2) + 32 * c;
+                                tc::tmem_ld32(at, o);
                                 tc::tmem_ld_wait32(o);
 #pragma unroll
                                 for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                tc::tmem_st32(o_t + 32 * c, o);
+                                tc::tmem_st32(at, o);
                             }
                         }
                     }
                     const float ref = m == -INFINITY ? 0.f : -m;
                     const f32x2 r2 = pk(ref, ref);
-#pragma unroll 1
-                    for (int c = 0; c < nch; ++c) {
-                        uint32_t r[32], w[16];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        if (c >= nch) continue;
+                        uint32_t r[32];
                         load(r, c);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
@@ -520,17 +562,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                             a = ex2(a);
                             b2 = ex2(b2);
                             l2 = add2(l2, pk(a, b2));
-                            w[e] = pack_bf16(a, b2);
+                            w[16 * c + e] = pack_bf16(a, b2);
                         }
-                        tmem_st16(s_t + 16 * c, w);
                     }
-                    if (width & 15) {
+                    const uint32_t nv = n + 2 * (j - it.jb) + 1, slot_v = nv % SLOTS;
+                    const bool tail = width & 15, late_v = tail && !tc::mbar_wait(&bar_full[slot_v], (nv / SLOTS) & 1u, wc);
+                    if (any(late_v)) { dead = true; break; }
+                    // (both threads of every row have read their logits: the weights may go over them)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        if (c < nch) tmem_st16(s_t + 32 * half + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
+                    known = !any(m == -INFINITY);
+                    if (tail) {
                         // rows of V behind the last key, up to the next multiple of 16, may hold anything: cleared (by the warps of
                         // both query tiles, each before its own product)
-                        const uint32_t nv = n + 2 * (j - it.jb) + 1;
-                        if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_full[nv % SLOTS], (nv / SLOTS) & 1u, wc))) { dead = true; break; }
-                        uint8_t *v = ring + (nv % SLOTS) * SLOT_BYTES;
-                        for (int e = (warp & 3) * 32 + lane; e < ((width + 15) / 16 * 16 - width) * 8 * NB; e += 128) {
+                        uint8_t *v = ring + slot_v * SLOT_BYTES;
+                        for (int e = (warp & 7) * 32 + lane; e < ((width + 15) / 16 * 16 - width) * 8 * NB; e += 256) {
                             const int vr = width + e / (8 * NB), vc = e % (8 * NB);
                             *reinterpret_cast<uint4 *>(v + (vc >> 3) * BLOCK + vr * 128 + (vc & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                         }
@@ -544,12 +591,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 if (lane == 0) tc::mbar_arrive(&bar_p[x]);
             }
             if (dead) break;
-            const float l = sum2(l2);
-            if (started) {
-                if (!__all_sync(0xffffffffu, tc::mbar_wait(&bar_o[x], no & 1u, wc))) break;
-                ++no;
-                tc::tc_fence_after();
-            }
+            const float l = trade(sum2(l2), true);
+            if (any(started && !tc::mbar_wait(&bar_o[x], no & 1u, wc))) break;
+            no += started ? 1 : 0;
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
             const long long R = (((long long)b * p.kv_heads + it.h) * p.n_q + i) * p.G + g;
             const bool last = p.slots == 1;
@@ -558,8 +602,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             // The four lanes of a row then trade pieces so that each has 8 neighbouring channels of the four blocks: their stores
             // are whole sectors, eight rows at a time, where a row per thread would touch 32 lines with every store.
             const int quad = lane & 3;
-#pragma unroll 1
-            for (int hrow = 0; hrow < 32; hrow += 16) {
+            const int hrow = 16 * half;                  // a row's two warps store 16 rows each
+            {
                 float scale[2];
                 bool there[2];
                 long long to[2];
@@ -621,7 +665,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&bar_o_read[x]);
             }
-            if (real) {
+            if (real && half == 0) {
                 if (!last) p.part_lse[at] = lse2;
                 else if (p.lse_out) p.lse_out[((long long)b * p.kv_heads * p.G + it.h * p.G + g) * p.n_q + i] = natural_lse(lse2);
             }
@@ -629,7 +673,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (warp == 8) tc::tmem_dealloc(tmem, 512);
+    if (warp == 16) tc::tmem_dealloc(tmem, 512);
 }
 
 }  // namespace obf
