@@ -33,8 +33,8 @@ namespace obf {
 
 constexpr int AT_TILE = 128;
 constexpr int AT_THREADS = 608;
-constexpr float AT_RAISE = 64.f;
-constexpr int AT_POLY = 3;                                // of every three pairs of weights one by exp2_poly
+constexpr float AT_RAISE = 64.f, AT_WEIGHT_MAX = 18446744073709551616.f;     // and 2 to that power
+constexpr int AT_POLY = 4;                                // of every four pairs of weights one by exp2_poly
 
 template <int D>
 struct AttendTcShape {
@@ -209,11 +209,13 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
 // 2^x of a pair on the multiply-add units, for a share of the weights: the special-function unit's 16 results per cycle would
 // otherwise be the narrowest place.  x = n + f with |f| <= 1/2 (n by adding and subtracting 1.5 * 2^23), a polynomial of degree
 // four in f whose relative error is evenly spread (exchange algorithm; 2.7e-6 at most in fp32, 4e-8 on average), n added to the
-// exponent.  For x < 127; below -126 the result is 2^-126 (bf16 weights and an fp32 sum whose other terms are near one); not for NaN.
-__device__ __forceinline__ void exp2_poly(f32x2 x, float &a, float &b)
+// exponent.  For x < 127; below -126 the result is 2^-126 (bf16 weights and an fp32 sum whose other terms are near one); not for
+// NaN.  `mx` gathers the largest x, for the caller to see that.
+__device__ __forceinline__ void exp2_poly(f32x2 x, float &mx, float &a, float &b)
 {
     float x0, x1;
     upk(x, x0, x1);
+    mx = max3_nan(mx, x0, x1);
     x = pk(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
     const f32x2 y = add2(x, pk(12582912.f, 12582912.f)), f = fma2(add2(y, pk(-12582912.f, -12582912.f)), pk(-1.f, -1.f), x);
     f32x2 q = fma2(f, pk(0.009570102207362652f, 0.009570102207362652f), pk(0.05591785907745361f, 0.05591785907745361f));
@@ -437,12 +439,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             it = sm_item[ni & 1u];
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(&bar_item_read[ni & 1u]);
-            // the row
-            const int g = row % p.G, iq = row / p.G, bi = iq / it.ti, i = it.first_i(x) + iq - bi * it.ti, b = it.first_b(x) + bi;
-            bool real = pick(it.valid, x) && bi < it.nb && b < p.batch;
-            if (PREFIX) real = real && i < attend_q_len(p, b);
-            else real = real && i < it.ql;
-            const int t = PREFIX || !real ? 0 : it.t + i, sk = pick(it.sk, x), ja = pick(it.ja, x), jz = pick(it.jz, x), fa = pick(it.fa, x), fz = pick(it.fz, x);
+            // the row: head of the group, query, sequence, whether it is one
+            auto locate = [&](int &g, int &i, int &b) {
+                const int iq = row / p.G, bi = iq / it.ti;
+                g = row - iq * p.G;
+                i = it.first_i(x) + iq - bi * it.ti;
+                b = it.first_b(x) + bi;
+                return pick(it.valid, x) && bi < it.nb && b < p.batch && i < (PREFIX ? attend_q_len(p, min(b, p.batch - 1)) : it.ql);
+            };
+            int t, sk = pick(it.sk, x), ja = pick(it.ja, x), jz = pick(it.jz, x), fa = pick(it.fa, x), fz = pick(it.fz, x);
+            bool real;
+            {
+                int g, i, b;
+                real = locate(g, i, b);
+                t = PREFIX || !real ? 0 : it.t + i;
+            }
             float m = real ? -INFINITY : 0.f;            // (rows that are none have a reference from the start)
             f32x2 l2 = 0ull;
             bool started = false, known = false;          // known: all rows have references
@@ -471,39 +482,38 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     // every row has a reference, and a sum that the 2^-126 of exp2_poly for a hidden key does not show in
                     const bool full = j >= fa && j < fz;
                     const f32x2 r2 = pk(-m, -m);
-                    float mx = -INFINITY;
+                    float mx = -INFINITY;                 // of the logits that exp2_poly is for
                     f32x2 z = 0ull;
-                    uint32_t r[2][16];
-                    tmem_ld16(s_t + col0, r[0]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        tmem_ld_wait16(r[c & 1]);
-                        if (c < 3) tmem_ld16(s_t + col0 + 16 * (c + 1), r[(c + 1) & 1]);
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t r[32];
+                        tc::tmem_ld32(s_t + col0 + 32 * c, r);
+                        tc::tmem_ld_wait32(r);
                         if (!full) {
-                            const uint32_t bits = seen(c >> 1) >> (c & 1) * 16;
+                            const uint32_t bits = seen(c);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (!(bits >> e & 1u)) r[c & 1][e] = 0xFF800000u;
+                            for (int e = 0; e < 32; ++e)
+                                if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
                         }
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float s0 = __uint_as_float(r[c & 1][2 * e]), s1 = __uint_as_float(r[c & 1][2 * e + 1]);
-                            mx = max3_nan(mx, s0, s1);
-                            const f32x2 y = fma2(pk(s0, s1), c2, r2);
+                        for (int e = 0; e < 16; ++e) {
+                            const f32x2 y = fma2(pk(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, r2);
                             float a, b2;
-                            if ((8 * c + e) % AT_POLY == 1) {
-                                exp2_poly(y, a, b2);
+                            if (e % AT_POLY == 1) {
+                                exp2_poly(y, mx, a, b2);
                             } else {
                                 upk(y, a, b2);
                                 a = ex2(a);
                                 b2 = ex2(b2);
                             }
                             z = add2(z, pk(a, b2));
-                            w[8 * c + e] = pack_bf16(a, b2);
+                            w[16 * c + e] = pack_bf16(a, b2);
                         }
                     }
-                    // (a maximum that is not a number sends the tile the other way, too, where it spreads)
-                    if (!any(late || !(mx * p.c <= m + AT_RAISE || mx == -INFINITY))) {
+                    // No weight may be above 2^64 of the reference; a logit that is not a number sends the tile the other way, too,
+                    // where it spreads.
+                    const float zs = sum2(z);
+                    if (!any(late || !(zs <= AT_WEIGHT_MAX) || !(mx <= AT_RAISE))) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) tmem_st16(s_t + 32 * half + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                         l2 = add2(l2, z);
@@ -595,6 +605,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             if (any(started && !tc::mbar_wait(&bar_o[x], no & 1u, wc))) break;
             no += started ? 1 : 0;
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+            int g, i, b;
+            locate(g, i, b);
             const long long R = (((long long)b * p.kv_heads + it.h) * p.n_q + i) * p.G + g;
             const bool last = p.slots == 1;
             const long long at = (long long)(PREFIX ? it.part : p.p_slots + it.part) * p.rows_total + R;
