@@ -173,19 +173,6 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, c
     return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, w));
 }
 
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(taddr) : "memory");
-}
-
-__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
-}
-
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
@@ -360,13 +347,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 ++nt;
                 tc::tc_fence_after();
                 if (pending) {
-                    // 16 keys of V on: 2048 bytes, 128 in the descriptor
+                    // 16 keys of V on: 2048 bytes, 128 in the descriptor; their weights: 8 columns (those of the second 64 keys begin where
+                    // their logits did, so that a warp's stores touch its own logits alone)
                     const uint64_t vd = tc::smem_desc_sw128(ring_u + slot_v * SLOT_BYTES, BLOCK, 1024);
                     if (w16_prev == AT_TILE) {
 #pragma unroll
-                        for (int k = 0; k < AT_TILE / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
+                        for (int k = 0; k < AT_TILE / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k + (k & 4) * 8, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
                     } else {
-                        for (int k = 0; k < w16_prev / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
+                        for (int k = 0; k < w16_prev / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k + (k & 4) * 8, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
                     }
                     started = true;
                     umma_done(leader, &bar_empty[slot_v]);
@@ -410,14 +398,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         const int x = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, col0 = half * 64;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_t = tmem + 128 * x + lanes, o_t = tmem + 256 + 128 * x + lanes;
         const f32x2 c2 = pk(p.c, p.c);
-        // Whether the condition holds for some thread of the query tile; all 256 of them come here the same number of times,
-        // those whose wait ran out too, so that they leave together.
+        // Whether the condition holds for some thread of the two warps that share rows.  Both come here the same number of times,
+        // after a wait that ran out too, so that they leave together.
         auto any = [&](bool c) {
             uint32_t r;
             tc::tc_fence_before();
             __syncwarp();
-            asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %2, 0;\n barrier.cta.red.or.pred.aligned q, %1, 256, p;\n selp.u32 %0, 1, 0, q;\n}"
-                         : "=r"(r) : "r"(1 + x), "r"((int)c) : "memory");
+            asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %2, 0;\n barrier.cta.red.or.pred.aligned q, %1, 64, p;\n selp.u32 %0, 1, 0, q;\n}"
+                         : "=r"(r) : "r"(1 + 4 * x + quarter), "r"((int)c) : "memory");
             tc::tc_fence_after();
             return r != 0;
         };
@@ -515,7 +503,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     const float zs = sum2(z);
                     if (!any(late || !(zs <= AT_WEIGHT_MAX) || !(mx <= AT_RAISE))) {
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) tmem_st16(s_t + 32 * half + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
+                        for (int c = 0; c < 2; ++c) tmem_st16(s_t + col0 + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                         l2 = add2(l2, z);
                         formed = true;
                     }
@@ -578,10 +566,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     const uint32_t nv = n + 2 * (j - it.jb) + 1, slot_v = nv % SLOTS;
                     const bool tail = width & 15, late_v = tail && !tc::mbar_wait(&bar_full[slot_v], (nv / SLOTS) & 1u, wc);
                     if (any(late_v)) { dead = true; break; }
-                    // (both threads of every row have read their logits: the weights may go over them)
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
-                        if (c < nch) tmem_st16(s_t + 32 * half + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
+                        if (c < nch) tmem_st16(s_t + col0 + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                     known = !any(m == -INFINITY);
                     if (tail) {
                         // rows of V behind the last key, up to the next multiple of 16, may hold anything: cleared (by the warps of
