@@ -32,7 +32,7 @@
 namespace obf {
 
 constexpr int AT_TILE = 128;
-constexpr int AT_THREADS = 608;
+constexpr int AT_THREADS = 640;
 constexpr float AT_RAISE = 64.f, AT_WEIGHT_MAX = 18446744073709551616.f;     // and 2 to that power
 constexpr int AT_POLY = 4;                                // of every four pairs of weights one by exp2_poly
 
@@ -144,26 +144,11 @@ struct AttendTcItem {
     }
 };
 
-// The warp that issues the products runs as a whole, one lane of it issuing: with operands that the compiler knows to be the
-// same in all lanes they stay in uniform registers, and a product costs a handful of instructions.  (A single thread in a branch
-// of its own cost 110 cycles of issue per product, more than the 64 that the product takes.)
-__device__ __forceinline__ void umma_ss(bool leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+// D[tmem] (+)= A[tmem] * B, K = 16 per instruction: A holds two bf16 of a row per column.
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %5, 0;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"((int)leader) : "memory");
-}
-
-// The same with A in tensor memory, two bf16 of a row per column.
-__device__ __forceinline__ void umma_ts(bool leader, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
-{
-    asm volatile("{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 e, %5, 0;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"((int)leader) : "memory");
-}
-
-__device__ __forceinline__ void umma_done(bool leader, uint64_t *bar)
-{
-    asm volatile("{\n .reg .pred e;\n setp.ne.b32 e, %1, 0;\n @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}"
-                 ::"r"(tc::smem_u32(bar)), "r"((int)leader) : "memory");
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
 // tc::mbar_wait by a whole warp, which goes on as one.
@@ -257,7 +242,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         }
         tc::mbar_init_fence();
     }
-    if (warp == 16) tc::tmem_alloc(&s_tmem, 512);
+    if (warp == 0) tc::tmem_alloc(&s_tmem, 512);
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -266,7 +251,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     if (first && blockIdx.x == 0) attend_status(p);
 
     AttendTcItem<PREFIX> it;
-    if (warp == 18) {
+    if (warp == 2) {
         // ---------------- copies ----------------
         if (lane == 0) {
             uint32_t n = 0, nq = 0, ni = 0;
@@ -305,10 +290,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             for (uint32_t j = n > (uint32_t)SLOTS ? n - SLOTS : 0u; j < n; ++j) tc::mbar_drain(&bar_full[j % SLOTS], (j / SLOTS) & 1u, wc);
             if (nq) tc::mbar_drain(&bar_q_full, (nq - 1) & 1u, wc);
         }
-    } else if (warp >= 16) {
+    } else if (warp < 2) {
         // ---------------- products ----------------
         const bool leader = lane == 0;
-        const int x = warp_uniform(warp - 16);
+        const int x = warp_uniform(warp);
         const uint32_t tm_u = warp_uniform((int)tmem), q_u = warp_uniform((int)tc::smem_u32(q_sm)), ring_u = warp_uniform((int)tc::smem_u32(ring));
         const uint32_t s_t = tm_u + 128 * x, o_t = tm_u + 256 + 128 * x;
         const uint64_t qd = tc::smem_desc_sw128(q_u + x * SLOT_BYTES, 16, 1024);
@@ -346,43 +331,48 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 if (!mbar_wait_warp(&bar_turn[x], (nt & 1u) ^ (uint32_t)(x ^ 1), wc)) { dead = true; break; }
                 ++nt;
                 tc::tc_fence_after();
-                if (pending) {
-                    // 16 keys of V on: 2048 bytes, 128 in the descriptor; their weights: 8 columns (those of the second 64 keys begin where
-                    // their logits did, so that a warp's stores touch its own logits alone)
-                    const uint64_t vd = tc::smem_desc_sw128(ring_u + slot_v * SLOT_BYTES, BLOCK, 1024);
-                    if (w16_prev == AT_TILE) {
-#pragma unroll
-                        for (int k = 0; k < AT_TILE / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k + (k & 4) * 8, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
-                    } else {
-                        for (int k = 0; k < w16_prev / 16; ++k) umma_ts(leader, o_t, s_t + 8 * k + (k & 4) * 8, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
-                    }
-                    started = true;
-                    umma_done(leader, &bar_empty[slot_v]);
-                } else if (j > it.jb && leader) {
-                    tc::mbar_arrive(&bar_empty[slot_v]);
-                }
+                const bool was = pending;
                 pending = j < it.je && (j < sk || (j >= ja && j < jz));
                 if (pending) {
                     int j0, width;
                     it.tile(j, j0, width);
                     w16 = (width + 15) & ~15;
-                    const uint64_t kd = tc::smem_desc_sw128(ring_u + slot_k * SLOT_BYTES, 16, 1024);
-                    const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        // 16 channels on: 32 bytes, every 64 the next column block; descriptors count 16 bytes
-                        const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / 16;
-                        umma_ss(leader, s_t, qd + off, kd + off, idesc_s, k > 0);
-                    }
-                    umma_done(leader, &bar_s[x]);
-                    umma_done(leader, &bar_empty[slot_k]);
-                    ++ns;
-                } else if (j < it.je && leader) {
-                    tc::mbar_arrive(&bar_empty[slot_k]);
                 }
-                if (leader) tc::mbar_arrive(&bar_turn[x ^ 1]);
-                if (j == it.je - 1) umma_done(leader, &bar_q_empty);
-                if (j == it.je && started) umma_done(leader, &bar_o[x]);
+                if (leader) {
+                    if (was) {
+                        // 16 keys of V on: 2048 bytes, 128 in the descriptor; their weights: 8 columns (those of the second 64 keys
+                        // begin where their logits did, so that a warp's stores touch its own logits alone)
+                        const uint64_t vd = tc::smem_desc_sw128(ring_u + slot_v * SLOT_BYTES, BLOCK, 1024);
+                        if (w16_prev == AT_TILE) {
+#pragma unroll
+                            for (int k = 0; k < AT_TILE / 16; ++k) umma_ts(o_t, s_t + 8 * k + (k & 4) * 8, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
+                        } else {
+                            for (int k = 0; k < w16_prev / 16; ++k) umma_ts(o_t, s_t + 8 * k + (k & 4) * 8, vd + 128 * k, idesc_o, (started || k > 0) ? 1u : 0u);
+                        }
+                        tc::umma_commit(&bar_empty[slot_v]);
+                    } else if (j > it.jb) {
+                        tc::mbar_arrive(&bar_empty[slot_v]);
+                    }
+                    if (pending) {
+                        const uint64_t kd = tc::smem_desc_sw128(ring_u + slot_k * SLOT_BYTES, 16, 1024);
+                        const uint32_t idesc_s = tc::idesc_bf16(128, 0, 0, 0) | ((uint32_t)(w16 >> 3) << 17);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            // 16 channels on: 32 bytes, every 64 the next column block; descriptors count 16 bytes
+                            const uint64_t off = ((k >> 2) * BLOCK + (k & 3) * 32) / 16;
+                            tc::umma_bf16(s_t, qd + off, kd + off, idesc_s, k > 0);
+                        }
+                        tc::umma_commit(&bar_s[x]);
+                        tc::umma_commit(&bar_empty[slot_k]);
+                    } else if (j < it.je) {
+                        tc::mbar_arrive(&bar_empty[slot_k]);
+                    }
+                    tc::mbar_arrive(&bar_turn[x ^ 1]);
+                    if (j == it.je - 1) tc::umma_commit(&bar_q_empty);
+                    if (j == it.je && (started || was)) tc::umma_commit(&bar_o[x]);
+                }
+                started = started || was;
+                ns += pending ? 1 : 0;
                 w16_prev = w16;
                 __syncwarp();
             }
@@ -390,12 +380,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             no += started ? 1 : 0;
         }
         // no product may be in flight when the block exits
-        umma_done(leader, &bar_drain[x]);
-        tc::mbar_drain(&bar_drain[x], 0, wc);
+        if (leader) {
+            tc::umma_commit(&bar_drain[x]);
+            tc::mbar_drain(&bar_drain[x], 0, wc);
+        }
         __syncwarp();
-    } else {
+    } else if (warp >= 4) {
         // ---------------- softmax ----------------
-        const int x = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, col0 = half * 64;
+        const int sw = warp - 4, x = sw >> 3, half = (sw >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, col0 = half * 64;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_t = tmem + 128 * x + lanes, o_t = tmem + 256 + 128 * x + lanes;
         const f32x2 c2 = pk(p.c, p.c);
         // Whether the condition holds for some thread of the two warps that share rows.  Both come here the same number of times,
@@ -574,7 +566,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         // rows of V behind the last key, up to the next multiple of 16, may hold anything: cleared (by the warps of
                         // both query tiles, each before its own product)
                         uint8_t *v = ring + slot_v * SLOT_BYTES;
-                        for (int e = (warp & 7) * 32 + lane; e < ((width + 15) / 16 * 16 - width) * 8 * NB; e += 256) {
+                        for (int e = (sw & 7) * 32 + lane; e < ((width + 15) / 16 * 16 - width) * 8 * NB; e += 256) {
                             const int vr = width + e / (8 * NB), vc = e % (8 * NB);
                             *reinterpret_cast<uint4 *>(v + (vc >> 3) * BLOCK + vr * 128 + (vc & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                         }
@@ -672,7 +664,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (warp == 16) tc::tmem_dealloc(tmem, 512);
+    if (warp == 0) tc::tmem_dealloc(tmem, 512);
 }
 
 }  // namespace obf
