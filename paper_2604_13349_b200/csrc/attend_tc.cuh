@@ -151,6 +151,15 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
                  ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+// One lane of the warp, always the same.  (Told apart like this the compiler knows that a single thread runs what depends on it, and
+// keeps the products' operands in uniform registers.)
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(r));
+    return r != 0;
+}
+
 // tc::mbar_wait by a whole warp, which goes on as one.
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, const tc::WaitCtx &w)
 {
@@ -292,7 +301,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         }
     } else if (warp < 2) {
         // ---------------- products ----------------
-        const bool leader = lane == 0;
         const int x = warp_uniform(warp);
         const uint32_t tm_u = warp_uniform((int)tmem), q_u = warp_uniform((int)tc::smem_u32(q_sm)), ring_u = warp_uniform((int)tc::smem_u32(ring));
         const uint32_t s_t = tm_u + 128 * x, o_t = tm_u + 256 + 128 * x;
@@ -310,7 +318,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             it.hi = warp_uniform(im.hi);
             it.nsink = warp_uniform(im.nsink);
             const int sk = warp_uniform(im.sk[x]), ja = warp_uniform(im.ja[x]), jz = warp_uniform(im.jz[x]);
-            if (leader) tc::mbar_arrive(&bar_item_read[ni & 1u]);
+            if (elect_one()) tc::mbar_arrive(&bar_item_read[ni & 1u]);
             __syncwarp();
             if (it.jb >= it.je) continue;
             if (!mbar_wait_warp(&bar_q_full, nq & 1u, wc)) break;
@@ -338,7 +346,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     it.tile(j, j0, width);
                     w16 = (width + 15) & ~15;
                 }
-                if (leader) {
+                if (elect_one()) {
                     if (was) {
                         // 16 keys of V on: 2048 bytes, 128 in the descriptor; their weights: 8 columns (those of the second 64 keys
                         // begin where their logits did, so that a warp's stores touch its own logits alone)
@@ -380,7 +388,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             no += started ? 1 : 0;
         }
         // no product may be in flight when the block exits
-        if (leader) {
+        if (elect_one()) {
             tc::umma_commit(&bar_drain[x]);
             tc::mbar_drain(&bar_drain[x], 0, wc);
         }
