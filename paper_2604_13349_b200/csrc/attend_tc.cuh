@@ -422,30 +422,34 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         };
         uint32_t n = 0, ni = 0, ns = 0, no = 0;
         bool dead = false;
-        for (int item = blockIdx.x; item < items && !dead; n += 2 * (it.je - it.jb), item += gridDim.x, ++ni) {
+        for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
             if (any(!tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc))) break;
-            it = sm_item[ni & 1u];
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&bar_item_read[ni & 1u]);
+            // (what only the beginning and the end of an item need is read from shared memory both times: registers are short)
+            const AttendTcItem<PREFIX> &im = sm_item[ni & 1u];
             // the row: head of the group, query, sequence, whether it is one
             auto locate = [&](int &g, int &i, int &b) {
-                const int iq = row / p.G, bi = iq / it.ti;
+                const int iq = row / p.G, bi = iq / im.ti;
                 g = row - iq * p.G;
-                i = it.first_i(x) + iq - bi * it.ti;
-                b = it.first_b(x) + bi;
-                return pick(it.valid, x) && bi < it.nb && b < p.batch && i < (PREFIX ? attend_q_len(p, min(b, p.batch - 1)) : it.ql);
+                i = im.first_i(x) + iq - bi * im.ti;
+                b = im.first_b(x) + bi;
+                return im.valid[x] && bi < im.nb && b < p.batch && i < (PREFIX ? attend_q_len(p, min(b, p.batch - 1)) : im.ql);
             };
-            int t, sk = pick(it.sk, x), ja = pick(it.ja, x), jz = pick(it.jz, x), fa = pick(it.fa, x), fz = pick(it.fz, x);
+            it.s = im.s;
+            it.lo = im.lo;
+            it.hi = im.hi;
+            it.nsink = im.nsink;
+            const int jb = im.jb, je = im.je, sk = im.sk[x], ja = im.ja[x], jz = im.jz[x], fa = im.fa[x], fz = im.fz[x];
+            int t;
             bool real;
             {
                 int g, i, b;
                 real = locate(g, i, b);
-                t = PREFIX || !real ? 0 : it.t + i;
+                t = PREFIX || !real ? 0 : im.t + i;
             }
             float m = real ? -INFINITY : 0.f;            // (rows that are none have a reference from the start)
             f32x2 l2 = 0ull;
             bool started = false, known = false;          // known: all rows have references
-            for (int j = it.jb; j < it.je; ++j) {
+            for (int j = jb; j < je; ++j) {
                 if (!(j < sk || (j >= ja && j < jz))) continue;
                 const bool late = !tc::mbar_wait(&bar_s[x], ns & 1u, wc);
                 ++ns;
@@ -563,7 +567,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                             w[16 * c + e] = pack_bf16(a, b2);
                         }
                     }
-                    const uint32_t nv = n + 2 * (j - it.jb) + 1, slot_v = nv % SLOTS;
+                    const uint32_t nv = n + 2 * (j - jb) + 1, slot_v = nv % SLOTS;
                     const bool tail = width & 15, late_v = tail && !tc::mbar_wait(&bar_full[slot_v], (nv / SLOTS) & 1u, wc);
                     if (any(late_v)) { dead = true; break; }
 #pragma unroll
@@ -588,15 +592,16 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 if (lane == 0) tc::mbar_arrive(&bar_p[x]);
             }
             if (dead) break;
+            n += 2 * (je - jb);
             const float l = trade(sum2(l2), true);
             if (any(started && !tc::mbar_wait(&bar_o[x], no & 1u, wc))) break;
             no += started ? 1 : 0;
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
             int g, i, b;
             locate(g, i, b);
-            const long long R = (((long long)b * p.kv_heads + it.h) * p.n_q + i) * p.G + g;
+            const long long R = (((long long)b * p.kv_heads + im.h) * p.n_q + i) * p.G + g;
             const bool last = p.slots == 1;
-            const long long at = (long long)(PREFIX ? it.part : p.p_slots + it.part) * p.rows_total + R;
+            const long long at = (long long)(PREFIX ? im.part : p.p_slots + im.part) * p.rows_total + R;
             // O is read as matrix fragments: of eight columns 8 b .. a lane has 2 (lane mod 4), + 1 of rows lane / 4 and lane / 4 + 8.
             // The four lanes of a row then trade pieces so that each has 8 neighbouring channels of the four blocks: their stores
             // are whole sectors, eight rows at a time, where a row per thread would touch 32 lines with every store.
@@ -606,7 +611,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 float scale[2];
                 bool there[2];
                 long long to[2];
-                const long long to_own = last ? b * p.os[0] + (long long)(it.h * p.G + g) * p.os[1] + (long long)i * p.os[2] : at * D;
+                const long long to_own = last ? b * p.os[0] + (long long)(im.h * p.G + g) * p.os[1] + (long long)i * p.os[2] : at * D;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const int from = hrow + 8 * u + lane / 4;
@@ -666,8 +671,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             }
             if (real && half == 0) {
                 if (!last) p.part_lse[at] = lse2;
-                else if (p.lse_out) p.lse_out[((long long)b * p.kv_heads * p.G + it.h * p.G + g) * p.n_q + i] = natural_lse(lse2);
+                else if (p.lse_out) p.lse_out[((long long)b * p.kv_heads * p.G + im.h * p.G + g) * p.n_q + i] = natural_lse(lse2);
             }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&bar_item_read[ni & 1u]);
         }
     }
     tc::tc_fence_before();
