@@ -40,13 +40,15 @@ template <int D>
 struct AttendTcShape {
     static constexpr int SLOT_BYTES = AT_TILE * D * 2;                    // a tile of Q, K or V
     static constexpr int SLOTS = D == 128 ? 5 : 8;
-    static constexpr int SMEM_BYTES = (2 + SLOTS) * SLOT_BYTES + 1024;
+    static constexpr int SMEM_BYTES = (2 + SLOTS) * SLOT_BYTES;           // beside what the kernel declares, and alignment to 1024
 };
 
 // Tensor maps and tile shape of the kernel.
 struct AttendTcMaps {
     CUtensorMap q, k, v;
+    CUtensorMap head[2], rest[2];                                         // K and V: the sinks, and what the sinks leave of a tile
     int32_t ti, nb;                                                       // queries and sequences of a tile of rows
+    int32_t head_rows;                                                    // rows that the sinks take: at most 64, or whole tiles
 };
 
 // Of two values, without an array that is indexed at run time.
@@ -58,7 +60,7 @@ template <bool PREFIX>
 struct AttendTcItem {
     int h, b, part;                  // KV head, first sequence, part of the keys
     int i0, ti, nb;                  // first query of the first tile, queries and sequences of a tile
-    int s, lo, hi, nsink;            // keys of the pair: s sinks in nsink tiles, then lo .. hi - 1
+    int head, lo, hi;                // keys of the pair: the sinks in `head` rows (zeros behind them), then lo .. hi - 1
     int jb, je;                      // the part's tiles
     // per tile of rows: some row sees tile j of the keys when j < sk or ja <= j < jz, every row sees all of it when fa <= j < fz
     int sk[2], ja[2], jz[2], fa[2], fz[2];
@@ -89,8 +91,8 @@ struct AttendTcItem {
             const int pairs = (p.n_q + 2 * ti - 1) / (2 * ti);
             i0 = (pairs - 1 - item) * 2 * ti;                             // the longest key ranges first
         }
+        head = lo = hi = t = ql = 0;
         if (PREFIX) {
-            s = lo = t = ql = nsink = 0;
             hi = p.prefix;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -103,15 +105,17 @@ struct AttendTcItem {
             const int len = attend_len(p, b);
             ql = attend_q_len(p, b);
             t = len - ql;
-            s = lo = hi = nsink = 0;
             valid[0] = i0 < ql;
             valid[1] = i0 + ti < ql;
             if (valid[0]) {
                 const KeyRange r = attend_range(p, t + i0, t + min(i0 + 2 * ti, ql) - 1, len);
-                s = r.s;
-                lo = r.lo;
                 hi = r.hi;
-                nsink = (s + AT_TILE - 1) / AT_TILE;
+                if (r.lo > p.sinks) {
+                    lo = r.lo;
+                    head = p.sinks ? tm.head_rows : 0;
+                }
+                // up to a multiple of 16 keys where there are more, which later queries see
+                hi = min(len, hi + (lo - hi - head & 15));
             }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -119,29 +123,20 @@ struct AttendTcItem {
                 if (valid[x]) {
                     const int ta = t + i0 + x * ti, tb = t + min(i0 + (x + 1) * ti, ql) - 1;      // positions of its first and last query
                     const KeyRange r = attend_range(p, ta, tb, len);
-                    sk[x] = nsink;
-                    ja[x] = nsink + (p.sinks > lo ? 0 : (r.lo - lo) / AT_TILE);
-                    jz[x] = nsink + (r.hi - lo + AT_TILE - 1) / AT_TILE;
-                    fa[x] = nsink + (p.window ? max(tb - p.window + 1 - lo + AT_TILE - 1, 0) / AT_TILE : 0);
-                    fz[x] = nsink + max(ta + 1 - lo, 0) / AT_TILE;
+                    sk[x] = (head + AT_TILE - 1) / AT_TILE;
+                    ja[x] = p.sinks > lo ? 0 : (head + r.lo - lo) / AT_TILE;
+                    jz[x] = r.hi > lo ? (head + r.hi - lo + AT_TILE - 1) / AT_TILE : 0;
+                    fa[x] = max(sk[x], p.window ? max(head + tb - p.window + 1 - lo + AT_TILE - 1, 0) / AT_TILE : 0);
+                    fz[x] = max(head + ta + 1 - lo, 0) / AT_TILE;
                 }
             }
         }
-        const int tiles = nsink + (hi - lo + AT_TILE - 1) / AT_TILE, per = (tiles + parts - 1) / parts;
+        const int tiles = (head + hi - lo + AT_TILE - 1) / AT_TILE, per = (tiles + parts - 1) / parts;
         jb = min(part * per, tiles);
         je = min(jb + per, tiles);
     }
 
-    __device__ __forceinline__ void tile(int j, int &j0, int &width) const
-    {
-        if (j < nsink) {
-            j0 = j * AT_TILE;
-            width = min(AT_TILE, s - j0);
-        } else {
-            j0 = lo + (j - nsink) * AT_TILE;
-            width = min(AT_TILE, hi - j0);
-        }
-    }
+    __device__ __forceinline__ int width(int j) const { return min(AT_TILE, head + hi - lo - j * AT_TILE); }
 };
 
 // D[tmem] (+)= A[tmem] * B, K = 16 per instruction: A holds two bf16 of a row per column.
@@ -187,6 +182,13 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
     return r;
 }
 
+// A box of keys or values: rows from `row` on, column block `block` (all of them for boxes that are that wide).
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int row, int block, int head, int seq)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(tc::smem_u32(bar)), "r"(0), "r"(row), "r"(block), "r"(head), "r"(seq) : "memory");
+}
+
 // 2^x of a pair on the multiply-add units, for a share of the weights: the special-function unit's 16 results per cycle would
 // otherwise be the narrowest place.  x = n + f with |f| <= 1/2 (n by adding and subtracting 1.5 * 2^23), a polynomial of degree
 // four in f whose relative error is evenly spread (exchange algorithm; 2.7e-6 at most in fp32, 4e-8 on average), n added to the
@@ -230,9 +232,17 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     __shared__ uint64_t bar_full[SLOTS], bar_empty[SLOTS], bar_q_full, bar_q_empty, bar_drain[2];
     __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2], bar_item[2], bar_item_read[2], bar_turn[2];
     __shared__ AttendTcItem<PREFIX> sm_item[2];
-    __shared__ float sm_row[2][AT_TILE];                  // a row's two threads trade their maxima and sums
+    __shared__ float sm_row[2][2][AT_TILE];               // a row's two threads trade their maxima and sums
     __shared__ uint32_t s_tmem, s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    {
+        uint32_t given;
+        asm("mov.u32 %0, %%dynamic_smem_size;" : "=r"(given));
+        if ((uint32_t)(base - at_smem_raw) + AttendTcShape<D>::SMEM_BYTES > given) {      // (the launch and this layout belong together)
+            if (tid == 0) atomicOr(p.status, OBF_DEV_INTERNAL);
+            return;
+        }
+    }
     tc::WaitCtx wc{&s_abort, p.status, p.wait_limit_ns};
     if (tid == 0) {
         s_abort = 0u;
@@ -272,15 +282,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 tc::mbar_arrive(&bar_item[ni & 1u]);
                 if (it.jb >= it.je) continue;
                 for (int j = it.jb; j < it.je && !dead; ++j) {
-                    int j0, width;
-                    it.tile(j, j0, width);
                     for (int kv = 0; kv < 2; ++kv, ++n) {
                         const uint32_t sl = n % SLOTS;
                         if (!tc::mbar_wait(&bar_empty[sl], ((n / SLOTS) & 1u) ^ 1u, wc)) { dead = true; break; }
                         tc::mbar_expect_tx(&bar_full[sl], SLOT_BYTES);
-                        asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %3, %5, %6}], [%2];"
-                                     ::"r"(tc::smem_u32(ring + sl * SLOT_BYTES)), "l"(kv ? &tm.v : &tm.k), "r"(tc::smem_u32(&bar_full[sl])), "r"(0), "r"(j0), "r"(it.h),
-                                       "r"(PREFIX ? 0 : it.b) : "memory");
+                        const uint32_t dst = tc::smem_u32(ring + sl * SLOT_BYTES);
+                        const int b = PREFIX ? 0 : it.b, j0 = j * AT_TILE;
+                        if (!PREFIX && j0 < it.head && it.head < AT_TILE) {
+                            for (int c = 0; c < NB; ++c) {
+                                tma_load_5d(dst + c * BLOCK, &tm.head[kv], &bar_full[sl], 0, c, it.h, b);
+                                tma_load_5d(dst + c * BLOCK + it.head * 128, &tm.rest[kv], &bar_full[sl], it.lo, c, it.h, b);
+                            }
+                        } else if (!PREFIX && j0 < it.head) {
+                            tma_load_5d(dst, &tm.head[kv], &bar_full[sl], j0, 0, it.h, b);
+                        } else {
+                            tma_load_5d(dst, kv ? &tm.v : &tm.k, &bar_full[sl], it.lo + j0 - it.head, 0, it.h, b);
+                        }
                     }
                     if (j > it.jb || dead) continue;
                     // the queries behind the first tile of keys, which need not wait until the last item's are done with
@@ -313,10 +330,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             const AttendTcItem<PREFIX> &im = sm_item[ni & 1u];
             it.jb = warp_uniform(im.jb);
             it.je = warp_uniform(im.je);
-            it.s = warp_uniform(im.s);
+            it.head = warp_uniform(im.head);
             it.lo = warp_uniform(im.lo);
             it.hi = warp_uniform(im.hi);
-            it.nsink = warp_uniform(im.nsink);
             const int sk = warp_uniform(im.sk[x]), ja = warp_uniform(im.ja[x]), jz = warp_uniform(im.jz[x]);
             if (elect_one()) tc::mbar_arrive(&bar_item_read[ni & 1u]);
             __syncwarp();
@@ -341,11 +357,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 tc::tc_fence_after();
                 const bool was = pending;
                 pending = j < it.je && (j < sk || (j >= ja && j < jz));
-                if (pending) {
-                    int j0, width;
-                    it.tile(j, j0, width);
-                    w16 = (width + 15) & ~15;
-                }
+                if (pending) w16 = (it.width(j) + 15) & ~15;
                 if (elect_one()) {
                     if (was) {
                         // 16 keys of V on: 2048 bytes, 128 in the descriptor; their weights: 8 columns (those of the second 64 keys
@@ -398,6 +410,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         const int sw = warp - 4, x = sw >> 3, half = (sw >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, col0 = half * 64;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_t = tmem + 128 * x + lanes, o_t = tmem + 256 + 128 * x + lanes;
         const f32x2 c2 = pk(p.c, p.c);
+        // the row's head of the group, and its query and sequence from the tile's first ones on
+        const int row_g = row % p.G, row_b = row / p.G / tm.ti, row_i = row / p.G - row_b * tm.ti;
         // Whether the condition holds for some thread of the two warps that share rows.  Both come here the same number of times,
         // after a wait that ran out too, so that they leave together.
         auto any = [&](bool c) {
@@ -409,43 +423,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             tc::tc_fence_after();
             return r != 0;
         };
-        // The larger, or the sum, of a value of the row's two threads.
-        auto trade = [&](float v, bool sum) {
-            if (half) sm_row[x][row] = v;
-            any(false);
-            if (!half) {
-                v = sum ? v + sm_row[x][row] : fmaxf(v, sm_row[x][row]);
-                sm_row[x][row] = v;
-            }
-            any(false);
-            return sm_row[x][row];
-        };
         uint32_t n = 0, ni = 0, ns = 0, no = 0;
         bool dead = false;
         for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
             if (any(!tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc))) break;
             // (what only the beginning and the end of an item need is read from shared memory both times: registers are short)
             const AttendTcItem<PREFIX> &im = sm_item[ni & 1u];
-            // the row: head of the group, query, sequence, whether it is one
-            auto locate = [&](int &g, int &i, int &b) {
-                const int iq = row / p.G, bi = iq / im.ti;
-                g = row - iq * p.G;
-                i = im.first_i(x) + iq - bi * im.ti;
-                b = im.first_b(x) + bi;
-                return im.valid[x] && bi < im.nb && b < p.batch && i < (PREFIX ? attend_q_len(p, min(b, p.batch - 1)) : im.ql);
-            };
-            it.s = im.s;
+            const int jb = im.jb, je = im.je, sk = im.sk[x], ja = im.ja[x], jz = im.jz[x], fa = im.fa[x], fz = im.fz[x];
+            it.head = im.head;
             it.lo = im.lo;
             it.hi = im.hi;
-            it.nsink = im.nsink;
-            const int jb = im.jb, je = im.je, sk = im.sk[x], ja = im.ja[x], jz = im.jz[x], fa = im.fa[x], fz = im.fz[x];
-            int t;
-            bool real;
+            bool real = im.valid[x] && row_b < im.nb;
             {
-                int g, i, b;
-                real = locate(g, i, b);
-                t = PREFIX || !real ? 0 : im.t + i;
+                const int i = im.first_i(x) + row_i, b = im.first_b(x) + row_b;
+                real = real && b < p.batch && i < (PREFIX ? attend_q_len(p, min(b, p.batch - 1)) : im.ql);
             }
+            const int t = PREFIX || !real ? 0 : im.t + im.first_i(x) + row_i;
             float m = real ? -INFINITY : 0.f;            // (rows that are none have a reference from the start)
             f32x2 l2 = 0ull;
             bool started = false, known = false;          // known: all rows have references
@@ -455,22 +448,23 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 ++ns;
                 __syncwarp();
                 tc::tc_fence_after();
-                int j0, width;
-                it.tile(j, j0, width);
+                const int width = it.width(j);
                 // of 32 columns from col0 + 32 c on, those that the row sees
                 auto seen = [&](int c) {
                     uint32_t bits = column_bits(0, width - col0 - 32 * c);
                     if (!PREFIX) {
                         // keys up to the row's position, and behind its window's lower end or among the first tokens
-                        const int a = j0 + col0 + 32 * c;
+                        const int v = j * AT_TILE + col0 + 32 * c, a = it.lo - it.head + v;
                         const uint32_t in = p.window ? column_bits(t - p.window + 1 - a, 32) | column_bits(0, p.sinks - a) : 0xFFFFFFFFu;
-                        bits &= real ? in & column_bits(0, t + 1 - a) : 0u;
+                        uint32_t keys = in & column_bits(0, t + 1 - a);
+                        if (v < it.head) keys = (keys & ~column_bits(0, it.head - v)) | column_bits(0, p.sinks - v);
+                        bits &= real ? keys : 0u;
                     }
                     return bits;
                 };
                 bool formed = false;                      // the tile's weights
                 uint32_t w[32];
-                if (known && width == AT_TILE) {
+                if (known && (width & 15) == 0) {
                     // every row has a reference, and a sum that the 2^-126 of exp2_poly for a hidden key does not show in
                     const bool full = j >= fa && j < fz;
                     const f32x2 r2 = pk(-m, -m);
@@ -513,7 +507,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     }
                 }
                 if (!formed) {
-                    if (any(late)) { dead = true; break; }
                     const int nch = min(2, max(0, width - col0 + 31) >> 5);
                     auto load = [&](uint32_t (&r)[32], int c) {
                         tc::tmem_ld32(s_t + col0 + 32 * c, r);
@@ -531,23 +524,25 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(r[e]), __uint_as_float(r[e + 1])));
                     }
-                    mx = trade(mx, false) * p.c;
+                    sm_row[half][x][row] = mx;
+                    if (any(late)) { dead = true; break; }
+                    mx = fmaxf(mx, sm_row[half ^ 1][x][row]) * p.c;
                     // (a maximum below the reference changes nothing)
-                    if (any(started ? mx > m + AT_RAISE : true)) {
+                    if (!started) {
+                        m = fmaxf(m, mx);
+                    } else if (any(mx > m + AT_RAISE)) {
                         const float f = mx > m ? ex2(m - mx) : 1.f;
                         m = fmaxf(m, mx);
                         l2 = mul2(l2, pk(f, f));
-                        if (started) {
 #pragma unroll 1
-                            for (int c = 0; c < D / 64; ++c) {
-                                uint32_t o[32];
-                                const uint32_t at = o_t + half * (D / 2) + 32 * c;
-                                tc::tmem_ld32(at, o);
-                                tc::tmem_ld_wait32(o);
+                        for (int c = 0; c < D / 64; ++c) {
+                            uint32_t o[32];
+                            const uint32_t at = o_t + half * (D / 2) + 32 * c;
+                            tc::tmem_ld32(at, o);
+                            tc::tmem_ld_wait32(o);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                tc::tmem_st32(at, o);
-                            }
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tc::tmem_st32(at, o);
                         }
                     }
                     const float ref = m == -INFINITY ? 0.f : -m;
@@ -569,11 +564,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     }
                     const uint32_t nv = n + 2 * (j - jb) + 1, slot_v = nv % SLOTS;
                     const bool tail = width & 15, late_v = tail && !tc::mbar_wait(&bar_full[slot_v], (nv / SLOTS) & 1u, wc);
-                    if (any(late_v)) { dead = true; break; }
+                    // (where every row has a reference from now on, the straight path takes over)
+                    known = !any(m == -INFINITY || late_v);
+                    if (tail && any(late_v)) { dead = true; break; }
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
                         if (c < nch) tmem_st16(s_t + col0 + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
-                    known = !any(m == -INFINITY);
                     if (tail) {
                         // rows of V behind the last key, up to the next multiple of 16, may hold anything: cleared (by the warps of
                         // both query tiles, each before its own product)
@@ -593,12 +589,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             }
             if (dead) break;
             n += 2 * (je - jb);
-            const float l = trade(sum2(l2), true);
+            float l = sum2(l2);
+            sm_row[half][x][row] = l;
             if (any(started && !tc::mbar_wait(&bar_o[x], no & 1u, wc))) break;
+            l = half ? sm_row[0][x][row] + l : l + sm_row[1][x][row];
             no += started ? 1 : 0;
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-            int g, i, b;
-            locate(g, i, b);
+            const int g = row_g, i = im.first_i(x) + row_i, b = im.first_b(x) + row_b;
             const long long R = (((long long)b * p.kv_heads + im.h) * p.n_q + i) * p.G + g;
             const bool last = p.slots == 1;
             const long long at = (long long)(PREFIX ? im.part : p.p_slots + im.part) * p.rows_total + R;

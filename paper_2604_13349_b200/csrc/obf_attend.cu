@@ -230,7 +230,15 @@ template <int D, bool PREFIX>
 static obf_status_t launch_attend_tc(const AttendDev &p, int first, cudaStream_t st)
 {
     static bool done[64];
-    OBF_TRY(set_smem_once(k_attend_tc<D, PREFIX>, AttendTcShape<D>::SMEM_BYTES, done));
+    // Dynamic shared memory begins behind the 1024 bytes that the system keeps and what the kernel declares; the tiles want
+    // multiples of 1024.
+    static const size_t smem = [] {
+        cudaFuncAttributes fa = {};
+        if (cudaFuncGetAttributes(&fa, k_attend_tc<D, PREFIX>) != cudaSuccess) { (void)cudaGetLastError(); return (size_t)0; }
+        return align_up(fa.sharedSizeBytes, 1024) - fa.sharedSizeBytes + AttendTcShape<D>::SMEM_BYTES;
+    }();
+    if (smem == 0) return OBF_ERR_CUDA;
+    OBF_TRY(set_smem_once(k_attend_tc<D, PREFIX>, smem, done));
     const TcTiles t = tc_tiles(p.G, p.n_q, p.batch, p.kv_heads, PREFIX);
     AttendTcMaps m;
     m.ti = t.ti;
@@ -241,18 +249,31 @@ static obf_status_t launch_attend_tc(const AttendDev &p, int first, cudaStream_t
         const cuuint32_t box[4] = {64, (cuuint32_t)p.G, (cuuint32_t)t.ti, (cuuint32_t)t.nb};
         OBF_TRY(encode_map(&m.q, p.q, 4, dims, strides, box));
     }
+    // the sinks take 16, 32, 48 or 64 rows at the front of the first tile of keys, more than that tiles of their own
+    m.head_rows = !PREFIX && p.window && p.sinks ? (p.sinks <= 64 ? (p.sinks + 15) / 16 * 16 : (p.sinks + AT_TILE - 1) / AT_TILE * AT_TILE) : 0;
     for (int i = 0; i < 2; ++i) {
         const long long *s3 = i ? p.vs : p.ks, *s2 = i ? p.pvs : p.pks;
+        const void *ptr = PREFIX ? (i ? p.pv : p.pk) : (i ? p.v : p.k);
         const cuuint64_t rows = PREFIX ? p.prefix : p.capacity, n = PREFIX ? 1 : nb;
-        const cuuint64_t dims[5] = {64, rows, D / 64, kv, n};
+        cuuint64_t dims[5] = {64, rows, D / 64, kv, n};
         const cuuint64_t strides[4] = {map_stride(PREFIX ? s2[1] : s3[2], rows), 128, map_stride(PREFIX ? s2[0] : s3[1], kv), PREFIX ? 16 : map_stride(s3[0], n)};
-        const cuuint32_t box[5] = {64, AT_TILE, D / 64, 1, 1};
-        OBF_TRY(encode_map(i ? &m.v : &m.k, PREFIX ? (i ? p.pv : p.pk) : (i ? p.v : p.k), 5, dims, strides, box));
+        cuuint32_t box[5] = {64, AT_TILE, D / 64, 1, 1};
+        OBF_TRY(encode_map(i ? &m.v : &m.k, ptr, 5, dims, strides, box));
+        if (m.head_rows == 0) continue;
+        const bool shared_tile = m.head_rows < AT_TILE;
+        if (shared_tile) {
+            box[1] = AT_TILE - m.head_rows;
+            box[2] = 1;
+            OBF_TRY(encode_map(&m.rest[i], ptr, 5, dims, strides, box));
+            box[1] = m.head_rows;
+        }
+        dims[1] = (cuuint64_t)p.sinks < rows ? p.sinks : rows;           // rows behind the sinks read as zero
+        OBF_TRY(encode_map(&m.head[i], ptr, 5, dims, strides, box));
     }
     const long long items = t.pairs * (PREFIX ? p.p_slots : p.slots - p.p_slots);
     if (items > INT_MAX / 2) return OBF_ERR_UNSUPPORTED;
     const int blocks = items < sm_count() ? (int)items : sm_count();
-    OBF_TRY(launch(k_attend_tc<D, PREFIX>, dim3(blocks), AT_THREADS, AttendTcShape<D>::SMEM_BYTES, st, p, m, (int)items, first));
+    OBF_TRY(launch(k_attend_tc<D, PREFIX>, dim3(blocks), AT_THREADS, smem, st, p, m, (int)items, first));
     ++g_last_launches;
     return OBF_OK;
 }
