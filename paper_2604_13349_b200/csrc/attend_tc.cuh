@@ -12,11 +12,11 @@
 //                       twice as long for its tile, and the products wait for it), weights to bf16 over the logits' columns,
 //                       their fp32 sum; after the last tile O / sum to memory
 //
-// Softmax: fp32 and bf16 have the same exponents, so a row's reference need not be its maximum, only within 2^64 of it: the
-// maximum of the first tile of keys that the row sees serves, the logits are read once, and their maximum is formed beside the
-// exponentials instead of before them.  Only when it exceeds the reference by more than 64 in the log2 domain (never for most
-// rows) are the tile's weights formed again against the new one and O and the sum rescaled - in place: the products before
-// have completed, since they were issued before the logits that the thread has waited for.
+// Softmax: fp32 and bf16 have the same exponents, so a row's reference need not be its maximum, only near enough for no weight
+// to leave fp32's range.  It starts as zero, and the logits are read once, without a search for their maximum before.  Only when
+// a weight comes out above 2^64, or those of a row's first tile add up to less than 2^-40 (logits beyond some 28 or 44; rows that
+// see nothing of that tile), is the tile done again against the rows' maxima, O and the sums rescaled - in place: the products
+// before have completed, since they were issued before the logits that the thread has waited for.
 // Tensor memory: S (P) and O of the two tiles, 512 columns.  Every wait is bounded.
 //
 // Rows of V past the last key may hold anything, and 0 * NaN is not 0: the product over a short tile runs over its keys rounded
@@ -33,7 +33,7 @@ namespace obf {
 
 constexpr int AT_TILE = 128;
 constexpr int AT_THREADS = 640;
-constexpr float AT_RAISE = 64.f, AT_WEIGHT_MAX = 18446744073709551616.f;     // and 2 to that power
+constexpr float AT_RAISE = 64.f, AT_WEIGHT_MAX = 18446744073709551616.f, AT_WEIGHT_MIN = 9.094947017729282e-13f;     // 2^64, 2^-40
 constexpr int AT_POLY = 4;                                // of every four pairs of weights one by exp2_poly
 
 template <int D>
@@ -439,9 +439,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 real = real && b < p.batch && i < (PREFIX ? attend_q_len(p, min(b, p.batch - 1)) : im.ql);
             }
             const int t = PREFIX || !real ? 0 : im.t + im.first_i(x) + row_i;
-            float m = real ? -INFINITY : 0.f;            // (rows that are none have a reference from the start)
+            float m = 0.f;
             f32x2 l2 = 0ull;
-            bool started = false, known = false;          // known: all rows have references
+            bool started = false, known = true;           // known: all rows have references
             for (int j = jb; j < je; ++j) {
                 if (!(j < sk || (j >= ja && j < jz))) continue;
                 const bool late = !tc::mbar_wait(&bar_s[x], ns & 1u, wc);
@@ -496,10 +496,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                             w[16 * c + e] = pack_bf16(a, b2);
                         }
                     }
-                    // No weight may be above 2^64 of the reference; a logit that is not a number sends the tile the other way, too,
-                    // where it spreads.
+                    // No weight may be above 2^64 of the reference, and those of an item's first tile add up to something; a logit
+                    // that is not a number sends the tile the other way, too, where it spreads.
                     const float zs = sum2(z);
-                    if (!any(late || !(zs <= AT_WEIGHT_MAX) || !(mx <= AT_RAISE))) {
+                    if (!any(late || !(zs <= AT_WEIGHT_MAX) || !(mx <= AT_RAISE) || (!started && real && zs < AT_WEIGHT_MIN))) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) tmem_st16(s_t + col0 + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                         l2 = add2(l2, z);
@@ -516,6 +516,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         for (int e = 0; e < 32; ++e)
                             if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
                     };
+                    if (!started) m = real ? -INFINITY : 0.f;            // (rows that are none have a reference)
                     float mx = -INFINITY;
 #pragma unroll 1
                     for (int c = 0; c < nch; ++c) {
