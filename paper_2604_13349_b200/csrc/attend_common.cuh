@@ -9,6 +9,7 @@
 #pragma once
 
 #include <climits>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -119,95 +120,148 @@ __device__ __forceinline__ void store4(T *dst, float4 v)
     }
 }
 
+// Lets the stream's next kernel be set up while this one runs (it waits by itself for what it reads).  Behind pdl_wait(): what
+// that kernel reads and this one does not write is there by then.
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---- join -------------------------------------------------------------------------------------------------
-// Blocks 0 .. rows_total - 1: a row each, its parts dealt out to four warps, a lane D / 32 channels.  The blocks behind them
-// (only where masses are asked for) own AJ_KEYS keys of a (sequence, KV head) each: they need the lse of the head's at most 64
-// rows, which they work out from the parts themselves, so that masses do not wait for the rows' blocks.
-// Bound by latency: a few kilobytes per row.
+// A row is joined by one warp where there are many rows, by the four warps of a block where there are few: a lane holds D / 32
+// channels, its loads of the parts are independent of one another.  The blocks behind the rows' (only where masses are asked
+// for) own AJ_KEYS keys of a (sequence, KV head) each; they work out the lse of the head's at most 64 rows from the parts
+// themselves, so that masses do not wait for the rows' blocks.
+// Bound by latency where the parts are few, else by reading them from the L2 cache.
 constexpr int AJ_NT = 128;
 constexpr int AJ_KEYS = 512;
+constexpr int AJ_MAX_SLOTS = 256;
 
-__device__ __forceinline__ float join_lse(const AttendDev &p, long long R)
+// Weights of a row's parts, the lanes of a warp working together: w[slot] = 2^(lse - common lse), and the common lse (log2).
+// The weights add up to one; a row without keys gets zeros and -inf.
+__device__ __forceinline__ float join_weights(const AttendDev &p, long long R, int lane, float *w)
 {
-    float m = -INFINITY;
-    for (int i = 0; i < p.slots; ++i) m = fmaxf(m, p.part_lse[(long long)i * p.rows_total + R]);
-    if (!(m > -INFINITY)) return m;                       // no key (or only NaN: fmaxf drops it, the sum below keeps it)
+    float m = -INFINITY, l[AJ_MAX_SLOTS / 32];
+#pragma unroll
+    for (int k = 0; k < AJ_MAX_SLOTS / 32; ++k) {
+        const int sl = 32 * k + lane;
+        l[k] = sl < p.slots ? p.part_lse[(long long)sl * p.rows_total + R] : -INFINITY;
+        m = fmaxf(m, l[k]);
+    }
+    m = warp_max(m);
     float z = 0.f;
-    for (int i = 0; i < p.slots; ++i) z += exp2f(p.part_lse[(long long)i * p.rows_total + R] - m);
-    return m + log2f(z);
+#pragma unroll
+    for (int k = 0; k < AJ_MAX_SLOTS / 32; ++k) {
+        l[k] = l[k] == -INFINITY ? 0.f : exp2f(l[k] - m);          // (a lse that is not a number spreads, the maximum ignores it)
+        z += l[k];
+    }
+    z = warp_sum(z);
+    const float inv = z == 0.f ? 0.f : 1.f / z;
+#pragma unroll
+    for (int k = 0; k < AJ_MAX_SLOTS / 32; ++k)
+        if (32 * k + lane < p.slots) w[32 * k + lane] = l[k] * inv;
+    __syncwarp();
+    return z == 0.f ? -INFINITY : m + log2f(z);
 }
 
-template <typename TIN, int D>
-__global__ void __launch_bounds__(AJ_NT) k_attend_join(const __grid_constant__ AttendDev p)
+template <typename TIN, int D, int WARPS>
+__global__ void __launch_bounds__(AJ_NT) k_attend_join(const __grid_constant__ AttendDev p, const int row_blocks)
 {
     pdl_wait();
-    __shared__ float sh[4][D + 2];
+    pdl_trigger();
+    constexpr int C = D / 32, ROWS = AJ_NT / 32 / WARPS;            // rows of a block
+    typedef typename std::conditional<C == 4, float4, float2>::type vec;
+    __shared__ float wt[4][AJ_MAX_SLOTS];
+    __shared__ vec sh[4][32];
     const int rows_bh = p.n_q * p.G;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if ((long long)blockIdx.x < p.rows_total) {
-        constexpr int C = D / 32;
-        const long long R = blockIdx.x;
-        const int bh = (int)(R / rows_bh), r = (int)(R - (long long)bh * rows_bh);
+    if ((int)blockIdx.x < row_blocks) {
+        const long long R = (long long)blockIdx.x * ROWS + warp / WARPS;
+        const bool there = R < p.rows_total;
+        const int bh = there ? (int)(R / rows_bh) : 0, r = there ? (int)(R - (long long)bh * rows_bh) : 0;
         const int b = bh / p.kv_heads, h = bh - b * p.kv_heads, i = r / p.G, g = r - i * p.G;
-        if (i >= attend_q_len(p, b)) return;
-        float m = -INFINITY, z = 0.f, o[C];
+        if (!there || i >= attend_q_len(p, b)) return;              // (the same in every warp of a row)
+        const float lse2 = join_weights(p, R, lane, wt[warp]);
+        float o[C];
 #pragma unroll
         for (int e = 0; e < C; ++e) o[e] = 0.f;
-        for (int sl = warp; sl < p.slots; sl += 4) {
-            const float l = p.part_lse[(long long)sl * p.rows_total + R];
-            if (l == -INFINITY) continue;
-            const float mn = fmaxf(m, l), f = exp2f(m - mn), w = exp2f(l - mn);
-            const float *src = p.part_o + ((long long)sl * p.rows_total + R) * D + lane * C;
-            z = z * f + w;
-#pragma unroll
-            for (int e = 0; e < C; ++e) o[e] = o[e] * f + w * src[e];
-            m = mn;
+        const float *src = p.part_o + R * D + lane * C;
+#pragma unroll 8
+        for (int sl = warp % WARPS; sl < p.slots; sl += WARPS) {
+            const float w = wt[warp][sl];
+            if (w == 0.f) continue;                                  // nothing was written there
+            const vec v = *reinterpret_cast<const vec *>(src + (long long)sl * p.rows_total * D);
+            o[0] += w * v.x;
+            o[1] += w * v.y;
+            if constexpr (C == 4) { o[2] += w * v.z; o[3] += w * v.w; }
         }
+        if constexpr (WARPS > 1) {
+            vec v;
+            v.x = o[0];
+            v.y = o[1];
+            if constexpr (C == 4) { v.z = o[2]; v.w = o[3]; }
+            sh[warp][lane] = v;
+            __syncthreads();
+            if (warp != 0) return;
 #pragma unroll
-        for (int e = 0; e < C; ++e) sh[warp][lane * C + e] = o[e];
-        if (lane == 0) { sh[warp][D] = m; sh[warp][D + 1] = z; }
-        __syncthreads();
-        const float M = fmaxf(fmaxf(sh[0][D], sh[1][D]), fmaxf(sh[2][D], sh[3][D]));
-        float Z = 0.f, f[4];
+            for (int e = 0; e < C; ++e) o[e] = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) { f[w] = sh[w][D + 1] == 0.f ? 0.f : exp2f(sh[w][D] - M); Z += f[w] * sh[w][D + 1]; }
-        const float inv = Z == 0.f ? 0.f : 1.f / Z;
-        for (int e = threadIdx.x; e < D / 4; e += AJ_NT) {
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                v.x += f[w] * sh[w][4 * e]; v.y += f[w] * sh[w][4 * e + 1]; v.z += f[w] * sh[w][4 * e + 2]; v.w += f[w] * sh[w][4 * e + 3];
+            for (int k = 0; k < 4; ++k) {
+                const vec u = sh[k][lane];
+                o[0] += u.x;
+                o[1] += u.y;
+                if constexpr (C == 4) { o[2] += u.z; o[3] += u.w; }
             }
-            v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
-            store4(static_cast<TIN *>(p.out) + b * p.os[0] + (long long)(h * p.G + g) * p.os[1] + (long long)i * p.os[2] + 4 * e, v);
         }
-        if (p.lse_out && threadIdx.x == 0)
-            p.lse_out[((long long)b * p.kv_heads * p.G + h * p.G + g) * p.n_q + i] = Z == 0.f ? -INFINITY : natural_lse(M + log2f(Z));
+        TIN *dst = static_cast<TIN *>(p.out) + b * p.os[0] + (long long)(h * p.G + g) * p.os[1] + (long long)i * p.os[2] + lane * C;
+        if constexpr (C == 4) {
+            store4(dst, make_float4(o[0], o[1], o[2], o[3]));
+        } else if constexpr (sizeof(TIN) == 4) {
+            *reinterpret_cast<float2 *>(dst) = make_float2(o[0], o[1]);
+        } else {
+            *reinterpret_cast<uint32_t *>(dst) = pack_bf16(o[0], o[1]);
+        }
+        if (p.lse_out && lane == 0) p.lse_out[((long long)b * p.kv_heads * p.G + h * p.G + g) * p.n_q + i] = natural_lse(lse2);
         return;
     }
     // masses
     __shared__ float lse[64];
     const int per = (p.capacity + AJ_KEYS - 1) / AJ_KEYS;
-    const long long blk = (long long)blockIdx.x - p.rows_total;
-    const int bh = (int)(blk / per), j0 = (int)(blk - (long long)bh * per) * AJ_KEYS;
+    const int blk = (int)blockIdx.x - row_blocks;
+    const int bh = blk / per, j0 = (blk - bh * per) * AJ_KEYS;
     const int b = bh / p.kv_heads;
     const int len = attend_len(p, b), ql = attend_q_len(p, b);
     if (j0 >= len) return;
     const int rows = ql * p.G;
-    for (int r = threadIdx.x; r < rows; r += AJ_NT) lse[r] = join_lse(p, (long long)bh * rows_bh + r);
-    __syncthreads();
-    for (int j = j0 + threadIdx.x; j < min(j0 + AJ_KEYS, len); j += AJ_NT) {
-        float sum = 0.f;
-        for (int i = 0; i < ql; ++i) {
-            if (!attend_sees(p, len - ql + i, j)) continue;
-            for (int g = 0; g < p.G; ++g) {
-                const int r = i * p.G + g;
-                sum += exp2f(p.logits[((long long)bh * rows_bh + r) * p.capacity + j] - lse[r]);
-            }
-        }
-        const long long at = (long long)bh * p.capacity + j;
-        p.mass_out[at] = (p.mass_in ? p.decay * p.mass_in[at] : 0.f) + sum;
+    constexpr int K = AJ_KEYS / AJ_NT;
+    const long long at = (long long)bh * p.capacity + j0 + threadIdx.x;
+    float in[K], sum[K];
+#pragma unroll
+    for (int e = 0; e < K; ++e) {
+        sum[e] = 0.f;
+        in[e] = p.mass_in && j0 + (int)threadIdx.x + e * AJ_NT < len ? p.mass_in[at + e * AJ_NT] : 0.f;
     }
+    for (int r = warp; r < rows; r += AJ_NT / 32) {
+        const float l = join_weights(p, (long long)bh * rows_bh + r, lane, wt[warp]);
+        if (lane == 0) lse[r] = l;
+    }
+    __syncthreads();
+    for (int i = 0; i < ql; ++i) {
+        const int t = len - ql + i;
+        bool sees[K];
+#pragma unroll
+        for (int e = 0; e < K; ++e) {
+            const int j = j0 + (int)threadIdx.x + e * AJ_NT;
+            sees[e] = j < len && attend_sees(p, t, j);
+        }
+        const float *x = p.logits + ((long long)bh * rows_bh + i * p.G) * p.capacity + j0 + threadIdx.x;
+#pragma unroll 4
+        for (int g = 0; g < p.G; ++g) {
+#pragma unroll
+            for (int e = 0; e < K; ++e)
+                if (sees[e]) sum[e] += exp2f(x[(long long)g * p.capacity + e * AJ_NT] - lse[i * p.G + g]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < K; ++e)
+        if (j0 + (int)threadIdx.x + e * AJ_NT < len) p.mass_out[at + e * AJ_NT] = p.decay * in[e] + sum[e];
 }
 
 }  // namespace obf

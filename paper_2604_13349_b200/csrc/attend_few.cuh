@@ -56,7 +56,10 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
 {
     extern __shared__ __align__(128) unsigned char af_sm[];
     constexpr int KS = D / 16, CH = D / 8, ST = AF_STAGES<D>, ROWS = 8 * NT, LR = 32 / CH;
-    pdl_wait();
+    // Behind the kernel of the shared prefix these blocks start as its make room: they read nothing of it, and what it waited for is
+    // there.  Their own end waits for it, so that the join behind them sees both.
+    if (first) pdl_wait();
+    pdl_trigger();
     if (first && blockIdx.x == 0) attend_status(p);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rows_seq = p.n_q * p.G;
@@ -285,6 +288,7 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
             if (c == 0) p.part_lse[at] = lse2;
         }
     }
+    if (!first) pdl_wait();
 }
 
 }  // namespace obf

@@ -20,7 +20,8 @@ constexpr size_t attend_generic_smem() { return (size_t)(3 * AG_TILE * TD_LD<D> 
 template <typename TIN, int D, bool PREFIX>
 __global__ void __launch_bounds__(AG_NT) k_attend_generic(const __grid_constant__ AttendDev p, const int first)
 {
-    pdl_wait();
+    if (first) pdl_wait();                               // (else as in k_attend_few)
+    pdl_trigger();
     extern __shared__ float sm[];
     float *Qs = sm, *Ks = Qs + AG_TILE * TD_LD<D>, *Vs = Ks + AG_TILE * TD_LD<D>, *Ps = Vs + AG_TILE * TD_LD<D>;
     constexpr int P_LD = AG_TILE + 4, VEC = 16 / sizeof(TIN), CH = D / VEC, CT = D / 16;
@@ -184,6 +185,7 @@ __global__ void __launch_bounds__(AG_NT) k_attend_generic(const __grid_constant_
             if (tx == 0) p.part_lse[at] = lse2;
         }
     }
+    if (!first) pdl_wait();
 }
 
 }  // namespace obf

@@ -266,7 +266,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = s_tmem;
-    pdl_wait();
+    if (first) pdl_wait();                               // (else as in k_attend_few)
+    pdl_trigger();
     if (first && blockIdx.x == 0) attend_status(p);
 
     AttendTcItem<PREFIX> it;
@@ -678,6 +679,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     tc::tc_fence_before();
     __syncthreads();
     if (warp == 0) tc::tmem_dealloc(tmem, 512);
+    if (!first) pdl_wait();
 }
 
 }  // namespace obf

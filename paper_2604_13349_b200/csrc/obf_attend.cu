@@ -294,10 +294,14 @@ static obf_status_t run_attend(const AttendLayout &L, const AttendDev &p, cudaSt
     if (p.prefix) OBF_TRY((launch_attend<TIN, D, true>(L.p_path, p, 1, st)));
     OBF_TRY((launch_attend<TIN, D, false>(L.own_path, p, p.prefix == 0, st)));
     if (p.slots > 1 || p.mass_out) {
-        long long blocks = p.rows_total;
+        // a warp per row fills the chip from some thousand rows on; fewer are joined by four warps each
+        const bool many = p.rows_total >= 4 * 148;
+        const long long row_blocks = many ? (p.rows_total + 3) / 4 : p.rows_total;
+        long long blocks = row_blocks;
         if (p.mass_out) blocks += (long long)p.batch * p.kv_heads * ((p.capacity + AJ_KEYS - 1) / AJ_KEYS);
         if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
-        OBF_TRY(launch(k_attend_join<TIN, D>, dim3((unsigned)blocks), AJ_NT, 0, st, p));
+        if (many) OBF_TRY(launch(k_attend_join<TIN, D, 1>, dim3((unsigned)blocks), AJ_NT, 0, st, p, (int)row_blocks));
+        else OBF_TRY(launch(k_attend_join<TIN, D, 4>, dim3((unsigned)blocks), AJ_NT, 0, st, p, (int)row_blocks));
         ++g_last_launches;
     }
     return OBF_OK;
