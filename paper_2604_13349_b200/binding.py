@@ -387,79 +387,72 @@ def _refuse(name: str, t, shape, dtype, device) -> None:
         name, dtype, tuple(shape), device, "%s %s on %s" % (t.dtype, tuple(t.shape), t.device) if isinstance(t, torch.Tensor) else type(t).__name__))
 
 
-def _rows(t: torch.Tensor, shape, dtype, device, name: str):
+def _rows(t: torch.Tensor, shape, dtype, device: int, name: str):
     """Checks a tensor of rows of contiguous channels and gives its strides."""
-    if t.shape != shape or t.dtype != dtype or t.device != device:
-        _refuse(name, t, shape, dtype, device)
     st = t.stride()
-    if st[-1] != 1:
-        raise ValueError("%s: channels must be contiguous" % name)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or st[-1] != 1:
+        _refuse(name + " (contiguous channels)", t, shape, dtype, device)
     return st
 
 
-def _dense(t: Optional[torch.Tensor], shape, dtype, device, name: str) -> int:
+def _dense(t: Optional[torch.Tensor], shape, dtype, device: int, name: str) -> int:
     if t is None:
         return 0
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
         _refuse(name + " (contiguous)", t, shape, dtype, device)
     return t.data_ptr()
 
 
 def _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags) -> bytes:
-    dt, dev = q.dtype, q.device
-    if dt not in _DTYPES or dev.type != "cuda" or q.dim() != 4 or k.dim() != 4:
+    dt, dev = q.dtype, q.get_device()
+    if dt not in _DTYPES or dev < 0 or q.dim() != 4 or k.dim() != 4:
         raise ValueError("q, k: float32 or bfloat16 device tensors [batch, heads, rows, head_dim] expected")
-    B, hq, n_q, d = shape_q = q.shape
-    kv, cap = k.shape[1], k.shape[2]
-    shape_k = (B, kv, cap, d)
+    shape_q, shape_k = q.shape, k.shape
+    B, hq, n_q, d = shape_q
+    _, kv, cap, _ = shape_k
+    if shape_k[0] != B or shape_k[3] != d:
+        _refuse("k", k, (B, kv, cap, d), dt, dev)
+    f32, i32 = torch.float32, torch.int32
     sq, so = _rows(q, shape_q, dt, dev, "q"), _rows(out, shape_q, dt, dev, "out")
     sk, sv = _rows(k, shape_k, dt, dev, "k"), _rows(v, shape_k, dt, dev, "v")
     return _ATTEND.pack(
         B, kv, hq, d, n_q, cap, window, sinks, _DTYPES[dt], scale, decay, flags, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
         sq[0], sq[1], sq[2], sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], so[0], so[1], so[2],
-        _dense(lens, (B,), torch.int32, dev, "lens"), _dense(q_lens, (B,), torch.int32, dev, "q_lens"),
-        _dense(lse_out, (B, hq, n_q), torch.float32, dev, "lse_out"), _dense(mass_in, (B, kv, cap), torch.float32, dev, "mass_in"),
-        _dense(mass_out, (B, kv, cap), torch.float32, dev, "mass_out"))
+        _dense(lens, (B,), i32, dev, "lens"), _dense(q_lens, (B,), i32, dev, "q_lens"), _dense(lse_out, shape_q[:3], f32, dev, "lse_out"),
+        _dense(mass_in, shape_k[:3], f32, dev, "mass_in"), _dense(mass_out, shape_k[:3], f32, dev, "mass_out"))
 
 
-def _handle(stream, device: torch.device) -> int:
-    """The given stream's handle, else that of the device's current stream."""
+def _enqueue(name: str, device: int, args, stream) -> None:
+    """The call with the tensors' device current, on the given stream or the device's current one."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index)
-    return stream if isinstance(stream, int) else stream.cuda_stream
-
-
-def _enqueue(name: str, device: torch.device, *args) -> None:
-    """The call, with the tensors' device current."""
-    fn = _packed(name)
-    if device.index != torch.cuda.current_device():
+        stream = torch._C._cuda_getCurrentRawStream(device)
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    if device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            rc = fn(*args)
+            rc = _packed(name)(*args, stream)
     else:
-        rc = fn(*args)
+        rc = _packed(name)(*args, stream)
     if rc != OBF_OK:
         raise ObfError(rc, name)
 
 
 def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, stream):
-    dev = q.device
     if workspace is None:
         nb = ctypes.c_size_t(0)
         rc = _packed("obf_attend_workspace_bytes")(args, prefix, ctypes.addressof(nb))
         if rc != OBF_OK:
             raise ObfError(rc, name)
         size = nb.value
-        workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
         if stream is not None:                   # the allocator gives the memory on once the given stream is done with it
-            workspace.record_stream(torch.cuda.ExternalStream(stream, device=dev) if isinstance(stream, int) else stream)
+            workspace.record_stream(torch.cuda.ExternalStream(stream, device=q.device) if isinstance(stream, int) else stream)
     else:
-        if workspace.device != dev:
-            raise ValueError("workspace: on %s expected" % dev)
+        if workspace.device != q.device:
+            raise ValueError("workspace: on %s expected" % q.device)
         size = workspace.numel() * workspace.element_size()
-    if prefix is None:
-        _enqueue(name, dev, args, workspace.data_ptr(), size, _handle(stream, dev))
-    else:
-        _enqueue(name, dev, args, prefix, workspace.data_ptr(), size, _handle(stream, dev))
+    call = (args, workspace.data_ptr(), size) if prefix is None else (args, prefix, workspace.data_ptr(), size)
+    _enqueue(name, q.get_device(), call, stream)
     got = {"out": out, "workspace": workspace}
     if lse_out is not None:
         got["lse"] = lse_out
@@ -508,7 +501,7 @@ def attend_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tenso
         raise ValueError("k_prefix: [kv_heads, rows, head_dim] expected")
     rows = k_prefix.shape[1]
     shape = (k.shape[1], rows, q.shape[3])
-    sk, sv = _rows(k_prefix, shape, q.dtype, q.device, "k_prefix"), _rows(v_prefix, shape, q.dtype, q.device, "v_prefix")
+    sk, sv = _rows(k_prefix, shape, q.dtype, q.get_device(), "k_prefix"), _rows(v_prefix, shape, q.dtype, q.get_device(), "v_prefix")
     prefix = _PREFIX.pack(k_prefix.data_ptr(), v_prefix.data_ptr(), sk[0], sk[1], sv[0], sv[1], rows)
     return _attend_call("obf_attend_shared", args, prefix, q, out, lse_out, None, workspace, stream)
 
@@ -529,8 +522,8 @@ def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: in
     ``[batch, kv_heads, capacity]``: the first ``sinks``, the last ``recent`` and the heaviest others, in ascending order
     (``obf_evict_by_mass`` in include/obf.h).  ``k_out, v_out`` and ``mass_out`` may have more rows than ``keep``: the cache goes on
     there.  Returns ``K_out, V_out, idx, mass, lens``."""
-    dt, dev = k.dtype, k.device
-    if dt not in _DTYPES or dev.type != "cuda" or k.dim() != 4:
+    dt, dev, at = k.dtype, k.device, k.get_device()
+    if dt not in _DTYPES or at < 0 or k.dim() != 4:
         raise ValueError("k: a float32 or bfloat16 device tensor [batch, kv_heads, capacity, head_dim] expected")
     B, kv, cap, d = shape = k.shape
     make = torch.zeros if lens is not None or keep > cap else torch.empty        # rows behind a sequence's last one are not written
@@ -547,13 +540,13 @@ def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: in
     ko, vo, mo = k_out.shape[2], v_out.shape[2], mass_out.shape[2]
     if min(ko, vo, mo) < keep:
         raise ValueError("k_out, v_out and mass_out: at least `keep` rows expected")
-    sk, sv = _rows(k, shape, dt, dev, "k"), _rows(v, shape, dt, dev, "v")
-    s1, s2 = _rows(k_out, (B, kv, ko, d), dt, dev, "k_out"), _rows(v_out, (B, kv, vo, d), dt, dev, "v_out")
+    sk, sv = _rows(k, shape, dt, at, "k"), _rows(v, shape, dt, at, "v")
+    s1, s2 = _rows(k_out, (B, kv, ko, d), dt, at, "k_out"), _rows(v_out, (B, kv, vo, d), dt, at, "v_out")
     args = _EVICT.pack(
         B, kv, d, cap, _DTYPES[dt], keep, sinks, recent, k.data_ptr(), v.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
         sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], s1[0], s1[1], s1[2], s2[0], s2[1], s2[2],
-        _dense(mass, (B, kv, cap), torch.float32, dev, "mass"), _dense(lens, (B,), torch.int32, dev, "lens"),
-        _dense(idx_out, (B, kv, keep), torch.int32, dev, "idx_out"), _dense(mass_out, (B, kv, mo), torch.float32, dev, "mass_out"), mo,
-        _dense(lens_out, (B,), torch.int32, dev, "lens_out"))
-    _enqueue("obf_evict_by_mass", dev, args, _handle(stream, dev))
+        _dense(mass, (B, kv, cap), torch.float32, at, "mass"), _dense(lens, (B,), torch.int32, at, "lens"),
+        _dense(idx_out, (B, kv, keep), torch.int32, at, "idx_out"), _dense(mass_out, (B, kv, mo), torch.float32, at, "mass_out"), mo,
+        _dense(lens_out, (B,), torch.int32, at, "lens_out"))
+    _enqueue("obf_evict_by_mass", at, (args,), stream)
     return {"K_out": k_out, "V_out": v_out, "idx": idx_out, "mass": mass_out, "lens": lens_out}

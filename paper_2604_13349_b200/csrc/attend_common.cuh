@@ -30,6 +30,7 @@ struct AttendDev {
     int32_t batch, kv_heads, G, n_q, capacity, window, sinks;
     int32_t prefix;           // rows of the shared prefix, 0 without one
     int32_t p_slots, slots;   // parts of the prefix and all parts of a row (own keys: slots - p_slots); 1: no join
+    int32_t cluster;          // the parts of a row are a cluster of blocks, which joins them
     long long rows_total;     // batch * kv_heads * n_q * G
     // workspace
     uint32_t *status;

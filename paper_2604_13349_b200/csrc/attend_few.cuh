@@ -5,7 +5,8 @@
 // swizzled by the row so that matrix loads meet every bank once), so warps never wait for one another before the end.  Keys lie
 // on the M side of the 16 x 8 x 16 products: S^T = K Q^T and O^T += V^T P^T waste nothing for groups of up to eight rows, where
 // queries on the M side would leave half of every product empty.  Two to three blocks share a multiprocessor: 128 KB and more
-// of reads in flight.
+// of reads in flight.  Up to eight parts are a cluster, which joins them through shared memory: one launch, nothing in the
+// workspace.
 //
 // Softmax: a row's reference is its maximum at the time it was last raised; it is raised (and O and the sum rescaled) only when
 // a logit exceeds it by more than 8 in the log2 domain, so weights stay below 2^8 and the common step has no shuffles.  Weights
@@ -51,9 +52,35 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
     return r;
 }
 
-template <int D, int NT, bool PREFIX>
+// ---- a cluster's blocks: meeting, and reading one another's shared memory ----
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_addr(const void *own, int rank)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(own)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float4 cluster_load4(uint32_t a)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float cluster_load(uint32_t a)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// CLUSTER: the parts of a tile, at most eight, are a cluster, which joins them through its shared memory.
+template <int D, int NT, bool PREFIX, bool CLUSTER>
 __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ AttendDev p, const int first)
 {
+    static_assert(!(PREFIX && CLUSTER), "parts of a prefix are joined with those of the own keys");
     extern __shared__ __align__(128) unsigned char af_sm[];
     constexpr int KS = D / 16, CH = D / 8, ST = AF_STAGES<D>, ROWS = 8 * NT, LR = 32 / CH;
     // Behind the kernel of the shared prefix these blocks start as its make room: they read nothing of it, and what it waited for is
@@ -260,6 +287,12 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
     __syncthreads();
     const bool last = p.slots == 1 && !p.mass_out;
     constexpr int TR = D / 4;                             // threads of a row, four channels each
+    float *cl = ml + AF_WARPS * ROWS * 2, *cl_lse = cl + ROWS * LD;       // what the cluster's other blocks read
+    static_assert(((size_t)AF_WARPS * ROWS * (LD + 2) + ROWS * (LD + 1)) * 4 <= attend_few_smem<D>(), "");
+    auto put = [&](int b, int h2, int i, int c, const float4 &a, float lse2) {
+        store4(static_cast<__nv_bfloat16 *>(p.out) + b * p.os[0] + (long long)h2 * p.os[1] + (long long)i * p.os[2] + c, a);
+        if (p.lse_out && c == 0) p.lse_out[((long long)b * p.kv_heads * p.G + h2) * p.n_q + i] = natural_lse(lse2);
+    };
     for (int row = threadIdx.x / TR; row < ROWS; row += AF_NT / TR) {
         const int run = tile * ROWS + row, c = threadIdx.x % TR * 4;
         int b, r;
@@ -279,14 +312,42 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
         }
         const float inv = Z == 0.f ? 0.f : 1.f / Z, lse2 = Z == 0.f ? -INFINITY : M + log2f(Z);
         a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
-        if (last) {
-            store4(static_cast<__nv_bfloat16 *>(p.out) + b * p.os[0] + (long long)(h * p.G + g) * p.os[1] + (long long)i * p.os[2] + c, a);
-            if (p.lse_out && c == 0) p.lse_out[((long long)b * p.kv_heads * p.G + h * p.G + g) * p.n_q + i] = natural_lse(lse2);
+        if constexpr (CLUSTER) {
+            *reinterpret_cast<float4 *>(&cl[row * LD + c]) = a;
+            if (c == 0) cl_lse[row] = lse2;
+        } else if (last) {
+            put(b, h * p.G + g, i, c, a, lse2);
         } else {
             const long long at = (long long)(PREFIX ? part : p.p_slots + part) * p.rows_total + ((long long)b * p.kv_heads + h) * rows_seq + r;
             *reinterpret_cast<float4 *>(p.part_o + at * D + c) = a;
             if (c == 0) p.part_lse[at] = lse2;
         }
+    }
+    if constexpr (CLUSTER) {
+        cluster_sync();
+        for (int row = part + parts * (threadIdx.x / TR); row < ROWS; row += parts * (AF_NT / TR)) {
+            const int r = tile * ROWS + row, c = threadIdx.x % TR * 4, i = r / p.G;
+            if (r >= rows_run || i >= ql_own) continue;
+            float l[8], M = -INFINITY, Z = 0.f;
+            float4 u[8], a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < parts) {
+                    l[k] = cluster_load(cluster_addr(cl_lse + row, k));
+                    u[k] = cluster_load4(cluster_addr(cl + row * LD + c, k));
+                    M = fmaxf(M, l[k]);
+                }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < parts) {
+                    const float f = l[k] == -INFINITY ? 0.f : exp2f(l[k] - M);
+                    Z += f;
+                    a.x += f * u[k].x; a.y += f * u[k].y; a.z += f * u[k].z; a.w += f * u[k].w;
+                }
+            const float inv = Z == 0.f ? 0.f : 1.f / Z;
+            put(b_own, h * p.G + r - i * p.G, i, c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv), Z == 0.f ? -INFINITY : M + log2f(Z));
+        }
+        cluster_sync();                                   // nobody leaves while its memory is read
     }
     if (!first) pdl_wait();
 }

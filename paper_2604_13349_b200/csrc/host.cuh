@@ -62,11 +62,12 @@ inline obf_status_t set_smem(K kernel, size_t bytes)
     } while (0)
 
 // Launch that may be set up while the stream's kernel before it still runs: every kernel launched so begins with
-// pdl_wait().  Between two kernels of a call that is about a microsecond less.
+// pdl_wait().  Between two kernels of a call that is about a microsecond less.  `cluster`: blocks of a thread-block cluster, at most
+// eight, in the grid's first dimension.
 template <typename... P, typename... A>
-inline obf_status_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args)
+inline obf_status_t launch_clusters(int cluster, void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args)
 {
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
@@ -76,8 +77,20 @@ inline obf_status_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t 
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
+    if (cluster > 1) {
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = cluster;
+        at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
     OBF_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     return OBF_OK;
+}
+
+template <typename... P, typename... A>
+inline obf_status_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args)
+{
+    return launch_clusters(1, kernel, grid, threads, smem, st, args...);
 }
 
 // cuTensorMapEncodeTiled, looked up through the runtime so that the library does not link the driver.
