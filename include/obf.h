@@ -408,7 +408,7 @@ typedef struct {
     int64_t k_stride[3], v_stride[3], k_out_stride[3], v_out_stride[3];
     const float *mass;                  /* device [batch, kv_heads, capacity]                                    */
     const int32_t *lens;                /* device [batch], or NULL: capacity                                     */
-    int32_t *idx_out;                   /* device [batch, kv_heads, keep] kept positions, or NULL                */
+    int32_t *idx_out;                   /* device [batch, kv_heads, keep] kept positions                         */
     float *mass_out;                    /* device [batch, kv_heads, mass_out_rows] masses of the kept rows, or NULL */
     int32_t mass_out_rows;              /* >= keep (the capacity of the cache that the outputs go on as)         */
     int32_t *lens_out;                  /* device [batch], or NULL: min(keep, lens[b])                           */

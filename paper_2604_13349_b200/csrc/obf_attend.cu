@@ -358,9 +358,19 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *w
 template <int ROW_BYTES>
 static obf_status_t launch_evict(const EvictDev &p, cudaStream_t st)
 {
-    static bool done[64];
-    OBF_TRY(set_smem_once(k_evict_mass<ROW_BYTES>, evict_smem(EM_CACHE), done));
-    OBF_TRY(launch(k_evict_mass<ROW_BYTES>, dim3((unsigned)(p.batch * p.kv_heads * p.parts)), EM_NT, evict_smem(p.capacity), st, p));
+    const long long heads = (long long)p.batch * p.kv_heads;
+    if (p.capacity > EM_CACHE) {
+        const long long blocks = heads * ((p.keep + EC_ROWS - 1) / EC_ROWS);
+        if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
+        OBF_TRY(launch(k_evict_select, dim3((unsigned)heads), ES_NT, 0, st, p));
+        OBF_TRY(launch(k_evict_copy<ROW_BYTES>, dim3((unsigned)blocks), EM_NT, 0, st, p));
+        g_last_launches += 2;
+        return OBF_OK;
+    }
+    const dim3 grid((unsigned)(heads * p.parts));
+    if (p.capacity <= 4 * EM_NT) OBF_TRY(launch(k_evict_mass<ROW_BYTES, 4>, grid, EM_NT, 0, st, p));
+    else if (p.capacity <= 16 * EM_NT) OBF_TRY(launch(k_evict_mass<ROW_BYTES, 16>, grid, EM_NT, 0, st, p));
+    else OBF_TRY(launch(k_evict_mass<ROW_BYTES, 32>, grid, EM_NT, 0, st, p));
     ++g_last_launches;
     return OBF_OK;
 }
@@ -400,7 +410,7 @@ obf_status_t obf_evict_by_mass(const obf_evict_t *a, void *stream)
     if (a->dtype != OBF_F32 && a->dtype != OBF_BF16) return OBF_ERR_UNSUPPORTED;
     const long long heads = (long long)a->batch * a->kv_heads;
     if (heads > 1 << 24) return OBF_ERR_UNSUPPORTED;
-    if (!a->k || !a->v || !a->k_out || !a->v_out || !a->mass || misaligned(a->k) || misaligned(a->v) || misaligned(a->k_out) || misaligned(a->v_out))
+    if (!a->k || !a->v || !a->k_out || !a->v_out || !a->mass || !a->idx_out || misaligned(a->k) || misaligned(a->v) || misaligned(a->k_out) || misaligned(a->v_out))
         return OBF_ERR_INVALID_ARG;
     const void *words[] = {a->mass, a->lens, a->idx_out, a->mass_out, a->lens_out};
     for (const void *w : words)
@@ -418,11 +428,11 @@ obf_status_t obf_evict_by_mass(const obf_evict_t *a, void *stream)
     p.mass = a->mass; p.lens = a->lens; p.idx_out = a->idx_out; p.mass_out = a->mass_out; p.lens_out = a->lens_out;
     p.batch = a->batch; p.kv_heads = a->kv_heads; p.capacity = a->capacity; p.keep = a->keep; p.sinks = a->sinks; p.recent = a->recent;
     p.mass_out_rows = a->mass_out_rows;
-    // about four blocks per multiprocessor, at least 64 rows each
+    // as many blocks as run at once, two per multiprocessor, at least 64 rows each
     const int kept = a->keep < a->capacity ? a->keep : a->capacity;
-    long long parts = (4 * 148 + heads - 1) / heads;
+    long long parts = 2 * 148 / heads;
     if (parts > (kept + 63) / 64) parts = (kept + 63) / 64;
-    p.parts = (int)parts;
+    p.parts = parts < 1 ? 1 : (int)parts;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     switch (a->head_dim * es) {
     case 128: return launch_evict<128>(p, st);

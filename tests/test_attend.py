@@ -102,7 +102,7 @@ def test_attend_shared_refuses(lib, kw, px):
 
 def _evict_args(**kw):
     d = dict(batch=2, kv_heads=2, head_dim=64, capacity=100, dtype=P.OBF_BF16, keep=10, sinks=2, recent=3, k=0x1000, v=0x1000, k_out=0x1000, v_out=0x1000,
-             mass=0x1000, mass_out_rows=10)
+             mass=0x1000, idx_out=0x1000, mass_out_rows=10)
     strides = dict(k_stride=(12800, 6400, 64), v_stride=(12800, 6400, 64), k_out_stride=(1280, 640, 64), v_out_stride=(1280, 640, 64))
     for n, x in kw.items():
         (strides if n in strides else d)[n] = x
@@ -116,7 +116,7 @@ def _evict_args(**kw):
     (dict(batch=0), INVALID), (dict(kv_heads=0), INVALID), (dict(capacity=0), INVALID), (dict(keep=0), INVALID), (dict(keep=4), INVALID),
     (dict(sinks=-1), INVALID), (dict(recent=-1), INVALID), (dict(sinks=(1 << 31) - 1, recent=(1 << 31) - 1), INVALID), (dict(head_dim=80), UNSUPPORTED),
     (dict(dtype=3), UNSUPPORTED), (dict(k=0), INVALID), (dict(mass=0), INVALID), (dict(v_out=0x1008), INVALID), (dict(lens=0x1001), INVALID),
-    (dict(idx_out=0x1002), INVALID), (dict(mass_out=0x1000, mass_out_rows=9), INVALID), (dict(k_stride=(12800, 6400, 65)), INVALID),
+    (dict(idx_out=0x1002), INVALID), (dict(idx_out=0), INVALID), (dict(mass_out=0x1000, mass_out_rows=9), INVALID), (dict(k_stride=(12800, 6400, 65)), INVALID),
     (dict(v_out_stride=(1280, 0, 64)), INVALID), (dict(batch=1 << 20, kv_heads=32), UNSUPPORTED),
 ])
 def test_evict_by_mass_refuses(lib, kw, code):
@@ -281,7 +281,8 @@ def test_attend_scale_and_large_logits(dtype, flags):
 @pytest.mark.parametrize("d,dtype", [(64, BF16), (128, BF16), (128, F32)])
 @pytest.mark.parametrize("cap,lens,keep,sinks,recent", [
     (1, [1, 0], 1, 0, 0), (64, [64, 10], 16, 4, 4), (300, [300, 299], 299, 0, 0), (1000, [1000, 512], 101, 4, 16), (700, [700, 650], 64, 60, 4),
-    (500, [500, 3], 700, 5, 5), (2100, [2100, 2049], 1500, 0, 1), (20000, [20000, 17000], 300, 4, 100),
+    (500, [500, 3], 700, 5, 5), (2100, [2100, 2049], 1500, 0, 1), (8193, [8193, 8000], 5000, 1, 8), (16384, [16384, 16383], 2500, 2500, 0),
+    (20000, [20000, 17000], 300, 4, 100), (16385, [16385, 2], 16384, 0, 0),
 ])
 def test_evict_by_mass(d, dtype, cap, lens, keep, sinks, recent):
     gen = torch.Generator().manual_seed(cap)
