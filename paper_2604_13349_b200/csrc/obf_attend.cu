@@ -144,7 +144,7 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
             const int t = few_rows(rows_run);
             const long long tiles = runs * ((rows_run + t - 1) / t);
             if (8 * tiles <= FEW_RESIDENT && keys <= 4096) return parts_for(1, keys, 8, 64);
-            return parts_for(tiles, keys, 6 * 148, 256);
+            return parts_for(tiles, keys, 6 * 148, tiles * ((keys + 511) / 512) >= FEW_RESIDENT ? 512 : 256);
         }
         if (path == ATTEND_TC) return tc_parts(tc_tiles((int)(a->q_heads / a->kv_heads), a->n_q, a->batch, a->kv_heads, rows_run != rows_seq).pairs, keys);
         return parts_for(runs * ((rows_run + AG_TILE - 1) / AG_TILE), keys, 2 * 148, 4 * AG_TILE);
