@@ -34,7 +34,6 @@ namespace obf {
 constexpr int AT_TILE = 128;
 constexpr int AT_THREADS = 640;
 constexpr float AT_RAISE = 64.f, AT_WEIGHT_MAX = 18446744073709551616.f, AT_WEIGHT_MIN = 9.094947017729282e-13f;     // 2^64, 2^-40
-constexpr int AT_POLY = 4;                                // of every four pairs of weights one by exp2_poly
 
 template <int D>
 struct AttendTcShape {
@@ -162,6 +161,19 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, c
     return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, w));
 }
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
+
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
@@ -174,14 +186,6 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map
                  ::"r"(dst), "l"(map), "r"(tc::smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 
-// The larger of three, NaN if one is.
-__device__ __forceinline__ float max3_nan(float a, float b, float c)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-
 // A box of keys or values: rows from `row` on, column block `block` (all of them for boxes that are that wide).
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int row, int block, int head, int seq)
 {
@@ -189,27 +193,21 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map
                  ::"r"(dst), "l"(map), "r"(tc::smem_u32(bar)), "r"(0), "r"(row), "r"(block), "r"(head), "r"(seq) : "memory");
 }
 
-// 2^x of a pair on the multiply-add units, for a share of the weights: the special-function unit's 16 results per cycle would
-// otherwise be the narrowest place.  x = n + f with |f| <= 1/2 (n by adding and subtracting 1.5 * 2^23), a polynomial of degree
-// four in f whose relative error is evenly spread (exchange algorithm; 2.7e-6 at most in fp32, 4e-8 on average), n added to the
-// exponent.  For x < 127; below -126 the result is 2^-126 (bf16 weights and an fp32 sum whose other terms are near one); not for
-// NaN.  `mx` gathers the largest x, for the caller to see that.
-__device__ __forceinline__ void exp2_poly(f32x2 x, float &mx, float &a, float &b)
+// The values are there before the next load from tensor memory begins: otherwise the compiler begins it early and runs out of registers.
+__device__ __forceinline__ void hold16(uint32_t (&r)[16])
 {
-    float x0, x1;
-    upk(x, x0, x1);
-    mx = max3_nan(mx, x0, x1);
-    x = pk(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-    const f32x2 y = add2(x, pk(12582912.f, 12582912.f)), f = fma2(add2(y, pk(-12582912.f, -12582912.f)), pk(-1.f, -1.f), x);
-    f32x2 q = fma2(f, pk(0.009570102207362652f, 0.009570102207362652f), pk(0.05591785907745361f, 0.05591785907745361f));
-    q = fma2(q, f, pk(0.240247443318367f, 0.240247443318367f));
-    q = fma2(q, f, pk(0.6931217908859253f, 0.6931217908859253f));
-    q = fma2(q, f, pk(0.9999992847442627f, 0.9999992847442627f));
-    float q0, q1, y0, y1;
-    upk(q, q0, q1);
-    upk(y, y0, y1);
-    a = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(y0) << 23));
-    b = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(y1) << 23));
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+
+// 32 bytes to global memory, in two halves where the address is no multiple of 32.
+__device__ __forceinline__ void store32(void *dst, const uint32_t (&r)[8], bool wide)
+{
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(dst)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+        reinterpret_cast<uint4 *>(dst)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+    }
 }
 
 // Bits of columns a .. b - 1 of 32.
@@ -426,6 +424,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         };
         uint32_t n = 0, ni = 0, ns = 0, no = 0;
         bool dead = false;
+        const bool wide = (((reinterpret_cast<uintptr_t>(p.out) | (uintptr_t)(p.os[0] | p.os[1] | p.os[2]) * 2) & 31u) == 0);
         for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
             if (any(!tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc))) break;
             // (what only the beginning and the end of an item need is read from shared memory both times: registers are short)
@@ -466,10 +465,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                 bool formed = false;                      // the tile's weights
                 uint32_t w[32];
                 if (known && (width & 15) == 0) {
-                    // every row has a reference, and a sum that the 2^-126 of exp2_poly for a hidden key does not show in
+                    // every row has a reference
                     const bool full = j >= fa && j < fz;
                     const f32x2 r2 = pk(-m, -m);
-                    float mx = -INFINITY;                 // of the logits that exp2_poly is for
                     f32x2 z = 0ull;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -486,13 +484,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         for (int e = 0; e < 16; ++e) {
                             const f32x2 y = fma2(pk(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, r2);
                             float a, b2;
-                            if (e % AT_POLY == 1) {
-                                exp2_poly(y, mx, a, b2);
-                            } else {
-                                upk(y, a, b2);
-                                a = ex2(a);
-                                b2 = ex2(b2);
-                            }
+                            upk(y, a, b2);
+                            a = ex2(a);
+                            b2 = ex2(b2);
                             z = add2(z, pk(a, b2));
                             w[16 * c + e] = pack_bf16(a, b2);
                         }
@@ -500,7 +494,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     // No weight may be above 2^64 of the reference, and those of an item's first tile add up to something; a logit
                     // that is not a number sends the tile the other way, too, where it spreads.
                     const float zs = sum2(z);
-                    if (!any(late || !(zs <= AT_WEIGHT_MAX) || !(mx <= AT_RAISE) || (!started && real && zs < AT_WEIGHT_MIN))) {
+                    if (!any(late || !(zs <= AT_WEIGHT_MAX) || (!started && real && zs < AT_WEIGHT_MIN))) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) tmem_st16(s_t + col0 + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                         l2 = add2(l2, z);
@@ -601,65 +595,25 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             const long long R = (((long long)b * p.kv_heads + im.h) * p.n_q + i) * p.G + g;
             const bool last = p.slots == 1;
             const long long at = (long long)(PREFIX ? im.part : p.p_slots + im.part) * p.rows_total + R;
-            // O is read as matrix fragments: of eight columns 8 b .. a lane has 2 (lane mod 4), + 1 of rows lane / 4 and lane / 4 + 8.
-            // The four lanes of a row then trade pieces so that each has 8 neighbouring channels of the four blocks: their stores
-            // are whole sectors, eight rows at a time, where a row per thread would touch 32 lines with every store.
-            const int quad = lane & 3;
-            const int hrow = 16 * half;                  // a row's two warps store 16 rows each
-            {
-                float scale[2];
-                bool there[2];
-                long long to[2];
-                const long long to_own = last ? b * p.os[0] + (long long)(im.h * p.G + g) * p.os[1] + (long long)i * p.os[2] : at * D;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int from = hrow + 8 * u + lane / 4;
-                    scale[u] = __shfl_sync(0xffffffffu, inv, from);
-                    there[u] = __shfl_sync(0xffffffffu, (int)(real && (last || l != 0.f)), from) != 0;
-                    to[u] = __shfl_sync(0xffffffffu, to_own, from);
-                }
+            // each of a row's threads stores half of its channels, 32 bytes at a time
+            const long long to = (last ? b * p.os[0] + (long long)(im.h * p.G + g) * p.os[1] + (long long)i * p.os[2] : at * D) + half * (D / 2);
 #pragma unroll 1
-                for (int c = 0; c < D / 64; ++c) {
-                    uint32_t o[32];
-                    if (started) {
-                        tc::tmem_ld_frag(o_t + ((uint32_t)hrow << 16) + 64 * c, o);
-                        tc::tmem_ld_wait32(o);
-                    } else {
+            for (int c = 0; c < D / 2; c += 16) {
+                uint32_t o[16], u[8];
+                tmem_ld16(o_t + half * (D / 2) + c, o);          // (whatever lies there, where there was nothing to add up)
+                tmem_ld_wait16(o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0u;
-                    }
-                    if (last) {
+                for (int k = 0; k < 16; ++k) o[k] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
+                if (real && last) {
 #pragma unroll
-                        for (int u = 0; u < 2; ++u)
+                    for (int k = 0; k < 8; ++k) u[k] = pack_bf16(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+                    store32(static_cast<__nv_bfloat16 *>(p.out) + to + c, u, wide);
+                } else if (real && l != 0.f) {
 #pragma unroll
-                            for (int q4 = 0; q4 < 2; ++q4) {
-                                // blocks 4 q4 .. + 3: this lane's pair of columns of each, two at a time traded with the lane two, then one, on
-                                uint32_t a[4];
+                    for (int e = 0; e < 16; e += 8) {
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const int k = 4 * (4 * q4 + e) + 2 * u;
-                                    a[e] = scale[u] == 0.f ? 0u : pack_bf16(__uint_as_float(o[k]) * scale[u], __uint_as_float(o[k + 1]) * scale[u]);
-                                }
-                                const bool hi2 = quad & 2, hi1 = quad & 1;
-                                const uint32_t s0 = __shfl_xor_sync(0xffffffffu, hi2 ? a[0] : a[2], 2), s1 = __shfl_xor_sync(0xffffffffu, hi2 ? a[1] : a[3], 2);
-                                // now rows of a 2 x 2 of 2 x 2 blocks: c0, c1 from lanes quad and quad ^ 2 of blocks 2 (quad / 2), + 1
-                                const uint32_t c0 = hi2 ? s0 : a[0], c1 = hi2 ? s1 : a[1], c2_ = hi2 ? a[2] : s0, c3 = hi2 ? a[3] : s1;
-                                const uint32_t t0 = __shfl_xor_sync(0xffffffffu, hi1 ? c0 : c1, 1), t1 = __shfl_xor_sync(0xffffffffu, hi1 ? c2_ : c3, 1);
-                                uint4 w;
-                                w.x = hi1 ? t0 : c0;
-                                w.y = hi1 ? c1 : t0;
-                                w.z = hi1 ? t1 : c2_;
-                                w.w = hi1 ? c3 : t1;
-                                if (there[u]) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) + to[u] + 64 * c + 32 * q4 + 8 * quad) = w;
-                            }
-                    } else {
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                if (there[u])
-                                    *reinterpret_cast<float2 *>(p.part_o + to[u] + 64 * c + 8 * k + 2 * quad) =
-                                        make_float2(__uint_as_float(o[4 * k + 2 * u]) * scale[u], __uint_as_float(o[4 * k + 2 * u + 1]) * scale[u]);
+                        for (int k = 0; k < 8; ++k) u[k] = o[e + k];
+                        store32(p.part_o + to + c + e, u, true);
                     }
                 }
             }
