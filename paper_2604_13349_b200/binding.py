@@ -453,7 +453,7 @@ def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, strea
         size = workspace.numel() * workspace.element_size()
     call = (args, workspace.data_ptr(), size) if prefix is None else (args, prefix, workspace.data_ptr(), size)
     _enqueue(name, q.get_device(), call, stream)
-    got = {"out": out, "workspace": workspace}
+    got = {"out": out}
     if lse_out is not None:
         got["lse"] = lse_out
     if mass_out is not None:
@@ -479,10 +479,9 @@ def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, lens: Optional[
 
     ``lens``, ``q_lens``: int32 device tensors ``[batch]``, the rows of a sequence's cache and its queries that count (None: all);
     the queries are the last tokens of the cache.  Any strides with contiguous channels.  ``mass_out [batch, kv_heads, capacity]``
-    (fp32) receives ``decay * mass_in`` plus the attention mass of every key; it may be ``mass_in``.  ``workspace``: a uint8
-    device tensor of ``obf_attend_workspace_bytes``, else one is allocated; its status word is read with
-    ``obf_last_device_status``.  Returns ``out``, ``workspace`` and, where asked for, ``lse [batch, q_heads, n_q]`` (natural log)
-    and ``mass``.
+    (fp32) receives ``decay * mass_in`` plus the attention mass of every key; it may be ``mass_in``.  ``workspace``: one that
+    ``attend_workspace`` made for these shapes, whose status word ``obf_last_device_status`` reads afterwards; else one is
+    allocated for the call.  Returns ``out`` and, where asked for, ``lse [batch, q_heads, n_q]`` (natural log) and ``mass``.
     """
     out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse)
     args = _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags)
@@ -504,6 +503,20 @@ def attend_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tenso
     sk, sv = _rows(k_prefix, shape, q.dtype, q.get_device(), "k_prefix"), _rows(v_prefix, shape, q.dtype, q.get_device(), "v_prefix")
     prefix = _PREFIX.pack(k_prefix.data_ptr(), v_prefix.data_ptr(), sk[0], sk[1], sv[0], sv[1], rows)
     return _attend_call("obf_attend_shared", args, prefix, q, out, lse_out, None, workspace, stream)
+
+
+def attend_workspace(q: torch.Tensor, k: torch.Tensor, *, window: int = 0, sinks: int = 0, mass: bool = False, prefix_rows: int = 0,
+                     flags: int = 0) -> torch.Tensor:
+    """A workspace for ``attend`` (``prefix_rows`` 0) or ``attend_shared`` calls of these shapes."""
+    B, hq, n_q, d = q.shape
+    kv, cap = k.shape[1], k.shape[2]
+    args = _ATTEND.pack(B, kv, hq, d, n_q, cap, window, sinks, _DTYPES[q.dtype], 0.0, 1.0, flags, *([0] * 16), 0, 0, 0, 0, 1 if mass else 0)
+    prefix = _PREFIX.pack(0, 0, 0, 0, 0, 0, prefix_rows) if prefix_rows else None
+    nb = ctypes.c_size_t(0)
+    rc = _packed("obf_attend_workspace_bytes")(args, prefix, ctypes.addressof(nb))
+    if rc != OBF_OK:
+        raise ObfError(rc, "obf_attend_workspace_bytes")
+    return torch.zeros(nb.value, dtype=torch.uint8, device=q.device)
 
 
 def obf_attend_workspace_bytes(args: ObfAttend, prefix: Optional[ObfPrefix] = None) -> int:

@@ -191,13 +191,14 @@ def _attend_case(B, kv, G, d, n_q, cap, lens, q_lens, dtype, window=0, sinks=0, 
         qd, out = dev(q), torch.full((B, kv * G, n_q, d), SENTINEL, dtype=dtype, device="cuda")
     lse = torch.full((B, kv * G, n_q), SENTINEL, device="cuda")
     ln, ql = torch.tensor(lens, dtype=torch.int32, device="cuda"), torch.tensor(q_lens, dtype=torch.int32, device="cuda")
+    ws = P.attend_workspace(qd, dev(k), window=window, sinks=sinks, mass=mass, prefix_rows=prefix_rows, flags=flags)
     if prefix_rows:
-        r = P.attend_shared(qd, dev(px[0]), dev(px[1]), dev(k), dev(v), lens=ln, q_lens=ql, scale=scale, out=out, lse_out=lse, flags=flags)
+        P.attend_shared(qd, dev(px[0]), dev(px[1]), dev(k), dev(v), lens=ln, q_lens=ql, scale=scale, out=out, lse_out=lse, flags=flags, workspace=ws)
     else:
         m_out = torch.full((B, kv, cap), SENTINEL, device="cuda") if mass else None
-        r = P.attend(qd, dev(k), dev(v), lens=ln, q_lens=ql, window=window, sinks=sinks, scale=scale, out=out, lse_out=lse,
+        P.attend(qd, dev(k), dev(v), lens=ln, q_lens=ql, workspace=ws, window=window, sinks=sinks, scale=scale, out=out, lse_out=lse,
                      mass_in=dev(mass_in) if mass else None, mass_out=m_out, decay=decay, flags=flags)
-    assert P.obf_last_device_status(r["workspace"]) == 0
+    assert P.obf_last_device_status(ws) == 0
     for b in range(B):
         assert (out[b, :, q_lens[b]:] == SENTINEL).all() and (lse[b, :, q_lens[b]:] == SENTINEL).all(), "written behind the queries"
         out[b, :, q_lens[b]:] = 0
@@ -309,3 +310,184 @@ def test_evict_by_mass(d, dtype, cap, lens, keep, sinks, recent):
             assert torch.equal(k_out[b, h, :n].cpu(), k[b, h, w]) and torch.equal(v_out[b, h, :n].cpu(), v[b, h, w])
             assert (k_out[b, h, n:] == SENTINEL).all() and (v_out[b, h, n:] == SENTINEL).all()
             assert torch.equal(m_out[b, h, :n].cpu().nan_to_num(nan=-5.0), mass[b, h, w].nan_to_num(nan=-5.0))
+
+
+# ---- in use -----------------------------------------------------------------------------------------------------------
+def _small(dtype=BF16, B=2, kv=2, G=4, d=128, n_q=1, cap=600, seed=1):
+    gen = torch.Generator().manual_seed(seed)
+    q, k, v = _data(gen, B, kv, G, d, n_q, cap, dtype)
+    return q.cuda(), k.cuda(), v.cuda()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_q", [1, 50])
+def test_the_same_call_gives_the_same_bits_on_any_stream_and_whatever_the_workspace_held(n_q):
+    q, k, v = _small(n_q=n_q)
+    first = P.attend(q, k, v, window=300, sinks=3, want_lse=True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ws = P.attend_workspace(q, k, window=300, sinks=3)
+    ws.fill_(0xFF)
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (side, side.cuda_stream, None):
+        again = P.attend(q, k, v, window=300, sinks=3, want_lse=True, workspace=ws, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(again["out"], first["out"]) and torch.equal(again["lse"], first["lse"])
+        assert P.obf_last_device_status(ws) == 0
+    with torch.cuda.stream(side):
+        again = P.attend(q, k, v, window=300, sinks=3, want_lse=True)              # the current stream, its own workspace
+    torch.cuda.synchronize()
+    assert torch.equal(again["out"], first["out"])
+
+
+@pytest.mark.gpu
+def test_calls_at_once_on_two_streams():
+    cases = [_small(seed=s, n_q=n, cap=900) for s, n in ((1, 1), (2, 1), (3, 90), (4, 90))]
+    want = [P.attend(*c)["out"] for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[P.attend(*c, stream=s)["out"] for c, s in zip(cases, streams)] for _ in range(10)]
+    torch.cuda.synchronize()
+    for r in got:
+        assert all(torch.equal(a, b) for a, b in zip(r, want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n_q", [1, 33])
+def test_captured_calls_follow_the_lengths(dtype, n_q):
+    q, k, v = _small(dtype, n_q=n_q)
+    lens = torch.tensor([100, 40], dtype=torch.int32, device="cuda")
+    ws = P.attend_workspace(q, k, window=200, sinks=2)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:3], device="cuda")
+    P.attend(q, k, v, lens=lens, window=200, sinks=2, out=out, lse_out=lse, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.attend(q, k, v, lens=lens, window=200, sinks=2, out=out, lse_out=lse, workspace=ws)
+    for pair in ([600, 599], [1, 0], [333, 257]):
+        lens.copy_(torch.tensor(pair, dtype=torch.int32))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = P.attend(q, k, v, lens=lens, window=200, sinks=2, want_lse=True)
+        assert torch.equal(out, want["out"]) and torch.equal(lse, want["lse"])
+        w = ref.attend(q.cpu(), k.cpu(), v.cpu(), pair, [n_q, n_q], 200, 2)
+        _check(out, w[0], w[1], "out")
+
+
+@pytest.mark.gpu
+def test_lengths_out_of_range_are_clamped_and_reported():
+    for n_q in (1, 40):
+        q, k, v = _small(n_q=n_q)
+        ws = P.attend_workspace(q, k)
+        want = P.attend(q, k, v, lens=torch.tensor([600, 0], dtype=torch.int32, device="cuda"))["out"]
+        got = P.attend(q, k, v, lens=torch.tensor([60000, -5], dtype=torch.int32, device="cuda"), workspace=ws)["out"]
+        assert P.obf_last_device_status(ws) == binding.OBF_DEV_INTERNAL
+        assert torch.equal(got, want)
+        P.attend(q, k, v, workspace=ws)
+        assert P.obf_last_device_status(ws) == 0                                   # the next call's word is its own
+
+
+@pytest.mark.gpu
+def test_masses_in_place_and_without_a_start():
+    q, k, v = _small()
+    m = torch.rand(2, 2, 600, device="cuda")
+    want = P.attend(q, k, v, mass_in=m.clone(), mass_out=torch.zeros_like(m), decay=0.5)["mass"]
+    got = P.attend(q, k, v, mass_in=m, mass_out=m, decay=0.5)["mass"]
+    assert got is m and torch.equal(got, want)
+    bare = P.attend(q, k, v, mass_out=torch.full_like(m, 3.0))["mass"]
+    assert torch.allclose(bare.sum(-1), torch.full((2, 2), 4.0, device="cuda"), atol=1e-3)      # four query rows, each one in all
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_q", [1, 60])
+def test_values_that_are_not_finite_reach_the_queries_that_see_them(n_q):
+    q, k, v = _small(n_q=n_q, cap=200)
+    k[0, 0, 150, 3] = math.nan
+    v[1, 1, 10, 5] = math.inf
+    out = P.attend(q, k, v)["out"]
+    t = torch.arange(200 - n_q, 200)
+    assert out[0, :4, t >= 150].isnan().all() and out[0, 4:].isfinite().all()
+    hit = out[1, 4:, :, 5]
+    assert not hit.isfinite().any() and out[1, 4:, :, 6].isfinite().all() and out[1, :4].isfinite().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_q", [1, 64])
+def test_offsets_beyond_32_bits(n_q):
+    # the second sequence's rows lie more than 2^32 bytes (and 2^31 elements) behind the first's
+    cap, d = 1100, 128
+    big = torch.empty(2, (1 << 31) + 4096, dtype=BF16, device="cuda")
+    k = big.as_strided((2, 1, cap, d), (big.stride(0), 0, d, 1))
+    v = big.as_strided((2, 1, cap, d), (big.stride(0), 0, d, 1), cap * d)
+    gen = torch.Generator().manual_seed(5)
+    q, kc, vc = _data(gen, 2, 1, 2, d, n_q, cap, BF16)
+    k.copy_(kc)
+    v.copy_(vc)
+    w = ref.attend(q, kc, vc, [cap, cap - 7], [n_q, n_q], 500, 4)
+    out = P.attend(q.cuda(), k, v, lens=torch.tensor([cap, cap - 7], dtype=torch.int32, device="cuda"), window=500, sinks=4)["out"]
+    _check(out, w[0], w[1], "out")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_strided_caches_and_outputs(n_q):
+    gen = torch.Generator().manual_seed(9)
+    q, kc, vc = _data(gen, 2, 3, 2, 64, n_q, 150, BF16)
+    kv = torch.zeros(2, 150, 3, 2, 64, dtype=BF16)                                   # token-major, keys and values in turn
+    kv[:, :, :, 0], kv[:, :, :, 1] = kc.transpose(1, 2), vc.transpose(1, 2)
+    kv = kv.cuda()
+    out = torch.zeros(2, n_q, 6, 72, dtype=BF16, device="cuda")[..., :64].transpose(1, 2)       # rows 144 bytes apart: no multiple of 32
+    P.attend(q.cuda(), kv[:, :, :, 0].transpose(1, 2), kv[:, :, :, 1].transpose(1, 2), window=60, sinks=5, out=out)
+    w = ref.attend(q, kc, vc, [150, 150], [n_q, n_q], 60, 5)
+    _check(out, w[0], w[1], "out")
+
+
+@pytest.mark.gpu
+def test_chain_relay_attention_masses_and_eviction():
+    """A prompt is compressed, the relay is shared by a batch that decodes over it, and a cache that has grown is evicted from by the
+    masses that its tokens gathered: every step against the plain form on what the library left of the step before."""
+    layers, kv, G, d, T, W = 1, 2, 4, 128, 512, 8
+    gen = torch.Generator().manual_seed(3)
+    K, V = (torch.randn(layers, kv, T, d, generator=gen).to(BF16) for _ in range(2))
+    Q = torch.randn(layers, kv * G, W, d, generator=gen).to(BF16)
+    # what an earlier relay's keys take of the observation queries' softmax
+    old = torch.randn(1, kv, 70, d, generator=gen).to(BF16)
+    extra = P.attend(Q.cuda(), old.cuda(), old.cuda(), want_lse=True)                 # causal: the last of the 70 keys' positions
+    full = P.attend_shared(Q.cuda(), old[0].cuda(), old[0].cuda(), old.cuda(), old.cuda(), lens=torch.zeros(1, dtype=torch.int32, device="cuda"), want_lse=True)
+    x = torch.einsum("bhtd,bhjd->bhtj", Q.double().reshape(1, kv, G * W, d), old.double()) / math.sqrt(d)
+    assert torch.allclose(full["lse"].double().cpu().reshape(1, kv, G * W), torch.logsumexp(x, -1), atol=1e-5)
+    assert (extra["lse"] <= full["lse"] + 1e-5).all()
+    params = P.make_params(layers, kv, kv * G, d, W, 2, P.OBF_BF16)
+    r = P.compress_caches(params, [{"K": K.cuda(), "V": V.cuda(), "Q": Q.cuda(), "budget": 100, "lse_extra": full["lse"].contiguous()}], want_scores=True)[0]
+    torch.cuda.synchronize()
+    relay_k, relay_v = r["K_out"][0], r["V_out"][0]
+    # three agents, one token each, over the shared relay
+    q, k, v = _data(gen, 3, kv, G, d, 1, 30, BF16)
+    lens = [30, 11, 1]
+    got = P.attend_shared(q.cuda(), relay_k, relay_v, k.cuda(), v.cuda(), lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    w = ref.attend(q, k, v, lens, [1, 1, 1], prefix=(relay_k.cpu(), relay_v.cpu()))
+    _check(got["out"], w[0], w[1], "out")
+    # one agent goes on: its cache is the relay and room for more, its masses begin as the selection's
+    cap = 140
+    ck, cv = (torch.zeros(1, kv, cap, d, dtype=BF16, device="cuda") for _ in range(2))
+    ck[0, :, :100], cv[0, :, :100] = relay_k, relay_v
+    mass = torch.zeros(1, kv, cap, device="cuda")
+    mass[0, :, :100] = torch.gather(r["scores"][0], 1, r["idx"][0].long())
+    length = torch.tensor([100], dtype=torch.int32, device="cuda")
+    for step in range(20):
+        q1, k1, v1 = _data(gen, 1, kv, G, d, 1, 1, BF16)
+        ck[0, :, 100 + step], cv[0, :, 100 + step] = k1[0, :, 0].cuda(), v1[0, :, 0].cuda()
+        length += 1
+        before = mass.cpu()
+        got = P.attend(q1.cuda(), ck, cv, lens=length, window=64, sinks=4, mass_in=mass, mass_out=mass, decay=0.9)
+        w = ref.attend(q1, ck.cpu(), cv.cpu(), [101 + step], [1], 64, 4, mass_in=before, decay=0.9, want_mass=True)
+        _check(got["out"], w[0], w[1], "out")
+        _check(mass, w[4], w[5], "mass")
+    e = P.evict_by_mass(ck, cv, mass, 48, lens=length, sinks=4, recent=8)
+    kept = ref.evict(mass.cpu(), [120], 48, 4, 8)
+    assert e["lens"].tolist() == [48]
+    for h in range(kv):
+        assert e["idx"][0, h].tolist() == kept[0][h]
+        assert torch.equal(e["K_out"][0, h], ck[0, h, kept[0][h]]) and torch.equal(e["V_out"][0, h], cv[0, h, kept[0][h]])
