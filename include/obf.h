@@ -355,8 +355,8 @@ typedef struct {
     void *out;                          /* [batch, q_heads, n_q, head_dim], must not overlap the inputs          */
     int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
                                         /* elements from one sequence, head and row to the next; channels are
-                                           contiguous.  Multiples of 16 bytes, at least head_dim where there is more
-                                           than one of them, in any order ([batch, n_q, q_heads, head_dim] is one)   */
+                                           contiguous.  Multiples of 16 bytes, at least head_dim and less than 2^40
+                                           bytes where there is more than one of them, in any order ([batch, n_q, q_heads, head_dim] is one)   */
     const int32_t *lens;                /* device [batch], or NULL: capacity                                     */
     const int32_t *q_lens;              /* device [batch], or NULL: n_q                                          */
     float *lse_out;                     /* device [batch, q_heads, n_q], or NULL                                 */
@@ -380,7 +380,8 @@ obf_status_t obf_attend_workspace_bytes(const obf_attend_t *args, const obf_pref
  * Enqueues the attention on `stream`; allocates nothing and never synchronises, can be captured into a graph.  `workspace`:
  * at least obf_attend_workspace_bytes(), 256-byte aligned, private to the call until its work is done (two captured graphs
  * that share one must not overlap); nothing in it is kept from call to call except the status word that
- * obf_last_device_status reads.  Device-side waits are bounded, as in obf_compress.
+ * obf_last_device_status reads.  Device-side waits are bounded, as in obf_compress.  The first call of a kind on a device raises its
+ * kernels' shared-memory limits: make it before a stream capture.
  */
 obf_status_t obf_attend(const obf_attend_t *args, void *workspace, size_t workspace_bytes, void *stream);
 

@@ -369,6 +369,7 @@ _PREFIX = struct.Struct("@2P4qi4x")
 _EVICT = struct.Struct("@8i4P12q4Pi4xP")
 assert (_ATTEND.size, _PREFIX.size, _EVICT.size) == (ctypes.sizeof(ObfAttend), ctypes.sizeof(ObfPrefix), ctypes.sizeof(ObfEvict))
 _packed_calls: Dict[str, object] = {}
+_MOST = 0x7FFFFFFF                      # windows and numbers of first tokens beyond any position are as good
 
 
 def _packed(name: str):
@@ -416,7 +417,7 @@ def _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass
     sq, so = _rows(q, shape_q, dt, dev, "q"), _rows(out, shape_q, dt, dev, "out")
     sk, sv = _rows(k, shape_k, dt, dev, "k"), _rows(v, shape_k, dt, dev, "v")
     return _ATTEND.pack(
-        B, kv, hq, d, n_q, cap, window, sinks, _DTYPES[dt], scale, decay, flags, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+        B, kv, hq, d, n_q, cap, min(window, _MOST), min(sinks, _MOST), _DTYPES[dt], scale, decay, flags, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
         sq[0], sq[1], sq[2], sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], so[0], so[1], so[2],
         _dense(lens, (B,), i32, dev, "lens"), _dense(q_lens, (B,), i32, dev, "q_lens"), _dense(lse_out, shape_q[:3], f32, dev, "lse_out"),
         _dense(mass_in, shape_k[:3], f32, dev, "mass_in"), _dense(mass_out, shape_k[:3], f32, dev, "mass_out"))

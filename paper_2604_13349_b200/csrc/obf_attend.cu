@@ -14,7 +14,7 @@ static obf_status_t check_stride(const int64_t *st, const int64_t *n, int dims, 
 {
     for (int i = 0; i < dims; ++i) {
         if (n[i] < 2) continue;                           // never stepped over
-        if (st[i] < head_dim || st[i] > (int64_t)1 << 40 || st[i] * esize % 16 != 0) return OBF_ERR_INVALID_ARG;
+        if (st[i] < head_dim || st[i] >= ((int64_t)1 << 40) / esize || st[i] * esize % 16 != 0) return OBF_ERR_INVALID_ARG;
     }
     return OBF_OK;
 }

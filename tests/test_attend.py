@@ -63,7 +63,7 @@ def test_attend_refuses_bad_shapes(lib, kw, code):
 @pytest.mark.parametrize("kw", [
     dict(q=0), dict(k=0), dict(v=0), dict(out=0), dict(q=0x1008), dict(k=0x1002), dict(v=0x1004), dict(out=0x1008), dict(lens=0x1002), dict(q_lens=0x1001),
     dict(lse_out=0x1002), dict(mass_out=0x1002), dict(q_stride=(1536, 192, 63)), dict(k_stride=(12800, 6400, 68)), dict(v_stride=(12800, -6400, 64)),
-    dict(out_stride=(1536, 0, 64)), dict(k_stride=(1 << 41, 6400, 64)),
+    dict(out_stride=(1536, 0, 64)), dict(k_stride=(1 << 39, 6400, 64)),
 ])
 def test_attend_refuses_bad_pointers_and_strides(lib, kw):
     assert lib.obf_attend(ctypes.byref(_args(**kw)), 0x100, 1 << 50, None) == INVALID
@@ -276,6 +276,26 @@ def test_attend_shared(dtype, flags, d, B, G, n_q, cap, lens, q_lens, rows):
 def test_attend_scale_and_large_logits(dtype, flags):
     _attend_case(1, 2, 4, 64, 1, 500, [500], [1], dtype, scale=3.0, flags=flags)           # logits of hundreds: one weight near one
     _attend_case(1, 2, 4, 128, 90, 200, [200], [90], dtype, scale=2.5, flags=flags, window=50, sinks=3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,flags", PATHS)
+@pytest.mark.parametrize("n_q", [1, 64])
+@pytest.mark.parametrize("low,high", [(-400.0, 400.0), (400.0, -400.0), (-500.0, -480.0), (480.0, 500.0), (-60.0, -40.0)])
+def test_attend_logits_that_drift(dtype, flags, n_q, low, high):
+    # logits (before the scale, which is one) run from low to high along the cache, far beyond what an exponential in fp32 holds
+    gen = torch.Generator().manual_seed(11)
+    d, cap, kv, G = 64, 900, 2, 4
+    u = torch.full((d,), 0.125)
+    ramp = torch.linspace(low, high, cap)
+    q = (u + 0.01 * torch.randn(1, kv * G, n_q, d, generator=gen)).to(dtype)
+    k = (ramp[:, None] * u + 0.05 * torch.randn(1, kv, cap, d, generator=gen)).to(dtype)
+    v = torch.randn(1, kv, cap, d, generator=gen).to(dtype)
+    for window, sinks in ((0, 0), (700, 5)):
+        want = ref.attend(q, k, v, [cap], [n_q], window, sinks, 1.0)
+        got = P.attend(q.cuda(), k.cuda(), v.cuda(), window=window, sinks=sinks, scale=1.0, want_lse=True, flags=flags)
+        _check(got["out"], want[0], want[1], "out")
+        _check(got["lse"], want[2], want[3], "lse")
 
 
 @pytest.mark.gpu
