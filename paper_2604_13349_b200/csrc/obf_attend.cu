@@ -134,6 +134,19 @@ static int tc_parts(long long pairs, long long keys)
     return best;
 }
 
+// Parts of the keys for k_attend_few: as many as make its rounds of resident blocks cheapest, a block costing its keys and, to
+// begin and to end, as much as 120 more; at least 256 keys each.  (16 sequences of 8192 keys, 128 tiles: 9 parts 95 us, 7 parts
+// 100, 14 parts 97; 32 of up to 8192 with a window of 4096: 1 part 73.6, 5 parts 80.4; 4 of 131072: 18 parts 278, 28 parts 292.)
+static int few_parts(long long tiles, long long keys)
+{
+    long long best = 1, cost = LLONG_MAX;
+    for (long long s = 1; s <= 128 && (s == 1 || s * 256 <= keys); ++s) {
+        const long long c = (tiles * s + FEW_RESIDENT - 1) / FEW_RESIDENT * ((keys + s - 1) / s + 120);
+        if (c < cost) { cost = c; best = s; }
+    }
+    return (int)best;
+}
+
 static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
 {
     AttendLayout L;
@@ -144,7 +157,7 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
             const int t = few_rows(rows_run);
             const long long tiles = runs * ((rows_run + t - 1) / t);
             if (8 * tiles <= FEW_RESIDENT && keys <= 4096) return parts_for(1, keys, 8, 64);
-            return parts_for(tiles, keys, 6 * 148, tiles * ((keys + 511) / 512) >= FEW_RESIDENT ? 512 : 256);
+            return few_parts(tiles, keys);
         }
         if (path == ATTEND_TC) return tc_parts(tc_tiles((int)(a->q_heads / a->kv_heads), a->n_q, a->batch, a->kv_heads, rows_run != rows_seq).pairs, keys);
         return parts_for(runs * ((rows_run + AG_TILE - 1) / AG_TILE), keys, 2 * 148, 4 * AG_TILE);
