@@ -76,6 +76,86 @@ __device__ __forceinline__ float cluster_load(uint32_t a)
     return v;
 }
 
+// The end of a block with few rows: its warps' results, in shared memory, are weighed together and stored, or joined with those of
+// the cluster's other blocks first.  osm: O as [warp][row][D + 4], ml: references and sums as [warp][row][2], room for one more
+// result behind them.
+template <int D, int ROWS>
+__host__ __device__ constexpr size_t few_finish_smem() { return ((size_t)AF_WARPS * ROWS * (D + 4 + 2) + ROWS * (D + 4 + 1)) * 4; }
+
+template <typename TIN, int D, int ROWS, bool PREFIX, bool CLUSTER>
+__device__ __forceinline__ void few_finish(const AttendDev &p, const float *osm, float *ml, int tile, int part, int parts, int rows_run, int rows_seq, int h,
+                                           int b_own, int ql_own)
+{
+    auto locate_row = [&](int run, int &b, int &r) {
+        b = PREFIX ? run / rows_seq : b_own;
+        r = PREFIX ? run - b * rows_seq : run;
+    };
+    const bool last = p.slots == 1 && !p.mass_out;
+    constexpr int TR = D / 4;                             // threads of a row, four channels each
+    constexpr int LD = D + 4;
+    float *cl = ml + AF_WARPS * ROWS * 2, *cl_lse = cl + ROWS * LD;       // what the cluster's other blocks read
+    auto put = [&](int b, int h2, int i, int c, const float4 &a, float lse2) {
+        store4(static_cast<TIN *>(p.out) + b * p.os[0] + (long long)h2 * p.os[1] + (long long)i * p.os[2] + c, a);
+        if (p.lse_out && c == 0) p.lse_out[((long long)b * p.kv_heads * p.G + h2) * p.n_q + i] = natural_lse(lse2);
+    };
+    for (int row = threadIdx.x / TR; row < ROWS; row += AF_NT / TR) {
+        const int run = tile * ROWS + row, c = threadIdx.x % TR * 4;
+        int b, r;
+        locate_row(run, b, r);
+        const int i = r / p.G, g = r - i * p.G;
+        if (run >= rows_run || i >= (PREFIX ? attend_q_len(p, b) : ql_own)) continue;
+        float M = -INFINITY, Z = 0.f;
+#pragma unroll
+        for (int w = 0; w < AF_WARPS; ++w) M = fmaxf(M, ml[(w * ROWS + row) * 2]);
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < AF_WARPS; ++w) {
+            const float z = ml[(w * ROWS + row) * 2 + 1], f = z == 0.f ? 0.f : exp2f(ml[(w * ROWS + row) * 2] - M);
+            const float4 u = *reinterpret_cast<const float4 *>(&osm[(w * ROWS + row) * LD + c]);
+            Z += f * z;
+            a.x += f * u.x; a.y += f * u.y; a.z += f * u.z; a.w += f * u.w;
+        }
+        const float inv = Z == 0.f ? 0.f : 1.f / Z, lse2 = Z == 0.f ? -INFINITY : M + log2f(Z);
+        a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
+        if constexpr (CLUSTER) {
+            *reinterpret_cast<float4 *>(&cl[row * LD + c]) = a;
+            if (c == 0) cl_lse[row] = lse2;
+        } else if (last) {
+            put(b, h * p.G + g, i, c, a, lse2);
+        } else {
+            const long long at = (long long)(PREFIX ? part : p.p_slots + part) * p.rows_total + ((long long)b * p.kv_heads + h) * rows_seq + r;
+            *reinterpret_cast<float4 *>(p.part_o + at * D + c) = a;
+            if (c == 0) p.part_lse[at] = lse2;
+        }
+    }
+    if constexpr (CLUSTER) {
+        cluster_sync();
+        for (int row = part + parts * (threadIdx.x / TR); row < ROWS; row += parts * (AF_NT / TR)) {
+            const int r = tile * ROWS + row, c = threadIdx.x % TR * 4, i = r / p.G;
+            if (r >= rows_run || i >= ql_own) continue;
+            float l[8], M = -INFINITY, Z = 0.f;
+            float4 u[8], a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < parts) {
+                    l[k] = cluster_load(cluster_addr(cl_lse + row, k));
+                    u[k] = cluster_load4(cluster_addr(cl + row * LD + c, k));
+                    M = fmaxf(M, l[k]);
+                }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < parts) {
+                    const float f = l[k] == -INFINITY ? 0.f : exp2f(l[k] - M);
+                    Z += f;
+                    a.x += f * u[k].x; a.y += f * u[k].y; a.z += f * u[k].z; a.w += f * u[k].w;
+                }
+            const float inv = Z == 0.f ? 0.f : 1.f / Z;
+            put(b_own, h * p.G + r - i * p.G, i, c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv), Z == 0.f ? -INFINITY : M + log2f(Z));
+        }
+        cluster_sync();                                   // nobody leaves while its memory is read
+    }
+}
+
 // CLUSTER: the parts of a tile, at most eight, are a cluster, which joins them through its shared memory.
 template <int D, int NT, bool PREFIX, bool CLUSTER>
 __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ AttendDev p, const int first)
@@ -269,7 +349,7 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
     // the warps' results: O as [warp][row][D + 4], then references and sums
     constexpr int LD = D + 4;
     float *osm = reinterpret_cast<float *>(af_sm), *ml = osm + AF_WARPS * ROWS * LD;
-    static_assert((size_t)AF_WARPS * ROWS * (LD + 2) * 4 <= attend_few_smem<D>(), "");
+    static_assert(few_finish_smem<D, ROWS>() <= attend_few_smem<D>(), "");
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -285,70 +365,7 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
                 for (int u = 0; u < 2; ++u) osm[(warp * ROWS + row) * LD + 16 * k + 8 * u + lane / 4] = o[nt][k][2 * u + e];
         }
     __syncthreads();
-    const bool last = p.slots == 1 && !p.mass_out;
-    constexpr int TR = D / 4;                             // threads of a row, four channels each
-    float *cl = ml + AF_WARPS * ROWS * 2, *cl_lse = cl + ROWS * LD;       // what the cluster's other blocks read
-    static_assert(((size_t)AF_WARPS * ROWS * (LD + 2) + ROWS * (LD + 1)) * 4 <= attend_few_smem<D>(), "");
-    auto put = [&](int b, int h2, int i, int c, const float4 &a, float lse2) {
-        store4(static_cast<__nv_bfloat16 *>(p.out) + b * p.os[0] + (long long)h2 * p.os[1] + (long long)i * p.os[2] + c, a);
-        if (p.lse_out && c == 0) p.lse_out[((long long)b * p.kv_heads * p.G + h2) * p.n_q + i] = natural_lse(lse2);
-    };
-    for (int row = threadIdx.x / TR; row < ROWS; row += AF_NT / TR) {
-        const int run = tile * ROWS + row, c = threadIdx.x % TR * 4;
-        int b, r;
-        locate_row(run, b, r);
-        const int i = r / p.G, g = r - i * p.G;
-        if (run >= rows_run || i >= (PREFIX ? attend_q_len(p, b) : ql_own)) continue;
-        float M = -INFINITY, Z = 0.f;
-#pragma unroll
-        for (int w = 0; w < AF_WARPS; ++w) M = fmaxf(M, ml[(w * ROWS + row) * 2]);
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < AF_WARPS; ++w) {
-            const float z = ml[(w * ROWS + row) * 2 + 1], f = z == 0.f ? 0.f : exp2f(ml[(w * ROWS + row) * 2] - M);
-            const float4 u = *reinterpret_cast<const float4 *>(&osm[(w * ROWS + row) * LD + c]);
-            Z += f * z;
-            a.x += f * u.x; a.y += f * u.y; a.z += f * u.z; a.w += f * u.w;
-        }
-        const float inv = Z == 0.f ? 0.f : 1.f / Z, lse2 = Z == 0.f ? -INFINITY : M + log2f(Z);
-        a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
-        if constexpr (CLUSTER) {
-            *reinterpret_cast<float4 *>(&cl[row * LD + c]) = a;
-            if (c == 0) cl_lse[row] = lse2;
-        } else if (last) {
-            put(b, h * p.G + g, i, c, a, lse2);
-        } else {
-            const long long at = (long long)(PREFIX ? part : p.p_slots + part) * p.rows_total + ((long long)b * p.kv_heads + h) * rows_seq + r;
-            *reinterpret_cast<float4 *>(p.part_o + at * D + c) = a;
-            if (c == 0) p.part_lse[at] = lse2;
-        }
-    }
-    if constexpr (CLUSTER) {
-        cluster_sync();
-        for (int row = part + parts * (threadIdx.x / TR); row < ROWS; row += parts * (AF_NT / TR)) {
-            const int r = tile * ROWS + row, c = threadIdx.x % TR * 4, i = r / p.G;
-            if (r >= rows_run || i >= ql_own) continue;
-            float l[8], M = -INFINITY, Z = 0.f;
-            float4 u[8], a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k < parts) {
-                    l[k] = cluster_load(cluster_addr(cl_lse + row, k));
-                    u[k] = cluster_load4(cluster_addr(cl + row * LD + c, k));
-                    M = fmaxf(M, l[k]);
-                }
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k < parts) {
-                    const float f = l[k] == -INFINITY ? 0.f : exp2f(l[k] - M);
-                    Z += f;
-                    a.x += f * u[k].x; a.y += f * u[k].y; a.z += f * u[k].z; a.w += f * u[k].w;
-                }
-            const float inv = Z == 0.f ? 0.f : 1.f / Z;
-            put(b_own, h * p.G + r - i * p.G, i, c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv), Z == 0.f ? -INFINITY : M + log2f(Z));
-        }
-        cluster_sync();                                   // nobody leaves while its memory is read
-    }
+    few_finish<__nv_bfloat16, D, ROWS, PREFIX, CLUSTER>(p, osm, ml, tile, part, parts, rows_run, rows_seq, h, b_own, ql_own);
     if (!first) pdl_wait();
 }
 

@@ -14,16 +14,25 @@ constexpr int AG_NT = 256;
 constexpr int AG_TILE = 64;
 
 template <int D>
-constexpr size_t attend_generic_smem() { return (size_t)(3 * AG_TILE * TD_LD<D> + AG_TILE * (AG_TILE + 4)) * sizeof(float); }
+constexpr size_t attend_generic_smem() { return (size_t)(3 * AG_TILE * TD_LD<D>) * sizeof(float); }
+static_assert(TD_LD<64> >= AG_TILE + 4, "the weights lie over the keys");
+
+__device__ __forceinline__ float4 scaled(f32x2 a, f32x2 b, float f)
+{
+    float4 v;
+    upk(a, v.x, v.y);
+    upk(b, v.z, v.w);
+    return make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+}
 
 // One of the call's two sets of keys: the sequences' own ones (PREFIX false) or the shared prefix.
 template <typename TIN, int D, bool PREFIX>
-__global__ void __launch_bounds__(AG_NT) k_attend_generic(const __grid_constant__ AttendDev p, const int first)
+__global__ void __launch_bounds__(AG_NT, 2) k_attend_generic(const __grid_constant__ AttendDev p, const int first)
 {
     if (first) pdl_wait();                               // (else as in k_attend_few)
     pdl_trigger();
     extern __shared__ float sm[];
-    float *Qs = sm, *Ks = Qs + AG_TILE * TD_LD<D>, *Vs = Ks + AG_TILE * TD_LD<D>, *Ps = Vs + AG_TILE * TD_LD<D>;
+    float *Qs = sm, *Ks = Qs + AG_TILE * TD_LD<D>, *Vs = Ks + AG_TILE * TD_LD<D>, *Ps = Ks;
     constexpr int P_LD = AG_TILE + 4, VEC = 16 / sizeof(TIN), CH = D / VEC, CT = D / 16;
     __shared__ int row_t[AG_TILE];                       // position of a row's query, INT_MIN: not a query of the call
     __shared__ long long row_at[AG_TILE];                // its number among the call's rows
@@ -85,13 +94,14 @@ __global__ void __launch_bounds__(AG_NT) k_attend_generic(const __grid_constant_
     const long long kst = PREFIX ? p.pks[1] : p.ks[2], vst = PREFIX ? p.pvs[1] : p.vs[2];
 
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-    float m[4], l[4], o[4][CT];
+    float m[4], l[4];
+    f32x2 o[4][CT / 2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         m[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
-        for (int e = 0; e < CT; ++e) o[i][e] = 0.f;
+        for (int e = 0; e < CT / 2; ++e) o[i][e] = 0ull;
     }
     for (int v = v0; v < v1; v += AG_TILE) {
         __syncthreads();
@@ -111,6 +121,7 @@ __global__ void __launch_bounds__(AG_NT) k_attend_generic(const __grid_constant_
         __syncthreads();
         float s[4][4];
         tile_dots<D>(Qs, Ks, ty, tx, s);
+        __syncthreads();                                 // the weights go where the keys were
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = row_t[ty + 16 * i];
@@ -136,12 +147,12 @@ __global__ void __launch_bounds__(AG_NT) k_attend_generic(const __grid_constant_
             l[i] = l[i] * f + z;
             m[i] = mx;
 #pragma unroll
-            for (int e = 0; e < CT; ++e) o[i][e] *= f;
+            for (int e = 0; e < CT / 2; ++e) o[i][e] = mul2(o[i][e], pk(f, f));
         }
         __syncwarp();                                    // a row's weights are written and read by the same half warp
 #pragma unroll 2
         for (int j = 0; j < AG_TILE; j += 2) {
-            float pw[4][2], w[2][CT];
+            float pw[4][2];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2 u = *reinterpret_cast<const float2 *>(&Ps[(ty + 16 * i) * P_LD + j]);
@@ -151,14 +162,15 @@ __global__ void __launch_bounds__(AG_NT) k_attend_generic(const __grid_constant_
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int e = 0; e < CT; e += 4) {
-                    const float4 u = *reinterpret_cast<const float4 *>(&Vs[(j + q) * TD_LD<D> + 4 * tx + 16 * e]);
-                    w[q][e] = u.x; w[q][e + 1] = u.y; w[q][e + 2] = u.z; w[q][e + 3] = u.w;
+                for (int e = 0; e < CT / 2; e += 2) {
+                    const ulonglong2 w = *reinterpret_cast<const ulonglong2 *>(&Vs[(j + q) * TD_LD<D> + 4 * tx + 32 * e]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x2 pp = pk(pw[i][q], pw[i][q]);
+                        o[i][e] = fma2(pp, w.x, o[i][e]);
+                        o[i][e + 1] = fma2(pp, w.y, o[i][e + 1]);
+                    }
                 }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < CT; ++e) o[i][e] += pw[i][0] * w[0][e] + pw[i][1] * w[1][e];
         }
         __syncwarp();
     }
@@ -174,14 +186,12 @@ __global__ void __launch_bounds__(AG_NT) k_attend_generic(const __grid_constant_
             const int bh = (int)(R / rows_seq), r = (int)(R - (long long)bh * rows_seq), b = bh / p.kv_heads, qi = r / p.G, hq = h * p.G + r - qi * p.G;
             TIN *dst = static_cast<TIN *>(p.out) + b * p.os[0] + (long long)hq * p.os[1] + (long long)qi * p.os[2];
 #pragma unroll
-            for (int e = 0; e < CT; e += 4)
-                store4(dst + 4 * tx + 16 * e, make_float4(o[i][e] * inv, o[i][e + 1] * inv, o[i][e + 2] * inv, o[i][e + 3] * inv));
+            for (int e = 0; e < CT / 2; e += 2) store4(dst + 4 * tx + 32 * e, scaled(o[i][e], o[i][e + 1], inv));
             if (p.lse_out && tx == 0) p.lse_out[((long long)b * p.kv_heads * p.G + hq) * p.n_q + qi] = natural_lse(lse2);
         } else {
             const long long at = (long long)(PREFIX ? part : p.p_slots + part) * p.rows_total + R;
 #pragma unroll
-            for (int e = 0; e < CT; e += 4)
-                *reinterpret_cast<float4 *>(p.part_o + at * D + 4 * tx + 16 * e) = make_float4(o[i][e] * inv, o[i][e + 1] * inv, o[i][e + 2] * inv, o[i][e + 3] * inv);
+            for (int e = 0; e < CT / 2; e += 2) *reinterpret_cast<float4 *>(p.part_o + at * D + 4 * tx + 32 * e) = scaled(o[i][e], o[i][e + 1], inv);
             if (tx == 0) p.part_lse[at] = lse2;
         }
     }

@@ -3,6 +3,7 @@
 
 #include "attend_common.cuh"
 #include "attend_few.cuh"
+#include "attend_few_f32.cuh"
 #include "attend_generic.cuh"
 #include "attend_tc.cuh"
 #include "evict_mass.cuh"
@@ -87,17 +88,19 @@ static long long most_keys(const obf_attend_t *a, int rows_of_queries)
     return n < a->capacity ? n : a->capacity;
 }
 
-// Up to 16 query rows (and a mass call's at most 64) go where the tensor cores' 128-row tiles would stay empty.
+// Up to 16 query rows (and a mass call's at most 64) go where a tile of 128 rows, or the generic kernel's 64, would stay empty.
 static AttendPath path_for(const obf_attend_t *a, long long rows)
 {
-    if (a->dtype != OBF_BF16 || (a->flags & OBF_FLAG_GENERIC_PATH)) return ATTEND_GENERIC;
+    if (a->flags & OBF_FLAG_GENERIC_PATH) return ATTEND_GENERIC;
     if (rows <= 16 || a->mass_out) return ATTEND_FEW;
+    if (a->dtype != OBF_BF16) return ATTEND_GENERIC;
     return a->q_heads / a->kv_heads <= AT_TILE ? ATTEND_TC : ATTEND_GENERIC;
 }
 
-constexpr int FEW_RESIDENT = 2 * 148;        // blocks of k_attend_few that run at once
+constexpr int FEW_RESIDENT = 2 * 148;        // blocks of k_attend_few that run at once; of k_attend_few_f32 twice as many
 
-static int few_rows(long long rows) { return rows <= 8 ? 8 : 16; }
+// Query rows of a tile of the kernels for few rows.
+static int few_rows(int dtype, long long rows) { return dtype == OBF_F32 ? (rows <= 4 ? 4 : 8) : rows <= 8 ? 8 : 16; }
 
 // Tiles of query rows on the tensor cores: `ti` queries of `nb` sequences with the G heads of the group.
 struct TcTiles {
@@ -137,11 +140,11 @@ static int tc_parts(long long pairs, long long keys)
 // Parts of the keys for k_attend_few: as many as make its rounds of resident blocks cheapest, a block costing its keys and, to
 // begin and to end, as much as 120 more; at least 256 keys each.  (16 sequences of 8192 keys, 128 tiles: 9 parts 95 us, 7 parts
 // 100, 14 parts 97; 32 of up to 8192 with a window of 4096: 1 part 73.6, 5 parts 80.4; 4 of 131072: 18 parts 278, 28 parts 292.)
-static int few_parts(long long tiles, long long keys)
+static int few_parts(long long tiles, long long keys, int resident)
 {
     long long best = 1, cost = LLONG_MAX;
     for (long long s = 1; s <= 128 && (s == 1 || s * 256 <= keys); ++s) {
-        const long long c = (tiles * s + FEW_RESIDENT - 1) / FEW_RESIDENT * ((keys + s - 1) / s + 120);
+        const long long c = (tiles * s + resident - 1) / resident * ((keys + s - 1) / s + 120);
         if (c < cost) { cost = c; best = s; }
     }
     return (int)best;
@@ -154,10 +157,10 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
     const auto parts = [&](AttendPath path, long long runs, long long rows_run, long long keys) {
         if (path == ATTEND_FEW) {
             // small calls: short parts, up to eight of them, a cluster each
-            const int t = few_rows(rows_run);
+            const int t = few_rows(a->dtype, rows_run);
             const long long tiles = runs * ((rows_run + t - 1) / t);
             if (8 * tiles <= FEW_RESIDENT && keys <= 4096) return parts_for(1, keys, 8, 64);
-            return few_parts(tiles, keys);
+            return few_parts(tiles, keys, a->dtype == OBF_F32 ? 2 * FEW_RESIDENT : FEW_RESIDENT);
         }
         if (path == ATTEND_TC) return tc_parts(tc_tiles((int)(a->q_heads / a->kv_heads), a->n_q, a->batch, a->kv_heads, rows_run != rows_seq).pairs, keys);
         return parts_for(runs * ((rows_run + AG_TILE - 1) / AG_TILE), keys, 2 * 148, 4 * AG_TILE);
@@ -175,7 +178,7 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
     // Parts that all fit the chip at once join themselves (a token over 1024 keys: 4.5 us instead of 5.2 with a join's launch); more
     // of them wait for places for whole clusters, which costs more than the join (batch of 32, 1024 blocks: 81 us instead of 77).
     L.cluster = L.own_path == ATTEND_FEW && !x && !a->mass_out && slots > 1 && slots <= 8 &&
-                heads * ((rows_seq + few_rows(rows_seq) - 1) / few_rows(rows_seq)) * slots <= FEW_RESIDENT;
+                heads * ((rows_seq + few_rows(a->dtype, rows_seq) - 1) / few_rows(a->dtype, rows_seq)) * slots <= FEW_RESIDENT;
     const bool join = (slots > 1 && !L.cluster) || a->mass_out;
     L.off_part_o = o;
     if (join) o = align_up(o + (size_t)slots * rows * a->head_dim * sizeof(float), 256);
@@ -212,27 +215,39 @@ static obf_status_t launch_attend_generic(const AttendDev &p, int first, cudaStr
     return OBF_OK;
 }
 
-template <int D, int NT, bool PREFIX, bool CLUSTER>
-static obf_status_t launch_attend_few_nt(const AttendDev &p, int first, cudaStream_t st)
+template <int ROWS, bool PREFIX, bool CLUSTER, typename K>
+static obf_status_t launch_few(K kernel, size_t smem, const AttendDev &p, int first, cudaStream_t st)
 {
-    static bool done[64];
-    OBF_TRY(set_smem_once(k_attend_few<D, NT, PREFIX, CLUSTER>, attend_few_smem<D>(), done));
     const int parts = PREFIX ? p.p_slots : p.slots - p.p_slots;
-    const long long rows = (PREFIX ? (long long)p.batch : 1) * p.n_q * p.G, tiles = (rows + 8 * NT - 1) / (8 * NT);
+    const long long rows = (PREFIX ? (long long)p.batch : 1) * p.n_q * p.G, tiles = (rows + ROWS - 1) / ROWS;
     const long long blocks = parts * tiles * p.kv_heads * (PREFIX ? 1 : p.batch);
     if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
-    OBF_TRY(launch_clusters(CLUSTER ? parts : 1, k_attend_few<D, NT, PREFIX, CLUSTER>, dim3((unsigned)blocks), AF_NT, attend_few_smem<D>(), st, p, first));
+    OBF_TRY(launch_clusters(CLUSTER ? parts : 1, kernel, dim3((unsigned)blocks), AF_NT, smem, st, p, first));
     ++g_last_launches;
     return OBF_OK;
 }
 
-template <int D, bool PREFIX>
+template <typename TIN, int D, int ROWS, bool PREFIX, bool CLUSTER>
+static obf_status_t launch_attend_few_rows(const AttendDev &p, int first, cudaStream_t st)
+{
+    if constexpr (sizeof(TIN) == 4) {
+        return launch_few<ROWS, PREFIX, CLUSTER>(k_attend_few_f32<D, ROWS, PREFIX, CLUSTER>, 0, p, first, st);
+    } else {
+        static bool done[64];
+        OBF_TRY(set_smem_once(k_attend_few<D, ROWS / 8, PREFIX, CLUSTER>, attend_few_smem<D>(), done));
+        return launch_few<ROWS, PREFIX, CLUSTER>(k_attend_few<D, ROWS / 8, PREFIX, CLUSTER>, attend_few_smem<D>(), p, first, st);
+    }
+}
+
+template <typename TIN, int D, bool PREFIX>
 static obf_status_t launch_attend_few(const AttendDev &p, int first, cudaStream_t st)
 {
+    constexpr int SMALL = sizeof(TIN) == 4 ? 4 : 8;
     const long long rows = (PREFIX ? (long long)p.batch : 1) * p.n_q * p.G;
+    const bool small = few_rows(sizeof(TIN) == 4 ? OBF_F32 : OBF_BF16, rows) == SMALL;
     if constexpr (!PREFIX)
-        if (p.cluster) return few_rows(rows) == 8 ? launch_attend_few_nt<D, 1, false, true>(p, first, st) : launch_attend_few_nt<D, 2, false, true>(p, first, st);
-    return few_rows(rows) == 8 ? launch_attend_few_nt<D, 1, PREFIX, false>(p, first, st) : launch_attend_few_nt<D, 2, PREFIX, false>(p, first, st);
+        if (p.cluster) return small ? launch_attend_few_rows<TIN, D, SMALL, false, true>(p, first, st) : launch_attend_few_rows<TIN, D, 2 * SMALL, false, true>(p, first, st);
+    return small ? launch_attend_few_rows<TIN, D, SMALL, PREFIX, false>(p, first, st) : launch_attend_few_rows<TIN, D, 2 * SMALL, PREFIX, false>(p, first, st);
 }
 
 // Strides of dimensions that are never stepped over may be anything for the caller, not for a tensor map.
@@ -307,8 +322,8 @@ static obf_status_t launch_attend_tc(const AttendDev &p, int first, cudaStream_t
 template <typename TIN, int D, bool PREFIX>
 static obf_status_t launch_attend(AttendPath path, const AttendDev &p, int first, cudaStream_t st)
 {
+    if (path == ATTEND_FEW) return launch_attend_few<TIN, D, PREFIX>(p, first, st);
     if constexpr (sizeof(TIN) == 2) {
-        if (path == ATTEND_FEW) return launch_attend_few<D, PREFIX>(p, first, st);
         if (path == ATTEND_TC) return launch_attend_tc<D, PREFIX>(p, first, st);
     }
     return launch_attend_generic<TIN, D, PREFIX>(p, first, st);
