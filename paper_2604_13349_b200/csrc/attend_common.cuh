@@ -31,6 +31,7 @@ struct AttendDev {
     int32_t prefix;           // rows of the shared prefix, 0 without one
     int32_t p_slots, slots;   // parts of the prefix and all parts of a row (own keys: slots - p_slots); 1: no join
     int32_t cluster;          // the parts of a row are a cluster of blocks, which joins them
+    int32_t with_prefix;      // rows of a prefix that each sequence's blocks read by themselves (small calls; `prefix` is 0 then)
     long long rows_total;     // batch * kv_heads * n_q * G
     // workspace
     uint32_t *status;

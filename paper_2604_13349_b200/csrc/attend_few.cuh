@@ -156,7 +156,8 @@ __device__ __forceinline__ void few_finish(const AttendDev &p, const float *osm,
     }
 }
 
-// CLUSTER: the parts of a tile, at most eight, are a cluster, which joins them through its shared memory.
+// CLUSTER: the parts of a tile, at most eight, are a cluster, which joins them through its shared memory; a shared prefix, in small
+// calls, is walked as keys in front of each sequence's own.
 template <int D, int NT, bool PREFIX, bool CLUSTER>
 __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ AttendDev p, const int first)
 {
@@ -187,7 +188,8 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
         const int i0 = tile * ROWS / p.G, i1 = min((min((tile + 1) * ROWS, rows_seq) - 1) / p.G, ql_own - 1);
         if (i0 <= i1) kr = attend_range(p, len_own - ql_own + i0, len_own - ql_own + i1, len_own);
     }
-    const int n = kr.count(), per = ((n + 63) / 64 + parts - 1) / parts * 64;
+    const int pre = CLUSTER ? p.with_prefix : 0;             // rows of the prefix walked before the own keys
+    const int n = pre + kr.count(), per = ((n + 63) / 64 + parts - 1) / parts * 64;
     const int v0 = min((long long)part * per, (long long)n), v1 = min(v0 + per, n);
 
     const __nv_bfloat16 *kb = PREFIX ? static_cast<const __nv_bfloat16 *>(p.pk) + h * p.pks[0]
@@ -208,10 +210,16 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
             for (int i = 0; i < AF_KEYS / LR; ++i) {
                 const int r = lr + i * LR, v = va + r;
                 const bool real = v < v1;
-                const long long j = kr.key(real ? v : v0);
+                const int u = real ? v : v0;
                 const uint32_t at = (uint32_t)(r * D * 2 + (lc ^ (r & 7)) * 16);
-                cp_async16(kd + at, kb + j * kst + lc * 8, real);
-                cp_async16(vd + at, vb + j * vst + lc * 8, real);
+                if (CLUSTER && u < pre) {
+                    cp_async16(kd + at, static_cast<const __nv_bfloat16 *>(p.pk) + h * p.pks[0] + u * p.pks[1] + lc * 8, real);
+                    cp_async16(vd + at, static_cast<const __nv_bfloat16 *>(p.pv) + h * p.pvs[0] + u * p.pvs[1] + lc * 8, real);
+                } else {
+                    const long long j = kr.key(u - pre);
+                    cp_async16(kd + at, kb + j * kst + lc * 8, real);
+                    cp_async16(vd + at, vb + j * vst + lc * 8, real);
+                }
             }
         }
         cp_commit();
@@ -292,12 +300,12 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
         bool raise = false;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int v = va + 8 * u, j = kr.key(v);
+            const int v = va + 8 * u, j = kr.key(v - pre);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const bool sees = v < v1 && (PREFIX || one_t || attend_sees(p, row_t[nt][e], j));
+                    const bool sees = v < v1 && (PREFIX || one_t || v < pre || attend_sees(p, row_t[nt][e], j));
                     float &y = s[nt][2 * u + e];
                     y = sees ? y * p.c : -INFINITY;
                     if (!PREFIX && p.mass_out && sees && row_t[nt][e] != INT_MIN) p.logits[row_at[nt][e] * p.capacity + j] = y;

@@ -36,7 +36,8 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few_f32(const __grid_constant_
         const int i0 = tile * R / p.G, i1 = min((min((tile + 1) * R, rows_seq) - 1) / p.G, ql_own - 1);
         if (i0 <= i1) kr = attend_range(p, len_own - ql_own + i0, len_own - ql_own + i1, len_own);
     }
-    const int n = kr.count(), per = ((n + 63) / 64 + parts - 1) / parts * 64;
+    const int pre = CLUSTER ? p.with_prefix : 0;         // (as in k_attend_few)
+    const int n = pre + kr.count(), per = ((n + 63) / 64 + parts - 1) / parts * 64;
     const int v0 = min((long long)part * per, (long long)n), v1 = min(v0 + per, n);
     const float *kb = (PREFIX ? static_cast<const float *>(p.pk) + h * p.pks[0] : static_cast<const float *>(p.k) + b_own * p.ks[0] + h * p.ks[1]) + 4 * wl;
     const float *vb = (PREFIX ? static_cast<const float *>(p.pv) + h * p.pvs[0] : static_cast<const float *>(p.v) + b_own * p.vs[0] + h * p.vs[1]) + 4 * wl;
@@ -50,9 +51,14 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few_f32(const __grid_constant_
             const int v = va + grp + GROUPS * e;
             kn[e] = vn[e] = make_ulonglong2(0ull, 0ull);
             if (v < v1) {
-                const long long j = kr.key(v);
-                kn[e] = __ldcs(reinterpret_cast<const ulonglong2 *>(kb + j * kst));
-                vn[e] = __ldcs(reinterpret_cast<const ulonglong2 *>(vb + j * vst));
+                const long long j = kr.key(v - pre);
+                const float *ka = kb + j * kst, *va2 = vb + j * vst;
+                if (CLUSTER && v < pre) {
+                    ka = static_cast<const float *>(p.pk) + h * p.pks[0] + v * p.pks[1] + 4 * wl;
+                    va2 = static_cast<const float *>(p.pv) + h * p.pvs[0] + v * p.pvs[1] + 4 * wl;
+                }
+                kn[e] = __ldcs(reinterpret_cast<const ulonglong2 *>(ka));
+                vn[e] = __ldcs(reinterpret_cast<const ulonglong2 *>(va2));
             }
         }
     };
@@ -117,8 +123,8 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few_f32(const __grid_constant_
             }
 #pragma unroll
             for (; off >= 1; off /= 2) d[0] += __shfl_xor_sync(0xffffffffu, d[0], off);
-            const int v = va + grp + GROUPS * e, j = kr.key(v);
-            const bool sees = v < v1 && (PREFIX || one_t || attend_sees(p, t, j));
+            const int v = va + grp + GROUPS * e, j = kr.key(v - pre);
+            const bool sees = v < v1 && (PREFIX || one_t || v < pre || attend_sees(p, t, j));
             s[e] = sees ? d[0] * p.c : -INFINITY;
             if (!PREFIX && p.mass_out && sees && t != INT_MIN && wl % SHARE == 0) p.logits[at + j] = s[e];
             raise = raise || s[e] > m + AF_RAISE;

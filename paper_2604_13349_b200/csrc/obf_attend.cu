@@ -68,6 +68,7 @@ struct AttendLayout {
     AttendPath own_path, p_path;
     int p_slots, own_slots;          // parts of the prefix and of a sequence's own keys
     bool cluster;                    // the parts join themselves
+    bool with_prefix;                // and walk the prefix as well
     size_t off_part_o, off_part_lse, off_logits, total;
 };
 
@@ -169,7 +170,12 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
     L.own_slots = parts(L.own_path, heads, rows_seq, most_keys(a, AG_TILE));
     L.p_path = ATTEND_GENERIC;
     L.p_slots = 0;
-    if (x) {
+    // A small call over a prefix: three launches would take longer than reading it once per sequence, from the L2 cache.
+    const long long few_tiles = heads * ((rows_seq + few_rows(a->dtype, rows_seq) - 1) / few_rows(a->dtype, rows_seq));
+    L.with_prefix = x && L.own_path == ATTEND_FEW && 8 * few_tiles <= FEW_RESIDENT && x->rows + a->capacity <= 4096;
+    if (L.with_prefix) {
+        L.own_slots = parts_for(1, x->rows + a->capacity, 8, 64);
+    } else if (x) {
         L.p_path = path_for(a, a->batch * rows_seq);
         L.p_slots = parts(L.p_path, a->kv_heads, a->batch * rows_seq, x->rows);
     }
@@ -177,8 +183,7 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
     size_t o = 256;
     // Parts that all fit the chip at once join themselves (a token over 1024 keys: 4.5 us instead of 5.2 with a join's launch); more
     // of them wait for places for whole clusters, which costs more than the join (batch of 32, 1024 blocks: 81 us instead of 77).
-    L.cluster = L.own_path == ATTEND_FEW && !x && !a->mass_out && slots > 1 && slots <= 8 &&
-                heads * ((rows_seq + few_rows(a->dtype, rows_seq) - 1) / few_rows(a->dtype, rows_seq)) * slots <= FEW_RESIDENT;
+    L.cluster = L.with_prefix || (L.own_path == ATTEND_FEW && !x && !a->mass_out && slots > 1 && slots <= 8 && few_tiles * slots <= FEW_RESIDENT);
     const bool join = (slots > 1 && !L.cluster) || a->mass_out;
     L.off_part_o = o;
     if (join) o = align_up(o + (size_t)slots * rows * a->head_dim * sizeof(float), 256);
@@ -359,7 +364,8 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *w
     p.q = a->q; p.k = a->k; p.v = a->v; p.out = a->out;
     for (int i = 0; i < 3; ++i) { p.qs[i] = a->q_stride[i]; p.ks[i] = a->k_stride[i]; p.vs[i] = a->v_stride[i]; p.os[i] = a->out_stride[i]; }
     if (x) {
-        p.pk = x->k; p.pv = x->v; p.prefix = x->rows;
+        p.pk = x->k; p.pv = x->v;
+        (L.with_prefix ? p.with_prefix : p.prefix) = x->rows;
         for (int i = 0; i < 2; ++i) { p.pks[i] = x->k_stride[i]; p.pvs[i] = x->v_stride[i]; }
     }
     p.lens = a->lens; p.q_lens = a->q_lens; p.lse_out = a->lse_out; p.mass_in = a->mass_in; p.mass_out = a->mass_out;
