@@ -388,7 +388,7 @@ obf_status_t obf_attend(const obf_attend_t *args, void *workspace, size_t worksp
 /*
  * The same over a prefix that all sequences share and each sequence's own keys behind it: every query sees all rows of the
  * prefix and the keys of its own sequence up to its own position (t counts own keys; with t < 0 the prefix alone).  The
- * prefix is read once for the queries of all sequences together.  window, sinks, mass_in and mass_out must be 0 / NULL.
+ * prefix is read from memory once for the queries of all sequences together.  window, sinks, mass_in and mass_out must be 0 / NULL.
  */
 obf_status_t obf_attend_shared(const obf_attend_t *args, const obf_prefix_t *prefix, void *workspace, size_t workspace_bytes,
                                void *stream);
