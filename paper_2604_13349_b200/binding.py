@@ -7,6 +7,7 @@ built (``python -m paper_2604_13349_b200.build``) loading it raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -445,9 +446,11 @@ def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, strea
         if rc != OBF_OK:
             raise ObfError(rc, name)
         size = nb.value
-        workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
-        if stream is not None:                   # the allocator gives the memory on once the given stream is done with it
-            workspace.record_stream(torch.cuda.ExternalStream(stream, device=q.device) if isinstance(stream, int) else stream)
+        if stream is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+        else:
+            with _allocating(stream, q.device):
+                workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     else:
         if workspace.device != q.device:
             raise ValueError("workspace: on %s expected" % q.device)
@@ -462,12 +465,21 @@ def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, strea
     return got
 
 
-def _attend_outputs(q, q_lens, out, lse_out, want_lse):
-    make = torch.empty if q_lens is None else torch.zeros        # what lies behind a sequence's queries is not written
-    if out is None:
-        out = make(q.shape, dtype=q.dtype, device=q.device)
-    if lse_out is None and want_lse:
-        lse_out = make(q.shape[:3], dtype=torch.float32, device=q.device)
+def _allocating(stream, device: torch.device):
+    """Memory for a call on `stream` is allocated, and cleared, on that stream."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
+
+
+def _attend_outputs(q, q_lens, out, lse_out, want_lse, stream):
+    if out is None or (lse_out is None and want_lse):
+        make = torch.empty if q_lens is None else torch.zeros    # what lies behind a sequence's queries is not written
+        with _allocating(stream, q.device):
+            if out is None:
+                out = make(q.shape, dtype=q.dtype, device=q.device)
+            if lse_out is None and want_lse:
+                lse_out = make(q.shape[:3], dtype=torch.float32, device=q.device)
     return out, lse_out
 
 
@@ -484,7 +496,7 @@ def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, lens: Optional[
     ``attend_workspace`` made for these shapes, whose status word ``obf_last_device_status`` reads afterwards; else one is
     allocated for the call.  Returns ``out`` and, where asked for, ``lse [batch, q_heads, n_q]`` (natural log) and ``mass``.
     """
-    out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse)
+    out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
     args = _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags)
     return _attend_call("obf_attend", args, None, q, out, lse_out, mass_out, workspace, stream)
 
@@ -495,7 +507,7 @@ def attend_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tenso
                   workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
     """The same for a batch whose sequences all see ``k_prefix, v_prefix [kv_heads, rows, d]`` before their own keys
     (``obf_attend_shared``): the prefix is read once for all of them."""
-    out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse)
+    out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
     args = _attend_args(q, k, v, lens, q_lens, 0, 0, scale, out, lse_out, None, None, 1.0, flags)
     if k_prefix.dim() != 3:
         raise ValueError("k_prefix: [kv_heads, rows, head_dim] expected")
@@ -541,16 +553,17 @@ def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: in
         raise ValueError("k: a float32 or bfloat16 device tensor [batch, kv_heads, capacity, head_dim] expected")
     B, kv, cap, d = shape = k.shape
     make = torch.zeros if lens is not None or keep > cap else torch.empty        # rows behind a sequence's last one are not written
-    if k_out is None:
-        k_out = make((B, kv, keep, d), dtype=dt, device=dev)
-    if v_out is None:
-        v_out = make((B, kv, keep, d), dtype=dt, device=dev)
-    if idx_out is None:
-        idx_out = make((B, kv, keep), dtype=torch.int32, device=dev)
-    if mass_out is None:
-        mass_out = make((B, kv, keep), dtype=torch.float32, device=dev)
-    if lens_out is None:
-        lens_out = torch.empty((B,), dtype=torch.int32, device=dev)
+    with _allocating(stream, dev):
+        if k_out is None:
+            k_out = make((B, kv, keep, d), dtype=dt, device=dev)
+        if v_out is None:
+            v_out = make((B, kv, keep, d), dtype=dt, device=dev)
+        if idx_out is None:
+            idx_out = make((B, kv, keep), dtype=torch.int32, device=dev)
+        if mass_out is None:
+            mass_out = make((B, kv, keep), dtype=torch.float32, device=dev)
+        if lens_out is None:
+            lens_out = torch.empty((B,), dtype=torch.int32, device=dev)
     ko, vo, mo = k_out.shape[2], v_out.shape[2], mass_out.shape[2]
     if min(ko, vo, mo) < keep:
         raise ValueError("k_out, v_out and mass_out: at least `keep` rows expected")

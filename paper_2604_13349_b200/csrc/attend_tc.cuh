@@ -14,7 +14,7 @@
 //
 // Softmax: fp32 and bf16 have the same exponents, so a row's reference need not be its maximum, only near enough for no weight
 // to leave fp32's range.  It starts as zero, and the logits are read once, without a search for their maximum before.  Only when
-// a weight comes out above 2^64, or those of a row's first tile add up to less than 2^-40 (logits beyond some 28 or 44; rows that
+// a weight comes out above 2^32, or those of a row's first tile add up to less than 2^-40 (logits beyond some 22 or -28; rows that
 // see nothing of that tile), is the tile done again against the rows' maxima, O and the sums rescaled - in place: the products
 // before have completed, since they were issued before the logits that the thread has waited for.
 // Tensor memory: S (P) and O of the two tiles, 512 columns.  Every wait is bounded.
@@ -33,7 +33,7 @@ namespace obf {
 
 constexpr int AT_TILE = 128;
 constexpr int AT_THREADS = 640;
-constexpr float AT_RAISE = 64.f, AT_WEIGHT_MAX = 18446744073709551616.f, AT_WEIGHT_MIN = 9.094947017729282e-13f;     // 2^64, 2^-40
+constexpr float AT_RAISE = 32.f, AT_WEIGHT_MAX = 4294967296.f, AT_WEIGHT_MIN = 9.094947017729282e-13f;     // 2^32, 2^-40
 
 template <int D>
 struct AttendTcShape {
@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                             w[16 * c + e] = pack_bf16(a, b2);
                         }
                     }
-                    // No weight may be above 2^64 of the reference, and those of an item's first tile add up to something; a logit
+                    // No weight may be above 2^32 of the reference, and those of an item's first tile add up to something; a logit
                     // that is not a number sends the tile the other way, too, where it spreads.
                     const float zs = sum2(z);
                     if (!any(late || !(zs <= AT_WEIGHT_MAX) || (!started && real && zs < AT_WEIGHT_MIN))) {

@@ -361,6 +361,25 @@ def test_the_same_call_gives_the_same_bits_on_any_stream_and_whatever_the_worksp
 
 
 @pytest.mark.gpu
+def test_outputs_made_for_another_stream_are_cleared_on_it():
+    q, k, v = _small(n_q=4)
+    lens = torch.tensor([600, 500], dtype=torch.int32, device="cuda")
+    ql = torch.tensor([4, 2], dtype=torch.int32, device="cuda")
+    m = torch.rand(2, 2, 600, device="cuda")
+    want = P.attend(q, k, v, lens=lens, q_lens=ql)["out"]
+    kept = P.evict_by_mass(k, v, m, 550, lens=lens)
+    side, busy = torch.cuda.Stream(), torch.rand(1 << 26, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for _ in range(20):
+            busy.mul_(1.0)                                                         # the current stream is behind
+        got, e = P.attend(q, k, v, lens=lens, q_lens=ql, stream=side)["out"], P.evict_by_mass(k, v, m, 550, lens=lens, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and (got[1, :, 2:] == 0).all()
+        assert all(torch.equal(e[n], kept[n]) for n in kept)
+
+
+@pytest.mark.gpu
 def test_calls_at_once_on_two_streams():
     cases = [_small(seed=s, n_q=n, cap=900) for s, n in ((1, 1), (2, 1), (3, 90), (4, 90))]
     want = [P.attend(*c)["out"] for c in cases]
@@ -431,6 +450,16 @@ def test_values_that_are_not_finite_reach_the_queries_that_see_them(n_q):
     assert out[0, :4, t >= 150].isnan().all() and out[0, 4:].isfinite().all()
     hit = out[1, 4:, :, 5]
     assert not hit.isfinite().any() and out[1, 4:, :, 6].isfinite().all() and out[1, :4].isfinite().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_q", [1, 64])
+def test_very_large_values(n_q):
+    gen = torch.Generator().manual_seed(21)
+    q, k, v = _data(gen, 1, 2, 2, 128, n_q, 300, BF16)
+    q, v = (q.float() * 2).to(BF16), (v.float() * 1e27).to(BF16)                     # logits of up to some 20
+    w = ref.attend(q, k, v, [300], [n_q])
+    _check(P.attend(q.cuda(), k.cuda(), v.cuda())["out"], w[0], w[1], "out")
 
 
 @pytest.mark.gpu
