@@ -476,9 +476,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         tc::tmem_ld_wait32(r);
                         if (!full) {
                             const uint32_t bits = seen(c);
+                            if (__any_sync(0xffffffffu, bits != 0xFFFFFFFFu)) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
+                                for (int e = 0; e < 32; ++e)
+                                    if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
+                            }
                         }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
