@@ -144,13 +144,16 @@ __device__ __forceinline__ float join_weights(const AttendDev &p, long long R, i
 #pragma unroll
     for (int k = 0; k < AJ_MAX_SLOTS / 32; ++k) {
         const int sl = 32 * k + lane;
-        l[k] = sl < p.slots ? p.part_lse[(long long)sl * p.rows_total + R] : -INFINITY;
+        l[k] = -INFINITY;
+        if (32 * k >= p.slots) continue;
+        if (sl < p.slots) l[k] = p.part_lse[(long long)sl * p.rows_total + R];
         m = fmaxf(m, l[k]);
     }
     m = warp_max(m);
     float z = 0.f;
 #pragma unroll
     for (int k = 0; k < AJ_MAX_SLOTS / 32; ++k) {
+        if (32 * k >= p.slots) continue;
         l[k] = l[k] == -INFINITY ? 0.f : exp2f(l[k] - m);          // (a lse that is not a number spreads, the maximum ignores it)
         z += l[k];
     }
