@@ -362,6 +362,7 @@ def compress_caches(params: ObfParams, caches_in: Sequence[Dict[str, object]], *
 # operators on a relayed cache
 # ---------------------------------------------------------------------------
 _DTYPES = {torch.float32: OBF_F32, torch.bfloat16: OBF_BF16}
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 
 # A single token's attention takes some microseconds on the device, so these wrappers hand the structs over as packed bytes
 # (building a ctypes structure field by field takes longer than the kernels).
@@ -370,6 +371,8 @@ _PREFIX = struct.Struct("@2P4qi4x")
 _EVICT = struct.Struct("@8i4P12q4Pi4xP")
 assert (_ATTEND.size, _PREFIX.size, _EVICT.size) == (ctypes.sizeof(ObfAttend), ctypes.sizeof(ObfPrefix), ctypes.sizeof(ObfEvict))
 _packed_calls: Dict[str, object] = {}
+_STATUS_ONLY = 256
+_status_words: Dict[int, torch.Tensor] = {}
 _MOST = 0x7FFFFFFF                      # windows and numbers of first tokens beyond any position are as good
 
 
@@ -407,21 +410,24 @@ def _dense(t: Optional[torch.Tensor], shape, dtype, device: int, name: str) -> i
 
 def _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags) -> bytes:
     dt, dev = q.dtype, q.get_device()
-    if dt not in _DTYPES or dev < 0 or q.dim() != 4 or k.dim() != 4:
-        raise ValueError("q, k: float32 or bfloat16 device tensors [batch, heads, rows, head_dim] expected")
+    code = OBF_BF16 if dt is _BF16 else OBF_F32 if dt is _F32 else -1
     shape_q, shape_k = q.shape, k.shape
+    if code < 0 or dev < 0 or len(shape_q) != 4 or len(shape_k) != 4:
+        raise ValueError("q, k: float32 or bfloat16 device tensors [batch, heads, rows, head_dim] expected")
     B, hq, n_q, d = shape_q
-    _, kv, cap, _ = shape_k
-    if shape_k[0] != B or shape_k[3] != d:
-        _refuse("k", k, (B, kv, cap, d), dt, dev)
-    f32, i32 = torch.float32, torch.int32
-    sq, so = _rows(q, shape_q, dt, dev, "q"), _rows(out, shape_q, dt, dev, "out")
-    sk, sv = _rows(k, shape_k, dt, dev, "k"), _rows(v, shape_k, dt, dev, "v")
+    b, kv, cap, dk = shape_k
+    sq, sk, sv, so = q.stride(), k.stride(), v.stride(), out.stride()
+    if not (b == B and dk == d and v.shape == shape_k and out.shape == shape_q and k.dtype is dt and v.dtype is dt and out.dtype is dt and
+            k.get_device() == dev and v.get_device() == dev and out.get_device() == dev and sq[3] == sk[3] == sv[3] == so[3] == 1):
+        for t, shape, name in ((q, shape_q, "q"), (k, (B, kv, cap, d), "k"), (v, (B, kv, cap, d), "v"), (out, shape_q, "out")):
+            _rows(t, shape, dt, dev, name)                       # names the one that is wrong
     return _ATTEND.pack(
-        B, kv, hq, d, n_q, cap, min(window, _MOST), min(sinks, _MOST), _DTYPES[dt], scale, decay, flags, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+        B, kv, hq, d, n_q, cap, min(window, _MOST), min(sinks, _MOST), code, scale, decay, flags, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
         sq[0], sq[1], sq[2], sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], so[0], so[1], so[2],
-        _dense(lens, (B,), i32, dev, "lens"), _dense(q_lens, (B,), i32, dev, "q_lens"), _dense(lse_out, shape_q[:3], f32, dev, "lse_out"),
-        _dense(mass_in, shape_k[:3], f32, dev, "mass_in"), _dense(mass_out, shape_k[:3], f32, dev, "mass_out"))
+        0 if lens is None else _dense(lens, (B,), _I32, dev, "lens"), 0 if q_lens is None else _dense(q_lens, (B,), _I32, dev, "q_lens"),
+        0 if lse_out is None else _dense(lse_out, shape_q[:3], _F32, dev, "lse_out"),
+        0 if mass_in is None else _dense(mass_in, shape_k[:3], _F32, dev, "mass_in"),
+        0 if mass_out is None else _dense(mass_out, shape_k[:3], _F32, dev, "mass_out"))
 
 
 def _enqueue(name: str, device: int, args, stream) -> None:
@@ -446,7 +452,13 @@ def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, strea
         if rc != OBF_OK:
             raise ObfError(rc, name)
         size = nb.value
-        if stream is None:
+        if size <= _STATUS_ONLY:                 # a status word that nobody asks for: one per device does for all
+            workspace = _status_words.get(q.get_device())
+            if workspace is None:
+                workspace = torch.zeros(_STATUS_ONLY, dtype=torch.uint8, device=q.device)
+                if not torch.cuda.is_current_stream_capturing():          # (a graph's memory goes with the graph)
+                    _status_words[q.get_device()] = workspace
+        elif stream is None:
             workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
         else:
             with _allocating(stream, q.device):
@@ -549,31 +561,38 @@ def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: in
     (``obf_evict_by_mass`` in include/obf.h).  ``k_out, v_out`` and ``mass_out`` may have more rows than ``keep``: the cache goes on
     there.  Returns ``K_out, V_out, idx, mass, lens``."""
     dt, dev, at = k.dtype, k.device, k.get_device()
-    if dt not in _DTYPES or at < 0 or k.dim() != 4:
+    code = OBF_BF16 if dt is _BF16 else OBF_F32 if dt is _F32 else -1
+    shape = k.shape
+    if code < 0 or at < 0 or len(shape) != 4:
         raise ValueError("k: a float32 or bfloat16 device tensor [batch, kv_heads, capacity, head_dim] expected")
-    B, kv, cap, d = shape = k.shape
-    make = torch.zeros if lens is not None or keep > cap else torch.empty        # rows behind a sequence's last one are not written
-    with _allocating(stream, dev):
-        if k_out is None:
-            k_out = make((B, kv, keep, d), dtype=dt, device=dev)
-        if v_out is None:
-            v_out = make((B, kv, keep, d), dtype=dt, device=dev)
-        if idx_out is None:
-            idx_out = make((B, kv, keep), dtype=torch.int32, device=dev)
-        if mass_out is None:
-            mass_out = make((B, kv, keep), dtype=torch.float32, device=dev)
-        if lens_out is None:
-            lens_out = torch.empty((B,), dtype=torch.int32, device=dev)
-    ko, vo, mo = k_out.shape[2], v_out.shape[2], mass_out.shape[2]
+    B, kv, cap, d = shape
+    if k_out is None or v_out is None or idx_out is None or mass_out is None or lens_out is None:
+        make = torch.zeros if lens is not None or keep > cap else torch.empty    # rows behind a sequence's last one are not written
+        with _allocating(stream, dev):
+            if k_out is None:
+                k_out = make((B, kv, keep, d), dtype=dt, device=dev)
+            if v_out is None:
+                v_out = make((B, kv, keep, d), dtype=dt, device=dev)
+            if idx_out is None:
+                idx_out = make((B, kv, keep), dtype=_I32, device=dev)
+            if mass_out is None:
+                mass_out = make((B, kv, keep), dtype=_F32, device=dev)
+            if lens_out is None:
+                lens_out = torch.empty((B,), dtype=_I32, device=dev)
+    shape_ko, shape_vo, mo = k_out.shape, v_out.shape, mass_out.shape[-1]
+    ko, vo = shape_ko[-2], shape_vo[-2]
     if min(ko, vo, mo) < keep:
         raise ValueError("k_out, v_out and mass_out: at least `keep` rows expected")
-    sk, sv = _rows(k, shape, dt, at, "k"), _rows(v, shape, dt, at, "v")
-    s1, s2 = _rows(k_out, (B, kv, ko, d), dt, at, "k_out"), _rows(v_out, (B, kv, vo, d), dt, at, "v_out")
+    sk, sv, s1, s2 = k.stride(), v.stride(), k_out.stride(), v_out.stride()
+    if not (v.shape == shape and shape_ko == (B, kv, ko, d) and shape_vo == (B, kv, vo, d) and v.dtype is dt and k_out.dtype is dt and v_out.dtype is dt and
+            v.get_device() == at and k_out.get_device() == at and v_out.get_device() == at and sk[3] == sv[3] == s1[3] == s2[3] == 1):
+        for t, want, name in ((k, shape, "k"), (v, shape, "v"), (k_out, (B, kv, ko, d), "k_out"), (v_out, (B, kv, vo, d), "v_out")):
+            _rows(t, want, dt, at, name)                         # names the one that is wrong
     args = _EVICT.pack(
-        B, kv, d, cap, _DTYPES[dt], keep, sinks, recent, k.data_ptr(), v.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+        B, kv, d, cap, code, keep, sinks, recent, k.data_ptr(), v.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
         sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], s1[0], s1[1], s1[2], s2[0], s2[1], s2[2],
-        _dense(mass, (B, kv, cap), torch.float32, at, "mass"), _dense(lens, (B,), torch.int32, at, "lens"),
-        _dense(idx_out, (B, kv, keep), torch.int32, at, "idx_out"), _dense(mass_out, (B, kv, mo), torch.float32, at, "mass_out"), mo,
-        _dense(lens_out, (B,), torch.int32, at, "lens_out"))
+        _dense(mass, shape[:3], _F32, at, "mass"), 0 if lens is None else _dense(lens, (B,), _I32, at, "lens"),
+        _dense(idx_out, (B, kv, keep), _I32, at, "idx_out"), _dense(mass_out, (B, kv, mo), _F32, at, "mass_out"), mo,
+        _dense(lens_out, (B,), _I32, at, "lens_out"))
     _enqueue("obf_evict_by_mass", at, (args,), stream)
     return {"K_out": k_out, "V_out": v_out, "idx": idx_out, "mass": mass_out, "lens": lens_out}

@@ -416,6 +416,40 @@ def test_captured_calls_follow_the_lengths(dtype, n_q):
 
 
 @pytest.mark.gpu
+def test_a_call_captured_first_leaves_nothing_of_the_graph_behind():
+    q, k, v = _small(cap=100)
+    want = P.attend(q, k, v)["out"]
+    binding._status_words.clear()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = P.attend(q, k, v)["out"]
+    assert not binding._status_words
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    del graph, got
+    assert torch.equal(P.attend(q, k, v)["out"], want)
+
+
+@pytest.mark.gpu
+def test_refusals_name_the_tensor():
+    q, k, v = _small(cap=100)
+    for kw, name in ((dict(v=v[:, :, :50]), "v"), (dict(v=v.float()), "v"), (dict(k=k[:, :, :, :64]), "k"), (dict(lens=torch.ones(3, dtype=torch.int32, device="cuda")), "lens"),
+                     (dict(lens=torch.ones(2, dtype=torch.int64, device="cuda")), "lens"), (dict(out=q.float()), "out"), (dict(v=v.cpu()), "v"),
+                     (dict(mass_out=torch.zeros(2, 2, 99, device="cuda")), "mass_out"), (dict(q=q.transpose(2, 3)), "q")):
+        args = dict(q=q, k=k, v=v)
+        args.update(kw)
+        with pytest.raises(ValueError, match=name):
+            P.attend(args.pop("q"), args.pop("k"), args.pop("v"), **args)
+    m = torch.rand(2, 2, 100, device="cuda")
+    for kw, name in ((dict(v=v[:, :1]), "v"), (dict(mass=m.double()), "mass"), (dict(k_out=k[:, :, :5]), "k_out"), (dict(k_out=k.float()), "k_out")):
+        args = dict(k=k, v=v, mass=m)
+        args.update(kw)
+        with pytest.raises(ValueError, match=name):
+            P.evict_by_mass(args.pop("k"), args.pop("v"), args.pop("mass"), 10, **args)
+
+
+@pytest.mark.gpu
 def test_lengths_out_of_range_are_clamped_and_reported():
     for n_q in (1, 40):
         q, k, v = _small(n_q=n_q)
