@@ -1,20 +1,25 @@
-// Attention over a relayed cache on the CUDA cores: fp32 caches, and bf16 where the tensor-core kernels do not apply or the
-// caller asks for these.
+// Attention over a relayed cache on the CUDA cores: fp32 caches with more than 16 query rows per KV head, and bf16 where the
+// tensor-core kernels do not apply or the caller asks for these.
 //
 // A block owns 64 query rows of a KV head and a part of their keys, in tiles of 64: logits as 4 x 4 register tiles of dot
-// products (tile_dots), a running maximum and sum per row, the weights to shared memory, and 4 rows x D / 16 channels of the
-// output per thread.  All in fp32.  Bound by the fp32 multiply-adds (two-wide) and the shared-memory reads that feed them.
+// products (tile_dots), a running maximum and sum per row, the weights over the tile of keys in shared memory, and 4 rows x D / 16
+// channels of the output per thread, two channels per multiply-add.  All in fp32.  Bound by the multiply-adds and the shared-memory
+// reads that feed them: 32 TFLOP/s on a causal fp32 prompt of 4096 with heads of 64 channels (28 before the next tile was copied
+// ahead), 21 with a window of 300, where half of every tile is masked and 512 blocks make two rounds of 296.
 #pragma once
 
-#include "attend_common.cuh"
+#include "attend_few.cuh"
 
 namespace obf {
 
 constexpr int AG_NT = 256;
 constexpr int AG_TILE = 64;
 
-template <int D>
-constexpr size_t attend_generic_smem() { return (size_t)(3 * AG_TILE * TD_LD<D>) * sizeof(float); }
+// fp32 heads of 64 channels: the next tile of keys and values is copied while this one is worked on.
+template <typename TIN, int D>
+constexpr bool AG_ASYNC = sizeof(TIN) == 4 && D == 64;
+template <typename TIN, int D>
+constexpr size_t attend_generic_smem() { return (size_t)((AG_ASYNC<TIN, D> ? 5 : 3) * AG_TILE * TD_LD<D>) * sizeof(float); }
 static_assert(TD_LD<64> >= AG_TILE + 4, "the weights lie over the keys");
 
 __device__ __forceinline__ float4 scaled(f32x2 a, f32x2 b, float f)
@@ -32,7 +37,9 @@ __global__ void __launch_bounds__(AG_NT, 2) k_attend_generic(const __grid_consta
     if (first) pdl_wait();                               // (else as in k_attend_few)
     pdl_trigger();
     extern __shared__ float sm[];
-    float *Qs = sm, *Ks = Qs + AG_TILE * TD_LD<D>, *Vs = Ks + AG_TILE * TD_LD<D>, *Ps = Ks;
+    constexpr int TILE = AG_TILE * TD_LD<D>;
+    constexpr bool ASYNC = AG_ASYNC<TIN, D>;
+    float *Qs = sm, *Ks = Qs + TILE, *Vs = Ks + TILE;
     constexpr int P_LD = AG_TILE + 4, VEC = 16 / sizeof(TIN), CH = D / VEC, CT = D / 16;
     __shared__ int row_t[AG_TILE];                       // position of a row's query, INT_MIN: not a query of the call
     __shared__ long long row_at[AG_TILE];                // its number among the call's rows
@@ -74,15 +81,19 @@ __global__ void __launch_bounds__(AG_NT, 2) k_attend_generic(const __grid_consta
     }
     __syncthreads();
 
+    int t0 = INT_MAX, t1 = INT_MIN;                      // positions of the tile's first and last query
+    bool whole = true;                                   // all its rows are queries
+    for (int rr = 0; rr < AG_TILE; ++rr) {
+        if (row_t[rr] == INT_MIN) { whole = false; continue; }
+        t0 = min(t0, row_t[rr]);
+        t1 = max(t1, row_t[rr]);
+    }
     // the keys
     KeyRange kr;
     if (PREFIX) {
         kr.s = kr.lo = 0;
         kr.hi = p.prefix;
     } else {
-        int t0 = INT_MAX, t1 = INT_MIN;
-        for (int rr = 0; rr < AG_TILE; ++rr)
-            if (row_t[rr] != INT_MIN) { t0 = min(t0, row_t[rr]); t1 = max(t1, row_t[rr]); }
         kr.s = kr.lo = kr.hi = 0;
         if (t1 != INT_MIN) kr = attend_range(p, t0, t1, attend_len(p, b_own));
     }
@@ -103,8 +114,28 @@ __global__ void __launch_bounds__(AG_NT, 2) k_attend_generic(const __grid_consta
 #pragma unroll
         for (int e = 0; e < CT / 2; ++e) o[i][e] = 0ull;
     }
-    for (int v = v0; v < v1; v += AG_TILE) {
+    auto fetch = [&](int v, float *kd, float *vd) {
+        for (int i = threadIdx.x; i < AG_TILE * CH; i += AG_NT) {
+            const int rr = i / CH, ch = i - rr * CH;
+            const bool there = v + rr < v1;
+            const long long j = kr.key(there ? v + rr : v0);
+            const uint32_t at = (uint32_t)(rr * TD_LD<D> + ch * VEC) * 4;
+            cp_async16((uint32_t)__cvta_generic_to_shared(kd) + at, kb + j * kst + ch * VEC, there);
+            cp_async16((uint32_t)__cvta_generic_to_shared(vd) + at, vb + j * vst + ch * VEC, there);
+        }
+        cp_commit();
+    };
+    if (ASYNC && v0 < v1) fetch(v0, Ks, Vs);
+    for (int v = v0, turn = 0; v < v1; v += AG_TILE, turn ^= 1) {
         __syncthreads();
+        if constexpr (ASYNC) {
+            // (the other buffers' last readers are through)
+            Ks = Qs + TILE + 2 * turn * TILE;
+            Vs = Ks + TILE;
+            if (v + AG_TILE < v1) fetch(v + AG_TILE, Qs + TILE + 2 * (turn ^ 1) * TILE, Qs + 2 * TILE + 2 * (turn ^ 1) * TILE);
+            else cp_commit();
+            cp_wait<1>();
+        } else
         for (int i = threadIdx.x; i < AG_TILE * CH; i += AG_NT) {
             const int rr = i / CH, ch = i - rr * CH;
             float f[VEC], w[VEC];
@@ -122,6 +153,10 @@ __global__ void __launch_bounds__(AG_NT, 2) k_attend_generic(const __grid_consta
         float s[4][4];
         tile_dots<D>(Qs, Ks, ty, tx, s);
         __syncthreads();                                 // the weights go where the keys were
+        float *Ps = Ks;
+        // whether every row sees every key of the tile (not asked for heads of 128 channels, whose registers are full)
+        const int ja = kr.key(v), jb = kr.key(v + AG_TILE - 1);
+        const bool full = D == 64 && whole && v + AG_TILE <= v1 && (PREFIX || ((v >= kr.s || v + AG_TILE <= kr.s) && jb <= t0 && (p.window == 0 || ja > t1 - p.window || jb < p.sinks)));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = row_t[ty + 16 * i];
@@ -129,7 +164,7 @@ __global__ void __launch_bounds__(AG_NT, 2) k_attend_generic(const __grid_consta
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int vv = v + tx + 16 * e, j = vv < v1 ? kr.key(vv) : 0;
-                const bool sees = vv < v1 && t != INT_MIN && (PREFIX || attend_sees(p, t, j));
+                const bool sees = full || (vv < v1 && t != INT_MIN && (PREFIX || attend_sees(p, t, j)));
                 s[i][e] = sees ? s[i][e] * p.c : -INFINITY;
                 if (!PREFIX && p.mass_out && sees) p.logits[row_at[ty + 16 * i] * p.capacity + j] = s[i][e];
                 mx = fmaxf(mx, s[i][e]);

@@ -2,14 +2,14 @@
 //
 // A block (one per multiprocessor, persistent) works on items: two tiles of up to 128 query rows of a KV head and a part of the
 // keys that they see.  A tile is `ti` queries x the G heads of the group (so its rows see nearly the same keys and a window
-// wastes little), over a shared prefix also `nb` sequences.  Keys come in tiles of 128: first the sinks, in a tile of their own
-// that is only as wide as needed, then the window's range.
-//   warp 18, a thread   works out the items (ahead of the others, who read them from shared memory); Q, K and V tiles by TMA
+// wastes little), over a shared prefix also `nb` sequences.  Keys come in tiles of 128: the sinks first, padded with
+// zeros to 16, 32, 48 or 64 rows (more of them: to whole tiles), the window's range behind them in the same tile.
+//   warp 2, a thread    works out the items (ahead of the others, who read them from shared memory); Q, K and V tiles by TMA
 //                       (128-byte swizzle) into a ring of K and V slots
-//   warps 16, 17        products of the first and the second query tile: S = Q K^T into tensor memory, O += P V with P from
+//   warps 0, 1          products of the first and the second query tile: S = Q K^T into tensor memory, O += P V with P from
 //                       tensor memory; those of one tile run while the softmax of the other does
-//   warps 0-7, 8-15     softmax of the first and the second query tile, two threads per row with 64 keys each (one would take
-//                       twice as long for its tile, and the products wait for it), weights to bf16 over the logits' columns,
+//   warps 4-11, 12-19   softmax of the first and the second query tile, two threads per row with 64 keys each (one warp alone on a
+//                       scheduler leaves the special-function unit idle between its instructions), weights to bf16 over the logits' columns,
 //                       their fp32 sum; after the last tile O / sum to memory
 //
 // Softmax: fp32 and bf16 have the same exponents, so a row's reference need not be its maximum, only near enough for no weight
@@ -23,7 +23,9 @@
 // up to 16, and the softmax warps clear the rows in between.
 //
 // Bound by the exponentials (16 per cycle and multiprocessor: 1024 cycles a tile of 128 x 128) and the two products (512 cycles
-// each) alike.
+// each) alike, and by the chain from one to the other: a pair of tiles takes 2900 to 3200 cycles, not 2048.  Prompt of 8192, 32
+// heads over 8, 128 channels: causal 549 us (1002 TFLOP/s, 61 % of the measured burst rate), with a window of 1024 and 4 sinks 158
+// us (816; 166 in long runs, at the power limit).
 #pragma once
 
 #include "attend_common.cuh"
@@ -49,10 +51,6 @@ struct AttendTcMaps {
     int32_t ti, nb;                                                       // queries and sequences of a tile of rows
     int32_t head_rows;                                                    // rows that the sinks take: at most 64, or whole tiles
 };
-
-// Of two values, without an array that is indexed at run time.
-template <typename T>
-__device__ __forceinline__ T pick(const T (&a)[2], int x) { return x ? a[1] : a[0]; }
 
 // What every role of a block knows about an item.
 template <bool PREFIX>
@@ -191,12 +189,6 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map
 {
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
                  ::"r"(dst), "l"(map), "r"(tc::smem_u32(bar)), "r"(0), "r"(row), "r"(block), "r"(head), "r"(seq) : "memory");
-}
-
-// The values are there before the next load from tensor memory begins: otherwise the compiler begins it early and runs out of registers.
-__device__ __forceinline__ void hold16(uint32_t (&r)[16])
-{
-    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
 }
 
 // 32 bytes to global memory, in two halves where the address is no multiple of 32.

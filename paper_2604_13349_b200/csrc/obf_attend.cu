@@ -211,11 +211,11 @@ template <typename TIN, int D, bool PREFIX>
 static obf_status_t launch_attend_generic(const AttendDev &p, int first, cudaStream_t st)
 {
     static bool done[64];
-    OBF_TRY(set_smem_once(k_attend_generic<TIN, D, PREFIX>, attend_generic_smem<D>(), done));
+    OBF_TRY(set_smem_once(k_attend_generic<TIN, D, PREFIX>, attend_generic_smem<TIN, D>(), done));
     const long long rows = (PREFIX ? (long long)p.batch : 1) * p.n_q * p.G, tiles = (rows + AG_TILE - 1) / AG_TILE;
     const long long blocks = (PREFIX ? p.p_slots : p.slots - p.p_slots) * tiles * p.kv_heads * (PREFIX ? 1 : p.batch);
     if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
-    OBF_TRY(launch(k_attend_generic<TIN, D, PREFIX>, dim3((unsigned)blocks), AG_NT, attend_generic_smem<D>(), st, p, first));
+    OBF_TRY(launch(k_attend_generic<TIN, D, PREFIX>, dim3((unsigned)blocks), AG_NT, attend_generic_smem<TIN, D>(), st, p, first));
     ++g_last_launches;
     return OBF_OK;
 }
