@@ -84,7 +84,7 @@ __host__ __device__ constexpr size_t few_finish_smem() { return ((size_t)AF_WARP
 
 template <typename TIN, int D, int ROWS, bool PREFIX, bool CLUSTER>
 __device__ __forceinline__ void few_finish(const AttendDev &p, const float *osm, float *ml, int tile, int part, int parts, int rows_run, int rows_seq, int h,
-                                           int b_own, int ql_own)
+                                           int b_own, int len_own, int ql_own, const KeyRange &kr, int v0, int v1)
 {
     auto locate_row = [&](int run, int &b, int &r) {
         b = PREFIX ? run / rows_seq : b_own;
@@ -151,6 +151,40 @@ __device__ __forceinline__ void few_finish(const AttendDev &p, const float *osm,
                 }
             const float inv = Z == 0.f ? 0.f : 1.f / Z;
             put(b_own, h * p.G + r - i * p.G, i, c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv), Z == 0.f ? -INFINITY : M + log2f(Z));
+        }
+        if (p.mass_out) {
+            // Masses, in calls whose rows of a (sequence, KV head) are one tile: every block knows the lse of all rows now and adds up
+            // the weights of its own keys, whose logits it has left in the workspace; of the keys that nobody sees it takes a share.
+            __shared__ float lse[ROWS];
+            const int rows = ql_own * p.G;
+            if ((int)threadIdx.x < rows) {
+                float l[8], M = -INFINITY, Z = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < parts) {
+                        l[k] = cluster_load(cluster_addr(cl_lse + threadIdx.x, k));
+                        M = fmaxf(M, l[k]);
+                    }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < parts) Z += l[k] == -INFINITY ? 0.f : exp2f(l[k] - M);
+                lse[threadIdx.x] = M + log2f(Z);
+            }
+            __syncthreads();
+            const long long bh = (long long)b_own * p.kv_heads + h;
+            const float *x = p.logits + bh * rows_seq * p.capacity;
+            const float *in = p.mass_in ? p.mass_in + bh * p.capacity : nullptr;
+            float *out = p.mass_out + bh * p.capacity;
+            for (int v = v0 + (int)threadIdx.x; v < v1; v += AF_NT) {
+                const int j = kr.key(v);
+                float sum = 0.f;
+                for (int r = 0; r < rows; ++r)
+                    if (attend_sees(p, len_own - ql_own + r / p.G, j)) sum += exp2f(x[(long long)r * p.capacity + j] - lse[r]);
+                out[j] = (in ? p.decay * in[j] : 0.f) + sum;
+            }
+            const int e = (int)((long long)len_own * (part + 1) / parts);
+            for (int j = (int)((long long)len_own * part / parts) + (int)threadIdx.x; j < e; j += AF_NT)
+                if (!(j < kr.s || (j >= kr.lo && j < kr.hi))) out[j] = in ? p.decay * in[j] : 0.f;
         }
         cluster_sync();                                   // nobody leaves while its memory is read
     }
@@ -373,7 +407,7 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few(const __grid_constant__ At
                 for (int u = 0; u < 2; ++u) osm[(warp * ROWS + row) * LD + 16 * k + 8 * u + lane / 4] = o[nt][k][2 * u + e];
         }
     __syncthreads();
-    few_finish<__nv_bfloat16, D, ROWS, PREFIX, CLUSTER>(p, osm, ml, tile, part, parts, rows_run, rows_seq, h, b_own, ql_own);
+    few_finish<__nv_bfloat16, D, ROWS, PREFIX, CLUSTER>(p, osm, ml, tile, part, parts, rows_run, rows_seq, h, b_own, len_own, ql_own, kr, v0, v1);
     if (!first) pdl_wait();
 }
 

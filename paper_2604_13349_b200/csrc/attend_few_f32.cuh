@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(AF_NT) k_attend_few_f32(const __grid_constant_
         ml[(warp * R + my) * 2 + 1] = l;
     }
     __syncthreads();
-    few_finish<float, D, R, PREFIX, CLUSTER>(p, osm, ml, tile, part, parts, rows_run, rows_seq, h, b_own, ql_own);
+    few_finish<float, D, R, PREFIX, CLUSTER>(p, osm, ml, tile, part, parts, rows_run, rows_seq, h, b_own, len_own, ql_own, kr, v0, v1);
     if (!first) pdl_wait();
 }
 

@@ -183,8 +183,10 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
     size_t o = 256;
     // Parts that all fit the chip at once join themselves (a token over 1024 keys: 4.5 us instead of 5.2 with a join's launch); more
     // of them wait for places for whole clusters, which costs more than the join (batch of 32, 1024 blocks: 81 us instead of 77).
-    L.cluster = L.with_prefix || (L.own_path == ATTEND_FEW && !x && !a->mass_out && slots > 1 && slots <= 8 && few_tiles * slots <= FEW_RESIDENT);
-    const bool join = (slots > 1 && !L.cluster) || a->mass_out;
+    // (masses: the blocks of a cluster have to see all rows of the head)
+    L.cluster = L.with_prefix || (L.own_path == ATTEND_FEW && !x && (a->mass_out ? rows_seq <= few_rows(a->dtype, rows_seq) : slots > 1) && slots <= 8 &&
+                                  few_tiles * slots <= FEW_RESIDENT);
+    const bool join = (slots > 1 || a->mass_out) && !L.cluster;
     L.off_part_o = o;
     if (join) o = align_up(o + (size_t)slots * rows * a->head_dim * sizeof(float), 256);
     L.off_part_lse = o;
@@ -339,7 +341,7 @@ static obf_status_t run_attend(const AttendLayout &L, const AttendDev &p, cudaSt
 {
     if (p.prefix) OBF_TRY((launch_attend<TIN, D, true>(L.p_path, p, 1, st)));
     OBF_TRY((launch_attend<TIN, D, false>(L.own_path, p, p.prefix == 0, st)));
-    if ((p.slots > 1 && !p.cluster) || p.mass_out) {
+    if ((p.slots > 1 || p.mass_out) && !p.cluster) {
         // a warp per row fills the chip from some thousand rows on; fewer are joined by four warps each
         const bool many = p.rows_total >= 4 * 148;
         const long long row_blocks = many ? (p.rows_total + 3) / 4 : p.rows_total;
