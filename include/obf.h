@@ -337,8 +337,11 @@ obf_status_t obf_static_scratch_status(void *stream, uint32_t *device_status);
  * obf_cache_t.lse_extra of a later compression is the lse of its observation queries over the keys outside the prompt.
  *
  * Numerics: products of the inputs accumulated in fp32, softmax in fp32; on the tensor cores the weights of a row, at most
- * one, are rounded to bf16 before they multiply the values (their sum is not), out is rounded once.  The result does not
- * depend on what else the batch holds except through the batch's sizes, and is the same in every run.
+ * one, are rounded to bf16 before they multiply the values (their sum is not), out is rounded once.  Weights are kept
+ * relative to a reference that may be off a row's maximum by factors of up to 2^32 or 2^-47: values beyond 2^90 may
+ * overflow in sums that would not, and of values below 2^-60 precision may be lost.  A sequence's result does not depend
+ * on what else the batch holds except through the batch's sizes - over a shared prefix, where rows of several sequences
+ * are worked on together, only in its rounding - and is the same in every run.
  */
 typedef struct {
     int32_t batch, kv_heads, q_heads;   /* q_heads % kv_heads == 0                                               */

@@ -535,7 +535,7 @@ def attend_workspace(q: torch.Tensor, k: torch.Tensor, *, window: int = 0, sinks
     """A workspace for ``attend`` (``prefix_rows`` 0) or ``attend_shared`` calls of these shapes."""
     B, hq, n_q, d = q.shape
     kv, cap = k.shape[1], k.shape[2]
-    args = _ATTEND.pack(B, kv, hq, d, n_q, cap, window, sinks, _DTYPES[q.dtype], 0.0, 1.0, flags, *([0] * 16), 0, 0, 0, 0, 1 if mass else 0)
+    args = _ATTEND.pack(B, kv, hq, d, n_q, cap, min(window, _MOST), min(sinks, _MOST), _DTYPES.get(q.dtype, -1), 0.0, 1.0, flags, *([0] * 16), 0, 0, 0, 0, 1 if mass else 0)
     prefix = _PREFIX.pack(0, 0, 0, 0, 0, 0, prefix_rows) if prefix_rows else None
     nb = ctypes.c_size_t(0)
     rc = _packed("obf_attend_workspace_bytes")(args, prefix, ctypes.addressof(nb))

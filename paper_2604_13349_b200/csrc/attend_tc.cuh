@@ -486,9 +486,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         }
                     }
                     // No weight may be above 2^32 of the reference, and those of an item's first tile add up to something; a logit
-                    // that is not a number sends the tile the other way, too, where it spreads.
+                    // that is not a number sends the tile the other way, too, where it spreads.  (What lies behind a sequence's queries has
+                    // no say in it: results do not depend on that.)
                     const float zs = sum2(z);
-                    if (!any(late || !(zs <= AT_WEIGHT_MAX) || (!started && real && zs < AT_WEIGHT_MIN))) {
+                    if (!any(late || (real && (!(zs <= AT_WEIGHT_MAX) || (!started && zs < AT_WEIGHT_MIN))))) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) tmem_st16(s_t + col0 + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                         l2 = add2(l2, z);
@@ -520,7 +521,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     // (a maximum below the reference changes nothing)
                     if (!started) {
                         m = fmaxf(m, mx);
-                    } else if (any(mx > m + AT_RAISE)) {
+                    } else if (any(real && mx > m + AT_RAISE)) {
                         const float f = mx > m ? ex2(m - mx) : 1.f;
                         m = fmaxf(m, mx);
                         l2 = mul2(l2, pk(f, f));

@@ -129,6 +129,13 @@ def test_struct_sizes_match_the_header():
     assert (ctypes.sizeof(binding.ObfAttend), ctypes.sizeof(binding.ObfPrefix), ctypes.sizeof(binding.ObfEvict)) == (216, 56, 208)
 
 
+def test_a_workspace_for_any_window_and_for_no_other_type():
+    q, k = torch.zeros(1, 4, 8, 64, dtype=BF16), torch.zeros(1, 2, 100, 64, dtype=BF16)
+    assert P.attend_workspace(q, k, window=1 << 40, sinks=1 << 33).numel() >= 256
+    with pytest.raises(P.ObfError):
+        P.attend_workspace(q.half(), k.half())
+
+
 def test_python_wrappers_refuse_host_tensors():
     with pytest.raises(ValueError):
         P.attend(torch.zeros(1, 4, 1, 64), torch.zeros(1, 2, 8, 64), torch.zeros(1, 2, 8, 64))
@@ -484,6 +491,22 @@ def test_values_that_are_not_finite_reach_the_queries_that_see_them(n_q):
     assert out[0, :4, t >= 150].isnan().all() and out[0, 4:].isfinite().all()
     hit = out[1, 4:, :, 5]
     assert not hit.isfinite().any() and out[1, 4:, :, 6].isfinite().all() and out[1, :4].isfinite().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_q,window", [(4, 0), (50, 0), (50, 70), (300, 0)])
+def test_what_lies_behind_a_sequence_s_queries_changes_no_bit(n_q, window):
+    gen = torch.Generator().manual_seed(23)
+    q, k, v = (x.cuda() for x in _data(gen, 2, 2, 2, 128, n_q, 500, BF16))
+    ql = torch.tensor([n_q - 1, n_q // 2], dtype=torch.int32, device="cuda")
+    got = []
+    for fill in (0.0, 300.0, -300.0, math.inf, math.nan):
+        x = q.clone()
+        for b in range(2):
+            x[b, :, int(ql[b]):] = fill
+        got.append(P.attend(x, k, v, q_lens=ql, window=window, sinks=3, want_lse=True))
+    for g in got[1:]:
+        assert torch.equal(g["out"], got[0]["out"]) and torch.equal(g["lse"], got[0]["lse"])
 
 
 @pytest.mark.gpu
