@@ -2,7 +2,7 @@
 //
 // A block (one per multiprocessor, persistent) works on items: two tiles of up to 128 query rows of a KV head and a part of the
 // keys that they see.  A tile is `ti` queries x the G heads of the group (so its rows see nearly the same keys and a window
-// wastes little), over a shared prefix also `nb` sequences.  Keys come in tiles of 128: the sinks first, padded with
+// wastes little), over a shared prefix, where all rows see the same, also `nb` sequences: as many of either as make the fewest tiles.  Keys come in tiles of 128: the sinks first, padded with
 // zeros to 16, 32, 48 or 64 rows (more of them: to whole tiles), the window's range behind them in the same tile.
 //   warp 2, a thread    works out the items (ahead of the others, who read them from shared memory); Q, K and V tiles by TMA
 //                       (128-byte swizzle) into a ring of K and V slots
@@ -55,8 +55,9 @@ struct AttendTcMaps {
 // What every role of a block knows about an item.
 template <bool PREFIX>
 struct AttendTcItem {
-    int h, b, part;                  // KV head, first sequence, part of the keys
-    int i0, ti, nb;                  // first query of the first tile, queries and sequences of a tile
+    int h, b, part;                  // KV head, sequence (of own keys), part of the keys
+    int ti, nb;                      // queries and sequences of a tile
+    int fi[2], fb[2];                // first query and sequence of the tiles
     int head, lo, hi;                // keys of the pair: the sinks in `head` rows (zeros behind them), then lo .. hi - 1
     int jb, je;                      // the part's tiles
     // per tile of rows: some row sees tile j of the keys when j < sk or ja <= j < jz, every row sees all of it when fa <= j < fz
@@ -64,10 +65,6 @@ struct AttendTcItem {
     bool valid[2];
     int t;                           // position of a sequence's first query
     int ql;
-    bool seqs;                       // the pair's tiles are of different sequences (all their queries fit a tile)
-
-    __device__ __forceinline__ int first_i(int x) const { return seqs ? 0 : i0 + x * ti; }
-    __device__ __forceinline__ int first_b(int x) const { return seqs ? b + x * nb : b; }
 
     __device__ __forceinline__ void init(const AttendDev &p, const AttendTcMaps &tm, int item)
     {
@@ -76,29 +73,30 @@ struct AttendTcItem {
         const int parts = PREFIX ? p.p_slots : p.slots - p.p_slots;
         part = item % parts;
         item /= parts;
-        seqs = PREFIX && ti >= p.n_q;
         h = item % p.kv_heads;
         item /= p.kv_heads;
-        if (seqs) {
-            b = item * 2 * nb;
-            i0 = 0;
-        } else {
-            b = item % p.batch;
-            item /= p.batch;
-            const int pairs = (p.n_q + 2 * ti - 1) / (2 * ti);
-            i0 = (pairs - 1 - item) * 2 * ti;                             // the longest key ranges first
-        }
-        head = lo = hi = t = ql = 0;
+        b = head = lo = hi = t = ql = 0;
         if (PREFIX) {
             hi = p.prefix;
+            const int groups = (p.batch + nb - 1) / nb;                   // of sequences; tiles go through them first
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                valid[x] = first_b(x) < p.batch && first_i(x) < p.n_q;
+                const int tile = 2 * item + x;
+                fi[x] = tile / groups * ti;
+                fb[x] = tile % groups * nb;
+                valid[x] = fi[x] < p.n_q;
                 sk[x] = ja[x] = fa[x] = 0;
                 jz[x] = valid[x] ? (hi + AT_TILE - 1) / AT_TILE : 0;
                 fz[x] = hi / AT_TILE;
             }
         } else {
+            b = item % p.batch;
+            item /= p.batch;
+            const int pairs = (p.n_q + 2 * ti - 1) / (2 * ti);
+            const int i0 = (pairs - 1 - item) * 2 * ti;                   // the longest key ranges first
+            fi[0] = i0;
+            fi[1] = i0 + ti;
+            fb[0] = fb[1] = b;
             const int len = attend_len(p, b);
             ql = attend_q_len(p, b);
             t = len - ql;
@@ -299,7 +297,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     for (int x = 0; x < 2; ++x)
                         if (it.valid[x])
                             for (int c = 0; c < NB; ++c)
-                                tma_load_4d(tc::smem_u32(q_sm + x * SLOT_BYTES + c * BLOCK), &tm.q, &bar_q_full, 64 * c, it.h * p.G, it.first_i(x), it.first_b(x));
+                                tma_load_4d(tc::smem_u32(q_sm + x * SLOT_BYTES + c * BLOCK), &tm.q, &bar_q_full, 64 * c, it.h * p.G, it.fi[x], it.fb[x]);
                     ++nq;
                 }
             }
@@ -427,10 +425,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             it.hi = im.hi;
             bool real = im.valid[x] && row_b < im.nb;
             {
-                const int i = im.first_i(x) + row_i, b = im.first_b(x) + row_b;
+                const int i = im.fi[x] + row_i, b = im.fb[x] + row_b;
                 real = real && b < p.batch && i < (PREFIX ? attend_q_len(p, min(b, p.batch - 1)) : im.ql);
             }
-            const int t = PREFIX || !real ? 0 : im.t + im.first_i(x) + row_i;
+            const int t = PREFIX || !real ? 0 : im.t + im.fi[x] + row_i;
             float m = 0.f;
             f32x2 l2 = 0ull;
             bool started = false, known = true;           // known: all rows have references
@@ -586,7 +584,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             l = half ? sm_row[0][x][row] + l : l + sm_row[1][x][row];
             no += started ? 1 : 0;
             const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-            const int g = row_g, i = im.first_i(x) + row_i, b = im.first_b(x) + row_b;
+            const int g = row_g, i = im.fi[x] + row_i, b = im.fb[x] + row_b;
             const long long R = (((long long)b * p.kv_heads + im.h) * p.n_q + i) * p.G + g;
             const bool last = p.slots == 1;
             const long long at = (long long)(PREFIX ? im.part : p.p_slots + im.part) * p.rows_total + R;

@@ -114,12 +114,16 @@ static TcTiles tc_tiles(int G, int n_q, int batch, int kv_heads, bool prefix)
     TcTiles t;
     t.ti = AT_TILE / G < n_q ? AT_TILE / G : n_q;
     t.nb = 1;
-    if (prefix && t.ti == n_q) {
-        t.nb = AT_TILE / (G * n_q) < batch ? AT_TILE / (G * n_q) : batch;
-        t.pairs = (long long)kv_heads * ((batch + 2 * t.nb - 1) / (2 * t.nb));
-    } else {
-        t.pairs = (long long)kv_heads * batch * ((n_q + 2 * t.ti - 1) / (2 * t.ti));
+    t.pairs = (long long)kv_heads * batch * ((n_q + 2 * t.ti - 1) / (2 * t.ti));
+    if (!prefix) return t;
+    // 8 sequences of 40 queries x 4 heads: 10 full tiles of 8 queries of 4 sequences, not 16 of a sequence's 32 or 8 queries
+    long long fewest = LLONG_MAX;
+    for (int ti = t.ti; ti >= 1; --ti) {
+        const int nb = AT_TILE / (G * ti) < batch ? AT_TILE / (G * ti) : batch;
+        const long long tiles = (long long)((n_q + ti - 1) / ti) * ((batch + nb - 1) / nb);
+        if (tiles < fewest) { fewest = tiles; t.ti = ti; t.nb = nb; }
     }
+    t.pairs = kv_heads * ((fewest + 1) / 2);
     return t;
 }
 
