@@ -5,8 +5,9 @@
 // swizzled by the row so that matrix loads meet every bank once), so warps never wait for one another before the end.  Keys lie
 // on the M side of the 16 x 8 x 16 products: S^T = K Q^T and O^T += V^T P^T waste nothing for groups of up to eight rows, where
 // queries on the M side would leave half of every product empty.  Two blocks share a multiprocessor: 128 KB
-// and more of reads in flight; 4 sequences of 131072 keys 282 us (6.7 TB/s), 32 of up to 8192 with a window of 4096 74 us (6.1 TB/s).  Up to eight parts are a cluster, which joins them through shared memory: one launch, nothing in the
-// workspace.
+// and more of reads in flight; 4 sequences of up to 131072 keys 287 us (6.6 TB/s), 32 of up to 8192 with a window of 4096 75 us
+// (5.95 TB/s).  Up to eight parts are a cluster, which joins them through shared memory and forms the masses of its own keys: one
+// launch (one token over 1000 keys: 3.8 us on the device).
 //
 // Softmax: a row's reference is its maximum at the time it was last raised; it is raised (and O and the sum rescaled) only when
 // a logit exceeds it by more than 8 in the log2 domain, so weights stay below 2^8 and the common step has no shuffles.  Weights

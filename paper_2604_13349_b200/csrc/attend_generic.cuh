@@ -4,8 +4,10 @@
 // A block owns 64 query rows of a KV head and a part of their keys, in tiles of 64: logits as 4 x 4 register tiles of dot
 // products (tile_dots), a running maximum and sum per row, the weights over the tile of keys in shared memory, and 4 rows x D / 16
 // channels of the output per thread, two channels per multiply-add.  All in fp32.  Bound by the multiply-adds and the shared-memory
-// reads that feed them: 32 TFLOP/s on a causal fp32 prompt of 4096 with heads of 64 channels (28 before the next tile was copied
-// ahead), 21 with a window of 300, where half of every tile is masked and 512 blocks make two rounds of 296.
+// reads that feed them (a 16-byte read costs four cycles of the shared-memory path also where the lanes read the same): 32 TFLOP/s on
+// a causal fp32 prompt of 4096 with heads of 64 channels (28 before the next tile was copied ahead), 21 with a window of 300, where 512
+// blocks of five tiles each make two rounds of 296.  8 x 2 and 8 x 4 logits per thread measured 30 and 29: the one reads as much per
+// multiply-add, the other leaves half the warps to cover the latencies.
 #pragma once
 
 #include "attend_few.cuh"
