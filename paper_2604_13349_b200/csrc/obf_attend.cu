@@ -128,14 +128,17 @@ static TcTiles tc_tiles(int G, int n_q, int batch, int kv_heads, bool prefix)
 }
 
 // Parts of the keys for the persistent kernel: as many as make its last round of items (one per multiprocessor) fullest,
-// counting an item's fixed cost as that of one tile of keys.
-static int tc_parts(long long pairs, long long keys)
+// counting an item's fixed cost as that of one tile of keys, a join where there would be none (no other keys: `joined` false) as
+// two tiles, and a pair's partial results on their way there as a hundredth.  (32 heads over 8, on the device: prompt of 512 alone
+// 15.4 us in 1 part, 23.1 in 2; 4 x 64 queries over 600 keys 17.9 in 1, 19.7 in 3; 256 queries over 2048 keys 24.5 in 4.)
+static int tc_parts(long long pairs, long long keys, bool joined)
 {
     const long long tiles = (keys + AT_TILE - 1) / AT_TILE;
     int best = 1;
     double cost = 1e300;
     for (int s = 1; s <= 128 && s <= (tiles + 1) / 2; ++s) {
-        const double c = (double)((pairs * s + 147) / 148) * ((double)((tiles + s - 1) / s) + 1.0 + (s > 1 ? 0.5 : 0.0));
+        const double c = (double)((pairs * s + 147) / 148) * ((double)((tiles + s - 1) / s) + 1.0 + (s > 1 ? 0.5 : 0.0)) +
+                         (s > 1 && !joined ? 2.0 : 0.0) + (s > 1 || joined ? 0.01 * (double)(s * pairs) : 0.0);
         if (c < cost * 0.97) { cost = c; best = s; }
         if (pairs * s > 148 * 4) break;
     }
@@ -167,7 +170,7 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
             if (8 * tiles <= FEW_RESIDENT && keys <= 4096) return parts_for(1, keys, 8, 64);
             return few_parts(tiles, keys, a->dtype == OBF_F32 ? 2 * FEW_RESIDENT : FEW_RESIDENT);
         }
-        if (path == ATTEND_TC) return tc_parts(tc_tiles((int)(a->q_heads / a->kv_heads), a->n_q, a->batch, a->kv_heads, rows_run != rows_seq).pairs, keys);
+        if (path == ATTEND_TC) return tc_parts(tc_tiles((int)(a->q_heads / a->kv_heads), a->n_q, a->batch, a->kv_heads, rows_run != rows_seq).pairs, keys, x != nullptr);
         return parts_for(runs * ((rows_run + AG_TILE - 1) / AG_TILE), keys, 2 * 148, 4 * AG_TILE);
     };
     L.own_path = path_for(a, rows_seq);
