@@ -1,0 +1,144 @@
+"""Forms of the attention over a relayed cache that come with the size of a call: blocks that work through several items, keys in one
+part, in more parts than a cluster takes or a warp has lanes, with masses and without; references that have to follow the logits."""
+import pytest
+import torch
+
+import paper_2604_13349_b200 as P
+from tests import _attend_ref as ref
+from tests.test_attend import BF16, F32, GENERIC, _attend_case, _check
+
+MULTIPROCESSORS = 148
+
+
+def _workspace(B, kv, G, d, n_q, cap, dtype, window=0, sinks=0, mass=False, prefix_rows=0):
+    q, k = torch.empty(B, kv * G, n_q, d, dtype=dtype, device="meta"), torch.empty(B, kv, cap, d, dtype=dtype, device="meta")
+    return P.attend_workspace(q, k, window=window, sinks=sinks, mass=mass, prefix_rows=prefix_rows).numel()
+
+
+def _parts(B, kv, G, d, n_q, cap, dtype, **kw):
+    """All parts of a row of a call whose parts are joined by a kernel of their own; 0: no such join.  (A part leaves d + 1 fp32 words per
+    row, a mass call a logit per row and key; sections are aligned to 256 bytes.)"""
+    rows = B * kv * G * n_q
+    size = _workspace(B, kv, G, d, n_q, cap, dtype, **kw) - 256
+    if kw.get("mass"):
+        size -= (rows * cap * 4 + 255) // 256 * 256
+    return size // (rows * (d + 1) * 4)
+
+
+# ---- blocks of the tensor-core kernel that work through more than one item ------------------------------------------------------
+
+
+def _ragged(n_q, cap):
+    q_lens = [n_q if b % 4 == 0 else 0 if b % 4 == 1 else (b * 7) % n_q + 1 if b % 4 == 2 else 1 + b // 4 for b in range(24)]
+    lens = [cap - 5 * b if b % 3 else max(q_lens[b] - b % 2, 1) for b in range(24)]
+    return lens, q_lens
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q,cap,window,sinks", [
+    (130, 200, 0, 0),                # three pairs of tiles per (sequence, head): 576 items for 148 blocks, many of them without queries
+    (130, 333, 70, 3),
+    (65, 260, 40, 90),               # the second tile of a pair empty or of one query, more sinks than the window
+])
+def test_blocks_work_through_many_items(d, n_q, cap, window, sinks):
+    lens, q_lens = _ragged(n_q, cap)
+    _attend_case(24, 8, 4, d, n_q, cap, lens, q_lens, BF16, window, sinks, seed=n_q + cap, token_major=window == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_blocks_work_through_many_items_of_parts(d):
+    # two parts of the keys and more; of the short sequences' keys the later parts hold nothing
+    B, kv, G, n_q, cap = 18, 5, 4, 40, 4111
+    assert _parts(B, kv, G, d, n_q, cap, BF16) >= 2 and B * kv * _parts(B, kv, G, d, n_q, cap, BF16) > MULTIPROCESSORS
+    lens = [cap if b % 5 == 0 else 40 + 9 * b if b % 5 < 3 else cap // 2 for b in range(B)]
+    _attend_case(B, kv, G, d, n_q, cap, lens, [n_q if b % 3 else b for b in range(B)], BF16, seed=7)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q,rows", [(130, 200), (9, 900)])
+def test_blocks_work_through_many_items_of_a_shared_prefix(d, n_q, rows):
+    # 49 pairs of tiles per KV head, and 4 of them in several parts
+    lens, q_lens = _ragged(n_q, 150)
+    _attend_case(24, 8, 4, d, n_q, 150, lens, q_lens, BF16, prefix_rows=rows, seed=rows)
+
+
+# ---- few query rows: parts ---------------------------------------------------------------------------------------------------------
+TYPES = [pytest.param(BF16, id="bf16"), pytest.param(F32, id="f32")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,flags", [pytest.param(BF16, 0, id="bf16"), pytest.param(BF16, GENERIC, id="bf16-generic"), pytest.param(F32, 0, id="f32")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n_q,cap,lens,window,sinks", [
+    (1, 1, 1, [1, 0], 0, 0),
+    (4, 1, 700, [700, 3], 100, 4),
+    (3, 1, 1300, [1300, 1025], 1000, 77),
+    (8, 2, 257, [257, 255], 50, 51),
+    (7, 2, 400, [399, 1], 16, 1),
+    (16, 1, 130, [130, 17], 0, 0),
+])
+def test_few_queries_without_masses(dtype, flags, d, G, n_q, cap, lens, window, sinks):
+    _attend_case(2, 2, G, d, n_q, cap, lens, [min(n_q, n) for n in lens], dtype, window, sinks, flags=flags, seed=cap)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n_q,window,sinks", [(4, 1, 0, 0), (4, 1, 300, 4), (3, 3, 77, 90), (8, 2, 0, 0)])
+def test_few_queries_in_one_part(dtype, d, G, n_q, window, sinks):
+    B, kv, cap = 80, 8, 500
+    assert _workspace(B, kv, G, d, n_q, cap, dtype, window=window, sinks=sinks) == 256                # the blocks store the rows themselves
+    _attend_case(B, kv, G, d, n_q, cap, [cap - 6 * b for b in range(B)], [n_q if b % 7 else b % 2 for b in range(B)], dtype, window, sinks, seed=G)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mass", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,kv,cap,lens,window,sinks,least", [
+    (1, 1, 5000, [4999], 0, 0, 9),                                     # more parts than a cluster has
+    (3, 1, 5200, [5200, 300, 1], 4700, 4, 9),                          # and most of them empty
+    (1, 1, 70001, [70001], 0, 0, 33),                                  # more than a warp's lanes join at once
+    (2, 1, 40000, [39000, 20], 30011, 200, 33),
+])
+def test_few_queries_in_many_parts(mass, dtype, d, B, kv, cap, lens, window, sinks, least):
+    assert _parts(B, kv, 4, d, 1, cap, dtype, window=window, sinks=sinks, mass=mass) >= least
+    _attend_case(B, kv, 4, d, 1, cap, lens, [1] * B, dtype, window, sinks, mass=mass, decay=0.5, seed=cap)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mass", [False, True])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_queries_joined_a_warp_per_row(mass, dtype, d):
+    # rows enough for a warp each, in two parts and more
+    B, kv, G, n_q, cap = 20, 4, 4, 2, 6000
+    assert _parts(B, kv, G, d, n_q, cap, dtype, mass=mass) >= 2
+    _attend_case(B, kv, G, d, n_q, cap, [cap - 290 * b for b in range(B)], [n_q if b % 6 else 1 for b in range(B)], dtype, mass=mass, decay=0.9, seed=6)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,G,n_q,cap,lens,rows", [
+    (3, 4, 1, 40, [40, 0, 17], 5000),                                  # few rows over the prefix, too
+    (2, 2, 4, 30, [30, 3], 4100),
+    (1, 8, 2, 70, [70], 9001),
+    (4, 1, 1, 4500, [4500, 2, 0, 4097], 130),
+    (2, 3, 1, 9, [9, 1], 66000),
+    (40, 4, 1, 300, [300 - 7 * b for b in range(40)], 2500),           # many over the prefix, few of each sequence
+])
+def test_few_queries_over_a_long_shared_prefix(dtype, d, B, G, n_q, cap, lens, rows):
+    assert _parts(B, 2, G, d, n_q, cap, dtype, prefix_rows=rows) >= 2
+    _attend_case(B, 2, G, d, n_q, cap, lens, [n_q] * B, dtype, prefix_rows=rows, seed=rows)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B", [4, 5, 8])
+def test_few_queries_on_either_side_of_one_launch(dtype, B):
+    # a prefix that each sequence's blocks read by themselves, or that is read once and joined
+    _attend_case(B, 8, 4, 128, 1, 40, [40 - 5 * b for b in range(B)], [1] * B, dtype, prefix_rows=1012, seed=B)
