@@ -338,8 +338,9 @@ obf_status_t obf_static_scratch_status(void *stream, uint32_t *device_status);
  *
  * Numerics: products of the inputs accumulated in fp32, softmax in fp32; on the tensor cores the weights of a row, at most
  * one, are rounded to bf16 before they multiply the values (their sum is not), out is rounded once.  Weights are kept
- * relative to a reference that may be off a row's maximum by factors of up to 2^32 or 2^-47: values beyond 2^90 may
- * overflow in sums that would not, and of values below 2^-60 precision may be lost.  A sequence's result does not depend
+ * relative to a reference that may be off a row's maximum by factors of up to 2^32 or 2^-47: values beyond 2^90, or beyond
+ * 2^100 divided by the number of keys that a query sees, may overflow in sums that would not, and of values below 2^-60
+ * precision may be lost.  A sequence's result does not depend
  * on what else the batch holds except through the batch's sizes - over a shared prefix, where rows of several sequences
  * are worked on together, only in its rounding - and is the same in every run.
  */

@@ -14,9 +14,10 @@
 //
 // Softmax: fp32 and bf16 have the same exponents, so a row's reference need not be its maximum, only near enough for no weight
 // to leave fp32's range.  It starts as zero, and the logits are read once, without a search for their maximum before.  Only when
-// a weight comes out above 2^32, or those of a row's first tile add up to less than 2^-40 (logits beyond some 22 or -28; rows that
+// 64 weights add up to more than 2^32, or those of a row's first tile to less than 2^-40 (logits beyond some 18 to 22, or -28; rows that
 // see nothing of that tile), is the tile done again against the rows' maxima, O and the sums rescaled - in place: the products
-// before have completed, since they were issued before the logits that the thread has waited for.
+// before have completed, since they were issued before the logits that the thread has waited for.  n keys' weights add up to less
+// than 2^26 (n + 128), so values of up to 2^90, and of up to 2^100 / n, overflow nothing.
 // Tensor memory: S (P) and O of the two tiles, 512 columns.  Every wait is bounded.
 //
 // Rows of V past the last key may hold anything, and 0 * NaN is not 0: the product over a short tile runs over its keys rounded
@@ -35,7 +36,10 @@ namespace obf {
 
 constexpr int AT_TILE = 128;
 constexpr int AT_THREADS = 640;
-constexpr float AT_RAISE = 32.f, AT_WEIGHT_MAX = 4294967296.f, AT_WEIGHT_MIN = 9.094947017729282e-13f;     // 2^32, 2^-40
+// A thread's 64 weights of a tile may add up to 2^32 (those of an item's first tile have to reach 2^-40).  More than that takes a logit
+// of more than 26 above the reference (log2), so a tile turned down for it raises the reference, whose margin of 25 leaves room for the
+// rounding of the sum.
+constexpr float AT_RAISE = 25.f, AT_WEIGHT_MAX = 4294967296.f, AT_WEIGHT_MIN = 9.094947017729282e-13f;     // 2^32, 2^-40
 
 template <int D>
 struct AttendTcShape {
@@ -483,7 +487,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                             w[16 * c + e] = pack_bf16(a, b2);
                         }
                     }
-                    // No weight may be above 2^32 of the reference, and those of an item's first tile add up to something; a logit
+                    // The weights may not add up to more than 2^32, and those of an item's first tile add up to something; a logit
                     // that is not a number sends the tile the other way, too, where it spreads.  (What lies behind a sequence's queries has
                     // no say in it: results do not depend on that.)
                     const float zs = sum2(z);

@@ -142,3 +142,30 @@ def test_few_queries_over_a_long_shared_prefix(dtype, d, B, G, n_q, cap, lens, r
 def test_few_queries_on_either_side_of_one_launch(dtype, B):
     # a prefix that each sequence's blocks read by themselves, or that is read once and joined
     _attend_case(B, 8, 4, 128, 1, 40, [40 - 5 * b for b in range(B)], [1] * B, dtype, prefix_rows=1012, seed=B)
+
+
+# ---- references that follow the logits ---------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (4000, 5)])
+@pytest.mark.parametrize("logit", [17.9, 19.0, 21.0, 22.5])
+@pytest.mark.parametrize("cap,power", [(1400, 89), (9000, 86)])
+def test_many_large_weights_behind_small_ones_do_not_overflow(d, window, sinks, logit, cap, power):
+    # the first tiles' logits leave every row's reference at zero; of the others, 2^25.8 to 2^32.5 above it, each alone keeps its weight
+    # within range, but not all of them together.  Values times keys stay below 2^100.
+    gen = torch.Generator().manual_seed(3)
+    n_q, kv, G = 74, 4, 128                                                         # 148 pairs of tiles: keys in one part, all rows alike
+    assert _workspace(1, kv, G, d, n_q, cap, BF16, window=window, sinks=sinks) == 256
+    u = torch.full((d,), 1 / 8 if d == 64 else 1 / 16)
+    level = torch.zeros(cap)
+    level[300:] = logit * (1 if d == 64 else 2)
+    q = u.expand(1, 1, n_q, d).to(BF16)
+    k = (level[:, None] * u).expand(1, 1, cap, d).to(BF16)
+    v = ((1 + 0.25 * torch.rand(1, 1, cap, d, generator=gen)) * 2.0 ** (power - 1)).to(BF16)
+    want = ref.attend(q, k, v, [cap], [n_q], window, sinks, 1.0)
+    got = P.attend(q.repeat(1, kv * G, 1, 1).cuda(), k.repeat(1, kv, 1, 1).cuda(), v.repeat(1, kv, 1, 1).cuda(), window=window, sinks=sinks, scale=1.0,
+                   want_lse=True)
+    for h in (0, 1, kv * G // 2, kv * G - 1):
+        _check(got["out"][:, h:h + 1], want[0], want[1], "out")
+        _check(got["lse"][:, h:h + 1], want[2], want[3], "lse")
+    assert torch.equal(got["out"], got["out"][:, :1].expand_as(got["out"])) and torch.equal(got["lse"], got["lse"][:, :1].expand_as(got["lse"]))
