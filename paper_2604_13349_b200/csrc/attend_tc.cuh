@@ -559,7 +559,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     const bool tail = width & 15, late_v = tail && !tc::mbar_wait(&bar_full[slot_v], (nv / SLOTS) & 1u, wc);
                     // (where every row has a reference from now on, the straight path takes over)
                     known = !any(m == -INFINITY || late_v);
-                    if (tail && any(late_v)) { dead = true; break; }
+                    if (tail && any(late_v)) {
+                        tc::tmem_st_wait();               // (O may be on its way back)
+                        dead = true;
+                        break;
+                    }
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
                         if (c < nch) tmem_st16(s_t + col0 + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
