@@ -115,7 +115,9 @@ typedef enum { OBF_F32 = 0, OBF_BF16 = 1 } obf_dtype_t;
                                       status word carries OBF_DEV_TIMEOUT and the outputs hold valid positions but no
                                       meaningful selection.  Accepted only for at most 4 (layer, KV head) pairs in all,
                                       every T <= 2048, on the tuned bf16 path; else
-                                      OBF_ERR_INVALID_ARG                                                         */
+                                      OBF_ERR_INVALID_ARG.  In obf_attend, for that of the tensor-core kernel: no block
+                                      fetches the values of its first tile of keys, out and lse hold anything; for
+                                      batch * kv_heads <= 4 and n_q, capacity <= 2048, where that kernel is used  */
 
 #define OBF_MAX_CACHES 32          /* caches per call                                              */
 #define OBF_MAX_T (1 << 20)        /* prompt positions per cache                                   */
@@ -354,7 +356,8 @@ typedef struct {
     int32_t dtype;                      /* obf_dtype_t of q, k, v, out                                           */
     float scale;                        /* factor of the logits, > 0; 0: 1 / sqrt(head_dim)                      */
     float decay;                        /* >= 0; factor of mass_in                                               */
-    uint32_t flags;                     /* 0 or OBF_FLAG_GENERIC_PATH (CUDA-core kernels where the tensor cores apply) */
+    uint32_t flags;                     /* 0, OBF_FLAG_GENERIC_PATH (CUDA-core kernels where the tensor cores apply) or
+                                           OBF_FLAG_TEST_WAIT_EXPIRES                                            */
     const void *q, *k, *v;              /* device, 16-byte aligned                                               */
     void *out;                          /* [batch, q_heads, n_q, head_dim], must not overlap the inputs          */
     int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];

@@ -39,6 +39,7 @@ struct AttendDev {
     float *part_lse;          // [slots, rows_total], log2 domain, -inf: no keys (part_o is not written then)
     float *logits;            // [rows_total, capacity] when masses are asked for, visible keys only
     unsigned long long wait_limit_ns;
+    int32_t debug_drop_load;  // OBF_FLAG_TEST_WAIT_EXPIRES
 };
 
 __device__ __forceinline__ int attend_len(const AttendDev &p, int b)

@@ -278,6 +278,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     for (int kv = 0; kv < 2; ++kv, ++n) {
                         const uint32_t sl = n % SLOTS;
                         if (!tc::mbar_wait(&bar_empty[sl], ((n / SLOTS) & 1u) ^ 1u, wc)) { dead = true; break; }
+                        if (p.debug_drop_load && n == 1u) continue;                       // the first values never come
                         tc::mbar_expect_tx(&bar_full[sl], SLOT_BYTES);
                         const uint32_t dst = tc::smem_u32(ring + sl * SLOT_BYTES);
                         const int b = PREFIX ? 0 : it.b, j0 = j * AT_TILE;

@@ -27,7 +27,7 @@ static obf_status_t validate_attend(const obf_attend_t *a, const obf_prefix_t *x
     if (a->n_q < 1 || a->n_q > OBF_MAX_T || a->capacity < 1 || a->capacity > OBF_MAX_T) return OBF_ERR_INVALID_ARG;
     if (a->window < 0 || a->sinks < 0) return OBF_ERR_INVALID_ARG;
     if (!(a->scale >= 0.f) || !std::isfinite(a->scale) || !(a->decay >= 0.f) || !std::isfinite(a->decay)) return OBF_ERR_INVALID_ARG;
-    if (a->flags & ~(uint32_t)OBF_FLAG_GENERIC_PATH) return OBF_ERR_INVALID_ARG;
+    if (a->flags & ~(uint32_t)(OBF_FLAG_GENERIC_PATH | OBF_FLAG_TEST_WAIT_EXPIRES)) return OBF_ERR_INVALID_ARG;
     if (a->head_dim != 64 && a->head_dim != 128) return OBF_ERR_UNSUPPORTED;
     if (a->dtype != OBF_F32 && a->dtype != OBF_BF16) return OBF_ERR_UNSUPPORTED;
     if ((long long)a->batch * a->q_heads > (1 << 24) || (long long)a->batch * a->q_heads * a->n_q > 1ll << 30) return OBF_ERR_UNSUPPORTED;
@@ -156,6 +156,13 @@ static int few_parts(long long tiles, long long keys, int resident)
         if (c < cost) { cost = c; best = s; }
     }
     return (int)best;
+}
+
+// Whether the call may ask for waits that run out: small ones that the tensor-core kernel works on.
+static bool may_expire(const obf_attend_t *a, const obf_prefix_t *x)
+{
+    const long long rows = (long long)(a->q_heads / a->kv_heads) * a->n_q;
+    return !x && path_for(a, rows) == ATTEND_TC && (long long)a->batch * a->kv_heads <= 4 && a->n_q <= 2048 && a->capacity <= 2048;
 }
 
 static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
@@ -367,6 +374,7 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *w
     g_last_launches = 0;
     OBF_TRY(validate_attend(a, x));
     OBF_TRY(validate_attend_pointers(a, x));
+    if ((a->flags & OBF_FLAG_TEST_WAIT_EXPIRES) && !may_expire(a, x)) return OBF_ERR_INVALID_ARG;
     const AttendLayout L = attend_layout(a, x);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < L.total) return OBF_ERR_WORKSPACE;
     AttendDev p = {};
@@ -380,6 +388,10 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *w
     p.lens = a->lens; p.q_lens = a->q_lens; p.lse_out = a->lse_out; p.mass_in = a->mass_in; p.mass_out = a->mass_out;
     p.decay = a->decay;
     p.wait_limit_ns = tc::WAIT_LIMIT_NS;
+    if (a->flags & OBF_FLAG_TEST_WAIT_EXPIRES) {
+        p.wait_limit_ns = 20000000ull;
+        p.debug_drop_load = 1;
+    }
     p.c = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f;
     p.batch = a->batch; p.kv_heads = a->kv_heads; p.G = a->q_heads / a->kv_heads; p.n_q = a->n_q; p.capacity = a->capacity;
     // beyond any position a window or a number of first tokens changes nothing; clamped, positions minus windows cannot overflow
@@ -428,6 +440,7 @@ obf_status_t obf_attend_workspace_bytes(const obf_attend_t *args, const obf_pref
 {
     if (!bytes) return OBF_ERR_INVALID_ARG;
     OBF_TRY(validate_attend(args, prefix));
+    if ((args->flags & OBF_FLAG_TEST_WAIT_EXPIRES) && !may_expire(args, prefix)) return OBF_ERR_INVALID_ARG;
     *bytes = attend_layout(args, prefix).total;
     return OBF_OK;
 }
