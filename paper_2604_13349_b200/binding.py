@@ -464,8 +464,8 @@ def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, strea
             with _allocating(stream, q.device):
                 workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     else:
-        if workspace.device != q.device:
-            raise ValueError("workspace: on %s expected" % q.device)
+        if workspace.device != q.device or not workspace.is_contiguous():
+            raise ValueError("workspace: contiguous memory on %s expected" % q.device)
         size = workspace.numel() * workspace.element_size()
     call = (args, workspace.data_ptr(), size) if prefix is None else (args, prefix, workspace.data_ptr(), size)
     _enqueue(name, q.get_device(), call, stream)
