@@ -445,14 +445,14 @@ def _enqueue(name: str, device: int, args, stream) -> None:
         raise ObfError(rc, name)
 
 
-def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, stream):
+def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, want_status, stream):
     if workspace is None:
         nb = ctypes.c_size_t(0)
         rc = _packed("obf_attend_workspace_bytes")(args, prefix, ctypes.addressof(nb))
         if rc != OBF_OK:
             raise ObfError(rc, name)
         size = nb.value
-        if size <= _STATUS_ONLY:                 # a status word that nobody asks for: one per device does for all
+        if size <= _STATUS_ONLY and not want_status:                # a status word that nobody asks for: one per device does for all
             workspace = _status_words.get(q.get_device())
             if workspace is None:
                 workspace = torch.zeros(_STATUS_ONLY, dtype=torch.uint8, device=q.device)
@@ -474,6 +474,8 @@ def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, strea
         got["lse"] = lse_out
     if mass_out is not None:
         got["mass"] = mass_out
+    if want_status:
+        got["workspace"] = workspace
     return got
 
 
@@ -498,25 +500,27 @@ def _attend_outputs(q, q_lens, out, lse_out, want_lse, stream):
 def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, lens: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None,
            window: int = 0, sinks: int = 0, scale: float = 0.0, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
            want_lse: bool = False, mass_in: Optional[torch.Tensor] = None, mass_out: Optional[torch.Tensor] = None, decay: float = 1.0,
-           flags: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+           flags: int = 0, workspace: Optional[torch.Tensor] = None, want_status: bool = False, stream=None) -> Dict[str, torch.Tensor]:
     """Causal attention of ``q [batch, q_heads, n_q, d]`` over caches ``k, v [batch, kv_heads, capacity, d]`` with an optional sliding
     window whose first ``sinks`` keys stay visible (``obf_attend`` in include/obf.h).
 
     ``lens``, ``q_lens``: int32 device tensors ``[batch]``, the rows of a sequence's cache and its queries that count (None: all);
     the queries are the last tokens of the cache.  Any strides with contiguous channels.  ``mass_out [batch, kv_heads, capacity]``
     (fp32) receives ``decay * mass_in`` plus the attention mass of every key; it may be ``mass_in``.  ``workspace``: one that
-    ``attend_workspace`` made for these shapes, whose status word ``obf_last_device_status`` reads afterwards; else one is
-    allocated for the call.  Returns ``out`` and, where asked for, ``lse [batch, q_heads, n_q]`` (natural log) and ``mass``.
+    ``attend_workspace`` made for these shapes; else one is allocated for the call.  Returns ``out`` and, where asked for,
+    ``lse [batch, q_heads, n_q]`` (natural log), ``mass`` and, with ``want_status``, the call's ``workspace``:
+    ``obf_last_device_status`` waits for the stream and reads there whether a length was out of range (``OBF_DEV_INTERNAL``) or a
+    wait on the device ran out (``OBF_DEV_TIMEOUT``: the results are not to be used).  Without it nothing reports either.
     """
     out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
     args = _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags)
-    return _attend_call("obf_attend", args, None, q, out, lse_out, mass_out, workspace, stream)
+    return _attend_call("obf_attend", args, None, q, out, lse_out, mass_out, workspace, want_status, stream)
 
 
 def attend_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *,
                   lens: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None, scale: float = 0.0,
                   out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, want_lse: bool = False, flags: int = 0,
-                  workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+                  workspace: Optional[torch.Tensor] = None, want_status: bool = False, stream=None) -> Dict[str, torch.Tensor]:
     """The same for a batch whose sequences all see ``k_prefix, v_prefix [kv_heads, rows, d]`` before their own keys
     (``obf_attend_shared``): the prefix is read once for all of them."""
     out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
@@ -527,7 +531,7 @@ def attend_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tenso
     shape = (k.shape[1], rows, q.shape[3])
     sk, sv = _rows(k_prefix, shape, q.dtype, q.get_device(), "k_prefix"), _rows(v_prefix, shape, q.dtype, q.get_device(), "v_prefix")
     prefix = _PREFIX.pack(k_prefix.data_ptr(), v_prefix.data_ptr(), sk[0], sk[1], sv[0], sv[1], rows)
-    return _attend_call("obf_attend_shared", args, prefix, q, out, lse_out, None, workspace, stream)
+    return _attend_call("obf_attend_shared", args, prefix, q, out, lse_out, None, workspace, want_status, stream)
 
 
 def attend_workspace(q: torch.Tensor, k: torch.Tensor, *, window: int = 0, sinks: int = 0, mass: bool = False, prefix_rows: int = 0,
