@@ -408,6 +408,10 @@ def _dense(t: Optional[torch.Tensor], shape, dtype, device: int, name: str) -> i
     return t.data_ptr()
 
 
+def _refuse_graph(name: str) -> None:
+    raise ValueError("%s has no gradients: call it under torch.no_grad() or with detached tensors" % name)
+
+
 def _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags) -> bytes:
     dt, dev = q.dtype, q.get_device()
     code = OBF_BF16 if dt is _BF16 else OBF_F32 if dt is _F32 else -1
@@ -510,8 +514,11 @@ def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, lens: Optional[
     ``attend_workspace`` made for these shapes; else one is allocated for the call.  Returns ``out`` and, where asked for,
     ``lse [batch, q_heads, n_q]`` (natural log), ``mass`` and, with ``want_status``, the call's ``workspace``:
     ``obf_last_device_status`` waits for the stream and reads there whether a length was out of range (``OBF_DEV_INTERNAL``) or a
-    wait on the device ran out (``OBF_DEV_TIMEOUT``: the results are not to be used).  Without it nothing reports either.
+    wait on the device ran out (``OBF_DEV_TIMEOUT``: the results are not to be used).  Without it nothing reports either.  There are
+    no gradients: where autograd records, tensors that require one are refused.
     """
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or (mass_in is not None and mass_in.requires_grad)):
+        _refuse_graph("attend")
     out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
     args = _attend_args(q, k, v, lens, q_lens, window, sinks, scale, out, lse_out, mass_in, mass_out, decay, flags)
     return _attend_call("obf_attend", args, None, q, out, lse_out, mass_out, workspace, want_status, stream)
@@ -523,6 +530,8 @@ def attend_shared(q: torch.Tensor, k_prefix: torch.Tensor, v_prefix: torch.Tenso
                   workspace: Optional[torch.Tensor] = None, want_status: bool = False, stream=None) -> Dict[str, torch.Tensor]:
     """The same for a batch whose sequences all see ``k_prefix, v_prefix [kv_heads, rows, d]`` before their own keys
     (``obf_attend_shared``): the prefix is read once for all of them."""
+    if torch.is_grad_enabled() and (q.requires_grad or k_prefix.requires_grad or v_prefix.requires_grad or k.requires_grad or v.requires_grad):
+        _refuse_graph("attend_shared")
     out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
     args = _attend_args(q, k, v, lens, q_lens, 0, 0, scale, out, lse_out, None, None, 1.0, flags)
     if k_prefix.dim() != 3:
@@ -564,6 +573,8 @@ def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: in
     ``[batch, kv_heads, capacity]``: the first ``sinks``, the last ``recent`` and the heaviest others, in ascending order
     (``obf_evict_by_mass`` in include/obf.h).  ``k_out, v_out`` and ``mass_out`` may have more rows than ``keep``: the cache goes on
     there.  Returns ``K_out, V_out, idx, mass, lens``."""
+    if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or mass.requires_grad):
+        _refuse_graph("evict_by_mass")
     dt, dev, at = k.dtype, k.device, k.get_device()
     code = OBF_BF16 if dt is _BF16 else OBF_F32 if dt is _F32 else -1
     shape = k.shape

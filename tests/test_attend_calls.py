@@ -7,6 +7,38 @@ from paper_2604_13349_b200 import binding
 from tests.test_attend import _small
 
 
+def _calls(q, k, v, m):
+    return {"q": lambda x: P.attend(x(q), k, v), "k": lambda x: P.attend(q, x(k), v), "v": lambda x: P.attend(q, k, x(v)),
+            "mass_in": lambda x: P.attend(q, k, v, mass_in=x(m), mass_out=torch.zeros_like(m)),
+            "shared q": lambda x: P.attend_shared(x(q), k[0], v[0], k, v), "k_prefix": lambda x: P.attend_shared(q, x(k[0]), v[0], k, v),
+            "v_prefix": lambda x: P.attend_shared(q, k[0], x(v[0]), k, v), "shared k": lambda x: P.attend_shared(q, k[0], v[0], x(k), v),
+            "shared v": lambda x: P.attend_shared(q, k[0], v[0], k, x(v)), "evicted k": lambda x: P.evict_by_mass(x(k), v, m, 10),
+            "evicted v": lambda x: P.evict_by_mass(k, x(v), m, 10), "mass": lambda x: P.evict_by_mass(k, v, x(m), 10)}
+
+
+def _leaf(t):
+    return t.detach().clone().requires_grad_()
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    # (before anything else is looked at: nothing reaches a device)
+    for name, call in _calls(torch.zeros(1, 4, 1, 64), torch.zeros(1, 2, 30, 64), torch.zeros(1, 2, 30, 64), torch.zeros(1, 2, 30)).items():
+        with pytest.raises(ValueError, match="gradient"):
+            call(_leaf)
+            pytest.fail(name)
+
+
+@pytest.mark.gpu
+def test_without_a_graph_they_are_taken():
+    q, k, v = _small(cap=100)
+    for call in _calls(q, k, v, torch.rand(2, 2, 100, device="cuda")).values():
+        want = call(lambda t: t)
+        for mode in (torch.no_grad, torch.inference_mode):
+            with mode():
+                got = call(_leaf)
+            assert all(torch.equal(got[n], want[n]) for n in want)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n_q", [1, 40])
 def test_a_workspace_that_is_not_memory_of_its_own_is_refused(n_q):
