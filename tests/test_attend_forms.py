@@ -169,3 +169,87 @@ def test_many_large_weights_behind_small_ones_do_not_overflow(d, window, sinks, 
         _check(got["out"][:, h:h + 1], want[0], want[1], "out")
         _check(got["lse"][:, h:h + 1], want[2], want[3], "lse")
     assert torch.equal(got["out"], got["out"][:, :1].expand_as(got["out"])) and torch.equal(got["lse"], got["lse"][:, :1].expand_as(got["lse"]))
+
+
+# ---- layouts, and calls captured together ---------------------------------------------------------------------------------------------
+def _token_major(t):
+    """The same [.., heads, rows, d] values, laid out row by row with a gap of eight channels behind each."""
+    x = torch.zeros(*t.shape[:-3], t.shape[-2], t.shape[-3], t.shape[-1] + 8, dtype=t.dtype, device="cuda")[..., : t.shape[-1]].transpose(-3, -2)
+    return x.copy_(t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,flags", [pytest.param(BF16, 0, id="bf16"), pytest.param(BF16, GENERIC, id="bf16-generic"), pytest.param(F32, 0, id="f32")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,n_q,rows", [(2, 1, 200), (3, 1, 5000), (2, 40, 300), (40, 1, 600)])
+def test_strided_caches_prefixes_and_outputs(dtype, flags, d, B, n_q, rows):
+    gen = torch.Generator().manual_seed(B + rows)
+    kv, G, cap = 3, 2, 150
+    q, k, v = torch.randn(B, kv * G, n_q, d, generator=gen).to(dtype), *(torch.randn(B, kv, cap, d, generator=gen).to(dtype) for _ in range(2))
+    pk, pv = (torch.randn(kv, rows, d, generator=gen).to(dtype) for _ in range(2))
+    lens = [cap - b for b in range(B)]
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    qd, kd, vd, pkd, pvd = (_token_major(x) for x in (q, k, v, pk, pv))
+    out = _token_major(torch.zeros_like(q))
+    got = P.attend_shared(qd, pkd, pvd, kd, vd, lens=n, out=out, flags=flags)
+    w = ref.attend(q, k, v, lens, [n_q] * B, prefix=(pk, pv))
+    _check(got["out"], w[0], w[1], "out over a prefix")
+    m = torch.rand(B, kv, cap, generator=gen)
+    mass = n_q * G <= 64
+    out.zero_()
+    if mass:
+        got = P.attend(qd, kd, vd, lens=n, window=60, sinks=5, out=out, mass_in=m.cuda(), mass_out=torch.zeros(B, kv, cap, device="cuda"), flags=flags)
+    else:
+        got = P.attend(qd, kd, vd, lens=n, window=60, sinks=5, out=out, flags=flags)
+    w = ref.attend(q, k, v, lens, [n_q] * B, 60, 5, mass_in=m if mass else None, want_mass=mass)
+    _check(got["out"], w[0], w[1], "out")
+    if mass:
+        _check(got["mass"], w[4], w[5], "mass")
+    kept = P.evict_by_mass(kd, vd, m.cuda(), 40, lens=n, sinks=2, recent=5, k_out=_token_major(torch.zeros(B, kv, 50, d, dtype=dtype)),
+                           v_out=_token_major(torch.zeros(B, kv, 45, d, dtype=dtype)))
+    want = ref.evict(m, lens, 40, 2, 5)
+    for b in range(0, B, 7):
+        for h in range(kv):
+            assert kept["idx"][b, h].tolist() == want[b][h]
+            assert torch.equal(kept["K_out"][b, h, :40].cpu(), k[b, h, want[b][h]]) and torch.equal(kept["V_out"][b, h, :40].cpu(), v[b, h, want[b][h]])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,cap,rows", [(2, 300, 400), (3, 600, 5000), (40, 300, 700), (2, 17000, 300)])
+def test_a_captured_chain_follows_the_lengths(dtype, B, cap, rows):
+    # over a prefix, with masses, evicted by them, over what was kept; the library's kernels one behind the other, each started early
+    gen = torch.Generator().manual_seed(rows)
+    kv, G, d, keep = 2, 4, 128, 100
+    q, k, v = (torch.randn(B, h, n, d, generator=gen).to(dtype).cuda() for h, n in ((kv * G, 1), (kv, cap), (kv, cap)))
+    pk, pv = (torch.randn(kv, rows, d, generator=gen).to(dtype).cuda() for _ in range(2))
+    mass = torch.rand(B, kv, cap, generator=gen).cuda()
+    lens = torch.full((B,), cap, dtype=torch.int32, device="cuda")
+
+    def chain():
+        a = P.attend_shared(q, pk, pv, k, v, lens=lens, want_lse=True)
+        b = P.attend(a["out"], k, v, lens=lens, window=cap // 2, sinks=3, mass_in=mass, mass_out=torch.zeros_like(mass), decay=0.5)
+        e = P.evict_by_mass(k, v, b["mass"], keep, lens=lens, sinks=3, recent=9)
+        c = P.attend(b["out"], e["K_out"], e["V_out"], lens=e["lens"], want_lse=True)
+        return [a["out"], a["lse"], b["out"], b["mass"], *(e[n] for n in ("K_out", "V_out", "idx", "mass", "lens")), c["out"], c["lse"]]
+
+    chain()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = chain()
+    for shift in (0, 1, cap // 3):
+        lens.copy_(torch.tensor([max(cap - shift * (b + 1), b % 3) for b in range(B)], dtype=torch.int32))
+        for _ in range(2):
+            graph.replay()
+        torch.cuda.synchronize()
+        want = chain()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    n = lens.tolist()
+    w = ref.attend(q.cpu(), k.cpu(), v.cpu(), n, [1] * B, prefix=(pk.cpu(), pv.cpu()))
+    _check(got[0], w[0], w[1], "out over a prefix")
+    w = ref.attend(got[0].cpu(), k.cpu(), v.cpu(), n, [1] * B, cap // 2, 3, mass_in=mass.cpu(), decay=0.5, want_mass=True)
+    _check(got[2], w[0], w[1], "out")
+    _check(got[3], w[4], w[5], "mass")
+    kept = ref.evict(got[3].cpu(), n, keep, 3, 9)
+    assert all(got[6][b, h, : len(kept[b][h])].tolist() == kept[b][h] for b in range(B) for h in range(kv))
