@@ -39,6 +39,7 @@ constexpr int AT_THREADS = 640;
 // A thread's 64 weights of a tile may add up to 2^32 (those of an item's first tile have to reach 2^-40).  More than that takes a logit
 // of more than 26 above the reference (log2), so a tile turned down for it raises the reference, whose margin of 25 leaves room for the
 // rounding of the sum.
+constexpr float AT_FUSED_MAX = 4096.f;
 constexpr float AT_RAISE = 25.f, AT_WEIGHT_MAX = 4294967296.f, AT_WEIGHT_MIN = 9.094947017729282e-13f;     // 2^32, 2^-40
 
 template <int D>
@@ -520,7 +521,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     }
                     sm_row[half][x][row] = mx;
                     if (any(late)) { dead = true; break; }
-                    mx = fmaxf(mx, sm_row[half ^ 1][x][row]) * p.c;
+                    mx = __fmul_rn(fmaxf(mx, sm_row[half ^ 1][x][row]), p.c);
                     // (a maximum below the reference changes nothing)
                     if (!started) {
                         m = fmaxf(m, mx);
@@ -540,7 +541,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         }
                     }
                     const float ref = m == -INFINITY ? 0.f : -m;
-                    const f32x2 r2 = pk(ref, ref);
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         if (c >= nch) continue;
@@ -548,18 +548,19 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         load(r, c);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            float a, b2;
-                            upk(fma2(pk(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, r2), a, b2);
-                            a = ex2(a);
-                            b2 = ex2(b2);
+                            // (scaled, rounded and then subtracted, as the maximum was: of logits beyond 2^24 a fused product's exact
+                            // difference from a rounded reference may be anything.  Not mul2 and add2, which the assembler fuses.)
+                            const float a = ex2(__fadd_rn(__fmul_rn(__uint_as_float(r[2 * e]), p.c), ref));
+                            const float b2 = ex2(__fadd_rn(__fmul_rn(__uint_as_float(r[2 * e + 1]), p.c), ref));
                             l2 = add2(l2, pk(a, b2));
                             w[16 * c + e] = pack_bf16(a, b2);
                         }
                     }
                     const uint32_t nv = n + 2 * (j - jb) + 1, slot_v = nv % SLOTS;
                     const bool tail = width & 15, late_v = tail && !tc::mbar_wait(&bar_full[slot_v], (nv / SLOTS) & 1u, wc);
-                    // (where every row has a reference from now on, the straight path takes over)
-                    known = !any(m == -INFINITY || late_v);
+                    // (where every row has a reference from now on, the straight path takes over - but for references so large that its
+                    // fused products would differ from this path's rounded ones by more than weights are rounded by)
+                    known = !any((real && !(fabsf(m) <= AT_FUSED_MAX)) || late_v);
                     if (tail && any(late_v)) {
                         tc::tmem_st_wait();               // (O may be on its way back)
                         dead = true;

@@ -253,3 +253,34 @@ def test_a_captured_chain_follows_the_lengths(dtype, B, cap, rows):
     _check(got[3], w[4], w[5], "mass")
     kept = ref.evict(got[3].cpu(), n, keep, 3, 9)
     assert all(got[6][b, h, : len(kept[b][h])].tolist() == kept[b][h] for b in range(B) for h in range(kv))
+
+
+# ---- logits beyond fp32's whole numbers -------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,flags", [pytest.param(BF16, 0, id="bf16"), pytest.param(BF16, GENERIC, id="bf16-generic"), pytest.param(F32, 0, id="f32")])
+@pytest.mark.parametrize("n_q", [1, 64, 300])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("significand", [165 / 128, 219 / 128])
+@pytest.mark.parametrize("power", [10, 13, 20, 26, 30, 33, 100])
+def test_equal_logits_of_any_size_weigh_the_same(dtype, flags, n_q, sign, power, significand):
+    # the largest logit belongs to two keys in different tiles; a short significand, so the products and their sums are exact and the
+    # logits equal, though not the products with a constant; the other keys, 2^(power - 1) or more below, weigh nothing
+    gen = torch.Generator().manual_seed(power)
+    d, cap, first, second = 64, 700, 10, 500
+    u = torch.full((d,), 1 / 8)
+    top = sign * significand * 2.0 ** power
+    level = torch.full((cap,), top * (0.5 if sign > 0 else 2.0))
+    level[first] = level[second] = top
+    q = u.expand(1, 4, n_q, d).to(dtype)
+    k = (level[:, None] * u).expand(1, 2, cap, d).to(dtype)
+    v = torch.randn(1, 2, cap, d, generator=gen).to(dtype)
+    got = P.attend(q.cuda(), k.cuda(), v.cuda(), scale=1.0, want_lse=True, flags=flags)
+    t = torch.arange(cap - n_q, cap)
+    both = (t >= second)[None, None, :, None]
+    a, b = (v[:, :, j].double().repeat_interleave(2, 1)[:, :, None] for j in (first, second))
+    want = torch.where(both, (a + b) / 2, a.expand(1, 4, n_q, d))
+    # fp32 sums of one or two weights of one, one division, the output's rounding: 2^-22 of the magnitudes and half a step of the output
+    _check(got["out"], want, 2.0 ** -22 * (a.abs() + b.abs()) + ref.STEP[dtype] * want.abs() + 1e-30, "out")
+    lse = top + torch.where(both[..., 0], torch.log(torch.tensor(2.0, dtype=torch.float64)), 0.0).expand(1, 4, n_q)
+    # the scaling, the logarithm's addition and the way back to natural logarithms round once each, and so do the two constants
+    _check(got["lse"], lse, (2.0 ** -21 * lse.abs()), "lse")
