@@ -5,13 +5,14 @@
 // swizzled by the row so that matrix loads meet every bank once), so warps never wait for one another before the end.  Keys lie
 // on the M side of the 16 x 8 x 16 products: S^T = K Q^T and O^T += V^T P^T waste nothing for groups of up to eight rows, where
 // queries on the M side would leave half of every product empty.  Two blocks share a multiprocessor: 128 KB
-// and more of reads in flight; 4 sequences of up to 131072 keys 287 us (6.6 TB/s), 32 of up to 8192 with a window of 4096 75 us
-// (5.95 TB/s).  Up to eight parts are a cluster, which joins them through shared memory and forms the masses of its own keys: one
-// launch (one token over 1000 keys: 3.8 us on the device).
+// and more of reads in flight; 4 sequences of up to 131072 keys 288 us (6.6 TB/s), 32 of up to 8192 with a window of 4096 75.1 us
+// (6.0 TB/s).  Up to eight parts are a cluster, which joins them through shared memory and forms the masses of its own keys: one
+// launch (one token over 1024 keys, window of 256: 5.4 us replayed from a graph).
 //
 // Softmax: a row's reference is its maximum at the time it was last raised; it is raised (and O and the sum rescaled) only when
 // a logit exceeds it by more than 8 in the log2 domain, so weights stay below 2^8 and the common step has no shuffles.  Weights
-// are rounded to bf16 for the second product, the sum takes them in fp32.
+// are rounded to bf16 for the second product, whose other operand is bf16 (off by at most 2^-8 of a weight; a bf16 output by 2.3e-3 of its
+// norm where its own rounding alone makes 1.7e-3); the sum takes them in fp32.
 #pragma once
 
 #include "attend_common.cuh"

@@ -4,8 +4,8 @@
 // share a key, four channels each, straight from global memory into registers, the next KEYS keys on their way while these are
 // worked on.  A key's R products are summed over its lanes by trading halves - after log2 R steps every lane is left with the
 // sum of one row - so R rows cost R - 1 + 5 - log2 R shuffles instead of 5 R; that lane forms the row's weight and the others
-// fetch it for the second product.  References as in k_attend_few.  32 sequences of 8192 keys: 437 us (4.9 TB/s); with a window of
-// 4096 over lengths of 1024 to 8192 233 us (3.8 TB/s).
+// fetch it for the second product.  References as in k_attend_few.  32 sequences of 8192 keys: 445 us (4.8 TB/s); with a window of
+// 4096 over lengths of 1024 to 8192 238 us (3.7 TB/s).
 #pragma once
 
 #include "attend_few.cuh"

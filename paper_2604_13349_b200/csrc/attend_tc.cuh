@@ -9,8 +9,9 @@
 //   warps 0, 1          products of the first and the second query tile: S = Q K^T into tensor memory, O += P V with P from
 //                       tensor memory; those of one tile run while the softmax of the other does
 //   warps 4-11, 12-19   softmax of the first and the second query tile, two threads per row with 64 keys each (one warp alone on a
-//                       scheduler leaves the special-function unit idle between its instructions), weights to bf16 over the logits' columns,
-//                       their fp32 sum; after the last tile O / sum to memory
+//                       scheduler leaves the special-function unit idle between its instructions), weights to bf16 over the logits' columns
+//                       (a product takes both operands in one 16-bit type, and the values are bf16; off by at most 2^-8 of a weight, a bf16 output
+//                       by 2.3e-3 of its norm where its own rounding alone makes 1.7e-3), their fp32 sum; after the last tile O / sum to memory
 //
 // Softmax: fp32 and bf16 have the same exponents, so a row's reference need not be its maximum, only near enough for no weight
 // to leave fp32's range.  It starts as zero, and the logits are read once, without a search for their maximum before.  Only when
@@ -25,8 +26,8 @@
 //
 // Bound by the exponentials (16 per cycle and multiprocessor: 1024 cycles a tile of 128 x 128) and the two products (512 cycles
 // each) alike, and by the chain from one to the other: a pair of tiles takes 2900 to 3200 cycles, not 2048.  Prompt of 8192, 32
-// heads over 8, 128 channels: causal 549 us (1002 TFLOP/s, 61 % of the measured burst rate), with a window of 1024 and 4 sinks 158
-// us (816; 166 in long runs, at the power limit).
+// heads over 8, 128 channels: causal 552 us (997 TFLOP/s, 60 % of the measured burst rate), with a window of 1024 and 4 sinks 161
+// us (805; 175 in long runs, at the power limit).
 #pragma once
 
 #include "attend_common.cuh"

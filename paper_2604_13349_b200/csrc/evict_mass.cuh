@@ -7,8 +7,8 @@
 // block costs some microseconds of arithmetic and no traffic; sharing out slots, not positions, gives every block as many rows.
 // Longer caches, two launches: a block per (sequence, head) selects by histograms of the keys, 11 + 11 + 10 bits, and writes the
 // positions (k_evict_select); blocks over slots copy (k_evict_copy).
-// Bound by the copy: 2 rows read and written per kept position.  32 x 8 caches of 3001 to 8192 rows to 2048: 110 us (5.0 TB/s), 12 of
-// them the selection; 8 x 8 of 32768 to 16384 in two launches 218 us (5.0 TB/s).
+// Bound by the copy: 2 rows read and written per kept position.  32 x 8 caches of 3001 to 8192 rows to 2048: 112 us (4.9 TB/s), 12 of
+// them the selection; 8 x 8 of 32768 to 16384 in two launches 220 us (5.0 TB/s).
 #pragma once
 
 #include "attend_common.cuh"

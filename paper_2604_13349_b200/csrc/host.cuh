@@ -61,8 +61,10 @@ inline obf_status_t set_smem(K kernel, size_t bytes)
         if (s_ != OBF_OK) return s_;         \
     } while (0)
 
-// Launch that may be set up while the stream's kernel before it still runs: every kernel launched so begins with
-// pdl_wait().  Between two kernels of a call that is about a microsecond less.  `cluster`: blocks of a thread-block cluster, at most
+// Launch that may be set up while the stream's kernel before it still runs.  The first kernel of a call launched so begins with
+// pdl_wait(), before it lets the next one be set up; a later one does, too, unless it reads nothing that the one before writes: then it
+// may wait at its end instead, so that whatever follows it follows both.  Between two kernels of a call that is about a
+// microsecond less.  `cluster`: blocks of a thread-block cluster, at most
 // eight, in the grid's first dimension.
 template <typename... P, typename... A>
 inline obf_status_t launch_clusters(int cluster, void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args)
