@@ -146,9 +146,9 @@ static int tc_parts(long long pairs, long long keys, bool joined)
 }
 
 // Parts of the keys for k_attend_few: as many as make its rounds of resident blocks cheapest, a block costing its keys and, to
-// begin and to end, as much as 120 more; at least 256 keys each.  (Measured beside one another: 16 sequences of 8192 keys and their masses, 128 tiles: the rule's 9 parts
-// 96 us, 18 parts 99, 28 parts 101; 32 of up to 8192 with a window of 4096: the rule's 1 part 74.6, 9 parts 80; 4 of 131072: the rule's 37
-// parts 283, 9 parts 286, 18 parts 281, 28 parts, whose last round is the emptiest, 292.)
+// begin and to end, as much as 120 more; at least 256 keys each.  (Measured beside one another: 16 sequences of 8192
+// keys and their masses, 128 tiles: the rule's 9 parts 96 us, 18 parts 99, 28 parts 101; 32 of up to 8192 with a window of 4096: the rule's
+// 1 part 74.6, 9 parts 80; 4 of 131072: the rule's 37 parts 283, 9 parts 286, 18 parts 281, 28 parts, whose last round is the emptiest, 292.)
 static int few_parts(long long tiles, long long keys, int resident)
 {
     long long best = 1, cost = LLONG_MAX;
@@ -186,10 +186,10 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
     L.p_path = ATTEND_GENERIC;
     L.p_slots = 0;
     // A small call over a prefix: three launches would take longer than reading it once per sequence, from the L2 cache, as long as
-    // the clusters all run at once.  (us from Python, one launch and three, measured beside one another; 8 KV heads, relay of 1012 rows: 4 sequences 14.7 and 19.1; 5, whose
-    // 320 blocks do not fit, 17.2 and 19.7, replayed from a graph 16.3 and 13.6; 16: 34.9 and 19.7.  Of 256 rows 5 sequences 12.0 and
-    // 19.9, 32: 28.6 and 19.6.  4 sequences, 4000 rows: 15.8 and 19.1, from a graph 15.0 and 14.8; 4200: 17.2 and 19.7, 16.3 and 13.6;
-    // 12000: 35.4 and 20.2.)
+    // the clusters all run at once.  (us from Python, one launch and three, measured beside one another; 8 KV heads, relay of 1012 rows:
+    // 4 sequences 14.7 and 19.1; 5, whose 320 blocks do not fit, 17.2 and 19.7, replayed from a graph 16.3 and 13.6; 16: 34.9 and 19.7.  Of
+    // 256 rows 5 sequences 12.0 and 19.9, 32: 28.6 and 19.6.  4 sequences, 4000 rows: 15.8 and 19.1, from a graph 15.0 and 14.8; 4200:
+    // 17.2 and 19.7, 16.3 and 13.6; 12000: 35.4 and 20.2.)
     const long long few_tiles = heads * ((rows_seq + few_rows(a->dtype, rows_seq) - 1) / few_rows(a->dtype, rows_seq));
     L.with_prefix = x && L.own_path == ATTEND_FEW && 8 * few_tiles <= FEW_RESIDENT && x->rows + a->capacity <= 4096;
     if (L.with_prefix) {
