@@ -425,6 +425,77 @@ typedef struct {
 /* Enqueues the eviction on `stream`; needs no workspace, allocates nothing and never synchronises. */
 obf_status_t obf_evict_by_mass(const obf_evict_t *args, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * A relayed cache held in 8 or 4 bits: rows are quantised as they are written (obf_quantized_write), read back
+ * (obf_quantized_read) and attended over as they are (obf_attend_quantized).  A row of K or V is codes and scales, value = code * scale:
+ *
+ *   bits 8   int8 codes, head_dim bytes a row; one fp32 scale a row, max |x| / 127; code = round-half-even(x / scale), the quotient
+ *            rounded to fp32.  The int8 copy that obf_compress makes (k_q8_out, k_scale_out) is such a cache, its layers the batch.
+ *   bits 4   head_dim / 2 bytes a row, the code plus 8 of channel 2 i in the lower four bits of byte i and that of channel 2 i + 1 in the upper ones; one bfloat16
+ *            scale for each of head_dim / 32 groups of channels, group(c) = (c / 4) mod (head_dim / 32): max |x| / 7 over the
+ *            group's channels, rounded half to even to five significant bits; code = round-half-even(x / scale), -7 .. 7.  Such
+ *            values are bfloat16 numbers.  (Other scales, and the code -8, are read as they stand.)
+ *
+ * A row (8 bits) or group (4 bits) that holds a number which is not finite gets a scale that is not a number; one whose magnitudes are all
+ * below 2^-110 is held as zeros.
+ * ---------------------------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t bits;                       /* 8 or 4                                                                */
+    void *k, *v;                        /* device codes [batch, kv_heads, capacity, head_dim * bits / 8 bytes], 16-byte aligned */
+    void *k_scale, *v_scale;            /* device, bits 8: fp32 [batch, kv_heads, capacity], 4-byte aligned; bits 4: bfloat16
+                                           [batch, kv_heads, capacity, head_dim / 32], aligned to a row (head_dim / 16 bytes)  */
+    int64_t k_stride[3], v_stride[3];   /* bytes from one sequence, head and row to the next: multiples of 16, at least a row and
+                                           less than 2^40 where there is more than one of them                   */
+    int64_t k_scale_stride[3], v_scale_stride[3];   /* elements likewise: at least a row's and multiples of it   */
+} obf_quantized_t;
+
+/*
+ * Quantises rows of K and V as they are written.  The first new_lens[b] of sequence b's `rows` rows go, in order, to rows
+ * lens[b] - new_lens[b] .. lens[b] - 1 of its cache (the tokens that obf_attend takes for the last queries, with the same two arrays);
+ * rows that would stand outside 0 .. capacity - 1 are not written.  What else the cache holds is left as it was.  k_values and
+ * v_values receive the rows as the cache holds them, rounded to the rows' type (a bfloat16 or fp32 cache that a prompt's own attention can
+ * run over and see what later tokens will see); rows that are not written are left alone there too.  Inputs must not overlap
+ * outputs.  Two calls that write rows of one cache may overlap if the rows differ.
+ */
+typedef struct {
+    int32_t batch, kv_heads, head_dim, capacity;
+    int32_t rows;                       /* rows of k and v per sequence and KV head, 1 <= rows <= OBF_MAX_T      */
+    int32_t dtype;                      /* obf_dtype_t of k, v, k_values, v_values                               */
+    const void *k, *v;                  /* device [batch, kv_heads, rows, head_dim], 16-byte aligned             */
+    void *k_values, *v_values;          /* the same, both or neither (NULL)                                      */
+    int64_t k_stride[3], v_stride[3], k_values_stride[3], v_values_stride[3];   /* elements, as in obf_attend_t  */
+    const int32_t *lens;                /* device [batch] rows of each cache after the call, or NULL: new_lens   */
+    const int32_t *new_lens;            /* device [batch], clamped to 0 .. rows, or NULL: rows                   */
+} obf_quantized_write_t;
+
+/* Enqueues the writing on `stream`; needs no workspace, allocates nothing, never synchronises, can be captured into a graph. */
+obf_status_t obf_quantized_write(const obf_quantized_write_t *args, const obf_quantized_t *cache, void *stream);
+
+/* Reads rows first .. first + rows - 1 back as fp32 or bfloat16 numbers (rounded once), those below lens[b]; what stands behind them in the
+   outputs is left as it was.  As above otherwise. */
+typedef struct {
+    int32_t batch, kv_heads, head_dim, capacity;
+    int32_t first, rows;                /* 0 <= first, 1 <= rows, first + rows <= capacity                       */
+    int32_t dtype;                      /* obf_dtype_t of k_out, v_out                                           */
+    void *k_out, *v_out;                /* device [batch, kv_heads, rows, head_dim], 16-byte aligned             */
+    int64_t k_out_stride[3], v_out_stride[3];
+    const int32_t *lens;                /* device [batch], or NULL: capacity; clamped to 0 .. capacity           */
+} obf_quantized_read_t;
+
+obf_status_t obf_quantized_read(const obf_quantized_read_t *args, const obf_quantized_t *cache, void *stream);
+
+/*
+ * obf_attend over a cache held in 8 or 4 bits: single tokens to whole prompts, the same masks, lengths, strides and outputs.  args->k,
+ * v, mass_in and mass_out must be NULL (k_stride and v_stride are not looked at), flags 0 or OBF_FLAG_GENERIC_PATH (the kernel
+ * that multiplies codes whatever the number of query rows).
+ *
+ * Numerics: codes are exact in the products, scales are applied in fp32, queries of a row are scaled by a power of two.  A bf16 call's
+ * weights times the values' scales are rounded to bf16 before they multiply the codes.  Scales of keys beyond 2^100, or a value that obf_attend names as
+ * too large, may overflow.  A scale that is not a number spoils the queries that see its row, and may spoil those of the same head that do not.
+ */
+obf_status_t obf_attend_quantized_workspace_bytes(const obf_attend_t *args, const obf_quantized_t *cache, size_t *bytes);
+obf_status_t obf_attend_quantized(const obf_attend_t *args, const obf_quantized_t *cache, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static, never NULL. */
 const char *obf_status_string(obf_status_t status);
 

@@ -11,7 +11,7 @@ import contextlib
 import ctypes
 import os
 import struct
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, NamedTuple, Optional, Sequence
 
 import torch
 
@@ -58,7 +58,8 @@ EXPORTS = ("obf_workspace_bytes", "obf_compress", "evict_only", "obf_host_arena_
            "obf_compress_host", "obf_last_device_status", "obf_status_string",
            "obf_last_launch_count", "obf_compress_profiled", "obf_phase_name",
            "evict_only_static", "obf_static_scratch_status",
-           "obf_attend_workspace_bytes", "obf_attend", "obf_attend_shared", "obf_evict_by_mass")
+           "obf_attend_workspace_bytes", "obf_attend", "obf_attend_shared", "obf_evict_by_mass",
+           "obf_quantized_write", "obf_quantized_read", "obf_attend_quantized_workspace_bytes", "obf_attend_quantized")
 OBF_STATIC_SCRATCH_BYTES = 8 << 20
 OBF_MAX_PHASES = 16
 
@@ -108,6 +109,24 @@ class ObfEvict(ctypes.Structure):
         (n, ctypes.c_void_p) for n in ("k", "v", "k_out", "v_out")] + [
         (n, ctypes.c_int64 * 3) for n in ("k_stride", "v_stride", "k_out_stride", "v_out_stride")] + [
         (n, ctypes.c_void_p) for n in ("mass", "lens", "idx_out", "mass_out")] + [("mass_out_rows", ctypes.c_int32), ("lens_out", ctypes.c_void_p)]
+
+
+class ObfQuantized(ctypes.Structure):
+    _fields_ = [("bits", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [
+        (n, ctypes.c_int64 * 3) for n in ("k_stride", "v_stride", "k_scale_stride", "v_scale_stride")]
+
+
+class ObfQuantizedWrite(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "kv_heads", "head_dim", "capacity", "rows", "dtype")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_values", "v_values")] + [
+        (n, ctypes.c_int64 * 3) for n in ("k_stride", "v_stride", "k_values_stride", "v_values_stride")] + [
+        (n, ctypes.c_void_p) for n in ("lens", "new_lens")]
+
+
+class ObfQuantizedRead(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "kv_heads", "head_dim", "capacity", "first", "rows", "dtype")] + [
+        (n, ctypes.c_void_p) for n in ("k_out", "v_out")] + [(n, ctypes.c_int64 * 3) for n in ("k_out_stride", "v_out_stride")] + [
+        ("lens", ctypes.c_void_p)]
 
 
 class ObfError(RuntimeError):
@@ -161,7 +180,12 @@ def load() -> ctypes.CDLL:
         lib.obf_attend.argtypes = [pa, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         lib.obf_attend_shared.argtypes = [pa, px, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         lib.obf_evict_by_mass.argtypes = [ctypes.POINTER(ObfEvict), ctypes.c_void_p]
-        for name in ("obf_attend_workspace_bytes", "obf_attend", "obf_attend_shared", "obf_evict_by_mass"):
+        pq = ctypes.POINTER(ObfQuantized)
+        lib.obf_quantized_write.argtypes = [ctypes.POINTER(ObfQuantizedWrite), pq, ctypes.c_void_p]
+        lib.obf_quantized_read.argtypes = [ctypes.POINTER(ObfQuantizedRead), pq, ctypes.c_void_p]
+        lib.obf_attend_quantized_workspace_bytes.argtypes = [pa, pq, ctypes.POINTER(ctypes.c_size_t)]
+        lib.obf_attend_quantized.argtypes = [pa, pq, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        for name in EXPORTS[EXPORTS.index("obf_attend_workspace_bytes"):]:
             getattr(lib, name).restype = ctypes.c_int
         lib.obf_last_launch_count.argtypes = []
         lib.obf_last_launch_count.restype = ctypes.c_int32
@@ -369,7 +393,11 @@ _F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 _ATTEND = struct.Struct("@9i2fI4P12q5P")
 _PREFIX = struct.Struct("@2P4qi4x")
 _EVICT = struct.Struct("@8i4P12q4Pi4xP")
-assert (_ATTEND.size, _PREFIX.size, _EVICT.size) == (ctypes.sizeof(ObfAttend), ctypes.sizeof(ObfPrefix), ctypes.sizeof(ObfEvict))
+_QUANTIZED = struct.Struct("@i4P12q")
+_QUANTIZED_WRITE = struct.Struct("@6i4P12q2P")
+_QUANTIZED_READ = struct.Struct("@7i2P6qP")
+assert [x.size for x in (_ATTEND, _PREFIX, _EVICT, _QUANTIZED, _QUANTIZED_WRITE, _QUANTIZED_READ)] == [
+    ctypes.sizeof(x) for x in (ObfAttend, ObfPrefix, ObfEvict, ObfQuantized, ObfQuantizedWrite, ObfQuantizedRead)]
 _packed_calls: Dict[str, object] = {}
 _STATUS_ONLY = 256
 _status_words: Dict[int, torch.Tensor] = {}
@@ -382,7 +410,9 @@ def _packed(name: str):
     if fn is None:
         bytes_, ptr, size = ctypes.c_char_p, ctypes.c_void_p, ctypes.c_size_t
         args = {"obf_attend_workspace_bytes": (bytes_, bytes_, ptr), "obf_attend": (bytes_, ptr, size, ptr),
-                "obf_attend_shared": (bytes_, bytes_, ptr, size, ptr), "obf_evict_by_mass": (bytes_, ptr)}[name]
+                "obf_attend_shared": (bytes_, bytes_, ptr, size, ptr), "obf_evict_by_mass": (bytes_, ptr),
+                "obf_quantized_write": (bytes_, bytes_, ptr), "obf_quantized_read": (bytes_, bytes_, ptr),
+                "obf_attend_quantized_workspace_bytes": (bytes_, bytes_, ptr), "obf_attend_quantized": (bytes_, bytes_, ptr, size, ptr)}[name]
         fn = _packed_calls[name] = ctypes.CFUNCTYPE(ctypes.c_int, *args)((name, load()))
     return fn
 
@@ -452,7 +482,7 @@ def _enqueue(name: str, device: int, args, stream) -> None:
 def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, want_status, stream):
     if workspace is None:
         nb = ctypes.c_size_t(0)
-        rc = _packed("obf_attend_workspace_bytes")(args, prefix, ctypes.addressof(nb))
+        rc = _packed("obf_attend_quantized_workspace_bytes" if name == "obf_attend_quantized" else "obf_attend_workspace_bytes")(args, prefix, ctypes.addressof(nb))
         if rc != OBF_OK:
             raise ObfError(rc, name)
         size = nb.value
@@ -611,3 +641,151 @@ def evict_by_mass(k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, keep: in
         _dense(lens_out, (B,), _I32, at, "lens_out"))
     _enqueue("obf_evict_by_mass", at, (args,), stream)
     return {"K_out": k_out, "V_out": v_out, "idx": idx_out, "mass": mass_out, "lens": lens_out}
+
+
+# ---------------------------------------------------------------------------
+# a relayed cache held in 8 or 4 bits
+# ---------------------------------------------------------------------------
+class QuantizedCache(NamedTuple):
+    """Keys and values of one layer of a batch held in 8 or 4 bits (``obf_quantized_t`` in include/obf.h).
+
+    8 bits: ``k, v`` int8 ``[batch, kv_heads, capacity, head_dim]``, ``k_scale, v_scale`` float32 ``[batch, kv_heads, capacity]`` (what
+    ``compress_caches`` returns as ``K_q8, V_q8, K_scale, V_scale`` is such a cache, its layers the batch).  4 bits: ``k, v`` uint8
+    ``[batch, kv_heads, capacity, head_dim / 2]``, ``k_scale, v_scale`` bfloat16 ``[batch, kv_heads, capacity, head_dim / 32]``.  Any
+    strides of 16 bytes with contiguous rows.
+    """
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def quantized_cache(batch: int, kv_heads: int, capacity: int, head_dim: int, bits: int = 4, device="cuda") -> QuantizedCache:
+    """An empty cache."""
+    if bits not in (8, 4) or head_dim not in (64, 128):
+        raise ValueError("quantized_cache: 8 or 4 bits and heads of 64 or 128 channels expected")
+    rows = (batch, kv_heads, capacity)
+    codes = (*rows, head_dim * bits // 8)
+    scales = rows if bits == 8 else (*rows, head_dim // 32)
+    return QuantizedCache(*(torch.zeros(codes, dtype=torch.int8 if bits == 8 else torch.uint8, device=device) for _ in range(2)),
+                          *(torch.zeros(scales, dtype=_F32 if bits == 8 else _BF16, device=device) for _ in range(2)))
+
+
+def _quantized_args(cache: QuantizedCache):
+    """Checks a cache; gives its struct, shape and device."""
+    k, v, ks, vs = cache
+    shape, dt, dev = k.shape, k.dtype, k.get_device()
+    bits = 8 if dt is torch.int8 else 4 if dt is torch.uint8 else 0
+    if not bits or dev < 0 or len(shape) != 4:
+        raise ValueError("cache.k: int8 [batch, kv_heads, capacity, head_dim] or uint8 [.., head_dim / 2] on a device expected")
+    B, kv, cap, row = shape
+    d = row * 8 // bits
+    sk, sv, ss, st = k.stride(), v.stride(), ks.stride(), vs.stride()
+    scales, sdt = ((B, kv, cap), _F32) if bits == 8 else ((B, kv, cap, d // 32), _BF16)
+    if not (v.shape == shape and v.dtype is dt and v.get_device() == dev and ks.shape == scales and vs.shape == scales and ks.dtype is sdt and vs.dtype is sdt and
+            ks.get_device() == dev and vs.get_device() == dev and sk[3] == sv[3] == 1 and (bits == 8 or ss[3] == st[3] == 1)):
+        for t, want, type_, name in ((k, shape, dt, "k"), (v, shape, dt, "v"), (ks, scales, sdt, "k_scale"), (vs, scales, sdt, "v_scale")):
+            if t.shape != want or t.dtype is not type_ or t.get_device() != dev or (t.dim() == 4 and t.stride(3) != 1):
+                _refuse("cache.%s (contiguous rows)" % name, t, want, type_, k.device)
+    return (_QUANTIZED.pack(bits, k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), sk[0], sk[1], sk[2], sv[0], sv[1], sv[2],
+                            ss[0], ss[1], ss[2], st[0], st[1], st[2]), (B, kv, cap, d), dev)
+
+
+def write_quantized(cache: QuantizedCache, k: torch.Tensor, v: torch.Tensor, *, lens: Optional[torch.Tensor] = None,
+                    new_lens: Optional[torch.Tensor] = None, k_values: Optional[torch.Tensor] = None, v_values: Optional[torch.Tensor] = None,
+                    want_values: bool = False, stream=None) -> Dict[str, torch.Tensor]:
+    """Quantises rows ``k, v [batch, kv_heads, rows, d]`` as they are written to a cache (``obf_quantized_write``).
+
+    The first ``new_lens[b]`` rows (int32 device tensor, None: all) go to the last rows of a cache that then holds ``lens[b]`` (None:
+    ``new_lens``), as ``attend_quantized`` takes them for its queries.  ``k_values, v_values``, or ``want_values``: the rows as the cache holds them,
+    in the type of ``k``, returned as ``K, V``.  Gradients do not pass: where autograd records, tensors that require one are refused.
+    """
+    if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad):
+        _refuse_graph("write_quantized")
+    packed, (B, kv, cap, d), dev = _quantized_args(cache)
+    dt = k.dtype
+    code = OBF_BF16 if dt is _BF16 else OBF_F32 if dt is _F32 else -1
+    if code < 0 or k.dim() != 4:
+        raise ValueError("k: a float32 or bfloat16 device tensor [batch, kv_heads, rows, head_dim] expected")
+    rows = k.shape[2]
+    shape = (B, kv, rows, d)
+    if want_values and (k_values is None or v_values is None):
+        make = torch.empty if new_lens is None and lens is None and rows <= cap else torch.zeros  # what is not written to the cache is not written here
+        with _allocating(stream, k.device):
+            k_values = make(shape, dtype=dt, device=k.device) if k_values is None else k_values
+            v_values = make(shape, dtype=dt, device=k.device) if v_values is None else v_values
+    if (k_values is None) != (v_values is None):
+        raise ValueError("k_values, v_values: both or neither expected")
+    sk, sv = _rows(k, shape, dt, dev, "k"), _rows(v, shape, dt, dev, "v")
+    none = (0, 0, 0)
+    s1, s2 = (none, none) if k_values is None else (_rows(k_values, shape, dt, dev, "k_values"), _rows(v_values, shape, dt, dev, "v_values"))
+    args = _QUANTIZED_WRITE.pack(
+        B, kv, d, cap, rows, code, k.data_ptr(), v.data_ptr(), 0 if k_values is None else k_values.data_ptr(), 0 if v_values is None else v_values.data_ptr(),
+        sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], s1[0], s1[1], s1[2], s2[0], s2[1], s2[2],
+        0 if lens is None else _dense(lens, (B,), _I32, dev, "lens"), 0 if new_lens is None else _dense(new_lens, (B,), _I32, dev, "new_lens"))
+    _enqueue("obf_quantized_write", dev, (args, packed), stream)
+    return {} if k_values is None else {"K": k_values, "V": v_values}
+
+
+def read_quantized(cache: QuantizedCache, *, dtype: Optional[torch.dtype] = None, lens: Optional[torch.Tensor] = None, first: int = 0, rows: Optional[int] = None,
+                   k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Reads rows ``first .. first + rows - 1`` (None: the rest) of a cache back (``obf_quantized_read``), those of sequence b below ``lens[b]``,
+    as ``dtype`` (that of ``k_out``, else bfloat16).  Returns ``K, V [batch, kv_heads, rows, d]``."""
+    packed, (B, kv, cap, d), dev = _quantized_args(cache)
+    rows = cap - first if rows is None else rows
+    given = k_out if k_out is not None else v_out
+    dt = dtype if dtype is not None else _BF16 if given is None else given.dtype
+    code = OBF_BF16 if dt is _BF16 else OBF_F32 if dt is _F32 else -1
+    if code < 0 or first < 0 or rows < 1 or first + rows > cap:
+        raise ValueError("read_quantized: float32 or bfloat16 and rows of the cache expected")
+    shape = (B, kv, rows, d)
+    if k_out is None or v_out is None:
+        make = torch.empty if lens is None else torch.zeros      # rows behind a sequence's last one are not written
+        with _allocating(stream, cache.k.device):
+            k_out = make(shape, dtype=dt, device=cache.k.device) if k_out is None else k_out
+            v_out = make(shape, dtype=dt, device=cache.k.device) if v_out is None else v_out
+    sk, sv = _rows(k_out, shape, dt, dev, "k_out"), _rows(v_out, shape, dt, dev, "v_out")
+    args = _QUANTIZED_READ.pack(B, kv, d, cap, first, rows, code, k_out.data_ptr(), v_out.data_ptr(), sk[0], sk[1], sk[2], sv[0], sv[1], sv[2],
+                                0 if lens is None else _dense(lens, (B,), _I32, dev, "lens"))
+    _enqueue("obf_quantized_read", dev, (args, packed), stream)
+    return {"K": k_out, "V": v_out}
+
+
+def _attend_quantized_args(q, shape, device, lens, q_lens, window, sinks, scale, out, lse_out, flags) -> bytes:
+    B, kv, cap, d = shape
+    dt = q.dtype
+    code = OBF_BF16 if dt is _BF16 else OBF_F32 if dt is _F32 else -1
+    shape_q = q.shape
+    if code < 0 or len(shape_q) != 4:
+        raise ValueError("q: a float32 or bfloat16 device tensor [batch, q_heads, n_q, head_dim] expected")
+    want = (B, shape_q[1], shape_q[2], d)
+    sq, so = _rows(q, want, dt, device, "q"), (0, 0, 0) if out is None else _rows(out, want, dt, device, "out")
+    return _ATTEND.pack(
+        B, kv, shape_q[1], d, shape_q[2], cap, min(window, _MOST), min(sinks, _MOST), code, scale, 1.0, flags,
+        q.data_ptr(), 0, 0, 0 if out is None else out.data_ptr(), sq[0], sq[1], sq[2], 0, 0, 0, 0, 0, 0, so[0], so[1], so[2],
+        0 if lens is None else _dense(lens, (B,), _I32, device, "lens"), 0 if q_lens is None else _dense(q_lens, (B,), _I32, device, "q_lens"),
+        0 if lse_out is None else _dense(lse_out, shape_q[:3], _F32, device, "lse_out"), 0, 0)
+
+
+def attend_quantized(q: torch.Tensor, cache: QuantizedCache, *, lens: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None,
+                     window: int = 0, sinks: int = 0, scale: float = 0.0, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
+                     want_lse: bool = False, flags: int = 0, workspace: Optional[torch.Tensor] = None, want_status: bool = False,
+                     stream=None) -> Dict[str, torch.Tensor]:
+    """``attend`` over a cache held in 8 or 4 bits (``obf_attend_quantized``): the same masks, lengths, strides, outputs and errors; no masses."""
+    if torch.is_grad_enabled() and q.requires_grad:
+        _refuse_graph("attend_quantized")
+    packed, shape, dev = _quantized_args(cache)
+    out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
+    args = _attend_quantized_args(q, shape, dev, lens, q_lens, window, sinks, scale, out, lse_out, flags)
+    return _attend_call("obf_attend_quantized", args, packed, q, out, lse_out, None, workspace, want_status, stream)
+
+
+def attend_quantized_workspace(q: torch.Tensor, cache: QuantizedCache, *, window: int = 0, sinks: int = 0, flags: int = 0) -> torch.Tensor:
+    """A workspace for ``attend_quantized`` calls of these shapes."""
+    packed, shape, dev = _quantized_args(cache)
+    nb = ctypes.c_size_t(0)
+    rc = _packed("obf_attend_quantized_workspace_bytes")(_attend_quantized_args(q, shape, dev, None, None, window, sinks, 0.0, None, None, flags), packed,
+                                                         ctypes.addressof(nb))
+    if rc != OBF_OK:
+        raise ObfError(rc, "obf_attend_quantized_workspace_bytes")
+    return torch.zeros(nb.value, dtype=torch.uint8, device=q.device)

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "_lib")
 LIB_PATH = os.path.join(LIB_DIR, "libobf_b200.so")
-SOURCES = ["obf_api.cu", "obf_attend.cu"]
+SOURCES = ["obf_api.cu", "obf_attend.cu", "obf_quant.cu"]
 
 
 def _newest_source_mtime() -> float:

@@ -5,20 +5,12 @@
 #include "attend_few.cuh"
 #include "attend_few_f32.cuh"
 #include "attend_generic.cuh"
+#include "attend_host.cuh"
 #include "attend_tc.cuh"
 #include "evict_mass.cuh"
 #include "host.cuh"
 
 namespace obf {
-
-static obf_status_t check_stride(const int64_t *st, const int64_t *n, int dims, int head_dim, int esize)
-{
-    for (int i = 0; i < dims; ++i) {
-        if (n[i] < 2) continue;                           // never stepped over
-        if (st[i] < head_dim || st[i] >= ((int64_t)1 << 40) / esize || st[i] * esize % 16 != 0) return OBF_ERR_INVALID_ARG;
-    }
-    return OBF_OK;
-}
 
 static obf_status_t validate_attend(const obf_attend_t *a, const obf_prefix_t *x)
 {
@@ -71,23 +63,6 @@ struct AttendLayout {
     bool with_prefix;                // and walk the prefix as well
     size_t off_part_o, off_part_lse, off_logits, total;
 };
-
-// Parts of `keys` keys for `tiles` tiles of query rows: about `blocks` blocks in all, at least `least` keys each.
-static int parts_for(long long tiles, long long keys, long long blocks, int least)
-{
-    long long s = (blocks + tiles - 1) / tiles, most = (keys + least - 1) / least;
-    if (s > most) s = most;
-    if (s > 128) s = 128;
-    return (int)(s < 1 ? 1 : s);
-}
-
-// Keys that a query row can see at most.
-static long long most_keys(const obf_attend_t *a, int rows_of_queries)
-{
-    if (a->window == 0) return a->capacity;
-    const long long n = (long long)a->window + rows_of_queries + a->sinks;
-    return n < a->capacity ? n : a->capacity;
-}
 
 // Up to 16 query rows (and a mass call's at most 64) go where a tile of 128 rows, or the generic kernel's 64, would stay empty.
 static AttendPath path_for(const obf_attend_t *a, long long rows)
@@ -143,20 +118,6 @@ static int tc_parts(long long pairs, long long keys, bool joined)
         if (pairs * s > 148 * 4) break;
     }
     return best;
-}
-
-// Parts of the keys for k_attend_few: as many as make its rounds of resident blocks cheapest, a block costing its keys and, to
-// begin and to end, as much as 120 more; at least 256 keys each.  (Measured beside one another: 16 sequences of 8192
-// keys and their masses, 128 tiles: the rule's 9 parts 96 us, 18 parts 99, 28 parts 101; 32 of up to 8192 with a window of 4096: the rule's
-// 1 part 74.6, 9 parts 80; 4 of 131072: the rule's 37 parts 283, 9 parts 286, 18 parts 281, 28 parts, whose last round is the emptiest, 292.)
-static int few_parts(long long tiles, long long keys, int resident)
-{
-    long long best = 1, cost = LLONG_MAX;
-    for (long long s = 1; s <= 128 && (s == 1 || s * 256 <= keys); ++s) {
-        const long long c = (tiles * s + resident - 1) / resident * ((keys + s - 1) / s + 120);
-        if (c < cost) { cost = c; best = s; }
-    }
-    return (int)best;
 }
 
 // Whether the call may ask for waits that run out: small ones that the tensor-core kernel works on.
@@ -216,18 +177,6 @@ static AttendLayout attend_layout(const obf_attend_t *a, const obf_prefix_t *x)
     if (a->mass_out) o = align_up(o + (size_t)rows * a->capacity * sizeof(float), 256);
     L.total = o;
     return L;
-}
-
-// Raises a kernel's shared-memory limit the first time it is used on a device.
-template <typename K>
-static obf_status_t set_smem_once(K kernel, size_t bytes, bool (&done)[64])
-{
-    int dev = 0;
-    OBF_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev >= 0 && dev < 64 && done[dev]) return OBF_OK;
-    OBF_TRY(set_smem(kernel, bytes));
-    if (dev >= 0 && dev < 64) done[dev] = true;
-    return OBF_OK;
 }
 
 template <typename TIN, int D, bool PREFIX>
@@ -362,17 +311,7 @@ static obf_status_t run_attend(const AttendLayout &L, const AttendDev &p, cudaSt
 {
     if (p.prefix) OBF_TRY((launch_attend<TIN, D, true>(L.p_path, p, 1, st)));
     OBF_TRY((launch_attend<TIN, D, false>(L.own_path, p, p.prefix == 0, st)));
-    if ((p.slots > 1 || p.mass_out) && !p.cluster) {
-        // a warp per row fills the chip from some thousand rows on; fewer are joined by four warps each
-        const bool many = p.rows_total >= 4 * 148;
-        const long long row_blocks = many ? (p.rows_total + 3) / 4 : p.rows_total;
-        long long blocks = row_blocks;
-        if (p.mass_out) blocks += (long long)p.batch * p.kv_heads * ((p.capacity + AJ_KEYS - 1) / AJ_KEYS);
-        if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
-        if (many) OBF_TRY(launch(k_attend_join<TIN, D, 1>, dim3((unsigned)blocks), AJ_NT, 0, st, p, (int)row_blocks));
-        else OBF_TRY(launch(k_attend_join<TIN, D, 4>, dim3((unsigned)blocks), AJ_NT, 0, st, p, (int)row_blocks));
-        ++g_last_launches;
-    }
+    if ((p.slots > 1 || p.mass_out) && !p.cluster) OBF_TRY((launch_join<TIN, D>(p, st)));
     return OBF_OK;
 }
 
