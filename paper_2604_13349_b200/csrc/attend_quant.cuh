@@ -20,6 +20,9 @@
 
 namespace obf {
 
+constexpr float AQ_NONE = -3e38f;                         // reference of a row that has seen no key: any logit raises it
+constexpr float AQ_BIAS = 75.f;                           // references lie so far below the maximum at which they were last raised
+
 template <int BITS, int D>
 struct QuantStage {
     typedef QuantRow<BITS, D> Row;
@@ -77,59 +80,42 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Codes as numbers.  Half n of a word's halves, four codes plus 8 each, as two fp16 numbers (1024 + u and 1024 + 16 u, less their offset)
-// or as two bf16 numbers (128 + u, less 136): exact.
-__device__ __forceinline__ uint32_t h2_sub(uint32_t x, float off)
+// The same on top of zeros, which take no registers.
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&x), __float2half2_rn(off));
-    return *reinterpret_cast<const uint32_t *>(&r);
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
-__device__ __forceinline__ void nibbles_f16(uint32_t (&r)[4], uint32_t x)
+
+// Codes as numbers, without arithmetic: the bits of a small whole number u are the fp16 number u 2^-24 (u < 2048) and the bf16 number
+// u 2^-133 (u < 256), and matrix products take such numbers exactly.  A word of two halves of four codes plus 8 gives, by masks,
+// pairs of codes 0 and 2 and, sixteen times as large, of codes 1 and 3 of the halves.
+__device__ __forceinline__ void nibbles(uint32_t (&r)[4], uint32_t x)
 {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t y = x >> (8 * i), lo = (y & 0x000f000fu) | 0x64006400u, hi = (y & 0x00f000f0u) | 0x64006400u;
-        r[2 * i] = h2_sub(lo, 1032.f);
-        const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&hi), __float2half2_rn(0.0625f), __float2half2_rn(-72.f));
-        r[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&v);
-    }
+    r[0] = x & 0x000f000fu;
+    r[1] = x & 0x00f000f0u;
+    r[2] = (x >> 8) & 0x000f000fu;
+    r[3] = (x >> 8) & 0x00f000f0u;
 }
-__device__ __forceinline__ uint32_t nibble_bf16(uint32_t x, int n)
+// Their offsets: of bf16 pairs, 8 in the first kind of place and 8 * 16 in the second; 128.
+constexpr uint32_t AQ_MINUS_8 = 0x80088008u, AQ_MINUS_128 = 0x80808080u;
+__device__ __forceinline__ uint32_t add_bf16(uint32_t x, uint32_t y)
 {
-    const uint32_t u = ((x >> (4 * n)) & 0x000f000fu) | 0x43004300u;
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), __float2bfloat162_rn(136.f));
-    return *reinterpret_cast<const uint32_t *>(&r);
+    uint32_t r;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
 }
-// Four int8 codes as two pairs of fp16 numbers.
-__device__ __forceinline__ void bytes_f16(uint32_t &lo, uint32_t &hi, uint32_t x)
+// Bytes n and n + 1 (n even) of two words as pairs.
+__device__ __forceinline__ void byte_pairs(uint32_t &lo, uint32_t &hi, uint32_t a, uint32_t b, int n)
 {
-    x ^= 0x80808080u;
-    lo = h2_sub(__byte_perm(x, 0x64646464u, 0x4140), 1152.f);
-    hi = h2_sub(__byte_perm(x, 0x64646464u, 0x4342), 1152.f);
-}
-// Byte n of two words (int8 codes plus 128) as a pair of bf16 numbers, by way of 2^23 + u.
-__device__ __forceinline__ uint32_t byte_pair_bf16(uint32_t a, uint32_t b, int n)
-{
-    const float x = __uint_as_float(__byte_perm(a, 0x4b000000u, 0x7440 + n)), y = __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7440 + n));
-    return pack_bf16(x - 8388736.f, y - 8388736.f);
+    const uint32_t x = __byte_perm(a, b, n == 0 ? 0x5410 : 0x7632);
+    lo = x & 0x00ff00ffu;
+    hi = __byte_perm(x, 0u, 0x4341);
 }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// Scales of a key, fp32.
-template <int BITS, int D>
-__device__ __forceinline__ void scales_of(float (&s)[QuantRow<BITS, D>::GROUPS], uint32_t a)
-{
-    if constexpr (BITS == 8) {
-        s[0] = __uint_as_float(lds1(a));
-    } else {
-        uint32_t w[D / 64];
-        lds(w, a);
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) { s[2 * i] = bf16_lo(w[i]); s[2 * i + 1] = bf16_hi(w[i]); }
-    }
-}
 
 // A pair of weights as bf16 numbers, in as many parts as the outputs' type needs (their sum is the weight but for the last part's rounding).
 template <int PARTS>
@@ -142,13 +128,17 @@ __device__ __forceinline__ void split_weights(uint32_t (&r)[PARTS], float x, flo
     }
 }
 
+// Blocks of a multiprocessor.
+template <typename TIN, int D, int NT>
+constexpr int AQ_BLOCKS = NT == 1 ? (sizeof(TIN) == 4 && D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
+
 template <typename TIN, int BITS, int D, int NT, bool CLUSTER>
-__global__ void __launch_bounds__(AF_NT) k_attend_quant(const __grid_constant__ AttendDev p, const __grid_constant__ QuantDev c)
+__global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant(const __grid_constant__ AttendDev p, const __grid_constant__ QuantDev c)
 {
     extern __shared__ __align__(128) unsigned char aq_sm[];
     typedef QuantStage<BITS, D> Stage;
     typedef QuantRow<BITS, D> Row;
-    constexpr int KS = D / 16, ROWS = 8 * NT, ST = Stage::STAGES, KEYS = Stage::KEYS, RB = Row::BYTES, CH = RB / 16, LR = 32 / CH, SB = Row::SCALE_BYTES, GR = Row::GROUPS;
+    constexpr int KS = D / 16, ROWS = 8 * NT, ST = Stage::STAGES, KEYS = Stage::KEYS, RB = Row::BYTES, CH = RB / 16, LR = 32 / CH, SB = Row::SCALE_BYTES, GR = Row::GROUPS, SUB = KEYS / 16;
     constexpr int PARTS = sizeof(TIN) == 4 ? 2 : 1;       // of a query
     constexpr int WPARTS = sizeof(TIN) == 4 ? 3 : 1;      // of a weight
     pdl_wait();
@@ -170,42 +160,69 @@ __global__ void __launch_bounds__(AF_NT) k_attend_quant(const __grid_constant__ 
     const int n = kr.count(), per = ((n + 63) / 64 + parts - 1) / parts * 64;
     const int v0 = min((long long)part * per, (long long)n), v1 = min(v0 + per, n);
 
-    const uint8_t *kb = c.k + b * c.ks[0] + h * c.ks[1], *vb = c.v + b * c.vs[0] + h * c.vs[1];
-    const uint8_t *ksb = c.k_scale + b * c.kss[0] + h * c.kss[1], *vsb = c.v_scale + b * c.vss[0] + h * c.vss[1];
-
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(aq_sm) + warp * ST * Stage::BYTES;
     const int lc = lane % CH, lr = lane / CH;
-    const int mine = (v1 - v0 + KEYS - 1) / KEYS;         // the part's stages, of which this warp does warp, warp + 4, ...
-    auto fetch = [&](int st, int slot) {
-        if (st < mine) {
-            const uint32_t kd = ring + slot * Stage::BYTES, vd = kd + Stage::CODES, sd = vd + Stage::CODES;
-            const int va = v0 + st * KEYS;
+    // This warp's stages begin at keys va = v0 + warp KEYS and every fourth stage from there.  The next one to be fetched has its rows at
+    // kp, vp (row lr of it) and scales at ksp, vsp (row `lane`) if it lies whole behind the sinks; where it does not, each row's place is worked out.
+    const long long j0 = (long long)v0 + warp * KEYS - kr.s + kr.lo;
+    const uint8_t *kp = c.k + b * c.ks[0] + h * c.ks[1] + (j0 + lr) * c.ks[2] + lc * 16, *vp = c.v + b * c.vs[0] + h * c.vs[1] + (j0 + lr) * c.vs[2] + lc * 16;
+    const uint8_t *ksp = c.k_scale + b * c.kss[0] + h * c.kss[1] + (j0 + lane) * c.kss[2], *vsp = c.v_scale + b * c.vss[0] + h * c.vss[1] + (j0 + lane) * c.vss[2];
+    const bool dense = c.ks[2] == RB && c.vs[2] == RB;    // neighbours in memory: constant steps
+    const uint32_t own_chunk = ring + chunk_at<RB>(lr, lc), own_scale = ring + 2 * Stage::CODES + lane * SB;
+    auto fetch = [&](int va, int slot) {
+        const uint32_t off = slot * Stage::BYTES;
+        if (va >= kr.s && va + KEYS <= v1) {
+            // (rows LR apart stand alike, but that at 128 bytes every second one has its chunks' halves exchanged)
+            const uint32_t at[2] = {own_chunk + off, (RB == 128 ? own_chunk ^ 64u : own_chunk) + off};
+            if (dense) {
 #pragma unroll
+                for (int i = 0; i < KEYS / LR; ++i) {
+                    cp_async16(at[i & 1] + i * LR * RB, kp + i * LR * RB, true);
+                    cp_async16(at[i & 1] + i * LR * RB + Stage::CODES, vp + i * LR * RB, true);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < KEYS / LR; ++i) {
+                    cp_async16(at[i & 1] + i * LR * RB, kp + i * LR * c.ks[2], true);
+                    cp_async16(at[i & 1] + i * LR * RB + Stage::CODES, vp + i * LR * c.vs[2], true);
+                }
+            }
+            if (KEYS == 32 || lane < KEYS) {
+                cp_async_small<SB>(own_scale + off, ksp, true);
+                cp_async_small<SB>(own_scale + off + Stage::SCALES, vsp, true);
+            }
+        } else if (va < v1) {
+            const int at_va = va - kr.s + kr.lo;
+#pragma unroll 1
             for (int i = 0; i < KEYS / LR; ++i) {
                 const int r = lr + i * LR, v = va + r;
-                const bool real = v < v1;
-                const long long j = kr.key(real ? v : v0);
-                const uint32_t at = chunk_at<RB>(r, lc);
-                cp_async16(kd + at, kb + j * c.ks[2] + lc * 16, real);
-                cp_async16(vd + at, vb + j * c.vs[2] + lc * 16, real);
+                const bool real = v < v1;                 // (behind the part: zeros, whatever the cache holds there)
+                const long long step = kr.key(real ? v : v0) - (at_va + lr);
+                const uint32_t at = ring + off + chunk_at<RB>(r, lc);
+                cp_async16(at, kp + step * c.ks[2], real);
+                cp_async16(at + Stage::CODES, vp + step * c.vs[2], real);
             }
             if (lane < KEYS) {
                 const int v = va + lane;
-                const bool real = v < v1;                 // (behind the part: zeros, whatever the cache holds there)
-                const long long j = kr.key(real ? v : v0);
-                cp_async_small<SB>(sd + lane * SB, ksb + j * c.kss[2], real);
-                cp_async_small<SB>(sd + Stage::SCALES + lane * SB, vsb + j * c.vss[2], real);
+                const bool real = v < v1;
+                const long long step = kr.key(real ? v : v0) - (at_va + lane);
+                cp_async_small<SB>(own_scale + off, ksp + step * c.kss[2], real);
+                cp_async_small<SB>(own_scale + off + Stage::SCALES, vsp + step * c.vss[2], real);
             }
         }
         cp_commit();
+        kp += AF_WARPS * KEYS * c.ks[2];
+        vp += AF_WARPS * KEYS * c.vs[2];
+        ksp += AF_WARPS * KEYS * c.kss[2];
+        vsp += AF_WARPS * KEYS * c.vss[2];
     };
 #pragma unroll
-    for (int s = 0; s < ST - 1; ++s) fetch(warp + s * AF_WARPS, s);
+    for (int s = 0; s < ST - 1; ++s) fetch(v0 + (warp + s * AF_WARPS) * KEYS, s);
 
     // Queries as B fragments: of row 8 nt + lane / 4 a lane holds a quarter of the channels, those of its words of a key.
     uint32_t qf[PARTS][NT][KS][2];
+    float q_off[NT][GR][2];                               // what their codes' offsets add up to
     float row_c[NT][2];                                   // what makes logits (log2) of a product's rows 8 nt + 2 (lane mod 4) + e
-    int row_t[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int r = tile * ROWS + nt * 8 + g8, i = r / p.G, g = r - i * p.G;
@@ -232,26 +249,37 @@ __global__ void __launch_bounds__(AF_NT) k_attend_quant(const __grid_constant__ 
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int e = min(max((int)(top >> 23), 27), 254);             // exponent of the largest, at least that of 2^-100
         const float up = __uint_as_float((uint32_t)(267 - e) << 23), down = __uint_as_float((uint32_t)(e - 13) << 23);
+        float sum[GR];
+#pragma unroll
+        for (int j = 0; j < GR; ++j) sum[j] = 0.f;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                // the pair's two channels among the lane's
+                // the pair's two channels among the lane's (4 bits: those of u = 1 meet codes sixteen times as large)
                 const int a = BITS == 8 ? 4 * k + 2 * u : 2 * k + u, a2 = BITS == 8 ? a + 1 : a + D / 8;
-                float y = q[a] * up, z = q[a2] * up;
+                const float f = BITS == 4 && u == 1 ? up * 0.0625f : up;
+                float y = q[a] * f, z = q[a2] * f;
 #pragma unroll
                 for (int part_q = 0; part_q < PARTS; ++part_q) {
                     const __half2 v = __floats2half2_rn(y, z);
                     qf[part_q][nt][k][u] = *reinterpret_cast<const uint32_t *>(&v);
                     y -= __low2float(v);
                     z -= __high2float(v);
+                    sum[BITS == 8 ? 0 : k >> 1] += (__low2float(v) + __high2float(v)) * (BITS == 4 && u == 1 ? 16.f : 1.f);
                 }
             }
 #pragma unroll
+        for (int j = 0; j < GR; ++j) {
+            sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
+            sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                q_off[nt][j][u] = __shfl_sync(0xffffffffu, sum[j], 4 * (2 * t4 + u)) * (BITS == 4 ? -0x1p-21f : -0x1p-17f);       // -8, -128 times 2^-24
+        }
+#pragma unroll
         for (int u = 0; u < 2; ++u) {
-            row_c[nt][u] = p.c * __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + u));
-            const int r2 = tile * ROWS + nt * 8 + 2 * t4 + u, i2 = r2 / p.G;
-            row_t[nt][u] = r2 < rows_seq && i2 < ql ? len - ql + i2 : INT_MIN;
+            row_c[nt][u] = p.c * 0x1p24f * __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + u));
         }
     }
 
@@ -259,190 +287,255 @@ __global__ void __launch_bounds__(AF_NT) k_attend_quant(const __grid_constant__ 
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) { m[nt][e] = -INFINITY; l[nt][e] = 0.f; }
+        for (int e = 0; e < 2; ++e) { m[nt][e] = AQ_NONE; l[nt][e] = 0.f; }
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[nt][k][e] = 0.f;
     }
-    const bool one_t = p.n_q == 1;                        // every row of the tile sees every key of the range
+    // keys wa .. wb - 1 of the walk are seen by every row of the tile
+    int wa = 0, wb = v1;
+    if (p.n_q > 1) {
+        const int t0 = len - ql + i0, t1 = len - ql + i1;
+        wb = min(v1, kr.s + max(0, t0 + 1 - kr.lo));
+        if (p.window && t1 - p.window + 1 > kr.lo) wa = kr.s + t1 - p.window + 1 - kr.lo;
+    }
     // Row r of a 16-key product stands for key  r / 2 + 4 (r mod 2)  of its half of eight: a lane then reads four neighbouring keys' values.
     const int key_s = (g8 >> 1) + 4 * (g8 & 1);
+    // What this lane reads of sixteen keys: of K words of keys key_s and key_s + 8, of V words of keys lane mod 4 + 4 i, the second half of
+    // eight keys 8 rows behind the first in both; scales of keys key_s and key_s + 8.
+    constexpr int W = RB / 32;                            // words of V
+    const uint32_t k_at = ring + (RB == 32 ? chunk_at<RB>(key_s, t4 >> 1) + (t4 & 1) * 8 : chunk_at<RB>(key_s, t4));
+    uint32_t v_at[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        v_at[i] = ring + Stage::CODES + (W == 4 ? chunk_at<RB>(t4 + 4 * i, g8) : W == 2 ? chunk_at<RB>(t4 + 4 * i, g8 >> 1) + (g8 & 1) * 8 : chunk_at<RB>(t4 + 4 * i, g8 >> 2) + (g8 & 3) * 4);
+    const uint32_t s_at = ring + 2 * Stage::CODES + key_s * SB;
     int slot = 0;
-    for (int st = warp; st < mine; st += AF_WARPS) {
+    for (int va = v0 + warp * KEYS; va < v1; va += AF_WARPS * KEYS) {
         cp_wait<ST - 2>();
         __syncwarp();
-        fetch(st + (ST - 1) * AF_WARPS, slot == 0 ? ST - 1 : slot - 1);
+        fetch(va + (ST - 1) * AF_WARPS * KEYS, slot == 0 ? ST - 1 : slot - 1);
+        const uint32_t off = slot * Stage::BYTES, kd = k_at + off, vd0 = v_at[0] + off, vd1 = v_at[1] + off, sd = s_at + off;
+        float s[SUB][NT][4];
+        // ---- logits (products that wait for one another are kept apart by those of the other sixteen keys) ----
+        if constexpr (BITS == 4) {
+            constexpr int KW = D / 32;                    // words of a lane
+            uint32_t w0[SUB][KW], w1[SUB][KW], f0[SUB][GR / 2], f1[SUB][GR / 2];
 #pragma unroll
-        for (int sub = 0; sub < KEYS / 16; ++sub) {
-            const uint32_t kd = ring + slot * Stage::BYTES + sub * 16 * RB, vd = kd + Stage::CODES;
-            const uint32_t sd = ring + slot * Stage::BYTES + 2 * Stage::CODES + (sub * 16 + key_s) * SB;
-            float s[NT][4];
-            // ---- logits ----
-            {
-                float k0[GR], k1[GR];
-                scales_of<BITS, D>(k0, sd);
-                scales_of<BITS, D>(k1, sd + 8 * SB);
-                if constexpr (BITS == 4) {
-                    constexpr int W = D / 32;             // words of a lane
-                    uint32_t w0[W], w1[W];
-                    if constexpr (D == 128) {
-                        lds(w0, kd + chunk_at<RB>(key_s, t4));
-                        lds(w1, kd + chunk_at<RB>(key_s + 8, t4));
-                    } else {
-                        lds(w0, kd + chunk_at<RB>(key_s, t4 >> 1) + (t4 & 1) * 8);
-                        lds(w1, kd + chunk_at<RB>(key_s + 8, t4 >> 1) + (t4 & 1) * 8);
-                    }
-#pragma unroll
-                    for (int j = 0; j < GR; ++j) {
-                        const int sel = j & 1 ? 0x7632 : 0x5410;
-                        uint32_t n0[4], n1[4];
-                        nibbles_f16(n0, __byte_perm(w0[j >> 1], w0[(j >> 1) + W / 2], sel));
-                        nibbles_f16(n1, __byte_perm(w1[j >> 1], w1[(j >> 1) + W / 2], sel));
-                        float acc[NT][4];
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[nt][e] = 0.f;
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const uint32_t a[4] = {n0[2 * i], n1[2 * i], n0[2 * i + 1], n1[2 * i + 1]};
-#pragma unroll
-                                for (int part_q = PARTS - 1; part_q >= 0; --part_q) mma_f16(acc[nt], a, qf[part_q][nt][2 * j + i][0], qf[part_q][nt][2 * j + i][1]);
-                            }
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float y = acc[nt][e] * (e < 2 ? k0[j] : k1[j]);
-                                s[nt][e] = j == 0 ? y : s[nt][e] + y;
-                            }
-                        }
-                    }
-                } else {
-                    uint32_t w0[KS], w1[KS];
-#pragma unroll
-                    for (int half = 0; half < KS / 4; ++half) {
-                        uint32_t u0[4], u1[4];
-                        lds(u0, kd + chunk_at<RB>(key_s, t4 + 4 * half));
-                        lds(u1, kd + chunk_at<RB>(key_s + 8, t4 + 4 * half));
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) { w0[4 * half + i] = u0[i]; w1[4 * half + i] = u1[i]; }
-                    }
-                    float acc[NT][2][4];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[nt][0][e] = acc[nt][1][e] = 0.f;
-#pragma unroll
-                    for (int k = 0; k < KS; ++k) {
-                        uint32_t a[4];
-                        bytes_f16(a[0], a[2], w0[k]);
-                        bytes_f16(a[1], a[3], w1[k]);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int part_q = PARTS - 1; part_q >= 0; --part_q) mma_f16(acc[nt][k & 1], a, qf[part_q][nt][k][0], qf[part_q][nt][k][1]);
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[nt][e] = (acc[nt][0][e] + acc[nt][1][e]) * (e < 2 ? k0[0] : k1[0]);
-                }
-            }
-            // ---- weights: s[nt][2 u + e] is key 8 u + key_s of the sixteen, row 8 nt + 2 (lane mod 4) + e ----
-            const int va = v0 + st * KEYS + sub * 16 + key_s;
-            bool raise = false;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int v = va + 8 * u, j = kr.key(v);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const bool sees = v < v1 && (one_t || attend_sees(p, row_t[nt][e], j));
-                        float &y = s[nt][2 * u + e];
-                        y = sees ? y * row_c[nt][e] : -INFINITY;
-                        raise = raise || y > m[nt][e] + AF_RAISE;
-                    }
-            }
-            if (__any_sync(0xffffffffu, raise)) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float mx = fmaxf(fmaxf(s[nt][e], s[nt][2 + e]), m[nt][e]);
-#pragma unroll
-                        for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                        const float f = mx == -INFINITY ? 1.f : ex2(m[nt][e] - mx);
-                        m[nt][e] = mx;
-                        l[nt][e] *= f;
-#pragma unroll
-                        for (int k = 0; k < KS; ++k) { o[nt][k][e] *= f; o[nt][k][2 + e] *= f; }
-                    }
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float r0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], r1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    s[nt][2 * u] = ex2(s[nt][2 * u] - r0);
-                    s[nt][2 * u + 1] = ex2(s[nt][2 * u + 1] - r1);
-                    l[nt][0] += s[nt][2 * u];
-                    l[nt][1] += s[nt][2 * u + 1];
-                }
-            }
-            // ---- values ----
-            float k0[GR], k1[GR];
-            scales_of<BITS, D>(k0, sd + Stage::SCALES);
-            scales_of<BITS, D>(k1, sd + Stage::SCALES + 8 * SB);
-            constexpr int W = RB / 32;                    // words of a lane
-            uint32_t w[4][W];                             // of keys lane mod 4 + 4 i
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = t4 + 4 * i;
-                if constexpr (W == 4) lds(w[i], vd + chunk_at<RB>(key, g8));
-                else if constexpr (W == 2) lds(w[i], vd + chunk_at<RB>(key, g8 >> 1) + (g8 & 1) * 8);
-                else lds(w[i], vd + chunk_at<RB>(key, g8 >> 2) + (g8 & 3) * 4);
-                if constexpr (BITS == 8) {
-#pragma unroll
-                    for (int q = 0; q < W; ++q) w[i][q] ^= 0x80808080u;
-                }
+            for (int sub = 0; sub < SUB; ++sub) {
+                lds(w0[sub], kd + sub * 16 * RB);
+                lds(w1[sub], kd + (sub * 16 + 8) * RB);
+                lds(f0[sub], sd + sub * 16 * SB);
+                lds(f1[sub], sd + (sub * 16 + 8) * SB);
             }
 #pragma unroll
             for (int j = 0; j < GR; ++j) {
-                uint32_t pf[NT][WPARTS][2];
+                const int sel = j & 1 ? 0x7632 : 0x5410;
+                uint32_t n0[SUB][4], n1[SUB][4];
+                float acc[SUB][NT][4];
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub) {
+                    nibbles(n0[sub], __byte_perm(w0[sub][j >> 1], w0[sub][(j >> 1) + KW / 2], sel));
+                    nibbles(n1[sub], __byte_perm(w1[sub][j >> 1], w1[sub][(j >> 1) + KW / 2], sel));
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int part_q = PARTS - 1; part_q >= 0; --part_q)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int sub = 0; sub < SUB; ++sub) {
+                                const uint32_t a[4] = {n0[sub][2 * i], n1[sub][2 * i], n0[sub][2 * i + 1], n1[sub][2 * i + 1]};
+                                if (i == 0 && part_q == PARTS - 1) mma_f16_first(acc[sub][nt], a, qf[part_q][nt][2 * j][0], qf[part_q][nt][2 * j][1]);
+                                else mma_f16(acc[sub][nt], a, qf[part_q][nt][2 * j + i][0], qf[part_q][nt][2 * j + i][1]);
+                            }
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub) {
+                    const float k0 = j & 1 ? bf16_hi(f0[sub][j >> 1]) : bf16_lo(f0[sub][j >> 1]), k1 = j & 1 ? bf16_hi(f1[sub][j >> 1]) : bf16_lo(f1[sub][j >> 1]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float f = e < 2 ? k0 : k1, y = acc[sub][nt][e] + q_off[nt][j][e & 1];
+                            s[sub][nt][e] = j == 0 ? y * f : fmaf(y, f, s[sub][nt][e]);
+                        }
+                }
+            }
+        } else {
+            float acc[SUB][NT][2][4];
+#pragma unroll
+            for (int half = 0; half < KS / 4; ++half) {
+                uint32_t w0[SUB][4], w1[SUB][4];
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub) {
+                    lds(w0[sub], (half ? kd ^ 64u : kd) + sub * 16 * RB);       // (rows of 128 bytes: chunks t and t + 4)
+                    lds(w1[sub], (half ? kd ^ 64u : kd) + (sub * 16 + 8) * RB);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int sub = 0; sub < SUB; ++sub) {
+                        const int k = 4 * half + i;
+                        const uint32_t x = w0[sub][i] ^ 0x80808080u, y = w1[sub][i] ^ 0x80808080u;
+                        const uint32_t a[4] = {__byte_perm(x, 0u, 0x4140), __byte_perm(y, 0u, 0x4140), __byte_perm(x, 0u, 0x4342), __byte_perm(y, 0u, 0x4342)};
+#pragma unroll
+                        for (int part_q = PARTS - 1; part_q >= 0; --part_q)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                if (k < 2 && part_q == PARTS - 1) mma_f16_first(acc[sub][nt][k], a, qf[part_q][nt][k][0], qf[part_q][nt][k][1]);
+                                else mma_f16(acc[sub][nt][k & 1], a, qf[part_q][nt][k][0], qf[part_q][nt][k][1]);
+                            }
+                    }
+            }
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub) {
+                const float k0 = __uint_as_float(lds1(sd + sub * 16 * SB)), k1 = __uint_as_float(lds1(sd + (sub * 16 + 8) * SB));
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const float f = u ? k1[j] : k0[j];
+                    for (int e = 0; e < 4; ++e) s[sub][nt][e] = (acc[sub][nt][0][e] + acc[sub][nt][1][e] + q_off[nt][0][e & 1]) * (e < 2 ? k0 : k1);
+            }
+        }
+        // ---- weights: s[sub][nt][2 u + e] is key 8 u + key_s of sixteen, row 8 nt + 2 (lane mod 4) + e ----
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[sub][nt][e] *= row_c[nt][e & 1];
+        if (va < wa || va + KEYS > wb) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int t = len - ql + (tile * ROWS + nt * 8 + 2 * t4 + e) / p.G;         // (of rows that are none: anything)
+#pragma unroll
+                    for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int v = va + 16 * sub + key_s + 8 * u;
+                            if (v >= v1 || !attend_sees(p, t, kr.key(v))) s[sub][nt][2 * u + e] = -INFINITY;
+                        }
+                }
+        }
+        float over = -INFINITY;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float top = fmaxf(s[0][nt][e], s[0][nt][2 + e]);
+#pragma unroll
+                for (int sub = 1; sub < SUB; ++sub) top = fmaxf(top, fmaxf(s[sub][nt][e], s[sub][nt][2 + e]));
+                over = fmaxf(over, top - m[nt][e]);
+            }
+        if (__any_sync(0xffffffffu, over > AQ_BIAS + AF_RAISE)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = s[0][nt][e];
+#pragma unroll
+                    for (int sub = 0; sub < SUB; ++sub) mx = fmaxf(mx, fmaxf(s[sub][nt][e], s[sub][nt][2 + e]));
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                    mx = fmaxf(mx - AQ_BIAS, m[nt][e]);
+                    const float f = ex2(m[nt][e] - mx);
+                    m[nt][e] = mx;
+                    l[nt][e] *= f;
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) { o[nt][k][e] *= f; o[nt][k][2 + e] *= f; }
+                }
+        }
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[sub][nt][e] = ex2(s[sub][nt][e] - m[nt][e & 1]);
+                    l[nt][e & 1] += s[sub][nt][e];
+                }
+        // ---- values ----
+        if constexpr (BITS == 4) {
+            uint32_t w[SUB][4][W], f0[SUB][GR / 2], f1[SUB][GR / 2];            // of keys lane mod 4 + 4 i
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) lds(w[sub][i], (i & 1 ? vd1 : vd0) + (sub * 16 + (i & 2) * 4) * RB);
+                lds(f0[sub], sd + Stage::SCALES + sub * 16 * SB);
+                lds(f1[sub], sd + Stage::SCALES + (sub * 16 + 8) * SB);
+            }
+#pragma unroll
+            for (int j = 0; j < GR; ++j) {
+                const int sel = j & 1 ? 0x7632 : 0x5410;
+                uint32_t pf[SUB][NT][WPARTS][2], ab[SUB][4], cd[SUB][4];
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const uint32_t fw = u ? f1[sub][j >> 1] : f0[sub][j >> 1];
+                            const float f = j & 1 ? bf16_hi(fw) : bf16_lo(fw);
+                            uint32_t pw[WPARTS];
+                            split_weights<WPARTS>(pw, s[sub][nt][2 * u] * f, s[sub][nt][2 * u + 1] * f);
+#pragma unroll
+                            for (int q = 0; q < WPARTS; ++q) pf[sub][nt][q][u] = transpose8x8(pw[q]);
+                        }
+                    nibbles(ab[sub], __byte_perm(w[sub][0][j >> 1], w[sub][1][j >> 1], sel));
+                    nibbles(cd[sub], __byte_perm(w[sub][2][j >> 1], w[sub][3][j >> 1], sel));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        ab[sub][i] = add_bf16(ab[sub][i], i & 1 ? AQ_MINUS_128 : AQ_MINUS_8);
+                        cd[sub][i] = add_bf16(cd[sub][i], i & 1 ? AQ_MINUS_128 : AQ_MINUS_8);
+                    }
+                }
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+                    for (int q = WPARTS - 1; q >= 0; --q)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const uint32_t a[4] = {ab[sub][2 * i], ab[sub][2 * i + 1], cd[sub][2 * i], cd[sub][2 * i + 1]};
+                                mma_bf16(o[nt][2 * j + i], a, pf[sub][nt][q][0], pf[sub][nt][q][1]);
+                            }
+            }
+        } else {
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub) {
+                uint32_t w[4][W], pf[NT][WPARTS][2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    lds(w[i], (i & 1 ? vd1 : vd0) + (sub * 16 + (i & 2) * 4) * RB);
+#pragma unroll
+                    for (int q = 0; q < W; ++q) w[i][q] ^= 0x80808080u;
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float f = __uint_as_float(lds1(sd + Stage::SCALES + (sub * 16 + 8 * u) * SB));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
                         uint32_t pw[WPARTS];
-                        split_weights<WPARTS>(pw, s[nt][2 * u] * f, s[nt][2 * u + 1] * f);
+                        split_weights<WPARTS>(pw, s[sub][nt][2 * u] * f, s[sub][nt][2 * u + 1] * f);
 #pragma unroll
                         for (int q = 0; q < WPARTS; ++q) pf[nt][q][u] = transpose8x8(pw[q]);
                     }
-                constexpr int MT = KS / GR;               // channel tiles of the group
-                if constexpr (BITS == 4) {
-                    const int sel = j & 1 ? 0x7632 : 0x5410;
-                    const uint32_t ab = __byte_perm(w[0][j >> 1], w[1][j >> 1], sel), cd = __byte_perm(w[2][j >> 1], w[3][j >> 1], sel);
+                }
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const uint32_t a[4] = {nibble_bf16(ab, 2 * i), nibble_bf16(ab, 2 * i + 1), nibble_bf16(cd, 2 * i), nibble_bf16(cd, 2 * i + 1)};
+                for (int i = 0; i < KS; ++i) {
+                    uint32_t a[4];
+                    byte_pairs(a[0], a[1], w[0][i >> 1], w[1][i >> 1], 2 * (i & 1));
+                    byte_pairs(a[2], a[3], w[2][i >> 1], w[3][i >> 1], 2 * (i & 1));
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                    for (int e = 0; e < 4; ++e) a[e] = add_bf16(a[e], AQ_MINUS_128);
 #pragma unroll
-                            for (int q = WPARTS - 1; q >= 0; --q) mma_bf16(o[nt][2 * j + i], a, pf[nt][q][0], pf[nt][q][1]);
-                    }
-                } else {
+                    for (int q = WPARTS - 1; q >= 0; --q)
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const int q0 = i >> 1, n0 = 2 * (i & 1);
-                        const uint32_t a[4] = {byte_pair_bf16(w[0][q0], w[1][q0], n0), byte_pair_bf16(w[0][q0], w[1][q0], n0 + 1),
-                                               byte_pair_bf16(w[2][q0], w[3][q0], n0), byte_pair_bf16(w[2][q0], w[3][q0], n0 + 1)};
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int q = WPARTS - 1; q >= 0; --q) mma_bf16(o[nt][i], a, pf[nt][q][0], pf[nt][q][1]);
-                    }
+                        for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][i], a, pf[nt][q][0], pf[nt][q][1]);
                 }
             }
         }
@@ -453,6 +546,7 @@ __global__ void __launch_bounds__(AF_NT) k_attend_quant(const __grid_constant__ 
 
     // the warps' results: O as [warp][row][D + 4], then references and sums; tile k of O holds channels (lane / 4) D / 8 + 2 k, + 1
     constexpr int LD = D + 4;
+    constexpr float O2 = BITS == 4 ? 0x1p63f : 0x1p67f;
     float *osm = reinterpret_cast<float *>(aq_sm), *ml = osm + AF_WARPS * ROWS * LD;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -465,7 +559,7 @@ __global__ void __launch_bounds__(AF_NT) k_attend_quant(const __grid_constant__ 
             if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt][e]; ml[(warp * ROWS + row) * 2 + 1] = z; }
 #pragma unroll
             for (int k = 0; k < KS; k += 2)
-                *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e], o[nt][k][2 + e], o[nt][k + 1][e], o[nt][k + 1][2 + e]);
+                *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e] * 0x1p66f * 0x1p67f, o[nt][k][2 + e] * 0x1p66f * O2, o[nt][k + 1][e] * 0x1p66f * 0x1p67f, o[nt][k + 1][2 + e] * 0x1p66f * O2);
         }
     __syncthreads();
     few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, kr, v0, v1);

@@ -174,7 +174,14 @@ struct QuantLayout {
 // Query rows of a tile.
 static int quant_rows(long long rows) { return rows <= 8 ? 8 : 16; }
 
-constexpr int QUANT_RESIDENT = 3 * 148;
+// Blocks of k_attend_quant that run at once.
+static int quant_resident(int dtype, int head_dim, int rows)
+{
+    const int f = rows == 8 ? (head_dim == 64 ? AQ_BLOCKS<float, 64, 1> : AQ_BLOCKS<float, 128, 1>) : (head_dim == 64 ? AQ_BLOCKS<float, 64, 2> : AQ_BLOCKS<float, 128, 2>);
+    const int h = rows == 8 ? (head_dim == 64 ? AQ_BLOCKS<__nv_bfloat16, 64, 1> : AQ_BLOCKS<__nv_bfloat16, 128, 1>)
+                            : (head_dim == 64 ? AQ_BLOCKS<__nv_bfloat16, 64, 2> : AQ_BLOCKS<__nv_bfloat16, 128, 2>);
+    return 148 * (dtype == OBF_F32 ? f : h);
+}
 
 static QuantLayout quant_layout(const obf_attend_t *a)
 {
@@ -182,9 +189,10 @@ static QuantLayout quant_layout(const obf_attend_t *a)
     const long long rows_seq = (long long)(a->q_heads / a->kv_heads) * a->n_q, heads = (long long)a->batch * a->kv_heads, rows = heads * rows_seq;
     const int t = quant_rows(rows_seq);
     const long long tiles = heads * ((rows_seq + t - 1) / t), keys = most_keys(a, t);
-    const bool small = 8 * tiles <= QUANT_RESIDENT && keys <= 4096;
-    L.slots = small ? parts_for(1, keys, 8, 64) : few_parts(tiles, keys, QUANT_RESIDENT);
-    L.cluster = L.slots > 1 && L.slots <= 8 && tiles * L.slots <= QUANT_RESIDENT;
+    const int resident = quant_resident(a->dtype, a->head_dim, t);
+    const bool small = 8 * tiles <= resident && keys <= 4096;
+    L.slots = small ? parts_for(1, keys, 8, 64) : few_parts(tiles, keys, resident);
+    L.cluster = L.slots > 1 && L.slots <= 8 && tiles * L.slots <= resident;
     const bool join = L.slots > 1 && !L.cluster;
     size_t o = 256;
     L.off_part_o = o;
