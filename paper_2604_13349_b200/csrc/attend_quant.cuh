@@ -29,7 +29,7 @@ struct QuantStage {
     static constexpr int KEYS = Row::BYTES == 128 ? 16 : 32;
     static constexpr int CODES = KEYS * Row::BYTES, SCALES = KEYS * Row::SCALE_BYTES;
     static constexpr int BYTES = 2 * CODES + 2 * SCALES;               // K's codes, V's codes, K's scales, V's scales
-    static constexpr int STAGES = BYTES > 4000 ? 3 : 4;
+    static constexpr int STAGES = BYTES > 4400 ? 2 : BYTES > 4000 ? 2 : 3;
 };
 
 template <int BITS, int D, int ROWS>
@@ -52,6 +52,12 @@ __device__ __forceinline__ uint32_t chunk_at(int key, int c)
     return (key ^ ((key >> 1) & 2)) * 32 + c * 16;
 }
 
+template <int N>
+__device__ __forceinline__ void cp_async_all(uint32_t dst, const void *src)
+{
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(N) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void cp_async_small(uint32_t dst, const void *src, bool real)
 {
@@ -98,8 +104,8 @@ __device__ __forceinline__ void nibbles(uint32_t (&r)[4], uint32_t x)
     r[2] = (x >> 8) & 0x000f000fu;
     r[3] = (x >> 8) & 0x00f000f0u;
 }
-// Their offsets: of bf16 pairs, 8 in the first kind of place and 8 * 16 in the second; 128.
-constexpr uint32_t AQ_MINUS_8 = 0x80088008u, AQ_MINUS_128 = 0x80808080u;
+// Their offsets: of bf16 pairs, 8 in the first kind of place, 8 * 16 in the second, both; 128 of bytes.
+constexpr uint32_t AQ_MINUS_8 = 0x80088008u, AQ_MINUS_128 = 0x80808080u, AQ_MINUS_136 = 0x80888088u;
 __device__ __forceinline__ uint32_t add_bf16(uint32_t x, uint32_t y)
 {
     uint32_t r;
@@ -128,6 +134,113 @@ __device__ __forceinline__ void split_weights(uint32_t (&r)[PARTS], float x, flo
     }
 }
 
+// A warp's way through its part of the keys: which it is, and the ring of stages that it copies them through.
+template <int BITS, int D>
+struct QuantWalk {
+    typedef QuantStage<BITS, D> Stage;
+    typedef QuantRow<BITS, D> Row;
+    static constexpr int ST = Stage::STAGES, KEYS = Stage::KEYS, RB = Row::BYTES, CH = RB / 16, LR = 32 / CH, SB = Row::SCALE_BYTES, NEXT = AF_WARPS * KEYS;
+    const QuantDev &c;
+    KeyRange kr;
+    int v0, v1;                            // the part: keys v0 .. v1 - 1 of the walk
+    int wa, wb;                            // keys wa .. wb - 1 are seen by every row of the tile
+    uint32_t ring, own_chunk, own_scale;
+    // This warp's stages begin at keys v0 + warp KEYS and every fourth stage from there.  The next one to be fetched has its rows at kp,
+    // vp (row lr of it) and scales at ksp, vsp (row `lane`) if it lies whole behind the sinks; where it does not, each row's place is worked out.
+    const uint8_t *kp, *vp, *ksp, *vsp;
+    int lane, lr, lc;
+    bool dense;                            // rows are neighbours in memory: constant steps
+
+    __device__ __forceinline__ QuantWalk(const AttendDev &p, const QuantDev &c, unsigned char *sm, int b, int h, int len, int ql, int i0, int i1, int part, int parts)
+        : c(c), kr{0, 0, 0}
+    {
+        const int warp = threadIdx.x >> 5;
+        lane = threadIdx.x & 31;
+        lc = lane % CH;
+        lr = lane / CH;
+        const int t0 = len - ql + i0, t1 = len - ql + i1;
+        if (i0 <= i1) kr = attend_range(p, t0, t1, len);
+        const int n = kr.count(), per = ((n + 63) / 64 + parts - 1) / parts * 64;
+        v0 = min((long long)part * per, (long long)n);
+        v1 = min(v0 + per, n);
+        wa = 0;
+        wb = v1;
+        if (p.n_q > 1) {
+            wb = min(v1, kr.s + max(0, t0 + 1 - kr.lo));
+            if (p.window && t1 - p.window + 1 > kr.lo) wa = kr.s + t1 - p.window + 1 - kr.lo;
+        }
+        ring = (uint32_t)__cvta_generic_to_shared(sm) + warp * ST * Stage::BYTES;
+        own_chunk = ring + chunk_at<RB>(lr, lc);
+        own_scale = ring + 2 * Stage::CODES + lane * SB;
+        const long long j0 = (long long)v0 + warp * KEYS - kr.s + kr.lo;
+        kp = c.k + b * c.ks[0] + h * c.ks[1] + (j0 + lr) * c.ks[2] + lc * 16;
+        vp = c.v + b * c.vs[0] + h * c.vs[1] + (j0 + lr) * c.vs[2] + lc * 16;
+        ksp = c.k_scale + b * c.kss[0] + h * c.kss[1] + (j0 + lane) * c.kss[2];
+        vsp = c.v_scale + b * c.vss[0] + h * c.vss[1] + (j0 + lane) * c.vss[2];
+        dense = c.ks[2] == RB && c.vs[2] == RB;
+#pragma unroll
+        for (int s = 0; s < ST - 1; ++s) fetch(v0 + (warp + s * AF_WARPS) * KEYS, s);
+    }
+    __device__ __forceinline__ int first() const { return v0 + (int)(threadIdx.x >> 5) * KEYS; }
+    __device__ __forceinline__ bool whole(int va) const { return va >= wa && va + KEYS <= wb; }
+
+    __device__ __forceinline__ void fetch(int va, int slot)
+    {
+        const uint32_t off = slot * Stage::BYTES;
+        if (va >= kr.s && va + KEYS <= v1) {
+            // (rows LR apart stand alike, but that at 128 bytes every second one has its chunks' halves exchanged)
+            const uint32_t at[2] = {own_chunk + off, (RB == 128 ? own_chunk ^ 64u : own_chunk) + off};
+            if (dense) {
+#pragma unroll
+                for (int i = 0; i < KEYS / LR; ++i) {
+                    cp_async_all<16>(at[i & 1] + i * LR * RB, kp + i * LR * RB);
+                    cp_async_all<16>(at[i & 1] + i * LR * RB + Stage::CODES, vp + i * LR * RB);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < KEYS / LR; ++i) {
+                    cp_async_all<16>(at[i & 1] + i * LR * RB, kp + i * LR * c.ks[2]);
+                    cp_async_all<16>(at[i & 1] + i * LR * RB + Stage::CODES, vp + i * LR * c.vs[2]);
+                }
+            }
+            if (KEYS == 32 || lane < KEYS) {
+                cp_async_all<SB>(own_scale + off, ksp);
+                cp_async_all<SB>(own_scale + off + Stage::SCALES, vsp);
+            }
+        } else if (va < v1) {
+            const int at_va = va - kr.s + kr.lo;
+#pragma unroll 1
+            for (int i = 0; i < KEYS / LR; ++i) {
+                const int r = lr + i * LR, v = va + r;
+                const bool real = v < v1;                 // (behind the part: zeros, whatever the cache holds there)
+                const long long step = kr.key(real ? v : v0) - (at_va + lr);
+                const uint32_t at = ring + off + chunk_at<RB>(r, lc);
+                cp_async16(at, kp + step * c.ks[2], real);
+                cp_async16(at + Stage::CODES, vp + step * c.vs[2], real);
+            }
+            if (lane < KEYS) {
+                const int v = va + lane;
+                const bool real = v < v1;
+                const long long step = kr.key(real ? v : v0) - (at_va + lane);
+                cp_async_small<SB>(own_scale + off, ksp + step * c.kss[2], real);
+                cp_async_small<SB>(own_scale + off + Stage::SCALES, vsp + step * c.vss[2], real);
+            }
+        }
+        cp_commit();
+        kp += NEXT * c.ks[2];
+        vp += NEXT * c.vs[2];
+        ksp += NEXT * c.kss[2];
+        vsp += NEXT * c.vss[2];
+    }
+    // Waits for the stage of keys va .., in `slot`, and has the one behind those under way fetched to the slot that was read last.
+    __device__ __forceinline__ void next(int va, int slot)
+    {
+        cp_wait<ST - 2>();
+        __syncwarp();
+        fetch(va + (ST - 1) * NEXT, slot == 0 ? ST - 1 : slot - 1);
+    }
+};
+
 // Blocks of a multiprocessor.
 template <typename TIN, int D, int NT>
 constexpr int AQ_BLOCKS = NT == 1 ? (sizeof(TIN) == 4 && D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
@@ -154,70 +267,9 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
     const int h = x % p.kv_heads, b = x / p.kv_heads;
     const int len = attend_len(p, b), ql = attend_q_len(p, b);
 
-    KeyRange kr = {0, 0, 0};
     const int i0 = tile * ROWS / p.G, i1 = min((min((tile + 1) * ROWS, rows_seq) - 1) / p.G, ql - 1);
-    if (i0 <= i1) kr = attend_range(p, len - ql + i0, len - ql + i1, len);
-    const int n = kr.count(), per = ((n + 63) / 64 + parts - 1) / parts * 64;
-    const int v0 = min((long long)part * per, (long long)n), v1 = min(v0 + per, n);
-
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(aq_sm) + warp * ST * Stage::BYTES;
-    const int lc = lane % CH, lr = lane / CH;
-    // This warp's stages begin at keys va = v0 + warp KEYS and every fourth stage from there.  The next one to be fetched has its rows at
-    // kp, vp (row lr of it) and scales at ksp, vsp (row `lane`) if it lies whole behind the sinks; where it does not, each row's place is worked out.
-    const long long j0 = (long long)v0 + warp * KEYS - kr.s + kr.lo;
-    const uint8_t *kp = c.k + b * c.ks[0] + h * c.ks[1] + (j0 + lr) * c.ks[2] + lc * 16, *vp = c.v + b * c.vs[0] + h * c.vs[1] + (j0 + lr) * c.vs[2] + lc * 16;
-    const uint8_t *ksp = c.k_scale + b * c.kss[0] + h * c.kss[1] + (j0 + lane) * c.kss[2], *vsp = c.v_scale + b * c.vss[0] + h * c.vss[1] + (j0 + lane) * c.vss[2];
-    const bool dense = c.ks[2] == RB && c.vs[2] == RB;    // neighbours in memory: constant steps
-    const uint32_t own_chunk = ring + chunk_at<RB>(lr, lc), own_scale = ring + 2 * Stage::CODES + lane * SB;
-    auto fetch = [&](int va, int slot) {
-        const uint32_t off = slot * Stage::BYTES;
-        if (va >= kr.s && va + KEYS <= v1) {
-            // (rows LR apart stand alike, but that at 128 bytes every second one has its chunks' halves exchanged)
-            const uint32_t at[2] = {own_chunk + off, (RB == 128 ? own_chunk ^ 64u : own_chunk) + off};
-            if (dense) {
-#pragma unroll
-                for (int i = 0; i < KEYS / LR; ++i) {
-                    cp_async16(at[i & 1] + i * LR * RB, kp + i * LR * RB, true);
-                    cp_async16(at[i & 1] + i * LR * RB + Stage::CODES, vp + i * LR * RB, true);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < KEYS / LR; ++i) {
-                    cp_async16(at[i & 1] + i * LR * RB, kp + i * LR * c.ks[2], true);
-                    cp_async16(at[i & 1] + i * LR * RB + Stage::CODES, vp + i * LR * c.vs[2], true);
-                }
-            }
-            if (KEYS == 32 || lane < KEYS) {
-                cp_async_small<SB>(own_scale + off, ksp, true);
-                cp_async_small<SB>(own_scale + off + Stage::SCALES, vsp, true);
-            }
-        } else if (va < v1) {
-            const int at_va = va - kr.s + kr.lo;
-#pragma unroll 1
-            for (int i = 0; i < KEYS / LR; ++i) {
-                const int r = lr + i * LR, v = va + r;
-                const bool real = v < v1;                 // (behind the part: zeros, whatever the cache holds there)
-                const long long step = kr.key(real ? v : v0) - (at_va + lr);
-                const uint32_t at = ring + off + chunk_at<RB>(r, lc);
-                cp_async16(at, kp + step * c.ks[2], real);
-                cp_async16(at + Stage::CODES, vp + step * c.vs[2], real);
-            }
-            if (lane < KEYS) {
-                const int v = va + lane;
-                const bool real = v < v1;
-                const long long step = kr.key(real ? v : v0) - (at_va + lane);
-                cp_async_small<SB>(own_scale + off, ksp + step * c.kss[2], real);
-                cp_async_small<SB>(own_scale + off + Stage::SCALES, vsp + step * c.vss[2], real);
-            }
-        }
-        cp_commit();
-        kp += AF_WARPS * KEYS * c.ks[2];
-        vp += AF_WARPS * KEYS * c.vs[2];
-        ksp += AF_WARPS * KEYS * c.kss[2];
-        vsp += AF_WARPS * KEYS * c.vss[2];
-    };
-#pragma unroll
-    for (int s = 0; s < ST - 1; ++s) fetch(v0 + (warp + s * AF_WARPS) * KEYS, s);
+    QuantWalk<BITS, D> walk(p, c, aq_sm, b, h, len, ql, i0, i1, part, parts);
+    const uint32_t ring = walk.ring;
 
     // Queries as B fragments: of row 8 nt + lane / 4 a lane holds a quarter of the channels, those of its words of a key.
     uint32_t qf[PARTS][NT][KS][2];
@@ -293,13 +345,6 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[nt][k][e] = 0.f;
     }
-    // keys wa .. wb - 1 of the walk are seen by every row of the tile
-    int wa = 0, wb = v1;
-    if (p.n_q > 1) {
-        const int t0 = len - ql + i0, t1 = len - ql + i1;
-        wb = min(v1, kr.s + max(0, t0 + 1 - kr.lo));
-        if (p.window && t1 - p.window + 1 > kr.lo) wa = kr.s + t1 - p.window + 1 - kr.lo;
-    }
     // Row r of a 16-key product stands for key  r / 2 + 4 (r mod 2)  of its half of eight: a lane then reads four neighbouring keys' values.
     const int key_s = (g8 >> 1) + 4 * (g8 & 1);
     // What this lane reads of sixteen keys: of K words of keys key_s and key_s + 8, of V words of keys lane mod 4 + 4 i, the second half of
@@ -312,10 +357,8 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
         v_at[i] = ring + Stage::CODES + (W == 4 ? chunk_at<RB>(t4 + 4 * i, g8) : W == 2 ? chunk_at<RB>(t4 + 4 * i, g8 >> 1) + (g8 & 1) * 8 : chunk_at<RB>(t4 + 4 * i, g8 >> 2) + (g8 & 3) * 4);
     const uint32_t s_at = ring + 2 * Stage::CODES + key_s * SB;
     int slot = 0;
-    for (int va = v0 + warp * KEYS; va < v1; va += AF_WARPS * KEYS) {
-        cp_wait<ST - 2>();
-        __syncwarp();
-        fetch(va + (ST - 1) * AF_WARPS * KEYS, slot == 0 ? ST - 1 : slot - 1);
+    for (int va = walk.first(); va < walk.v1; va += AF_WARPS * KEYS) {
+        walk.next(va, slot);
         const uint32_t off = slot * Stage::BYTES, kd = k_at + off, vd0 = v_at[0] + off, vd1 = v_at[1] + off, sd = s_at + off;
         float s[SUB][NT][4];
         // ---- logits (products that wait for one another are kept apart by those of the other sixteen keys) ----
@@ -405,7 +448,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[sub][nt][e] *= row_c[nt][e & 1];
-        if (va < wa || va + KEYS > wb) {
+        if (!walk.whole(va)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -416,7 +459,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
                             const int v = va + 16 * sub + key_s + 8 * u;
-                            if (v >= v1 || !attend_sees(p, t, kr.key(v))) s[sub][nt][2 * u + e] = -INFINITY;
+                            if (v >= walk.v1 || !attend_sees(p, t, walk.kr.key(v))) s[sub][nt][2 * u + e] = -INFINITY;
                         }
                 }
         }
@@ -562,7 +605,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
                 *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e] * 0x1p66f * 0x1p67f, o[nt][k][2 + e] * 0x1p66f * O2, o[nt][k + 1][e] * 0x1p66f * 0x1p67f, o[nt][k + 1][2 + e] * 0x1p66f * O2);
         }
     __syncthreads();
-    few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, kr, v0, v1);
+    few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, walk.kr, walk.v0, walk.v1);
 }
 
 }  // namespace obf

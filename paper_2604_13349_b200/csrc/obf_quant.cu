@@ -3,6 +3,7 @@
 
 #include "attend_host.cuh"
 #include "attend_quant.cuh"
+#include "attend_quant_few.cuh"
 #include "host.cuh"
 #include "quant_cache.cuh"
 
@@ -171,16 +172,14 @@ struct QuantLayout {
     size_t off_part_o, off_part_lse, total;
 };
 
-// Query rows of a tile.
-static int quant_rows(long long rows) { return rows <= 8 ? 8 : 16; }
+// Query rows of a tile: 4 and 8 of k_attend_quant_few, 16 of k_attend_quant.
+static int quant_rows(long long rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
 
-// Blocks of k_attend_quant that run at once.
+// Blocks that run at once.
 static int quant_resident(int dtype, int head_dim, int rows)
 {
-    const int f = rows == 8 ? (head_dim == 64 ? AQ_BLOCKS<float, 64, 1> : AQ_BLOCKS<float, 128, 1>) : (head_dim == 64 ? AQ_BLOCKS<float, 64, 2> : AQ_BLOCKS<float, 128, 2>);
-    const int h = rows == 8 ? (head_dim == 64 ? AQ_BLOCKS<__nv_bfloat16, 64, 1> : AQ_BLOCKS<__nv_bfloat16, 128, 1>)
-                            : (head_dim == 64 ? AQ_BLOCKS<__nv_bfloat16, 64, 2> : AQ_BLOCKS<__nv_bfloat16, 128, 2>);
-    return 148 * (dtype == OBF_F32 ? f : h);
+    if (rows == 16) return 148 * (head_dim == 64 ? 3 : 2);
+    return 148 * (dtype == OBF_F32 ? (rows == 4 ? AQF_BLOCKS<float, 1> : AQF_BLOCKS<float, 2>) : (rows == 4 ? AQF_BLOCKS<__nv_bfloat16, 1> : AQF_BLOCKS<__nv_bfloat16, 2>));
 }
 
 static QuantLayout quant_layout(const obf_attend_t *a)
@@ -208,10 +207,14 @@ static obf_status_t launch_quant_rows(const AttendDev &p, const QuantDev &d, cud
 {
     static bool done[64];
     constexpr size_t smem = attend_quant_smem<BITS, D, ROWS>();
-    OBF_TRY(set_smem_once(k_attend_quant<T, BITS, D, ROWS / 8, CLUSTER>, smem, done));
+    const auto kernel = [] {
+        if constexpr (ROWS == 16) return k_attend_quant<T, BITS, D, 2, CLUSTER>;
+        else return k_attend_quant_few<T, BITS, D, ROWS / 4, CLUSTER>;
+    }();
+    OBF_TRY(set_smem_once(kernel, smem, done));
     const long long blocks = (long long)p.slots * (((long long)p.n_q * p.G + ROWS - 1) / ROWS) * p.kv_heads * p.batch;
     if (blocks > INT_MAX) return OBF_ERR_UNSUPPORTED;
-    OBF_TRY(launch_clusters(CLUSTER ? p.slots : 1, k_attend_quant<T, BITS, D, ROWS / 8, CLUSTER>, dim3((unsigned)blocks), AF_NT, smem, st, p, d));
+    OBF_TRY(launch_clusters(CLUSTER ? p.slots : 1, kernel, dim3((unsigned)blocks), AF_NT, smem, st, p, d));
     ++g_last_launches;
     return OBF_OK;
 }
@@ -219,9 +222,15 @@ static obf_status_t launch_quant_rows(const AttendDev &p, const QuantDev &d, cud
 template <typename T, int BITS, int D>
 static obf_status_t launch_quant(const AttendDev &p, const QuantDev &d, cudaStream_t st)
 {
-    const bool few = quant_rows((long long)p.n_q * p.G) == 8;
-    if (p.cluster) return few ? launch_quant_rows<T, BITS, D, 8, true>(p, d, st) : launch_quant_rows<T, BITS, D, 16, true>(p, d, st);
-    OBF_TRY(few ? (launch_quant_rows<T, BITS, D, 8, false>(p, d, st)) : (launch_quant_rows<T, BITS, D, 16, false>(p, d, st)));
+    const auto rows = [&](auto cluster) -> obf_status_t {
+        switch (quant_rows((long long)p.n_q * p.G)) {
+        case 4: return launch_quant_rows<T, BITS, D, 4, cluster.value>(p, d, st);
+        case 8: return launch_quant_rows<T, BITS, D, 8, cluster.value>(p, d, st);
+        default: return launch_quant_rows<T, BITS, D, 16, cluster.value>(p, d, st);
+        }
+    };
+    if (p.cluster) return rows(std::true_type());
+    OBF_TRY(rows(std::false_type()));
     if (p.slots > 1) OBF_TRY((launch_join<T, D>(p, st)));
     return OBF_OK;
 }
