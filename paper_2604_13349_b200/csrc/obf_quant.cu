@@ -68,11 +68,10 @@ static obf_status_t with_shape(int dtype, int bits, int head_dim, F body)
     return dtype == OBF_F32 ? bits_dim(float()) : bits_dim(__nv_bfloat16());
 }
 
-// The rows of a call to write or read; UNSUPPORTED where they cannot be numbered in 31 bits.
-static obf_status_t rows_dev(RowsDev *p, int batch, int kv_heads, int rows, int first, int capacity, const int32_t *lens, unsigned *blocks, int head_dim)
+// The rows of a call to write or read, `per` a block; UNSUPPORTED where they cannot be numbered in 31 bits.
+static obf_status_t rows_dev(RowsDev *p, int batch, int kv_heads, int rows, int first, int capacity, const int32_t *lens, unsigned *blocks, int per)
 {
     const long long half = (long long)batch * kv_heads * rows;
-    const int per = QC_NT / (head_dim / 8) * QC_AHEAD;    // rows of a block
     if (2 * half > INT_MAX - per) return OBF_ERR_UNSUPPORTED;
     p->lens = lens;
     p->rows = rows; p->first = first; p->capacity = capacity;
@@ -109,7 +108,7 @@ static obf_status_t quant_write(const obf_quantized_write_t *a, const obf_quanti
     OBF_TRY(validate_words(a->lens, a->new_lens));
     RowsDev p = {};
     unsigned blocks;
-    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->rows, 0, a->capacity, a->lens, &blocks, a->head_dim));
+    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->rows, 0, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 16) * QC_AHEAD));
     p.new_lens = a->new_lens;
     p.k = a->k; p.v = a->v; p.k_out = a->k_values; p.v_out = a->v_values;
     for (int i = 0; i < 3; ++i) { p.ks[i] = a->k_stride[i]; p.vs[i] = a->v_stride[i]; p.kos[i] = a->k_values_stride[i]; p.vos[i] = a->v_values_stride[i]; }
@@ -139,7 +138,7 @@ static obf_status_t quant_read(const obf_quantized_read_t *a, const obf_quantize
     OBF_TRY(validate_words(a->lens, nullptr));
     RowsDev p = {};
     unsigned blocks;
-    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->rows, a->first, a->capacity, a->lens, &blocks, a->head_dim));
+    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->rows, a->first, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 8) * QR_AHEAD));
     p.k_out = a->k_out; p.v_out = a->v_out;
     for (int i = 0; i < 3; ++i) { p.kos[i] = a->k_out_stride[i]; p.vos[i] = a->v_out_stride[i]; }
     const QuantDev d = quant_dev(c);

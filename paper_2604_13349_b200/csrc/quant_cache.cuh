@@ -57,39 +57,44 @@ struct RowsDev {
 };
 
 constexpr int QC_NT = 256;
-constexpr int QC_AHEAD = 4;                // rows of a thread in flight
-
-// x * 1 / scale rounded to a whole number as the quotient would be.  bf16 numbers over a scale of five bits: the quotient is n + 1/2
-// exactly or at least 1/496 away from it (2 x and (2 n + 1) scale are multiples of an eighth of the scale's last bit), so rounding the
-// product to a multiple of 2^-10 first undoes its error of 2^-21.  fp32 numbers are divided.
-template <typename T>
-__device__ __forceinline__ float code4(float x, float scale, float inv)
-{
-    if constexpr (sizeof(T) == 4) return rintf(__fdiv_rn(x, scale));
-    constexpr float GRID = 12288.f;        // 1.5 * 2^13
-    return rintf(__fadd_rn(__fadd_rn(x * inv, GRID), -GRID));
-}
-
-// 8 bits: the code is the whole number nearest to the fp32 quotient, from which the product is off by at most 2.3e-5.
-__device__ __forceinline__ float code8(float x, float scale, float inv)
-{
-    const float pr = x * inv;
-    float v = rintf(pr);
-    if (fabsf(fabsf(pr - v) - 0.5f) < 2.44140625e-4f) v = rintf(__fdiv_rn(x, scale));
-    return v;
-}
+constexpr int QC_AHEAD = 2;                // rows of a thread in flight
 
 // Scale of numbers whose largest magnitude has the bits `top` (as integers, so that what is not a number counts as the largest): not a
 // number where one of them is not finite, zero where all are below 2^-110, whose scale would lose bits.
-template <int BITS>
-__device__ __forceinline__ float scale_of(uint32_t top)
+__device__ __forceinline__ float scale8(uint32_t top)
 {
-    if (top >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
-    if (top < (127u - 110u) << 23) return 0.f;
+    const float s = __fdiv_rn(__uint_as_float(top), 127.f);
+    return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : top < (127u - 110u) << 23 ? 0.f : s;
+}
+// max / 7 rounded half to even to five bits.  Of a bf16 maximum the product with 1 / 7, rounded to 17 bits first, will do: the quotient is halfway
+// between two numbers of five bits or at least 2^-12 of itself away from there.
+template <typename T>
+__device__ __forceinline__ float scale4(uint32_t top)
+{
     const float x = __uint_as_float(top);
-    if constexpr (BITS == 8) return __fdiv_rn(x, 127.f);
-    const uint32_t i = __float_as_uint(__fdiv_rn(x, 7.f));
-    return __uint_as_float((i + 0x3ffffu + ((i >> 19) & 1u)) & 0xfff80000u);
+    uint32_t i;
+    if constexpr (sizeof(T) == 4) i = __float_as_uint(__fdiv_rn(x, 7.f));
+    else i = (__float_as_uint(x * (1.f / 7.f)) + 0x40u) & ~0x7fu;
+    const float s = __uint_as_float((i + 0x3ffffu + ((i >> 19) & 1u)) & 0xfff80000u);
+    return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : top < (127u - 110u) << 23 ? 0.f : s;
+}
+
+// Codes as the low bits of fp32 numbers near 1.5 * 2^23, where a sum is rounded to a whole number, half to even.
+constexpr float QC_ONES = 12582912.f;
+
+// x / scale in 4 bits, plus QC_ONES + 8.  bf16 numbers over a scale of five bits: the quotient is n + 1/2 exactly or at least 1/496 away from it
+// (2 x and (2 n + 1) scale are multiples of an eighth of the scale's last bit), so rounding the product to a multiple of 2^-10 (at
+// 1.5 * 2^13) first undoes its error of 2^-20.  fp32 numbers: the product tells, or where it is too near to n + 1/2 for that, the quotient.
+template <typename T>
+__device__ __forceinline__ float code4(float x, float scale, float inv)
+{
+    if constexpr (sizeof(T) == 2) {
+        constexpr float GRID = 12288.f;
+        return __fadd_rn(__fmaf_rn(x, inv, GRID), QC_ONES + 8.f - GRID);
+    } else {
+        const float t = __fmaf_rn(x, inv, QC_ONES + 8.f), d = __fmaf_rn(x, inv, -(t - (QC_ONES + 8.f)));
+        return fabsf(d) > 0.49995f ? __fadd_rn(__fdiv_rn(x, scale), QC_ONES + 8.f) : t;
+    }
 }
 
 template <typename T>
@@ -140,135 +145,267 @@ __device__ __forceinline__ RowAt row_at(const RowsDev &p, uint32_t f)
     return r;
 }
 
-// Writing: D / 8 lanes a row, eight channels each; a thread's rows are all read before the first of them is worked on.  Bound by HBM where there
-// are many rows, by the latency of a launch and two dependent reads where there are few.
-template <typename T, int BITS, int D, bool VALUES>
-__global__ void __launch_bounds__(QC_NT) k_quant_write(const __grid_constant__ RowsDev p, const __grid_constant__ QuantDev c)
+// Sixteen neighbouring channels of a row, as loaded.
+template <typename T>
+struct Sixteen {
+    Eight<T> half[2];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        half[0].load(p);
+        half[1].load(p + 8);
+    }
+};
+
+// Largest magnitudes of the four groups that sixteen channels in 4 bits belong to (four neighbours each), as bits.
+template <typename T>
+__device__ __forceinline__ void tops4(uint32_t (&top)[4], const Sixteen<T> &in, int lanes)
 {
-    pdl_wait();
-    pdl_trigger();
-    constexpr int L = D / 8, R = QC_NT / L;              // lanes of a row, rows of a block at a time
+    if constexpr (sizeof(T) == 2) {
+        // two groups in a word: bf16 magnitudes compare as 16-bit numbers
+        uint32_t two[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint4 w = in.half[i].w[0];
+            const uint32_t a = __vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), b = __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu);
+            two[i] = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+        }
+        if (lanes == 4) two[0] = two[1] = __vmaxu2(two[0], two[1]);            // heads of 64 channels have two groups
+#pragma unroll
+        for (int w = 1; w < 8; w <<= 1) {
+            if (w >= lanes) continue;
+            two[0] = __vmaxu2(two[0], __shfl_xor_sync(0xffffffffu, two[0], w));
+            if (lanes == 8) two[1] = __vmaxu2(two[1], __shfl_xor_sync(0xffffffffu, two[1], w));
+        }
+        if (lanes == 4) two[1] = two[0];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) { top[2 * i] = two[i] << 16; top[2 * i + 1] = two[i] & 0xffff0000u; }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 w = in.half[i / 2].w[i % 2];
+            top[i] = max(max(w.x & 0x7fffffffu, w.y & 0x7fffffffu), max(w.z & 0x7fffffffu, w.w & 0x7fffffffu));
+        }
+        if (lanes == 4) { top[0] = top[2] = max(top[0], top[2]); top[1] = top[3] = max(top[1], top[3]); }
+#pragma unroll
+        for (int w = 1; w < 8; w <<= 1) {
+            if (w >= lanes) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], w));
+        }
+    }
+}
+
+// Writing: D / 16 lanes a row, sixteen channels each; a thread's rows are all read before the first of them is worked on.  Blocks whose rows are
+// all one head's have their places in common.  Bound by HBM where there are many rows (prompts of 3001 to 8192, with values: WRITE_US us), by
+// the latency of a launch and two dependent reads where there are few.
+template <typename T, int BITS, int D, bool VALUES, bool ONE>
+__device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c, const RowAt &head)
+{
+    constexpr int L = D / 16, R = QC_NT / L;              // lanes of a row, rows of a block at a time
     const int l = threadIdx.x % L;
-    const uint32_t f0 = blockIdx.x * (R * QC_AHEAD) + threadIdx.x / L;
-    Eight<T> in[QC_AHEAD];
+    Sixteen<T> in[QC_AHEAD];
     RowAt at[QC_AHEAD];
     int pos[QC_AHEAD];                                    // row of the cache, or -1: not written
 #pragma unroll
     for (int u = 0; u < QC_AHEAD; ++u) {
-        const uint32_t f = f0 + u * R;
+        const uint32_t k = u * R + threadIdx.x / L, f = blockIdx.x * (R * QC_AHEAD) + k;
         pos[u] = -1;
         in[u] = {};
-        if (f >= p.total) continue;
-        at[u] = row_at(p, f);
+        if (!ONE && f >= p.total) continue;
+        at[u] = ONE ? head : row_at(p, f);
+        if (ONE) at[u].i += k;
         const int n_new = p.new_lens ? min(max(p.new_lens[at[u].b], 0), p.rows) : p.rows;
         const long long to = (long long)(p.lens ? p.lens[at[u].b] : n_new) - n_new + at[u].i;
         if ((int)at[u].i >= n_new || to < 0 || to >= p.capacity) continue;
         pos[u] = (int)to;
         const long long *s = at[u].of_v ? p.vs : p.ks;
-        in[u].load(static_cast<const T *>(at[u].of_v ? p.v : p.k) + at[u].b * s[0] + at[u].h * s[1] + at[u].i * s[2] + 8 * l);
+        in[u].load(static_cast<const T *>(at[u].of_v ? p.v : p.k) + at[u].b * s[0] + at[u].h * s[1] + at[u].i * s[2] + 16 * l);
     }
 #pragma unroll
     for (int u = 0; u < QC_AHEAD; ++u) {
-        float x[8], y[8];
-        in[u].get(x);
-        uint32_t top[2] = {0u, 0u};
+        uint32_t top[4];
+        if constexpr (BITS == 4) {
+            tops4<T>(top, in[u], L);
+        } else {
+            top[0] = 0u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top[i / 4] = max(top[i / 4], __float_as_uint(x[i]) & 0x7fffffffu);
-        if constexpr (BITS == 8) top[0] = max(top[0], top[1]);
+            for (int i = 0; i < 2; ++i) {
+                float x[8];
+                in[u].half[i].get(x);
 #pragma unroll
-        for (int w = BITS == 4 && D == 128 ? 2 : 1; w < L; w <<= 1) {
-            top[0] = max(top[0], __shfl_xor_sync(0xffffffffu, top[0], w));
-            if constexpr (BITS == 4) top[1] = max(top[1], __shfl_xor_sync(0xffffffffu, top[1], w));
+                for (int k = 0; k < 8; ++k) top[0] = max(top[0], __float_as_uint(x[k]) & 0x7fffffffu);
+            }
+#pragma unroll
+            for (int w = 1; w < L; w <<= 1) top[0] = max(top[0], __shfl_xor_sync(0xffffffffu, top[0], w));
+        }
+        float s[4], inv[4];
+        if constexpr (BITS == 4) {
+            // each lane works one group's scale out and passes it on
+            const float own = scale4<T>(l & 2 ? (l & 1 ? top[3] : top[2]) : (l & 1 ? top[1] : top[0]));
+            const float own_inv = own > 0.f ? __frcp_rn(own) : 0.f;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                s[g] = __shfl_sync(0xffffffffu, own, g, 4);
+                inv[g] = __shfl_sync(0xffffffffu, own_inv, g, 4);
+            }
+        } else {
+            s[0] = scale8(top[0]);
+            inv[0] = s[0] > 0.f ? __frcp_rn(s[0]) : 0.f;
         }
         if (pos[u] < 0) continue;
         uint8_t *code = const_cast<uint8_t *>(at[u].of_v ? c.v : c.k), *scale = const_cast<uint8_t *>(at[u].of_v ? c.v_scale : c.k_scale);
         const long long *cs = at[u].of_v ? c.vs : c.ks, *ss = at[u].of_v ? c.vss : c.kss;
         code += at[u].b * cs[0] + at[u].h * cs[1] + pos[u] * cs[2];
         scale += at[u].b * ss[0] + at[u].h * ss[1] + pos[u] * ss[2];
-        float s[2], inv[2];
-#pragma unroll
-        for (int g = 0; g < (BITS == 4 ? 2 : 1); ++g) {
-            s[g] = scale_of<BITS>(top[g]);
-            inv[g] = s[g] > 0.f ? __frcp_rn(s[g]) : 0.f;
-        }
-        uint32_t word[2] = {0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int g = BITS == 4 ? i / 4 : 0;
-            float v = 0.f;                                // zeros where the scale is zero or not a number
-            if (s[g] > 0.f) v = BITS == 4 ? code4<T>(x[i], s[g], inv[g]) : code8(x[i], s[g], inv[g]);
-            y[i] = v * s[g];
-            if constexpr (BITS == 4) word[0] |= (uint32_t)((int)v + 8) << (4 * i);
-            else word[i / 4] |= (uint32_t)((int)v & 255) << (8 * (i % 4));
-        }
-        if constexpr (BITS == 4) {
-            *reinterpret_cast<uint32_t *>(code + 4 * l) = word[0];
-            if (l < D / 64) *reinterpret_cast<uint32_t *>(scale + 4 * l) = __float_as_uint(s[0]) >> 16 | (__float_as_uint(s[1]) & 0xffff0000u);
-        } else {
-            *reinterpret_cast<uint2 *>(code + 8 * l) = make_uint2(word[0], word[1]);
-            if (l == 0) *reinterpret_cast<float *>(scale) = s[0];
-        }
+        T *values = nullptr;
         if constexpr (VALUES) {
             const long long *s3 = at[u].of_v ? p.vos : p.kos;
-            Eight<T>::store(static_cast<T *>(at[u].of_v ? p.v_out : p.k_out) + at[u].b * s3[0] + at[u].h * s3[1] + at[u].i * s3[2] + 8 * l, y);
+            values = static_cast<T *>(at[u].of_v ? p.v_out : p.k_out) + at[u].b * s3[0] + at[u].h * s3[1] + at[u].i * s3[2] + 16 * l;
+        }
+        uint32_t word[4];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float x[8], y[8];
+            in[u].half[half].get(x);
+            if constexpr (BITS == 4) {
+                uint32_t w = 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int g = 2 * half + i / 4;
+                    // (a group that holds what is not finite has codes of zero)
+                    const float t = code4<T>(s[g] == s[g] ? x[i] : 0.f, s[g], inv[g]);
+                    w = (__float_as_uint(t) << (4 * i)) + w;
+                    y[i] = (t - (QC_ONES + 8.f)) * s[g];
+                }
+                word[half] = w - 0x4b400000u * 0x11111111u;      // (modulo 2^32: what the places of 1.5 * 2^23 add up to)
+            } else {
+                float v[8], worst = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (s[0] != s[0]) x[i] = 0.f;
+                    const float t = __fmaf_rn(x[i], inv[0], QC_ONES);
+                    v[i] = t - QC_ONES;
+                    worst = fmaxf(worst, fabsf(__fmaf_rn(x[i], inv[0], -v[i])));
+                }
+                // The code is the whole number nearest to the fp32 quotient, which the product is within 1.2e-5 of (|x / scale| <= 127): only
+                // where one is nearer than that to n + 1/2 the quotients are formed.
+                if (worst > 0.49998f && s[0] > 0.f) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = rintf(__fdiv_rn(x[i], s[0]));
+                }
+                uint32_t b[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    b[i] = __float_as_uint(v[i] + QC_ONES);
+                    y[i] = v[i] * s[0];
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    word[2 * half + i] = __byte_perm(__byte_perm(b[4 * i], b[4 * i + 1], 0x0040), __byte_perm(b[4 * i + 2], b[4 * i + 3], 0x0040), 0x5410);
+            }
+            if constexpr (VALUES) Eight<T>::store(values + 8 * half, y);
+        }
+        if constexpr (BITS == 4) {
+            *reinterpret_cast<uint2 *>(code + 8 * l) = make_uint2(word[0], word[1]);
+            const uint32_t s01 = __float_as_uint(s[0]) >> 16 | (__float_as_uint(s[1]) & 0xffff0000u), s23 = __float_as_uint(s[2]) >> 16 | (__float_as_uint(s[3]) & 0xffff0000u);
+            if (l == 0) {
+                if constexpr (D == 128) *reinterpret_cast<uint2 *>(scale) = make_uint2(s01, s23);
+                else *reinterpret_cast<uint32_t *>(scale) = s01;
+            }
+        } else {
+            *reinterpret_cast<uint4 *>(code + 16 * l) = make_uint4(word[0], word[1], word[2], word[3]);
+            if (l == 0) *reinterpret_cast<float *>(scale) = s[0];
         }
     }
 }
 
-// Eight neighbouring channels' values from their codes (a word, two words) and scales.
-template <int BITS>
-__device__ __forceinline__ void values8(float (&y)[8], uint2 code, float s0, float s1)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (BITS == 4) y[i] = (float)((int)(code.x >> (4 * i) & 15u) - 8) * (i < 4 ? s0 : s1);
-        else y[i] = (float)(int8_t)((i < 4 ? code.x : code.y) >> (8 * (i % 4))) * s0;
-    }
-}
-
-// Reading rows first .. first + rows - 1 back, laid out as for writing.
-template <typename T, int BITS, int D>
-__global__ void __launch_bounds__(QC_NT) k_quant_read(const __grid_constant__ RowsDev p, const __grid_constant__ QuantDev c)
+template <typename T, int BITS, int D, bool VALUES>
+__global__ void __launch_bounds__(QC_NT) k_quant_write(const __grid_constant__ RowsDev p, const __grid_constant__ QuantDev c)
 {
     pdl_wait();
     pdl_trigger();
+    constexpr uint32_t ROWS = QC_NT / (D / 16) * QC_AHEAD;
+    const RowAt head = row_at(p, blockIdx.x * ROWS);
+    if (head.i + ROWS <= (uint32_t)p.rows) quant_write<T, BITS, D, VALUES, true>(p, c, head);
+    else quant_write<T, BITS, D, VALUES, false>(p, c, head);
+}
+
+// Eight neighbouring channels' values from their codes (a word, two words) and scales (two bf16 ones in a word, one).
+template <typename T, int BITS>
+__device__ __forceinline__ void store_values8(T *dst, uint2 code, uint32_t scale)
+{
+    if constexpr (BITS == 4 && sizeof(T) == 2) {
+        // Four codes of either half of the word side by side as 128 + u, less 136, times the halves' scales: one rounding, of the product.
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t u = ((code.x >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+            const __nv_bfloat162 v = __hmul2(__hadd2(*reinterpret_cast<__nv_bfloat162 *>(&u), __float2bfloat162_rn(-136.f)), *reinterpret_cast<const __nv_bfloat162 *>(&scale));
+            r[i] = *reinterpret_cast<const uint32_t *>(&v);
+        }
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410), __byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632));
+    } else {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // codes plus an offset as the last bits of 2^23 + u
+            if constexpr (BITS == 4) {
+                y[i] = (__uint_as_float(((code.x >> (4 * i)) & 15u) | 0x4b000000u) - 8388616.f) * (i < 4 ? __uint_as_float(scale << 16) : __uint_as_float(scale & 0xffff0000u));
+            } else {
+                y[i] = (__uint_as_float(__byte_perm((i < 4 ? code.x : code.y) ^ 0x80808080u, 0x4b000000u, 0x7440 + i % 4)) - 8388736.f) * __uint_as_float(scale);
+            }
+        }
+        Eight<T>::store(dst, y);
+    }
+}
+
+// Reading rows first .. first + rows - 1 back, laid out as for writing: eight channels (fp32: two times four) at a time, so that a warp's stores are whole
+// lines.  Bound by HBM (caches of 3001 to 8192 rows in 4 bits: READ_US us).
+constexpr int QR_AHEAD = 4;
+
+template <typename T, int BITS, int D, bool ONE>
+__device__ __forceinline__ void quant_read(const RowsDev &p, const QuantDev &c, const RowAt &head)
+{
     constexpr int L = D / 8, R = QC_NT / L;
     const int l = threadIdx.x % L;
-    const uint32_t f0 = blockIdx.x * (R * QC_AHEAD) + threadIdx.x / L;
-    uint2 code[QC_AHEAD];
-    float s[QC_AHEAD][2];
-    RowAt at[QC_AHEAD];
-    bool real[QC_AHEAD];
+    uint2 code[QR_AHEAD];
+    uint32_t s[QR_AHEAD];
+    RowAt at[QR_AHEAD];
+    bool real[QR_AHEAD];
 #pragma unroll
-    for (int u = 0; u < QC_AHEAD; ++u) {
-        const uint32_t f = f0 + u * R;
-        real[u] = f < p.total;
+    for (int u = 0; u < QR_AHEAD; ++u) {
+        const uint32_t k = u * R + threadIdx.x / L, f = blockIdx.x * (R * QR_AHEAD) + k;
+        real[u] = ONE || f < p.total;
         if (!real[u]) continue;
-        at[u] = row_at(p, f);
+        at[u] = ONE ? head : row_at(p, f);
+        if (ONE) at[u].i += k;
         const int j = p.first + (int)at[u].i, n = p.lens ? min(p.lens[at[u].b], p.capacity) : p.capacity;
         real[u] = j < n;
         if (!real[u]) continue;
         const long long *cs = at[u].of_v ? c.vs : c.ks, *ss = at[u].of_v ? c.vss : c.kss;
         const uint8_t *from = (at[u].of_v ? c.v : c.k) + at[u].b * cs[0] + at[u].h * cs[1] + j * cs[2];
         const uint8_t *scale = (at[u].of_v ? c.v_scale : c.k_scale) + at[u].b * ss[0] + at[u].h * ss[1] + j * ss[2];
-        if constexpr (BITS == 4) {
-            code[u].x = *reinterpret_cast<const uint32_t *>(from + 4 * l);
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(scale + (D == 128 ? 4 * (l & 1) : 0));
-            s[u][0] = __uint_as_float(w << 16);
-            s[u][1] = __uint_as_float(w & 0xffff0000u);
-        } else {
-            code[u] = *reinterpret_cast<const uint2 *>(from + 8 * l);
-            s[u][0] = *reinterpret_cast<const float *>(scale);
-        }
+        if constexpr (BITS == 4) code[u].x = *reinterpret_cast<const uint32_t *>(from + 4 * l);
+        else code[u] = *reinterpret_cast<const uint2 *>(from + 8 * l);
+        s[u] = *reinterpret_cast<const uint32_t *>(scale + (BITS == 4 && D == 128 ? 4 * (l & 1) : 0));
     }
 #pragma unroll
-    for (int u = 0; u < QC_AHEAD; ++u) {
+    for (int u = 0; u < QR_AHEAD; ++u) {
         if (!real[u]) continue;
-        float y[8];
-        values8<BITS>(y, code[u], s[u][0], s[u][1]);
         const long long *s3 = at[u].of_v ? p.vos : p.kos;
-        Eight<T>::store(static_cast<T *>(at[u].of_v ? p.v_out : p.k_out) + at[u].b * s3[0] + at[u].h * s3[1] + at[u].i * s3[2] + 8 * l, y);
+        store_values8<T, BITS>(static_cast<T *>(at[u].of_v ? p.v_out : p.k_out) + at[u].b * s3[0] + at[u].h * s3[1] + at[u].i * s3[2] + 8 * l, code[u], s[u]);
     }
+}
+
+template <typename T, int BITS, int D>
+__global__ void __launch_bounds__(QC_NT) k_quant_read(const __grid_constant__ RowsDev p, const __grid_constant__ QuantDev c)
+{
+    pdl_wait();
+    pdl_trigger();
+    constexpr uint32_t ROWS = QC_NT / (D / 8) * QR_AHEAD;
+    const RowAt head = row_at(p, blockIdx.x * ROWS);
+    if (head.i + ROWS <= (uint32_t)p.rows) quant_read<T, BITS, D, true>(p, c, head);
+    else quant_read<T, BITS, D, false>(p, c, head);
 }
 
 }  // namespace obf
