@@ -145,6 +145,19 @@ __device__ __forceinline__ RowAt row_at(const RowsDev &p, uint32_t f)
     return r;
 }
 
+// Where a row of a call is read and written.  Rows of one head lie `step` apart.
+struct RowPlace {
+    const char *in;                        // rows to write / rows of the cache's codes
+    const uint8_t *in_scale;               // reading
+    uint8_t *code, *scale;                 // writing
+    char *out;                             // values
+};
+
+__device__ __forceinline__ const char *row_ptr(const void *base, const long long *st, const RowAt &at, long long row, int size)
+{
+    return static_cast<const char *>(base) + (at.b * st[0] + at.h * st[1] + row * st[2]) * size;
+}
+
 // Sixteen neighbouring channels of a row, as loaded.
 template <typename T>
 struct Sixteen {
@@ -204,22 +217,53 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
     constexpr int L = D / 16, R = QC_NT / L;              // lanes of a row, rows of a block at a time
     const int l = threadIdx.x % L;
     Sixteen<T> in[QC_AHEAD];
-    RowAt at[QC_AHEAD];
-    int pos[QC_AHEAD];                                    // row of the cache, or -1: not written
+    RowPlace at[QC_AHEAD];
+    bool real[QC_AHEAD];
+    const auto first_row = [&](int b) {                   // row of the cache that the sequence's first new row goes to
+        const int n_new = p.new_lens ? min(max(p.new_lens[b], 0), p.rows) : p.rows;
+        return make_int2(n_new, (p.lens ? p.lens[b] : n_new) - n_new);
+    };
+    const auto place = [&](const RowAt &r, int to) {
+        RowPlace q;
+        q.in = row_ptr(r.of_v ? p.v : p.k, r.of_v ? p.vs : p.ks, r, r.i, sizeof(T)) + 16 * l * sizeof(T);
+        q.code = reinterpret_cast<uint8_t *>(const_cast<char *>(row_ptr(r.of_v ? c.v : c.k, r.of_v ? c.vs : c.ks, r, to, 1)));
+        q.scale = reinterpret_cast<uint8_t *>(const_cast<char *>(row_ptr(r.of_v ? c.v_scale : c.k_scale, r.of_v ? c.vss : c.kss, r, to, 1)));
+        if constexpr (VALUES) q.out = const_cast<char *>(row_ptr(r.of_v ? p.v_out : p.k_out, r.of_v ? p.vos : p.kos, r, r.i, sizeof(T))) + 16 * l * sizeof(T);
+        return q;
+    };
+    if constexpr (ONE) {
+        const int2 new_at = first_row(head.b);
+        RowAt r = head;
+        r.i += threadIdx.x / L;
+        const RowPlace q = place(r, (int)r.i + new_at.y);
+        const long long in = (head.of_v ? p.vs : p.ks)[2] * (long long)sizeof(T) * R, code = (head.of_v ? c.vs : c.ks)[2] * R, scale = (head.of_v ? c.vss : c.kss)[2] * R,
+                        out = (head.of_v ? p.vos : p.kos)[2] * (long long)sizeof(T) * R;
+#pragma unroll
+        for (int u = 0; u < QC_AHEAD; ++u) {
+            const int i = (int)r.i + u * R;
+            real[u] = i < new_at.x && i + new_at.y >= 0 && i + new_at.y < p.capacity;
+            at[u].in = q.in + u * in;
+            at[u].code = q.code + u * code;
+            at[u].scale = q.scale + u * scale;
+            if constexpr (VALUES) at[u].out = q.out + u * out;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < QC_AHEAD; ++u) {
+            const uint32_t f = blockIdx.x * (R * QC_AHEAD) + u * R + threadIdx.x / L;
+            real[u] = f < p.total;
+            if (!real[u]) continue;
+            const RowAt r = row_at(p, f);
+            const int2 new_at = first_row(r.b);
+            const long long to = (long long)r.i + new_at.y;
+            real[u] = (int)r.i < new_at.x && to >= 0 && to < p.capacity;
+            at[u] = place(r, real[u] ? (int)to : 0);
+        }
+    }
 #pragma unroll
     for (int u = 0; u < QC_AHEAD; ++u) {
-        const uint32_t k = u * R + threadIdx.x / L, f = blockIdx.x * (R * QC_AHEAD) + k;
-        pos[u] = -1;
         in[u] = {};
-        if (!ONE && f >= p.total) continue;
-        at[u] = ONE ? head : row_at(p, f);
-        if (ONE) at[u].i += k;
-        const int n_new = p.new_lens ? min(max(p.new_lens[at[u].b], 0), p.rows) : p.rows;
-        const long long to = (long long)(p.lens ? p.lens[at[u].b] : n_new) - n_new + at[u].i;
-        if ((int)at[u].i >= n_new || to < 0 || to >= p.capacity) continue;
-        pos[u] = (int)to;
-        const long long *s = at[u].of_v ? p.vs : p.ks;
-        in[u].load(static_cast<const T *>(at[u].of_v ? p.v : p.k) + at[u].b * s[0] + at[u].h * s[1] + at[u].i * s[2] + 16 * l);
+        if (real[u]) in[u].load(reinterpret_cast<const T *>(at[u].in));
     }
 #pragma unroll
     for (int u = 0; u < QC_AHEAD; ++u) {
@@ -252,28 +296,28 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
             s[0] = scale8(top[0]);
             inv[0] = s[0] > 0.f ? __frcp_rn(s[0]) : 0.f;
         }
-        if (pos[u] < 0) continue;
-        uint8_t *code = const_cast<uint8_t *>(at[u].of_v ? c.v : c.k), *scale = const_cast<uint8_t *>(at[u].of_v ? c.v_scale : c.k_scale);
-        const long long *cs = at[u].of_v ? c.vs : c.ks, *ss = at[u].of_v ? c.vss : c.kss;
-        code += at[u].b * cs[0] + at[u].h * cs[1] + pos[u] * cs[2];
-        scale += at[u].b * ss[0] + at[u].h * ss[1] + pos[u] * ss[2];
-        T *values = nullptr;
-        if constexpr (VALUES) {
-            const long long *s3 = at[u].of_v ? p.vos : p.kos;
-            values = static_cast<T *>(at[u].of_v ? p.v_out : p.k_out) + at[u].b * s3[0] + at[u].h * s3[1] + at[u].i * s3[2] + 16 * l;
-        }
+        if (!real[u]) continue;
+        // a scale that is not a number: codes of zero, whatever the channels hold
+        bool whole = s[0] == s[0];
+        if constexpr (BITS == 4) whole = whole && s[1] == s[1] && s[2] == s[2] && s[3] == s[3];
         uint32_t word[4];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             float x[8], y[8];
             in[u].half[half].get(x);
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float f = s[BITS == 4 ? 2 * half + i / 4 : 0];
+                    if (f != f) x[i] = 0.f;
+                }
+            }
             if constexpr (BITS == 4) {
                 uint32_t w = 0u;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int g = 2 * half + i / 4;
-                    // (a group that holds what is not finite has codes of zero)
-                    const float t = code4<T>(s[g] == s[g] ? x[i] : 0.f, s[g], inv[g]);
+                    const float t = code4<T>(x[i], s[g], inv[g]);
                     w = (__float_as_uint(t) << (4 * i)) + w;
                     y[i] = (t - (QC_ONES + 8.f)) * s[g];
                 }
@@ -282,7 +326,6 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
                 float v[8], worst = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (s[0] != s[0]) x[i] = 0.f;
                     const float t = __fmaf_rn(x[i], inv[0], QC_ONES);
                     v[i] = t - QC_ONES;
                     worst = fmaxf(worst, fabsf(__fmaf_rn(x[i], inv[0], -v[i])));
@@ -291,7 +334,8 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
                 // where one is nearer than that to n + 1/2 the quotients are formed.
                 if (worst > 0.49998f && s[0] > 0.f) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = rintf(__fdiv_rn(x[i], s[0]));
+                    for (int i = 0; i < 8; ++i)
+                        if (fabsf(__fmaf_rn(x[i], inv[0], -v[i])) > 0.49998f) v[i] = rintf(__fdiv_rn(x[i], s[0]));
                 }
                 uint32_t b[8];
 #pragma unroll
@@ -303,18 +347,18 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
                 for (int i = 0; i < 2; ++i)
                     word[2 * half + i] = __byte_perm(__byte_perm(b[4 * i], b[4 * i + 1], 0x0040), __byte_perm(b[4 * i + 2], b[4 * i + 3], 0x0040), 0x5410);
             }
-            if constexpr (VALUES) Eight<T>::store(values + 8 * half, y);
+            if constexpr (VALUES) Eight<T>::store(reinterpret_cast<T *>(at[u].out) + 8 * half, y);
         }
         if constexpr (BITS == 4) {
-            *reinterpret_cast<uint2 *>(code + 8 * l) = make_uint2(word[0], word[1]);
+            *reinterpret_cast<uint2 *>(at[u].code + 8 * l) = make_uint2(word[0], word[1]);
             const uint32_t s01 = __float_as_uint(s[0]) >> 16 | (__float_as_uint(s[1]) & 0xffff0000u), s23 = __float_as_uint(s[2]) >> 16 | (__float_as_uint(s[3]) & 0xffff0000u);
             if (l == 0) {
-                if constexpr (D == 128) *reinterpret_cast<uint2 *>(scale) = make_uint2(s01, s23);
-                else *reinterpret_cast<uint32_t *>(scale) = s01;
+                if constexpr (D == 128) *reinterpret_cast<uint2 *>(at[u].scale) = make_uint2(s01, s23);
+                else *reinterpret_cast<uint32_t *>(at[u].scale) = s01;
             }
         } else {
-            *reinterpret_cast<uint4 *>(code + 16 * l) = make_uint4(word[0], word[1], word[2], word[3]);
-            if (l == 0) *reinterpret_cast<float *>(scale) = s[0];
+            *reinterpret_cast<uint4 *>(at[u].code + 16 * l) = make_uint4(word[0], word[1], word[2], word[3]);
+            if (l == 0) *reinterpret_cast<float *>(at[u].scale) = s[0];
         }
     }
 }
@@ -370,31 +414,50 @@ __device__ __forceinline__ void quant_read(const RowsDev &p, const QuantDev &c, 
     const int l = threadIdx.x % L;
     uint2 code[QR_AHEAD];
     uint32_t s[QR_AHEAD];
-    RowAt at[QR_AHEAD];
+    RowPlace at[QR_AHEAD];
     bool real[QR_AHEAD];
+    const auto rows_of = [&](int b) { return p.lens ? min(p.lens[b], p.capacity) : p.capacity; };
+    const auto place = [&](const RowAt &r) {
+        RowPlace q;
+        q.in = row_ptr(r.of_v ? c.v : c.k, r.of_v ? c.vs : c.ks, r, p.first + (long long)r.i, 1) + BITS * l;
+        q.in_scale = reinterpret_cast<const uint8_t *>(row_ptr(r.of_v ? c.v_scale : c.k_scale, r.of_v ? c.vss : c.kss, r, p.first + (long long)r.i, 1)) + (BITS == 4 && D == 128 ? 4 * (l & 1) : 0);
+        q.out = const_cast<char *>(row_ptr(r.of_v ? p.v_out : p.k_out, r.of_v ? p.vos : p.kos, r, r.i, sizeof(T))) + 8 * l * sizeof(T);
+        return q;
+    };
+    if constexpr (ONE) {
+        const int n = rows_of(head.b) - p.first;
+        RowAt r = head;
+        r.i += threadIdx.x / L;
+        const RowPlace q = place(r);
+        const long long in = (head.of_v ? c.vs : c.ks)[2] * R, scale = (head.of_v ? c.vss : c.kss)[2] * R, out = (head.of_v ? p.vos : p.kos)[2] * (long long)sizeof(T) * R;
 #pragma unroll
-    for (int u = 0; u < QR_AHEAD; ++u) {
-        const uint32_t k = u * R + threadIdx.x / L, f = blockIdx.x * (R * QR_AHEAD) + k;
-        real[u] = ONE || f < p.total;
-        if (!real[u]) continue;
-        at[u] = ONE ? head : row_at(p, f);
-        if (ONE) at[u].i += k;
-        const int j = p.first + (int)at[u].i, n = p.lens ? min(p.lens[at[u].b], p.capacity) : p.capacity;
-        real[u] = j < n;
-        if (!real[u]) continue;
-        const long long *cs = at[u].of_v ? c.vs : c.ks, *ss = at[u].of_v ? c.vss : c.kss;
-        const uint8_t *from = (at[u].of_v ? c.v : c.k) + at[u].b * cs[0] + at[u].h * cs[1] + j * cs[2];
-        const uint8_t *scale = (at[u].of_v ? c.v_scale : c.k_scale) + at[u].b * ss[0] + at[u].h * ss[1] + j * ss[2];
-        if constexpr (BITS == 4) code[u].x = *reinterpret_cast<const uint32_t *>(from + 4 * l);
-        else code[u] = *reinterpret_cast<const uint2 *>(from + 8 * l);
-        s[u] = *reinterpret_cast<const uint32_t *>(scale + (BITS == 4 && D == 128 ? 4 * (l & 1) : 0));
+        for (int u = 0; u < QR_AHEAD; ++u) {
+            real[u] = (int)r.i + u * R < n;
+            at[u].in = q.in + u * in;
+            at[u].in_scale = q.in_scale + u * scale;
+            at[u].out = q.out + u * out;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < QR_AHEAD; ++u) {
+            const uint32_t f = blockIdx.x * (R * QR_AHEAD) + u * R + threadIdx.x / L;
+            real[u] = f < p.total;
+            if (!real[u]) continue;
+            const RowAt r = row_at(p, f);
+            real[u] = p.first + (int)r.i < rows_of(r.b);
+            at[u] = place(r);
+        }
     }
 #pragma unroll
     for (int u = 0; u < QR_AHEAD; ++u) {
         if (!real[u]) continue;
-        const long long *s3 = at[u].of_v ? p.vos : p.kos;
-        store_values8<T, BITS>(static_cast<T *>(at[u].of_v ? p.v_out : p.k_out) + at[u].b * s3[0] + at[u].h * s3[1] + at[u].i * s3[2] + 8 * l, code[u], s[u]);
+        if constexpr (BITS == 4) code[u].x = *reinterpret_cast<const uint32_t *>(at[u].in);
+        else code[u] = *reinterpret_cast<const uint2 *>(at[u].in);
+        s[u] = *reinterpret_cast<const uint32_t *>(at[u].in_scale);
     }
+#pragma unroll
+    for (int u = 0; u < QR_AHEAD; ++u)
+        if (real[u]) store_values8<T, BITS>(reinterpret_cast<T *>(at[u].out), code[u], s[u]);
 }
 
 template <typename T, int BITS, int D>
