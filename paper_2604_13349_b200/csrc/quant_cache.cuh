@@ -57,7 +57,6 @@ struct RowsDev {
 };
 
 constexpr int QC_NT = 256;
-constexpr int QC_AHEAD = 2;                // rows of a thread in flight
 
 // Scale of numbers whose largest magnitude has the bits `top` (as integers, so that what is not a number counts as the largest): not a
 // number where one of them is not finite, zero where all are below 2^-110, whose scale would lose bits.
@@ -208,17 +207,23 @@ __device__ __forceinline__ void tops4(uint32_t (&top)[4], const Sixteen<T> &in, 
     }
 }
 
+// Rows of a thread in flight, and blocks of a multiprocessor (bf16 rows to 4 bits: 4 rows 81 us, 2 rows 84; to 8 bits 88 and 74).
+template <typename T, int BITS>
+constexpr int QW_AHEAD = sizeof(T) == 2 && BITS == 4 ? 4 : 2;
+template <typename T, int BITS>
+constexpr int QW_BLOCKS = sizeof(T) == 2 && BITS == 8 ? 4 : 3;
+
 // Writing: D / 16 lanes a row, sixteen channels each; a thread's rows are all read before the first of them is worked on.  Blocks whose rows are
 // all one head's have their places in common.  Bound by HBM where there are many rows (prompts of 3001 to 8192, with values: WRITE_US us), by
 // the latency of a launch and two dependent reads where there are few.
 template <typename T, int BITS, int D, bool VALUES, bool ONE>
 __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c, const RowAt &head)
 {
-    constexpr int L = D / 16, R = QC_NT / L;              // lanes of a row, rows of a block at a time
+    constexpr int L = D / 16, R = QC_NT / L, AHEAD = QW_AHEAD<T, BITS>;       // lanes of a row, rows of a block at a time
     const int l = threadIdx.x % L;
-    Sixteen<T> in[QC_AHEAD];
-    RowPlace at[QC_AHEAD];
-    bool real[QC_AHEAD];
+    Sixteen<T> in[AHEAD];
+    RowPlace at[AHEAD];
+    bool real[AHEAD];
     const auto first_row = [&](int b) {                   // row of the cache that the sequence's first new row goes to
         const int n_new = p.new_lens ? min(max(p.new_lens[b], 0), p.rows) : p.rows;
         return make_int2(n_new, (p.lens ? p.lens[b] : n_new) - n_new);
@@ -239,7 +244,7 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
         const long long in = (head.of_v ? p.vs : p.ks)[2] * (long long)sizeof(T) * R, code = (head.of_v ? c.vs : c.ks)[2] * R, scale = (head.of_v ? c.vss : c.kss)[2] * R,
                         out = (head.of_v ? p.vos : p.kos)[2] * (long long)sizeof(T) * R;
 #pragma unroll
-        for (int u = 0; u < QC_AHEAD; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             const int i = (int)r.i + u * R;
             real[u] = i < new_at.x && i + new_at.y >= 0 && i + new_at.y < p.capacity;
             at[u].in = q.in + u * in;
@@ -249,8 +254,8 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
         }
     } else {
 #pragma unroll
-        for (int u = 0; u < QC_AHEAD; ++u) {
-            const uint32_t f = blockIdx.x * (R * QC_AHEAD) + u * R + threadIdx.x / L;
+        for (int u = 0; u < AHEAD; ++u) {
+            const uint32_t f = blockIdx.x * (R * AHEAD) + u * R + threadIdx.x / L;
             real[u] = f < p.total;
             if (!real[u]) continue;
             const RowAt r = row_at(p, f);
@@ -261,12 +266,12 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
         }
     }
 #pragma unroll
-    for (int u = 0; u < QC_AHEAD; ++u) {
+    for (int u = 0; u < AHEAD; ++u) {
         in[u] = {};
         if (real[u]) in[u].load(reinterpret_cast<const T *>(at[u].in));
     }
 #pragma unroll
-    for (int u = 0; u < QC_AHEAD; ++u) {
+    for (int u = 0; u < AHEAD; ++u) {
         uint32_t top[4];
         if constexpr (BITS == 4) {
             tops4<T>(top, in[u], L);
@@ -364,11 +369,11 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
 }
 
 template <typename T, int BITS, int D, bool VALUES>
-__global__ void __launch_bounds__(QC_NT) k_quant_write(const __grid_constant__ RowsDev p, const __grid_constant__ QuantDev c)
+__global__ void __launch_bounds__(QC_NT, (QW_BLOCKS<T, BITS>)) k_quant_write(const __grid_constant__ RowsDev p, const __grid_constant__ QuantDev c)
 {
     pdl_wait();
     pdl_trigger();
-    constexpr uint32_t ROWS = QC_NT / (D / 16) * QC_AHEAD;
+    constexpr uint32_t ROWS = QC_NT / (D / 16) * QW_AHEAD<T, BITS>;
     const RowAt head = row_at(p, blockIdx.x * ROWS);
     if (head.i + ROWS <= (uint32_t)p.rows) quant_write<T, BITS, D, VALUES, true>(p, c, head);
     else quant_write<T, BITS, D, VALUES, false>(p, c, head);
