@@ -21,6 +21,8 @@ struct AttendDev {
     long long qs[3], ks[3], vs[3], os[3];
     const void *pk, *pv;      // shared prefix, or null
     long long pks[2], pvs[2];
+    const float *k_factor, *v_factor;    // of each key, or null: what its logits (scale and log2 e included) and weights are multiplied by,
+    long long factor_stride;             // rows of a (sequence, KV head) apart, 16-byte aligned, readable for 128 keys behind the last
     const int32_t *lens, *q_lens;
     float *lse_out;
     const float *mass_in;

@@ -8,6 +8,16 @@
 
 namespace obf {
 
+// obf_attend for entry points of other files (obf_attend.cu): whether a call's queries are many enough for the tensor cores' tiles of 128 rows, its
+// workspace, and the call itself, with a factor for each key's logits and weights where it goes to those tiles (AttendDev).
+struct AttendFactors {
+    const float *k, *v;
+    long long stride;
+};
+bool attends_in_tiles(const obf_attend_t *a);
+size_t attend_rows_bytes(const obf_attend_t *a);
+obf_status_t attend_rows(const obf_attend_t *a, const AttendFactors &factors, void *workspace, size_t bytes, void *stream);
+
 inline obf_status_t check_stride(const int64_t *st, const int64_t *n, int dims, int head_dim, int esize)
 {
     for (int i = 0; i < dims; ++i) {

@@ -59,7 +59,7 @@ struct AttendTcMaps {
 };
 
 // What every role of a block knows about an item.
-template <bool PREFIX>
+template <bool PREFIX, bool FACTORS>
 struct AttendTcItem {
     int h, b, part;                  // KV head, sequence (of own keys), part of the keys
     int ti, nb;                      // queries and sequences of a tile
@@ -111,8 +111,9 @@ struct AttendTcItem {
             if (valid[0]) {
                 const KeyRange r = attend_range(p, t + i0, t + min(i0 + 2 * ti, ql) - 1, len);
                 hi = r.hi;
-                if (r.lo > p.sinks) {
-                    lo = r.lo;
+                const int from = FACTORS ? r.lo & ~3 : r.lo;             // (factors are read four at a time)
+                if (from > p.sinks) {
+                    lo = from;
                     head = p.sinks ? tm.head_rows : 0;
                 }
                 // up to a multiple of 16 keys where there are more, which later queries see
@@ -215,7 +216,8 @@ __device__ __forceinline__ uint32_t column_bits(int a, int b)
     return (0xFFFFFFFFu >> (32 - b)) & (0xFFFFFFFFu << a);
 }
 
-template <int D, bool PREFIX>
+// FACTORS: keys and values come with a factor each (p.k_factor, p.v_factor), which a key's logits and weights are multiplied by in fp32.
+template <int D, bool PREFIX, bool FACTORS>
 __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_constant__ AttendDev p, const __grid_constant__ AttendTcMaps tm, const int items,
                                                            const int first)
 {
@@ -225,7 +227,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     uint8_t *q_sm = base, *ring = base + 2 * SLOT_BYTES;
     __shared__ uint64_t bar_full[SLOTS], bar_empty[SLOTS], bar_q_full, bar_q_empty, bar_drain[2];
     __shared__ uint64_t bar_s[2], bar_p[2], bar_o[2], bar_o_read[2], bar_item[2], bar_item_read[2], bar_turn[2];
-    __shared__ AttendTcItem<PREFIX> sm_item[2];
+    __shared__ AttendTcItem<PREFIX, FACTORS> sm_item[2];
     __shared__ float sm_row[2][2][AT_TILE];               // a row's two threads trade their maxima and sums
     __shared__ uint32_t s_tmem, s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -264,7 +266,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     pdl_trigger();
     if (first && blockIdx.x == 0) attend_status(p);
 
-    AttendTcItem<PREFIX> it;
+    AttendTcItem<PREFIX, FACTORS> it;
     if (warp == 2) {
         // ---------------- copies ----------------
         if (lane == 0) {
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         bool dead = false;
         for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
             if (!mbar_wait_warp(&bar_item[ni & 1u], (ni >> 1) & 1u, wc)) break;
-            const AttendTcItem<PREFIX> &im = sm_item[ni & 1u];
+            const AttendTcItem<PREFIX, FACTORS> &im = sm_item[ni & 1u];
             it.jb = warp_uniform(im.jb);
             it.je = warp_uniform(im.je);
             it.head = warp_uniform(im.head);
@@ -425,11 +427,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         for (int item = blockIdx.x; item < items && !dead; item += gridDim.x, ++ni) {
             if (any(!tc::mbar_wait(&bar_item[ni & 1u], (ni >> 1) & 1u, wc))) break;
             // (what only the beginning and the end of an item need is read from shared memory both times: registers are short)
-            const AttendTcItem<PREFIX> &im = sm_item[ni & 1u];
+            const AttendTcItem<PREFIX, FACTORS> &im = sm_item[ni & 1u];
             const int jb = im.jb, je = im.je, sk = im.sk[x], ja = im.ja[x], jz = im.jz[x], fa = im.fa[x], fz = im.fz[x];
             it.head = im.head;
             it.lo = im.lo;
             it.hi = im.hi;
+            if (FACTORS) { it.b = im.b; it.h = im.h; }
             bool real = im.valid[x] && row_b < im.nb;
             {
                 const int i = im.fi[x] + row_i, b = im.fb[x] + row_b;
@@ -459,6 +462,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     }
                     return bits;
                 };
+                // factors of four columns of the tiles of keys
+                auto factors = [&](const float *of, int v) {
+                    return reinterpret_cast<const float4 *>(of + ((long long)it.b * p.kv_heads + it.h) * p.factor_stride + (v < it.head ? v : it.lo + v - it.head));
+                };
                 bool formed = false;                      // the tile's weights
                 uint32_t w[32];
                 if (known && (width & 15) == 0) {
@@ -471,23 +478,52 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         uint32_t r[32];
                         tc::tmem_ld32(s_t + col0 + 32 * c, r);
                         tc::tmem_ld_wait32(r);
-                        if (!full) {
-                            const uint32_t bits = seen(c);
-                            if (__any_sync(0xffffffffu, bits != 0xFFFFFFFFu)) {
+                        if constexpr (FACTORS) {
+                            const uint32_t bits = full ? 0xFFFFFFFFu : seen(c);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e)
-                                    if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 kf = *factors(p.k_factor, j * AT_TILE + col0 + 32 * c + e);
+                                float4 vf = *factors(p.v_factor, j * AT_TILE + col0 + 32 * c + e);
+                                f32x2 y = fma2(pk(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), pk(kf.x, kf.y), r2);
+                                float a0, a1, a2, a3;
+                                upk(y, a0, a1);
+                                y = fma2(pk(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), pk(kf.z, kf.w), r2);
+                                upk(y, a2, a3);
+                                if (!full) {
+                                    // (factors of keys that are not seen may be anything)
+                                    if (!(bits >> e & 1u)) a0 = -INFINITY, vf.x = 0.f;
+                                    if (!(bits >> (e + 1) & 1u)) a1 = -INFINITY, vf.y = 0.f;
+                                    if (!(bits >> (e + 2) & 1u)) a2 = -INFINITY, vf.z = 0.f;
+                                    if (!(bits >> (e + 3) & 1u)) a3 = -INFINITY, vf.w = 0.f;
+                                }
+                                a0 = ex2(a0);
+                                a1 = ex2(a1);
+                                a2 = ex2(a2);
+                                a3 = ex2(a3);
+                                z = add2(z, pk(a0, a1));
+                                z = add2(z, pk(a2, a3));
+                                w[16 * c + e / 2] = pack_bf16(a0 * vf.x, a1 * vf.y);
+                                w[16 * c + e / 2 + 1] = pack_bf16(a2 * vf.z, a3 * vf.w);
                             }
-                        }
+                        } else {
+                            if (!full) {
+                                const uint32_t bits = seen(c);
+                                if (__any_sync(0xffffffffu, bits != 0xFFFFFFFFu)) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const f32x2 y = fma2(pk(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, r2);
-                            float a, b2;
-                            upk(y, a, b2);
-                            a = ex2(a);
-                            b2 = ex2(b2);
-                            z = add2(z, pk(a, b2));
-                            w[16 * c + e] = pack_bf16(a, b2);
+                                    for (int e = 0; e < 32; ++e)
+                                        if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
+                                }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const f32x2 y = fma2(pk(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, r2);
+                                float a, b2;
+                                upk(y, a, b2);
+                                a = ex2(a);
+                                b2 = ex2(b2);
+                                z = add2(z, pk(a, b2));
+                                w[16 * c + e] = pack_bf16(a, b2);
+                            }
                         }
                     }
                     // The weights may not add up to more than 2^32, and those of an item's first tile add up to something; a logit
@@ -507,10 +543,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         tc::tmem_ld32(s_t + col0 + 32 * c, r);
                         const uint32_t bits = seen(c);
                         tc::tmem_ld_wait32(r);
+                        if constexpr (FACTORS) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 kf = *factors(p.k_factor, j * AT_TILE + col0 + 32 * c + e);
+                                r[e] = __float_as_uint(__fmul_rn(__uint_as_float(r[e]), kf.x));
+                                r[e + 1] = __float_as_uint(__fmul_rn(__uint_as_float(r[e + 1]), kf.y));
+                                r[e + 2] = __float_as_uint(__fmul_rn(__uint_as_float(r[e + 2]), kf.z));
+                                r[e + 3] = __float_as_uint(__fmul_rn(__uint_as_float(r[e + 3]), kf.w));
+                            }
+                        }
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (!(bits >> e & 1u)) r[e] = 0xFF800000u;
                     };
+                    // (logits with factors are scaled already)
+                    auto scaled = [&](float y) { return FACTORS ? y : __fmul_rn(y, p.c); };
                     if (!started) m = real ? -INFINITY : 0.f;            // (rows that are none have a reference)
                     float mx = -INFINITY;
 #pragma unroll 1
@@ -522,7 +570,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     }
                     sm_row[half][x][row] = mx;
                     if (any(late)) { dead = true; break; }
-                    mx = __fmul_rn(fmaxf(mx, sm_row[half ^ 1][x][row]), p.c);
+                    mx = scaled(fmaxf(mx, sm_row[half ^ 1][x][row]));
                     // (a maximum below the reference changes nothing)
                     if (!started) {
                         m = fmaxf(m, mx);
@@ -551,9 +599,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         for (int e = 0; e < 16; ++e) {
                             // (scaled, rounded and then subtracted, as the maximum was: of logits beyond 2^24 a fused product's exact
                             // difference from a rounded reference may be anything.  Not mul2 and add2, which the assembler fuses.)
-                            const float a = ex2(__fadd_rn(__fmul_rn(__uint_as_float(r[2 * e]), p.c), ref));
-                            const float b2 = ex2(__fadd_rn(__fmul_rn(__uint_as_float(r[2 * e + 1]), p.c), ref));
+                            float a = ex2(__fadd_rn(scaled(__uint_as_float(r[2 * e])), ref));
+                            float b2 = ex2(__fadd_rn(scaled(__uint_as_float(r[2 * e + 1])), ref));
                             l2 = add2(l2, pk(a, b2));
+                            if constexpr (FACTORS) {
+                                const float2 vf = reinterpret_cast<const float2 *>(factors(p.v_factor, j * AT_TILE + col0 + 32 * c + 2 * e - (e & 1) * 2))[e & 1];
+                                a = r[2 * e] == 0xFF800000u ? 0.f : a * vf.x;
+                                b2 = r[2 * e + 1] == 0xFF800000u ? 0.f : b2 * vf.y;
+                            }
                             w[16 * c + e] = pack_bf16(a, b2);
                         }
                     }

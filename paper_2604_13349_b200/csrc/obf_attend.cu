@@ -244,7 +244,7 @@ static obf_status_t encode_map(CUtensorMap *m, const void *ptr, int rank, const 
     return OBF_OK;
 }
 
-template <int D, bool PREFIX>
+template <int D, bool PREFIX, bool FACTORS>
 static obf_status_t launch_attend_tc(const AttendDev &p, int first, cudaStream_t st)
 {
     static bool done[64];
@@ -252,11 +252,11 @@ static obf_status_t launch_attend_tc(const AttendDev &p, int first, cudaStream_t
     // multiples of 1024.
     static const size_t smem = [] {
         cudaFuncAttributes fa = {};
-        if (cudaFuncGetAttributes(&fa, k_attend_tc<D, PREFIX>) != cudaSuccess) { (void)cudaGetLastError(); return (size_t)0; }
+        if (cudaFuncGetAttributes(&fa, k_attend_tc<D, PREFIX, FACTORS>) != cudaSuccess) { (void)cudaGetLastError(); return (size_t)0; }
         return align_up(fa.sharedSizeBytes, 1024) - fa.sharedSizeBytes + AttendTcShape<D>::SMEM_BYTES;
     }();
     if (smem == 0) return OBF_ERR_CUDA;
-    OBF_TRY(set_smem_once(k_attend_tc<D, PREFIX>, smem, done));
+    OBF_TRY(set_smem_once(k_attend_tc<D, PREFIX, FACTORS>, smem, done));
     const TcTiles t = tc_tiles(p.G, p.n_q, p.batch, p.kv_heads, PREFIX);
     AttendTcMaps m;
     m.ti = t.ti;
@@ -291,7 +291,7 @@ static obf_status_t launch_attend_tc(const AttendDev &p, int first, cudaStream_t
     const long long items = t.pairs * (PREFIX ? p.p_slots : p.slots - p.p_slots);
     if (items > INT_MAX / 2) return OBF_ERR_UNSUPPORTED;
     const int blocks = items < sm_count() ? (int)items : sm_count();
-    OBF_TRY(launch(k_attend_tc<D, PREFIX>, dim3(blocks), AT_THREADS, smem, st, p, m, (int)items, first));
+    OBF_TRY(launch(k_attend_tc<D, PREFIX, FACTORS>, dim3(blocks), AT_THREADS, smem, st, p, m, (int)items, first));
     ++g_last_launches;
     return OBF_OK;
 }
@@ -301,7 +301,9 @@ static obf_status_t launch_attend(AttendPath path, const AttendDev &p, int first
 {
     if (path == ATTEND_FEW) return launch_attend_few<TIN, D, PREFIX>(p, first, st);
     if constexpr (sizeof(TIN) == 2) {
-        if (path == ATTEND_TC) return launch_attend_tc<D, PREFIX>(p, first, st);
+        if constexpr (!PREFIX)
+            if (path == ATTEND_TC && p.k_factor) return launch_attend_tc<D, PREFIX, true>(p, first, st);
+        if (path == ATTEND_TC) return launch_attend_tc<D, PREFIX, false>(p, first, st);
     }
     return launch_attend_generic<TIN, D, PREFIX>(p, first, st);
 }
@@ -315,7 +317,7 @@ static obf_status_t run_attend(const AttendLayout &L, const AttendDev &p, cudaSt
     return OBF_OK;
 }
 
-static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *workspace, size_t bytes, void *stream)
+static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, const AttendFactors &factors, void *workspace, size_t bytes, void *stream)
 {
     g_last_launches = 0;
     OBF_TRY(validate_attend(a, x));
@@ -338,6 +340,7 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *w
         p.wait_limit_ns = 20000000ull;
         p.debug_drop_load = 1;
     }
+    p.k_factor = factors.k; p.v_factor = factors.v; p.factor_stride = factors.stride;
     p.c = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f;
     p.batch = a->batch; p.kv_heads = a->kv_heads; p.G = a->q_heads / a->kv_heads; p.n_q = a->n_q; p.capacity = a->capacity;
     // beyond any position a window or a number of first tokens changes nothing; clamped, positions minus windows cannot overflow
@@ -354,6 +357,14 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, void *w
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (a->dtype == OBF_F32) return a->head_dim == 64 ? run_attend<float, 64>(L, p, st) : run_attend<float, 128>(L, p, st);
     return a->head_dim == 64 ? run_attend<__nv_bfloat16, 64>(L, p, st) : run_attend<__nv_bfloat16, 128>(L, p, st);
+}
+
+// (attend_host.cuh)
+bool attends_in_tiles(const obf_attend_t *a) { return path_for(a, (long long)(a->q_heads / a->kv_heads) * a->n_q) == ATTEND_TC; }
+size_t attend_rows_bytes(const obf_attend_t *a) { return attend_layout(a, nullptr).total; }
+obf_status_t attend_rows(const obf_attend_t *a, const AttendFactors &factors, void *workspace, size_t bytes, void *stream)
+{
+    return attend(a, nullptr, factors, workspace, bytes, stream);
 }
 
 template <int ROW_BYTES>
@@ -393,13 +404,13 @@ obf_status_t obf_attend_workspace_bytes(const obf_attend_t *args, const obf_pref
 
 obf_status_t obf_attend(const obf_attend_t *args, void *workspace, size_t workspace_bytes, void *stream)
 {
-    return attend(args, nullptr, workspace, workspace_bytes, stream);
+    return attend(args, nullptr, {}, workspace, workspace_bytes, stream);
 }
 
 obf_status_t obf_attend_shared(const obf_attend_t *args, const obf_prefix_t *prefix, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!prefix) return OBF_ERR_INVALID_ARG;
-    return attend(args, prefix, workspace, workspace_bytes, stream);
+    return attend(args, prefix, {}, workspace, workspace_bytes, stream);
 }
 
 obf_status_t obf_evict_by_mass(const obf_evict_t *a, void *stream)

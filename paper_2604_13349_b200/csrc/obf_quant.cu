@@ -144,7 +144,7 @@ static obf_status_t quant_read(const obf_quantized_read_t *a, const obf_quantize
     for (int i = 0; i < 3; ++i) { p.kos[i] = a->k_out_stride[i]; p.vos[i] = a->v_out_stride[i]; }
     const QuantDev d = quant_dev(c);
     return with_shape(a->dtype, c->bits, a->head_dim, [&](auto t, auto bits, auto dim) -> obf_status_t {
-        OBF_TRY(launch(k_quant_read<decltype(t), bits.value, dim.value>, dim3(blocks), QC_NT, 0, st, p, d));
+        OBF_TRY(launch(k_quant_read<decltype(t), bits.value, dim.value, false>, dim3(blocks), QC_NT, 0, st, p, d));
         ++g_last_launches;
         return OBF_OK;
     });
@@ -167,10 +167,19 @@ static obf_status_t validate_attend_quant(const obf_attend_t *a, const obf_quant
 }
 
 struct QuantLayout {
+    bool tiles;                      // rows read back first, attention over them in tiles of 128 query rows
     int slots;                       // parts of the keys
     bool cluster;                    // which join themselves
-    size_t off_part_o, off_part_lse, total;
+    size_t off_part_o, off_part_lse;
+    size_t rows_bytes, off_k, off_v, off_k_factor, off_v_factor;     // tiles: that attention's workspace, the rows, 8 bits: their factors
+    long long factor_stride;
+    size_t total;
 };
+
+// Query rows of a KV head from which on bf16 calls read the cache's rows back and attend over those on the tensor cores' tiles of 128 rows,
+// and what the rows may take of a workspace.
+constexpr long long QUANT_TILES_FROM = 97;
+constexpr size_t QUANT_ROWS_BYTES = (size_t)4 << 30;
 
 // Query rows of a tile: 4 and 8 of k_attend_quant_few, 16 of k_attend_quant.
 static int quant_rows(long long rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
@@ -182,10 +191,28 @@ static int quant_resident(int dtype, int head_dim, int rows)
     return 148 * (dtype == OBF_F32 ? (rows == 4 ? AQF_BLOCKS<float, 1> : AQF_BLOCKS<float, 2>) : (rows == 4 ? AQF_BLOCKS<__nv_bfloat16, 1> : AQF_BLOCKS<__nv_bfloat16, 2>));
 }
 
-static QuantLayout quant_layout(const obf_attend_t *a)
+static QuantLayout quant_layout(const obf_attend_t *a, int bits)
 {
-    QuantLayout L;
+    QuantLayout L = {};
     const long long rows_seq = (long long)(a->q_heads / a->kv_heads) * a->n_q, heads = (long long)a->batch * a->kv_heads, rows = heads * rows_seq;
+    const size_t rows_kv = (size_t)heads * a->capacity * a->head_dim * 2;
+    L.tiles = a->dtype == OBF_BF16 && !(a->flags & OBF_FLAG_GENERIC_PATH) && rows_seq >= QUANT_TILES_FROM && 2 * rows_kv <= QUANT_ROWS_BYTES && attends_in_tiles(a);
+    if (L.tiles) {
+        size_t o = L.rows_bytes = align_up(attend_rows_bytes(a), 256);
+        L.off_k = o;
+        o = align_up(o + rows_kv, 256);
+        L.off_v = o;
+        o = align_up(o + rows_kv, 256);
+        L.off_k_factor = o;
+        if (bits == 8) {
+            L.factor_stride = (long long)align_up(a->capacity, 4);
+            const size_t n = ((size_t)heads * L.factor_stride + 128) * sizeof(float);
+            L.off_v_factor = o = align_up(o + n, 256);
+            o = align_up(o + n, 256);
+        }
+        L.total = o;
+        return L;
+    }
     const int t = quant_rows(rows_seq);
     const long long tiles = heads * ((rows_seq + t - 1) / t), keys = most_keys(a, t);
     const int resident = quant_resident(a->dtype, a->head_dim, t);
@@ -235,6 +262,41 @@ static obf_status_t launch_quant(const AttendDev &p, const QuantDev &d, cudaStre
     return OBF_OK;
 }
 
+static float logit_factor(const obf_attend_t *a) { return (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f; }
+
+// The rows that the queries see are read back, in 4 bits as their values, which are bf16 numbers, in 8 bits as codes, which are too, with their
+// scales apart; attention goes over those.
+static obf_status_t attend_tiles(const QuantLayout &L, const obf_attend_t *a, const obf_quantized_t *c, char *ws, cudaStream_t st)
+{
+    RowsDev p = {};
+    unsigned blocks;
+    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->capacity, 0, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 8) * QR_AHEAD));
+    obf_attend_t r = *a;
+    r.k = p.k_out = ws + L.off_k;
+    r.v = p.v_out = ws + L.off_v;
+    const int64_t row = a->head_dim, head = row * a->capacity, seq = head * a->kv_heads, stride[3] = {seq, head, row};
+    for (int i = 0; i < 3; ++i) p.kos[i] = p.vos[i] = r.k_stride[i] = r.v_stride[i] = stride[i];
+    p.q_lens = a->q_lens; p.n_q = a->n_q;
+    p.window = a->window < 2 * OBF_MAX_T ? a->window : 2 * OBF_MAX_T;
+    p.sinks = a->sinks;
+    AttendFactors factors = {};
+    if (c->bits == 8) {
+        p.k_factor = reinterpret_cast<float *>(ws + L.off_k_factor);
+        p.v_factor = reinterpret_cast<float *>(ws + L.off_v_factor);
+        p.factor_stride = L.factor_stride;
+        p.c = logit_factor(a);
+        factors = {p.k_factor, p.v_factor, L.factor_stride};
+    }
+    const QuantDev d = quant_dev(c);
+    OBF_TRY(with_shape(OBF_BF16, c->bits, a->head_dim, [&](auto t, auto bits, auto dim) -> obf_status_t {
+        if constexpr (sizeof(t) == 2) OBF_TRY(launch(k_quant_read<decltype(t), bits.value, dim.value, bits.value == 8>, dim3(blocks), QC_NT, 0, st, p, d));
+        return OBF_OK;
+    }));
+    OBF_TRY(attend_rows(&r, factors, ws, L.rows_bytes, st));
+    ++g_last_launches;
+    return OBF_OK;
+}
+
 static obf_status_t attend_quant(const obf_attend_t *a, const obf_quantized_t *c, void *workspace, size_t bytes, cudaStream_t st)
 {
     g_last_launches = 0;
@@ -247,13 +309,14 @@ static obf_status_t attend_quant(const obf_attend_t *a, const obf_quantized_t *c
     OBF_TRY(check_stride(a->out_stride, nq, 3, a->head_dim, es));
     OBF_TRY(validate_words(a->lens, a->q_lens));
     OBF_TRY(validate_words(a->lse_out, nullptr));
-    const QuantLayout L = quant_layout(a);
+    const QuantLayout L = quant_layout(a, c->bits);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < L.total) return OBF_ERR_WORKSPACE;
+    if (L.tiles) return attend_tiles(L, a, c, static_cast<char *>(workspace), st);
     AttendDev p = {};
     p.q = a->q; p.out = a->out;
     for (int i = 0; i < 3; ++i) { p.qs[i] = a->q_stride[i]; p.os[i] = a->out_stride[i]; }
     p.lens = a->lens; p.q_lens = a->q_lens; p.lse_out = a->lse_out;
-    p.c = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f;
+    p.c = logit_factor(a);
     p.batch = a->batch; p.kv_heads = a->kv_heads; p.G = a->q_heads / a->kv_heads; p.n_q = a->n_q; p.capacity = a->capacity;
     p.window = a->window < 2 * OBF_MAX_T ? a->window : 2 * OBF_MAX_T;
     p.sinks = a->sinks < 2 * OBF_MAX_T ? a->sinks : 2 * OBF_MAX_T;
@@ -289,7 +352,7 @@ obf_status_t obf_attend_quantized_workspace_bytes(const obf_attend_t *args, cons
 {
     if (!bytes) return OBF_ERR_INVALID_ARG;
     OBF_TRY(validate_attend_quant(args, cache));
-    *bytes = quant_layout(args).total;
+    *bytes = quant_layout(args, cache->bits).total;
     return OBF_OK;
 }
 

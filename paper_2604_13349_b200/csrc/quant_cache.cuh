@@ -53,6 +53,13 @@ struct RowsDev {
     const int32_t *lens, *new_lens;
     int32_t rows, first, capacity;
     uint32_t total, half;                  // rows of K and V, of one of them
+    // Reading for attention: what the queries (q_lens, or n_q of each sequence) see through a window, and behind it the first tokens;
+    // of 8 bits the codes, with factors (AttendDev) apart.
+    const int32_t *q_lens;
+    int32_t n_q, window, sinks;
+    float *k_factor, *v_factor;
+    long long factor_stride;
+    float c;                               // of K's factors
     FastDiv by_rows, by_heads;
 };
 
@@ -150,6 +157,7 @@ struct RowPlace {
     const uint8_t *in_scale;               // reading
     uint8_t *code, *scale;                 // writing
     char *out;                             // values
+    float *factor, c;                      // reading codes: where the scale goes, times what
 };
 
 __device__ __forceinline__ const char *row_ptr(const void *base, const long long *st, const RowAt &at, long long row, int size)
@@ -412,7 +420,7 @@ __device__ __forceinline__ void store_values8(T *dst, uint2 code, uint32_t scale
 // lines.  Bound by HBM (caches of 3001 to 8192 rows in 4 bits: READ_US us).
 constexpr int QR_AHEAD = 4;
 
-template <typename T, int BITS, int D, bool ONE>
+template <typename T, int BITS, int D, bool CODES, bool ONE>
 __device__ __forceinline__ void quant_read(const RowsDev &p, const QuantDev &c, const RowAt &head)
 {
     constexpr int L = D / 8, R = QC_NT / L;
@@ -421,26 +429,38 @@ __device__ __forceinline__ void quant_read(const RowsDev &p, const QuantDev &c, 
     uint32_t s[QR_AHEAD];
     RowPlace at[QR_AHEAD];
     bool real[QR_AHEAD];
-    const auto rows_of = [&](int b) { return p.lens ? min(p.lens[b], p.capacity) : p.capacity; };
+    // rows x .. y - 1 and the first sinks are read
+    const auto rows_of = [&](int b) {
+        const int n = p.lens ? min(p.lens[b], p.capacity) : p.capacity;
+        int lo = 0;
+        if (p.window) lo = max(0, n - (p.q_lens ? min(max(p.q_lens[b], 0), p.n_q) : p.n_q) - p.window + 1) & ~3;
+        return make_int2(lo, n);
+    };
+    const auto is_read = [&](int2 range, int j) { return j < range.y && (j >= range.x || j < p.sinks); };
     const auto place = [&](const RowAt &r) {
         RowPlace q;
         q.in = row_ptr(r.of_v ? c.v : c.k, r.of_v ? c.vs : c.ks, r, p.first + (long long)r.i, 1) + BITS * l;
         q.in_scale = reinterpret_cast<const uint8_t *>(row_ptr(r.of_v ? c.v_scale : c.k_scale, r.of_v ? c.vss : c.kss, r, p.first + (long long)r.i, 1)) + (BITS == 4 && D == 128 ? 4 * (l & 1) : 0);
         q.out = const_cast<char *>(row_ptr(r.of_v ? p.v_out : p.k_out, r.of_v ? p.vos : p.kos, r, r.i, sizeof(T))) + 8 * l * sizeof(T);
+        if constexpr (CODES) {
+            q.factor = (r.of_v ? p.v_factor : p.k_factor) + ((long long)r.b * p.by_heads.d + r.h) * p.factor_stride + r.i;
+            q.c = r.of_v ? 1.f : p.c;
+        }
         return q;
     };
     if constexpr (ONE) {
-        const int n = rows_of(head.b) - p.first;
+        const int2 range = rows_of(head.b);
         RowAt r = head;
         r.i += threadIdx.x / L;
         const RowPlace q = place(r);
         const long long in = (head.of_v ? c.vs : c.ks)[2] * R, scale = (head.of_v ? c.vss : c.kss)[2] * R, out = (head.of_v ? p.vos : p.kos)[2] * (long long)sizeof(T) * R;
 #pragma unroll
         for (int u = 0; u < QR_AHEAD; ++u) {
-            real[u] = (int)r.i + u * R < n;
+            real[u] = is_read(range, p.first + (int)r.i + u * R);
             at[u].in = q.in + u * in;
             at[u].in_scale = q.in_scale + u * scale;
             at[u].out = q.out + u * out;
+            if constexpr (CODES) { at[u].factor = q.factor + u * R; at[u].c = q.c; }
         }
     } else {
 #pragma unroll
@@ -449,7 +469,7 @@ __device__ __forceinline__ void quant_read(const RowsDev &p, const QuantDev &c, 
             real[u] = f < p.total;
             if (!real[u]) continue;
             const RowAt r = row_at(p, f);
-            real[u] = p.first + (int)r.i < rows_of(r.b);
+            real[u] = is_read(rows_of(r.b), p.first + (int)r.i);
             at[u] = place(r);
         }
     }
@@ -461,19 +481,23 @@ __device__ __forceinline__ void quant_read(const RowsDev &p, const QuantDev &c, 
         s[u] = *reinterpret_cast<const uint32_t *>(at[u].in_scale);
     }
 #pragma unroll
-    for (int u = 0; u < QR_AHEAD; ++u)
-        if (real[u]) store_values8<T, BITS>(reinterpret_cast<T *>(at[u].out), code[u], s[u]);
+    for (int u = 0; u < QR_AHEAD; ++u) {
+        if (!real[u]) continue;
+        store_values8<T, BITS>(reinterpret_cast<T *>(at[u].out), code[u], CODES ? 0x3f800000u : s[u]);
+        if (CODES && l == 0) *at[u].factor = __uint_as_float(s[u]) * at[u].c;
+    }
 }
 
-template <typename T, int BITS, int D>
+// CODES (8 bits): the codes themselves, as bf16 numbers, and the scales apart.
+template <typename T, int BITS, int D, bool CODES>
 __global__ void __launch_bounds__(QC_NT) k_quant_read(const __grid_constant__ RowsDev p, const __grid_constant__ QuantDev c)
 {
     pdl_wait();
     pdl_trigger();
     constexpr uint32_t ROWS = QC_NT / (D / 8) * QR_AHEAD;
     const RowAt head = row_at(p, blockIdx.x * ROWS);
-    if (head.i + ROWS <= (uint32_t)p.rows) quant_read<T, BITS, D, true>(p, c, head);
-    else quant_read<T, BITS, D, false>(p, c, head);
+    if (head.i + ROWS <= (uint32_t)p.rows) quant_read<T, BITS, D, CODES, true>(p, c, head);
+    else quant_read<T, BITS, D, CODES, false>(p, c, head);
 }
 
 }  // namespace obf
