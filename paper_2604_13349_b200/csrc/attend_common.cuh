@@ -21,8 +21,10 @@ struct AttendDev {
     long long qs[3], ks[3], vs[3], os[3];
     const void *pk, *pv;      // shared prefix, or null
     long long pks[2], pvs[2];
-    const float *k_factor, *v_factor;    // of each key, or null: what its logits (scale and log2 e included) and weights are multiplied by,
-    long long factor_stride;             // rows of a (sequence, KV head) apart, 16-byte aligned, readable for 128 keys behind the last
+    // What logits (scale and log2 e included) and weights of every key are multiplied by, or null: two and two of neighbouring keys; those of
+    // a (sequence, KV head) factor_stride keys, a multiple of 4, behind the one before; readable for 128 keys behind the last.
+    const float4 *factors;
+    long long factor_stride;
     const int32_t *lens, *q_lens;
     float *lse_out;
     const float *mass_in;

@@ -11,7 +11,7 @@ namespace obf {
 // obf_attend for entry points of other files (obf_attend.cu): whether a call's queries are many enough for the tensor cores' tiles of 128 rows, its
 // workspace, and the call itself, with a factor for each key's logits and weights where it goes to those tiles (AttendDev).
 struct AttendFactors {
-    const float *k, *v;
+    const float4 *of;
     long long stride;
 };
 bool attends_in_tiles(const obf_attend_t *a);

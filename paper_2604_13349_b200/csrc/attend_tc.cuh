@@ -43,11 +43,12 @@ constexpr int AT_THREADS = 640;
 constexpr float AT_FUSED_MAX = 4096.f;
 constexpr float AT_RAISE = 25.f, AT_WEIGHT_MAX = 4294967296.f, AT_WEIGHT_MIN = 9.094947017729282e-13f;     // 2^32, 2^-40
 
-template <int D>
+template <int D, bool FACTORS>
 struct AttendTcShape {
     static constexpr int SLOT_BYTES = AT_TILE * D * 2;                    // a tile of Q, K or V
-    static constexpr int SLOTS = D == 128 ? 5 : 8;
-    static constexpr int SMEM_BYTES = (2 + SLOTS) * SLOT_BYTES;           // beside what the kernel declares, and alignment to 1024
+    static constexpr int SLOTS = D == 128 ? (FACTORS ? 4 : 5) : 8;
+    static constexpr int FACTOR_BYTES = FACTORS ? 16 * 512 : 0;           // of 64 keys for each warp of the softmax
+    static constexpr int SMEM_BYTES = (2 + SLOTS) * SLOT_BYTES + FACTOR_BYTES;         // beside what the kernel declares, and alignment to 1024
 };
 
 // Tensor maps and tile shape of the kernel.
@@ -216,12 +217,12 @@ __device__ __forceinline__ uint32_t column_bits(int a, int b)
     return (0xFFFFFFFFu >> (32 - b)) & (0xFFFFFFFFu << a);
 }
 
-// FACTORS: keys and values come with a factor each (p.k_factor, p.v_factor), which a key's logits and weights are multiplied by in fp32.
+// FACTORS: keys and values come with a factor each (p.factors), which a key's logits and weights are multiplied by in fp32.
 template <int D, bool PREFIX, bool FACTORS>
 __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_constant__ AttendDev p, const __grid_constant__ AttendTcMaps tm, const int items,
                                                            const int first)
 {
-    constexpr int SLOTS = AttendTcShape<D>::SLOTS, SLOT_BYTES = AttendTcShape<D>::SLOT_BYTES, BLOCK = AT_TILE * 128, NB = D / 64;
+    constexpr int SLOTS = AttendTcShape<D, FACTORS>::SLOTS, SLOT_BYTES = AttendTcShape<D, FACTORS>::SLOT_BYTES, BLOCK = AT_TILE * 128, NB = D / 64;
     extern __shared__ uint8_t at_smem_raw[];
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(at_smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *q_sm = base, *ring = base + 2 * SLOT_BYTES;
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
     {
         uint32_t given;
         asm("mov.u32 %0, %%dynamic_smem_size;" : "=r"(given));
-        if ((uint32_t)(base - at_smem_raw) + AttendTcShape<D>::SMEM_BYTES > given) {      // (the launch and this layout belong together)
+        if ((uint32_t)(base - at_smem_raw) + AttendTcShape<D, FACTORS>::SMEM_BYTES > given) {      // (the launch and this layout belong together)
             if (tid == 0) atomicOr(p.status, OBF_DEV_INTERNAL);
             return;
         }
@@ -408,6 +409,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
         const int sw = warp - 4, x = sw >> 3, half = (sw >> 2) & 1, quarter = warp & 3, row = quarter * 32 + lane, col0 = half * 64;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_t = tmem + 128 * x + lanes, o_t = tmem + 256 + 128 * x + lanes;
         const f32x2 c2 = pk(p.c, p.c);
+        float4 *factors = reinterpret_cast<float4 *>(ring + SLOTS * SLOT_BYTES) + sw * 32;
         // the row's head of the group, and its query and sequence from the tile's first ones on
         const int row_g = row % p.G, row_b = row / p.G / tm.ti, row_i = row / p.G - row_b * tm.ti;
         // Whether the condition holds for some thread of the two warps that share rows.  Both come here the same number of times,
@@ -444,8 +446,15 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             bool started = false, known = true;           // known: all rows have references
             for (int j = jb; j < je; ++j) {
                 if (!(j < sk || (j >= ja && j < jz))) continue;
+                float4 own_factors;
+                if constexpr (FACTORS) {
+                    // the warp's 64 keys' factors, two keys a lane, under way while the logits are waited for
+                    const int v = j * AT_TILE + col0 + 2 * lane;
+                    own_factors = p.factors[(((long long)it.b * p.kv_heads + it.h) * p.factor_stride + (v < it.head ? v : it.lo + v - it.head)) / 2];
+                }
                 const bool late = !tc::mbar_wait(&bar_s[x], ns & 1u, wc);
                 ++ns;
+                if constexpr (FACTORS) factors[lane] = own_factors;
                 __syncwarp();
                 tc::tc_fence_after();
                 const int width = it.width(j);
@@ -462,10 +471,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                     }
                     return bits;
                 };
-                // factors of four columns of the tiles of keys
-                auto factors = [&](const float *of, int v) {
-                    return reinterpret_cast<const float4 *>(of + ((long long)it.b * p.kv_heads + it.h) * p.factor_stride + (v < it.head ? v : it.lo + v - it.head));
-                };
                 bool formed = false;                      // the tile's weights
                 uint32_t w[32];
                 if (known && (width & 15) == 0) {
@@ -481,29 +486,23 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         if constexpr (FACTORS) {
                             const uint32_t bits = full ? 0xFFFFFFFFu : seen(c);
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float4 kf = *factors(p.k_factor, j * AT_TILE + col0 + 32 * c + e);
-                                float4 vf = *factors(p.v_factor, j * AT_TILE + col0 + 32 * c + e);
-                                f32x2 y = fma2(pk(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), pk(kf.x, kf.y), r2);
-                                float a0, a1, a2, a3;
-                                upk(y, a0, a1);
-                                y = fma2(pk(__uint_as_float(r[e + 2]), __uint_as_float(r[e + 3])), pk(kf.z, kf.w), r2);
-                                upk(y, a2, a3);
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                const float4 kv = factors[16 * c + e / 2];
+                                f32x2 v2 = pk(kv.z, kv.w);
+                                float a, b2;
+                                upk(fma2(pk(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), pk(kv.x, kv.y), r2), a, b2);
                                 if (!full) {
                                     // (factors of keys that are not seen may be anything)
-                                    if (!(bits >> e & 1u)) a0 = -INFINITY, vf.x = 0.f;
-                                    if (!(bits >> (e + 1) & 1u)) a1 = -INFINITY, vf.y = 0.f;
-                                    if (!(bits >> (e + 2) & 1u)) a2 = -INFINITY, vf.z = 0.f;
-                                    if (!(bits >> (e + 3) & 1u)) a3 = -INFINITY, vf.w = 0.f;
+                                    if (!(bits >> e & 1u)) a = -INFINITY;
+                                    if (!(bits >> (e + 1) & 1u)) b2 = -INFINITY;
+                                    v2 = pk(bits >> e & 1u ? kv.z : 0.f, bits >> (e + 1) & 1u ? kv.w : 0.f);
                                 }
-                                a0 = ex2(a0);
-                                a1 = ex2(a1);
-                                a2 = ex2(a2);
-                                a3 = ex2(a3);
-                                z = add2(z, pk(a0, a1));
-                                z = add2(z, pk(a2, a3));
-                                w[16 * c + e / 2] = pack_bf16(a0 * vf.x, a1 * vf.y);
-                                w[16 * c + e / 2 + 1] = pack_bf16(a2 * vf.z, a3 * vf.w);
+                                a = ex2(a);
+                                b2 = ex2(b2);
+                                z = add2(z, pk(a, b2));
+                                upk(mul2(pk(a, b2), v2), a, b2);
+                                w[16 * c + e / 2] = pack_bf16(a, b2);
                             }
                         } else {
                             if (!full) {
@@ -545,12 +544,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         tc::tmem_ld_wait32(r);
                         if constexpr (FACTORS) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float4 kf = *factors(p.k_factor, j * AT_TILE + col0 + 32 * c + e);
-                                r[e] = __float_as_uint(__fmul_rn(__uint_as_float(r[e]), kf.x));
-                                r[e + 1] = __float_as_uint(__fmul_rn(__uint_as_float(r[e + 1]), kf.y));
-                                r[e + 2] = __float_as_uint(__fmul_rn(__uint_as_float(r[e + 2]), kf.z));
-                                r[e + 3] = __float_as_uint(__fmul_rn(__uint_as_float(r[e + 3]), kf.w));
+                            for (int e = 0; e < 32; e += 2) {
+                                const float4 kv = factors[16 * c + e / 2];
+                                r[e] = __float_as_uint(__fmul_rn(__uint_as_float(r[e]), kv.x));
+                                r[e + 1] = __float_as_uint(__fmul_rn(__uint_as_float(r[e + 1]), kv.y));
                             }
                         }
 #pragma unroll
@@ -603,9 +600,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                             float b2 = ex2(__fadd_rn(scaled(__uint_as_float(r[2 * e + 1])), ref));
                             l2 = add2(l2, pk(a, b2));
                             if constexpr (FACTORS) {
-                                const float2 vf = reinterpret_cast<const float2 *>(factors(p.v_factor, j * AT_TILE + col0 + 32 * c + 2 * e - (e & 1) * 2))[e & 1];
-                                a = r[2 * e] == 0xFF800000u ? 0.f : a * vf.x;
-                                b2 = r[2 * e + 1] == 0xFF800000u ? 0.f : b2 * vf.y;
+                                const float4 kv = factors[16 * c + e];
+                                a = r[2 * e] == 0xFF800000u ? 0.f : a * kv.z;
+                                b2 = r[2 * e + 1] == 0xFF800000u ? 0.f : b2 * kv.w;
                             }
                             w[16 * c + e] = pack_bf16(a, b2);
                         }

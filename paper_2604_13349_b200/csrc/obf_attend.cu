@@ -253,7 +253,7 @@ static obf_status_t launch_attend_tc(const AttendDev &p, int first, cudaStream_t
     static const size_t smem = [] {
         cudaFuncAttributes fa = {};
         if (cudaFuncGetAttributes(&fa, k_attend_tc<D, PREFIX, FACTORS>) != cudaSuccess) { (void)cudaGetLastError(); return (size_t)0; }
-        return align_up(fa.sharedSizeBytes, 1024) - fa.sharedSizeBytes + AttendTcShape<D>::SMEM_BYTES;
+        return align_up(fa.sharedSizeBytes, 1024) - fa.sharedSizeBytes + AttendTcShape<D, FACTORS>::SMEM_BYTES;
     }();
     if (smem == 0) return OBF_ERR_CUDA;
     OBF_TRY(set_smem_once(k_attend_tc<D, PREFIX, FACTORS>, smem, done));
@@ -302,7 +302,7 @@ static obf_status_t launch_attend(AttendPath path, const AttendDev &p, int first
     if (path == ATTEND_FEW) return launch_attend_few<TIN, D, PREFIX>(p, first, st);
     if constexpr (sizeof(TIN) == 2) {
         if constexpr (!PREFIX)
-            if (path == ATTEND_TC && p.k_factor) return launch_attend_tc<D, PREFIX, true>(p, first, st);
+            if (path == ATTEND_TC && p.factors) return launch_attend_tc<D, PREFIX, true>(p, first, st);
         if (path == ATTEND_TC) return launch_attend_tc<D, PREFIX, false>(p, first, st);
     }
     return launch_attend_generic<TIN, D, PREFIX>(p, first, st);
@@ -340,7 +340,7 @@ static obf_status_t attend(const obf_attend_t *a, const obf_prefix_t *x, const A
         p.wait_limit_ns = 20000000ull;
         p.debug_drop_load = 1;
     }
-    p.k_factor = factors.k; p.v_factor = factors.v; p.factor_stride = factors.stride;
+    p.factors = factors.of; p.factor_stride = factors.stride;
     p.c = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)a->head_dim)) * 1.4426950408889634f;
     p.batch = a->batch; p.kv_heads = a->kv_heads; p.G = a->q_heads / a->kv_heads; p.n_q = a->n_q; p.capacity = a->capacity;
     // beyond any position a window or a number of first tokens changes nothing; clamped, positions minus windows cannot overflow

@@ -171,7 +171,7 @@ struct QuantLayout {
     int slots;                       // parts of the keys
     bool cluster;                    // which join themselves
     size_t off_part_o, off_part_lse;
-    size_t rows_bytes, off_k, off_v, off_k_factor, off_v_factor;     // tiles: that attention's workspace, the rows, 8 bits: their factors
+    size_t rows_bytes, off_k, off_v, off_factors;      // tiles: that attention's workspace, the rows, 8 bits: their factors
     long long factor_stride;
     size_t total;
 };
@@ -203,12 +203,10 @@ static QuantLayout quant_layout(const obf_attend_t *a, int bits)
         o = align_up(o + rows_kv, 256);
         L.off_v = o;
         o = align_up(o + rows_kv, 256);
-        L.off_k_factor = o;
+        L.off_factors = o;
         if (bits == 8) {
             L.factor_stride = (long long)align_up(a->capacity, 4);
-            const size_t n = ((size_t)heads * L.factor_stride + 128) * sizeof(float);
-            L.off_v_factor = o = align_up(o + n, 256);
-            o = align_up(o + n, 256);
+            o = align_up(o + ((size_t)heads * L.factor_stride + 128) * 2 * sizeof(float), 256);
         }
         L.total = o;
         return L;
@@ -281,11 +279,10 @@ static obf_status_t attend_tiles(const QuantLayout &L, const obf_attend_t *a, co
     p.sinks = a->sinks;
     AttendFactors factors = {};
     if (c->bits == 8) {
-        p.k_factor = reinterpret_cast<float *>(ws + L.off_k_factor);
-        p.v_factor = reinterpret_cast<float *>(ws + L.off_v_factor);
+        p.factors = reinterpret_cast<float *>(ws + L.off_factors);
         p.factor_stride = L.factor_stride;
         p.c = logit_factor(a);
-        factors = {p.k_factor, p.v_factor, L.factor_stride};
+        factors = {reinterpret_cast<const float4 *>(p.factors), L.factor_stride};
     }
     const QuantDev d = quant_dev(c);
     OBF_TRY(with_shape(OBF_BF16, c->bits, a->head_dim, [&](auto t, auto bits, auto dim) -> obf_status_t {

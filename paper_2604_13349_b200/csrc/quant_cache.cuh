@@ -57,7 +57,7 @@ struct RowsDev {
     // of 8 bits the codes, with factors (AttendDev) apart.
     const int32_t *q_lens;
     int32_t n_q, window, sinks;
-    float *k_factor, *v_factor;
+    float *factors;
     long long factor_stride;
     float c;                               // of K's factors
     FastDiv by_rows, by_heads;
@@ -443,7 +443,8 @@ __device__ __forceinline__ void quant_read(const RowsDev &p, const QuantDev &c, 
         q.in_scale = reinterpret_cast<const uint8_t *>(row_ptr(r.of_v ? c.v_scale : c.k_scale, r.of_v ? c.vss : c.kss, r, p.first + (long long)r.i, 1)) + (BITS == 4 && D == 128 ? 4 * (l & 1) : 0);
         q.out = const_cast<char *>(row_ptr(r.of_v ? p.v_out : p.k_out, r.of_v ? p.vos : p.kos, r, r.i, sizeof(T))) + 8 * l * sizeof(T);
         if constexpr (CODES) {
-            q.factor = (r.of_v ? p.v_factor : p.k_factor) + ((long long)r.b * p.by_heads.d + r.h) * p.factor_stride + r.i;
+            // two keys' factors of logits, two of weights (rows of a thread lie multiples of two apart)
+            q.factor = p.factors + (((long long)r.b * p.by_heads.d + r.h) * p.factor_stride + (r.i & ~1u)) * 2 + (r.of_v ? 2 : 0) + (r.i & 1u);
             q.c = r.of_v ? 1.f : p.c;
         }
         return q;
@@ -460,7 +461,7 @@ __device__ __forceinline__ void quant_read(const RowsDev &p, const QuantDev &c, 
             at[u].in = q.in + u * in;
             at[u].in_scale = q.in_scale + u * scale;
             at[u].out = q.out + u * out;
-            if constexpr (CODES) { at[u].factor = q.factor + u * R; at[u].c = q.c; }
+            if constexpr (CODES) { at[u].factor = q.factor + 2 * u * R; at[u].c = q.c; }
         }
     } else {
 #pragma unroll
