@@ -32,10 +32,13 @@ struct QuantStage {
     static constexpr int STAGES = BYTES > 4400 ? 2 : BYTES > 4000 ? 2 : 3;
 };
 
+// Shared memory of a block: the rings, `more` behind them, over all of it at the end the warps' results.
+template <int BITS, int D>
+constexpr int AQ_RING = AF_WARPS * QuantStage<BITS, D>::STAGES * QuantStage<BITS, D>::BYTES;
 template <int BITS, int D, int ROWS>
-__host__ __device__ constexpr size_t attend_quant_smem()
+__host__ __device__ constexpr size_t attend_quant_smem(size_t more)
 {
-    const size_t ring = (size_t)AF_WARPS * QuantStage<BITS, D>::STAGES * QuantStage<BITS, D>::BYTES, end = few_finish_smem<D, ROWS>();
+    const size_t ring = AQ_RING<BITS, D> + more, end = few_finish_smem<D, ROWS>();
     return ring > end ? ring : end;
 }
 
@@ -241,17 +244,27 @@ struct QuantWalk {
     }
 };
 
-// Blocks of a multiprocessor.
-template <typename TIN, int D, int NT>
-constexpr int AQ_BLOCKS = NT == 1 ? (sizeof(TIN) == 4 && D == 128 ? 3 : 4) : (D == 128 ? 2 : 3);
+// Blocks of a multiprocessor, as registers allow.  (16 x 16 query rows over 8192 keys in 8 bits: 3 blocks 64 us, 2 blocks 72; in 4 bits, where 3 spill,
+// 67 and 65, 64 query rows 199 and 185.)
+template <typename TIN, int BITS, int D, int NT>
+constexpr int AQ_BLOCKS = D == 64 ? (sizeof(TIN) == 2 && NT == 2 ? 4 : 3) : sizeof(TIN) == 2 && NT == 2 && BITS == 8 ? 3 : 2;
+
+// A tile's queries, which all warps of a block read over and over: fragments, what the codes' offsets add up to, factors of the logits.
+template <typename TIN, int BITS, int D, int NT>
+struct QuantQueries {
+    static constexpr int PARTS = sizeof(TIN) == 4 ? 2 : 1, KS = D / 16, GR = QuantRow<BITS, D>::GROUPS;
+    uint2 frag[PARTS][NT][KS][32];
+    float off[NT][GR][8], c[NT][8];
+};
 
 template <typename TIN, int BITS, int D, int NT, bool CLUSTER>
-__global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant(const __grid_constant__ AttendDev p, const __grid_constant__ QuantDev c)
+__global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend_quant(const __grid_constant__ AttendDev p, const __grid_constant__ QuantDev c)
 {
     extern __shared__ __align__(128) unsigned char aq_sm[];
     typedef QuantStage<BITS, D> Stage;
     typedef QuantRow<BITS, D> Row;
-    constexpr int KS = D / 16, ROWS = 8 * NT, ST = Stage::STAGES, KEYS = Stage::KEYS, RB = Row::BYTES, CH = RB / 16, LR = 32 / CH, SB = Row::SCALE_BYTES, GR = Row::GROUPS, SUB = KEYS / 16;
+    constexpr int KS = D / 16, ROWS = 8 * NT, ST = Stage::STAGES, KEYS = Stage::KEYS, RB = Row::BYTES, SB = Row::SCALE_BYTES, GR = Row::GROUPS, SUB = KEYS / 16;
+    constexpr int IL = NT <= 2 ? SUB : 1;                 // runs of sixteen keys worked on side by side
     constexpr int PARTS = sizeof(TIN) == 4 ? 2 : 1;       // of a query
     constexpr int WPARTS = sizeof(TIN) == 4 ? 3 : 1;      // of a weight
     pdl_wait();
@@ -272,11 +285,8 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
     const uint32_t ring = walk.ring;
 
     // Queries as B fragments: of row 8 nt + lane / 4 a lane holds a quarter of the channels, those of its words of a key.
-    uint32_t qf[PARTS][NT][KS][2];
-    float q_off[NT][GR][2];                               // what their codes' offsets add up to
-    float row_c[NT][2];                                   // what makes logits (log2) of a product's rows 8 nt + 2 (lane mod 4) + e
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    auto &qs = *reinterpret_cast<QuantQueries<TIN, BITS, D, NT> *>(aq_sm + AQ_RING<BITS, D>);
+    for (int nt = warp; nt < NT; nt += AF_WARPS) {
         const int r = tile * ROWS + nt * 8 + g8, i = r / p.G, g = r - i * p.G;
         const bool real = r < rows_seq && i < ql;
         const TIN *src = static_cast<const TIN *>(p.q) + b * p.qs[0] + (long long)(h * p.G + g) * p.qs[1] + (long long)i * p.qs[2];
@@ -305,7 +315,8 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
 #pragma unroll
         for (int j = 0; j < GR; ++j) sum[j] = 0.f;
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+        for (int k = 0; k < KS; ++k) {
+            uint2 frag[PARTS];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 // the pair's two channels among the lane's (4 bits: those of u = 1 meet codes sixteen times as large)
@@ -315,25 +326,29 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
 #pragma unroll
                 for (int part_q = 0; part_q < PARTS; ++part_q) {
                     const __half2 v = __floats2half2_rn(y, z);
-                    qf[part_q][nt][k][u] = *reinterpret_cast<const uint32_t *>(&v);
+                    (u ? frag[part_q].y : frag[part_q].x) = *reinterpret_cast<const uint32_t *>(&v);
                     y -= __low2float(v);
                     z -= __high2float(v);
                     sum[BITS == 8 ? 0 : k >> 1] += (__low2float(v) + __high2float(v)) * (BITS == 4 && u == 1 ? 16.f : 1.f);
                 }
             }
 #pragma unroll
+            for (int part_q = 0; part_q < PARTS; ++part_q) qs.frag[part_q][nt][k][lane] = frag[part_q];
+        }
+#pragma unroll
         for (int j = 0; j < GR; ++j) {
             sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
             sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                q_off[nt][j][u] = __shfl_sync(0xffffffffu, sum[j], 4 * (2 * t4 + u)) * (BITS == 4 ? -0x1p-21f : -0x1p-17f);       // -8, -128 times 2^-24
+            qs.off[nt][j][g8] = sum[j] * (BITS == 4 ? -0x1p-21f : -0x1p-17f);       // -8, -128 times 2^-24
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            row_c[nt][u] = p.c * 0x1p24f * __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + u));
-        }
+        qs.c[nt][g8] = p.c * 0x1p24f * down;
     }
+    __syncthreads();
+    float row_c[NT][2];                                   // what makes logits (log2) of a product's rows 8 nt + 2 (lane mod 4) + e
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) row_c[nt][e] = qs.c[nt][2 * t4 + e];
 
     float o[NT][KS][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -361,24 +376,26 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
         walk.next(va, slot);
         const uint32_t off = slot * Stage::BYTES, kd = k_at + off, vd0 = v_at[0] + off, vd1 = v_at[1] + off, sd = s_at + off;
         float s[SUB][NT][4];
-        // ---- logits (products that wait for one another are kept apart by those of the other sixteen keys) ----
+        // ---- logits (products that wait for one another are kept apart by those of other rows and of the other sixteen keys) ----
+#pragma unroll
+        for (int s0 = 0; s0 < SUB; s0 += IL) {
         if constexpr (BITS == 4) {
             constexpr int KW = D / 32;                    // words of a lane
-            uint32_t w0[SUB][KW], w1[SUB][KW], f0[SUB][GR / 2], f1[SUB][GR / 2];
+            uint32_t w0[IL][KW], w1[IL][KW], f0[IL][GR / 2], f1[IL][GR / 2];
 #pragma unroll
-            for (int sub = 0; sub < SUB; ++sub) {
-                lds(w0[sub], kd + sub * 16 * RB);
-                lds(w1[sub], kd + (sub * 16 + 8) * RB);
-                lds(f0[sub], sd + sub * 16 * SB);
-                lds(f1[sub], sd + (sub * 16 + 8) * SB);
+            for (int sub = 0; sub < IL; ++sub) {
+                lds(w0[sub], kd + (s0 + sub) * 16 * RB);
+                lds(w1[sub], kd + ((s0 + sub) * 16 + 8) * RB);
+                lds(f0[sub], sd + (s0 + sub) * 16 * SB);
+                lds(f1[sub], sd + ((s0 + sub) * 16 + 8) * SB);
             }
 #pragma unroll
             for (int j = 0; j < GR; ++j) {
                 const int sel = j & 1 ? 0x7632 : 0x5410;
-                uint32_t n0[SUB][4], n1[SUB][4];
-                float acc[SUB][NT][4];
+                uint32_t n0[IL][4], n1[IL][4];
+                float acc[IL][NT][4];
 #pragma unroll
-                for (int sub = 0; sub < SUB; ++sub) {
+                for (int sub = 0; sub < IL; ++sub) {
                     nibbles(n0[sub], __byte_perm(w0[sub][j >> 1], w0[sub][(j >> 1) + KW / 2], sel));
                     nibbles(n1[sub], __byte_perm(w1[sub][j >> 1], w1[sub][(j >> 1) + KW / 2], sel));
                 }
@@ -387,39 +404,41 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
 #pragma unroll
                     for (int part_q = PARTS - 1; part_q >= 0; --part_q)
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint2 qf = qs.frag[part_q][nt][2 * j + i][lane];
 #pragma unroll
-                            for (int sub = 0; sub < SUB; ++sub) {
+                            for (int sub = 0; sub < IL; ++sub) {
                                 const uint32_t a[4] = {n0[sub][2 * i], n1[sub][2 * i], n0[sub][2 * i + 1], n1[sub][2 * i + 1]};
-                                if (i == 0 && part_q == PARTS - 1) mma_f16_first(acc[sub][nt], a, qf[part_q][nt][2 * j][0], qf[part_q][nt][2 * j][1]);
-                                else mma_f16(acc[sub][nt], a, qf[part_q][nt][2 * j + i][0], qf[part_q][nt][2 * j + i][1]);
+                                if (i == 0 && part_q == PARTS - 1) mma_f16_first(acc[sub][nt], a, qf.x, qf.y);
+                                else mma_f16(acc[sub][nt], a, qf.x, qf.y);
                             }
+                        }
 #pragma unroll
-                for (int sub = 0; sub < SUB; ++sub) {
+                for (int sub = 0; sub < IL; ++sub) {
                     const float k0 = j & 1 ? bf16_hi(f0[sub][j >> 1]) : bf16_lo(f0[sub][j >> 1]), k1 = j & 1 ? bf16_hi(f1[sub][j >> 1]) : bf16_lo(f1[sub][j >> 1]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float f = e < 2 ? k0 : k1, y = acc[sub][nt][e] + q_off[nt][j][e & 1];
-                            s[sub][nt][e] = j == 0 ? y * f : fmaf(y, f, s[sub][nt][e]);
+                            const float f = e < 2 ? k0 : k1, y = acc[sub][nt][e] + qs.off[nt][j][2 * t4 + (e & 1)];
+                            s[s0 + sub][nt][e] = j == 0 ? y * f : fmaf(y, f, s[s0 + sub][nt][e]);
                         }
                 }
             }
         } else {
-            float acc[SUB][NT][2][4];
+            float acc[IL][NT][2][4];
 #pragma unroll
             for (int half = 0; half < KS / 4; ++half) {
-                uint32_t w0[SUB][4], w1[SUB][4];
+                uint32_t w0[IL][4], w1[IL][4];
 #pragma unroll
-                for (int sub = 0; sub < SUB; ++sub) {
-                    lds(w0[sub], (half ? kd ^ 64u : kd) + sub * 16 * RB);       // (rows of 128 bytes: chunks t and t + 4)
-                    lds(w1[sub], (half ? kd ^ 64u : kd) + (sub * 16 + 8) * RB);
+                for (int sub = 0; sub < IL; ++sub) {
+                    lds(w0[sub], (half ? kd ^ 64u : kd) + (s0 + sub) * 16 * RB);       // (rows of 128 bytes: chunks t and t + 4)
+                    lds(w1[sub], (half ? kd ^ 64u : kd) + ((s0 + sub) * 16 + 8) * RB);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int sub = 0; sub < SUB; ++sub) {
+                    for (int sub = 0; sub < IL; ++sub) {
                         const int k = 4 * half + i;
                         const uint32_t x = w0[sub][i] ^ 0x80808080u, y = w1[sub][i] ^ 0x80808080u;
                         const uint32_t a[4] = {__byte_perm(x, 0u, 0x4140), __byte_perm(y, 0u, 0x4140), __byte_perm(x, 0u, 0x4342), __byte_perm(y, 0u, 0x4342)};
@@ -427,19 +446,21 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
                         for (int part_q = PARTS - 1; part_q >= 0; --part_q)
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                if (k < 2 && part_q == PARTS - 1) mma_f16_first(acc[sub][nt][k], a, qf[part_q][nt][k][0], qf[part_q][nt][k][1]);
-                                else mma_f16(acc[sub][nt][k & 1], a, qf[part_q][nt][k][0], qf[part_q][nt][k][1]);
+                                const uint2 qf = qs.frag[part_q][nt][k][lane];
+                                if (k < 2 && part_q == PARTS - 1) mma_f16_first(acc[sub][nt][k], a, qf.x, qf.y);
+                                else mma_f16(acc[sub][nt][k & 1], a, qf.x, qf.y);
                             }
                     }
             }
 #pragma unroll
-            for (int sub = 0; sub < SUB; ++sub) {
-                const float k0 = __uint_as_float(lds1(sd + sub * 16 * SB)), k1 = __uint_as_float(lds1(sd + (sub * 16 + 8) * SB));
+            for (int sub = 0; sub < IL; ++sub) {
+                const float k0 = __uint_as_float(lds1(sd + (s0 + sub) * 16 * SB)), k1 = __uint_as_float(lds1(sd + ((s0 + sub) * 16 + 8) * SB));
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[sub][nt][e] = (acc[sub][nt][0][e] + acc[sub][nt][1][e] + q_off[nt][0][e & 1]) * (e < 2 ? k0 : k1);
+                    for (int e = 0; e < 4; ++e) s[s0 + sub][nt][e] = (acc[sub][nt][0][e] + acc[sub][nt][1][e] + qs.off[nt][0][2 * t4 + (e & 1)]) * (e < 2 ? k0 : k1);
             }
+        }
         }
         // ---- weights: s[sub][nt][2 u + e] is key 8 u + key_s of sixteen, row 8 nt + 2 (lane mod 4) + e ----
 #pragma unroll
@@ -502,20 +523,22 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
                 }
         // ---- values ----
         if constexpr (BITS == 4) {
-            uint32_t w[SUB][4][W], f0[SUB][GR / 2], f1[SUB][GR / 2];            // of keys lane mod 4 + 4 i
 #pragma unroll
-            for (int sub = 0; sub < SUB; ++sub) {
+            for (int s0 = 0; s0 < SUB; s0 += IL) {
+            uint32_t w[IL][4][W], f0[IL][GR / 2], f1[IL][GR / 2];            // of keys lane mod 4 + 4 i
 #pragma unroll
-                for (int i = 0; i < 4; ++i) lds(w[sub][i], (i & 1 ? vd1 : vd0) + (sub * 16 + (i & 2) * 4) * RB);
-                lds(f0[sub], sd + Stage::SCALES + sub * 16 * SB);
-                lds(f1[sub], sd + Stage::SCALES + (sub * 16 + 8) * SB);
+            for (int sub = 0; sub < IL; ++sub) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) lds(w[sub][i], (i & 1 ? vd1 : vd0) + ((s0 + sub) * 16 + (i & 2) * 4) * RB);
+                lds(f0[sub], sd + Stage::SCALES + (s0 + sub) * 16 * SB);
+                lds(f1[sub], sd + Stage::SCALES + ((s0 + sub) * 16 + 8) * SB);
             }
 #pragma unroll
             for (int j = 0; j < GR; ++j) {
                 const int sel = j & 1 ? 0x7632 : 0x5410;
-                uint32_t pf[SUB][NT][WPARTS][2], ab[SUB][4], cd[SUB][4];
+                uint32_t pf[IL][NT][WPARTS][2], ab[IL][4], cd[IL][4];
 #pragma unroll
-                for (int sub = 0; sub < SUB; ++sub) {
+                for (int sub = 0; sub < IL; ++sub) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -523,7 +546,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
                             const uint32_t fw = u ? f1[sub][j >> 1] : f0[sub][j >> 1];
                             const float f = j & 1 ? bf16_hi(fw) : bf16_lo(fw);
                             uint32_t pw[WPARTS];
-                            split_weights<WPARTS>(pw, s[sub][nt][2 * u] * f, s[sub][nt][2 * u + 1] * f);
+                            split_weights<WPARTS>(pw, s[s0 + sub][nt][2 * u] * f, s[s0 + sub][nt][2 * u + 1] * f);
 #pragma unroll
                             for (int q = 0; q < WPARTS; ++q) pf[sub][nt][q][u] = transpose8x8(pw[q]);
                         }
@@ -536,7 +559,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
                     }
                 }
 #pragma unroll
-                for (int sub = 0; sub < SUB; ++sub)
+                for (int sub = 0; sub < IL; ++sub)
 #pragma unroll
                     for (int q = WPARTS - 1; q >= 0; --q)
 #pragma unroll
@@ -546,6 +569,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, D, NT>)) k_attend_quant
                                 const uint32_t a[4] = {ab[sub][2 * i], ab[sub][2 * i + 1], cd[sub][2 * i], cd[sub][2 * i + 1]};
                                 mma_bf16(o[nt][2 * j + i], a, pf[sub][nt][q][0], pf[sub][nt][q][1]);
                             }
+            }
             }
         } else {
 #pragma unroll

@@ -176,19 +176,43 @@ struct QuantLayout {
     size_t total;
 };
 
-// Query rows of a KV head from which on bf16 calls read the cache's rows back and attend over those on the tensor cores' tiles of 128 rows,
-// and what the rows may take of a workspace.
-constexpr long long QUANT_TILES_FROM = 97;
+// Query rows of a KV head from which on bf16 calls read the cache's rows back and attend over those on the tensor cores' tiles of 128 rows.
+// (16 sequences of 7000 to 8192 keys of 128 channels, us, on codes and on rows read back: 4 bits, 64 rows 185 and 223, 96 rows 264 and 225; 8 bits, 96 rows
+// 214 and 296, 128 rows 295 and 297.  64 channels: 4 bits, 64 rows 109 and 155; 4 of 4096 keys, 128 rows 36.4 and 34.4.)
+static long long quant_tiles_from(int bits, int head_dim) { return bits == 8 ? 129 : head_dim == 128 ? 81 : 113; }
+// What the rows may take of a workspace.
 constexpr size_t QUANT_ROWS_BYTES = (size_t)4 << 30;
 
-// Query rows of a tile: 4 and 8 of k_attend_quant_few, 16 of k_attend_quant.
-static int quant_rows(long long rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
-
-// Blocks that run at once.
-static int quant_resident(int dtype, int head_dim, int rows)
+// Query rows of a tile: 4 and 8 of k_attend_quant_few, 16, 24 and 32 of k_attend_quant, whose registers hold no more than 16 in fp32, and 32 in 4 bits
+// only at 64 channels.  (16 sequences of 7000 to 8192 keys, us: 20 rows in a tile of 24 90, in two of 16 111; 64 rows of 128 channels in tiles of 32 and 16
+// 179 and 190 in 8 bits, 222 and 185 in 4 bits; of 64 channels in 4 bits 109 and 121.)
+static int quant_rows(int dtype, int bits, int head_dim, long long rows)
 {
-    if (rows == 16) return 148 * (head_dim == 64 ? 3 : 2);
-    return 148 * (dtype == OBF_F32 ? (rows == 4 ? AQF_BLOCKS<float, 1> : AQF_BLOCKS<float, 2>) : (rows == 4 ? AQF_BLOCKS<__nv_bfloat16, 1> : AQF_BLOCKS<__nv_bfloat16, 2>));
+    if (rows <= 8) return rows <= 4 ? 4 : 8;
+    if (dtype == OBF_F32 || rows <= 16) return 16;
+    return rows <= 24 ? 24 : bits == 8 || head_dim == 64 ? 32 : 16;
+}
+
+// Runs body with a tile's rows as a constant.
+template <typename T, int BITS, int D, typename F>
+static obf_status_t with_rows(int rows, F body)
+{
+    if (rows == 4) return body(std::integral_constant<int, 4>());
+    if (rows == 8) return body(std::integral_constant<int, 8>());
+    if constexpr (sizeof(T) == 2) {
+        if (rows == 24) return body(std::integral_constant<int, 24>());
+        if constexpr (BITS == 8 || D == 64)
+            if (rows == 32) return body(std::integral_constant<int, 32>());
+    }
+    return body(std::integral_constant<int, 16>());
+}
+
+// Blocks of a multiprocessor.
+template <typename T, int BITS, int D, int ROWS>
+static constexpr int blocks_of()
+{
+    if constexpr (ROWS >= 16) return AQ_BLOCKS<T, BITS, D, ROWS / 8>;
+    else return AQF_BLOCKS<T, ROWS / 4>;
 }
 
 static QuantLayout quant_layout(const obf_attend_t *a, int bits)
@@ -196,7 +220,7 @@ static QuantLayout quant_layout(const obf_attend_t *a, int bits)
     QuantLayout L = {};
     const long long rows_seq = (long long)(a->q_heads / a->kv_heads) * a->n_q, heads = (long long)a->batch * a->kv_heads, rows = heads * rows_seq;
     const size_t rows_kv = (size_t)heads * a->capacity * a->head_dim * 2;
-    L.tiles = a->dtype == OBF_BF16 && !(a->flags & OBF_FLAG_GENERIC_PATH) && rows_seq >= QUANT_TILES_FROM && 2 * rows_kv <= QUANT_ROWS_BYTES && attends_in_tiles(a);
+    L.tiles = a->dtype == OBF_BF16 && !(a->flags & OBF_FLAG_GENERIC_PATH) && rows_seq >= quant_tiles_from(bits, a->head_dim) && 2 * rows_kv <= QUANT_ROWS_BYTES && attends_in_tiles(a);
     if (L.tiles) {
         size_t o = L.rows_bytes = align_up(attend_rows_bytes(a), 256);
         L.off_k = o;
@@ -211,9 +235,15 @@ static QuantLayout quant_layout(const obf_attend_t *a, int bits)
         L.total = o;
         return L;
     }
-    const int t = quant_rows(rows_seq);
+    const int t = quant_rows(a->dtype, bits, a->head_dim, rows_seq);
     const long long tiles = heads * ((rows_seq + t - 1) / t), keys = most_keys(a, t);
-    const int resident = quant_resident(a->dtype, a->head_dim, t);
+    int resident = 0;                                     // blocks that run at once
+    (void)with_shape(a->dtype, bits, a->head_dim, [&](auto tin, auto nbits, auto dim) -> obf_status_t {
+        return with_rows<decltype(tin), nbits.value, dim.value>(t, [&](auto rows) -> obf_status_t {
+            resident = 148 * blocks_of<decltype(tin), nbits.value, dim.value, rows.value>();
+            return OBF_OK;
+        });
+    });
     const bool small = 8 * tiles <= resident && keys <= 4096;
     L.slots = small ? parts_for(1, keys, 8, 64) : few_parts(tiles, keys, resident);
     L.cluster = L.slots > 1 && L.slots <= 8 && tiles * L.slots <= resident;
@@ -231,9 +261,9 @@ template <typename T, int BITS, int D, int ROWS, bool CLUSTER>
 static obf_status_t launch_quant_rows(const AttendDev &p, const QuantDev &d, cudaStream_t st)
 {
     static bool done[64];
-    constexpr size_t smem = attend_quant_smem<BITS, D, ROWS>();
+    constexpr size_t smem = attend_quant_smem<BITS, D, ROWS>(ROWS >= 16 ? sizeof(QuantQueries<T, BITS, D, ROWS / 8>) : 0);
     const auto kernel = [] {
-        if constexpr (ROWS == 16) return k_attend_quant<T, BITS, D, 2, CLUSTER>;
+        if constexpr (ROWS >= 16) return k_attend_quant<T, BITS, D, ROWS / 8, CLUSTER>;
         else return k_attend_quant_few<T, BITS, D, ROWS / 4, CLUSTER>;
     }();
     OBF_TRY(set_smem_once(kernel, smem, done));
@@ -248,11 +278,8 @@ template <typename T, int BITS, int D>
 static obf_status_t launch_quant(const AttendDev &p, const QuantDev &d, cudaStream_t st)
 {
     const auto rows = [&](auto cluster) -> obf_status_t {
-        switch (quant_rows((long long)p.n_q * p.G)) {
-        case 4: return launch_quant_rows<T, BITS, D, 4, cluster.value>(p, d, st);
-        case 8: return launch_quant_rows<T, BITS, D, 8, cluster.value>(p, d, st);
-        default: return launch_quant_rows<T, BITS, D, 16, cluster.value>(p, d, st);
-        }
+        return with_rows<T, BITS, D>(quant_rows(sizeof(T) == 4 ? OBF_F32 : OBF_BF16, BITS, D, (long long)p.n_q * p.G),
+                                     [&](auto rows_tile) -> obf_status_t { return launch_quant_rows<T, BITS, D, rows_tile.value, cluster.value>(p, d, st); });
     };
     if (p.cluster) return rows(std::true_type());
     OBF_TRY(rows(std::false_type()));
