@@ -247,7 +247,7 @@ struct QuantWalk {
 // Blocks of a multiprocessor, as registers allow.  (16 x 16 query rows over 8192 keys in 8 bits: 3 blocks 64 us, 2 blocks 72; in 4 bits, where 3 spill,
 // 67 and 65, 64 query rows 199 and 185.)
 template <typename TIN, int BITS, int D, int NT>
-constexpr int AQ_BLOCKS = D == 64 ? (sizeof(TIN) == 2 && NT == 2 ? 4 : 3) : sizeof(TIN) == 2 && NT == 2 && BITS == 8 ? 3 : 2;
+constexpr int AQ_BLOCKS = D == 64 ? (sizeof(TIN) == 4 ? (NT == 2 ? 3 : 2) : NT == 2 ? 4 : 3) : sizeof(TIN) == 2 && NT == 2 && BITS == 8 ? 3 : 2;
 
 // A tile's queries, which all warps of a block read over and over: fragments, what the codes' offsets add up to, factors of the logits.
 template <typename TIN, int BITS, int D, int NT>

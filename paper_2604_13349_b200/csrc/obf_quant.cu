@@ -183,14 +183,15 @@ static long long quant_tiles_from(int bits, int head_dim) { return bits == 8 ? 1
 // What the rows may take of a workspace.
 constexpr size_t QUANT_ROWS_BYTES = (size_t)4 << 30;
 
-// Query rows of a tile: 4 and 8 of k_attend_quant_few, 16, 24 and 32 of k_attend_quant, whose registers hold no more than 16 in fp32, and 32 in 4 bits
-// only at 64 channels.  (16 sequences of 7000 to 8192 keys, us: 20 rows in a tile of 24 90, in two of 16 111; 64 rows of 128 channels in tiles of 32 and 16
-// 179 and 190 in 8 bits, 222 and 185 in 4 bits; of 64 channels in 4 bits 109 and 121.)
+// Query rows of a tile: 4 and 8 of k_attend_quant_few, 16, 24 and 32 of k_attend_quant: as many as registers hold, in fp32 no more than 24, in 4 bits at 128
+// channels more than 16 only where one tile does.  (16 sequences of 7000 to 8192 keys of 128 channels, us: 20 rows in a tile of 24 and in two of 16
+// 90 and 111, fp32 145 and 172; 64 rows in tiles of 32 and 16 179 and 190 in 8 bits, 222 and 185 in 4 bits, of 64 channels 109 and 121; fp32 in tiles of 24
+// and 16 340 and 308 in 4 bits.)
 static int quant_rows(int dtype, int bits, int head_dim, long long rows)
 {
     if (rows <= 8) return rows <= 4 ? 4 : 8;
-    if (dtype == OBF_F32 || rows <= 16) return 16;
-    return rows <= 24 ? 24 : bits == 8 || head_dim == 64 ? 32 : 16;
+    if (rows <= 24) return rows <= 16 ? 16 : 24;
+    return bits == 4 && head_dim == 128 ? 16 : dtype == OBF_F32 ? 24 : 32;
 }
 
 // Runs body with a tile's rows as a constant.
@@ -199,6 +200,8 @@ static obf_status_t with_rows(int rows, F body)
 {
     if (rows == 4) return body(std::integral_constant<int, 4>());
     if (rows == 8) return body(std::integral_constant<int, 8>());
+    if constexpr (sizeof(T) == 4)
+        if (rows == 24) return body(std::integral_constant<int, 24>());
     if constexpr (sizeof(T) == 2) {
         if (rows == 24) return body(std::integral_constant<int, 24>());
         if constexpr (BITS == 8 || D == 64)
