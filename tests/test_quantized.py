@@ -397,6 +397,45 @@ def test_attention_of_many_queries(bits, d, kw, dtype, flags):
     _attended(d=d, bits=bits, dtype=dtype, seed=bits + d + kw["cap"], flags=flags, five=True, **kw)
 
 
+BIG = [
+    # (channels, case): calls of enough rows and keys to read rows back first
+    (128, dict(B=2, kv=2, G=8, n_q=200, cap=1000, lens=[1000, 333], q_lens=[200, 77], token_major=True)),
+    (64, dict(B=1, kv=2, G=4, n_q=1050, cap=1050, window=1000, sinks=5)),
+    (128, dict(B=2, kv=1, G=6, n_q=600, cap=1101, lens=[1101, 0], q_lens=[600, 3], window=801, sinks=70)),
+    (64, dict(B=3, kv=1, G=8, n_q=300, cap=1115, lens=[1115, 7, 300], q_lens=[300, 13, 1], window=903, sinks=33)),
+    (128, dict(B=1, kv=1, G=128, n_q=50, cap=1100, scale=0.3)), (128, dict(B=1, kv=2, G=3, n_q=1301, cap=1301, size=15.0)),
+    (64, dict(B=2, kv=1, G=5, n_q=600, cap=1500, window=999, sinks=600)), (128, dict(B=1, kv=1, G=4, n_q=801, cap=4097, window=2050, sinks=17)),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits,five", [(4, True), (4, False), (8, True)])
+@pytest.mark.parametrize("d,kw", BIG)
+def test_attention_over_rows_read_back(bits, five, d, kw):
+    _attended(d=d, bits=bits, dtype=BF16, seed=bits + d + kw["cap"], five=five, **kw)
+    assert P.obf_last_launch_count() >= 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 8])
+def test_rows_read_back_hold_nothing_of_what_is_not_seen(bits):
+    # the workspace is full of what is not a number, and so is the cache behind the window and the last key
+    gen = torch.Generator().manual_seed(9)
+    cache = _held(gen, 1, 2, 1400, 128, bits)
+    q = torch.randn(1, 16, 900, 128, generator=gen).to(BF16).cuda()
+    lens = torch.tensor([1303], dtype=torch.int32, device="cuda")
+    kw = dict(lens=lens, window=301, sinks=3)
+    want = P.attend_quantized(q, cache, **kw)["out"]
+    lo = 1303 - 900 - 301 + 1
+    for t in cache[2:]:
+        t[:, :, 1303:] = math.nan
+        t[:, :, 3:lo] = math.inf
+    ws = P.attend_quantized_workspace(q, cache, window=301, sinks=3)
+    ws.fill_(0xFF)
+    assert torch.equal(P.attend_quantized(q, cache, workspace=ws, **kw)["out"], want)
+    assert P.obf_last_launch_count() >= 2
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [4, 8])
 def test_queries_of_any_size(bits):
@@ -419,15 +458,16 @@ def test_queries_of_any_size(bits):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("n_q", [1, 12, 50])
+@pytest.mark.parametrize("n_q", [1, 12, 50, 800])
 def test_scales_that_are_not_numbers_are_seen(bits, n_q):
     gen = torch.Generator().manual_seed(5)
-    cache = _held(gen, 2, 2, 100, 64, bits)
+    cap = max(100, n_q)
+    cache = _held(gen, 2, 2, cap, 64, bits)
     q = torch.randn(2, 8, n_q, 64, generator=gen).to(BF16).cuda()
     want = P.attend_quantized(q, cache)["out"]
-    cache.v_scale[0, 1, 50] = math.nan
+    cache.v_scale[0, 1, cap - n_q // 2 - 1] = math.nan
     got = P.attend_quantized(q, cache)["out"]
-    assert bool(torch.isnan(got[0, 4:]).any(-1).all()) and torch.equal(got[1], want[1]) and torch.equal(got[0, :4], want[0, :4])
+    assert bool(torch.isnan(got[0, 4:, n_q - n_q // 2 - 1 :]).any(-1).all()) and torch.equal(got[1], want[1]) and torch.equal(got[0, :4], want[0, :4])
 
 
 @pytest.mark.gpu
