@@ -21,7 +21,9 @@
 namespace obf {
 
 constexpr float AQ_NONE = -3e38f;                         // reference of a row that has seen no key: any logit raises it
-constexpr float AQ_BIAS = 75.f;                           // references lie so far below the maximum at which they were last raised
+// bf16 calls: references lie so far below the maximum at which they were last raised, since what weights multiply is in units of 2^-133.
+template <typename TIN>
+constexpr float AQ_BIAS = sizeof(TIN) == 4 ? 0.f : 75.f;
 
 template <int BITS, int D>
 struct QuantStage {
@@ -97,6 +99,31 @@ __device__ __forceinline__ void mma_f16_first(float (&c)[4], const uint32_t (&a)
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
+__device__ __forceinline__ void mma_bf16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+// c += a * (the sum of the parts): on top of c, or, EXACT, by itself and then added, since matrix products cut off what their sums cannot hold, which
+// over thousands of keys all goes one way.
+template <bool EXACT, int PARTS>
+__device__ __forceinline__ void mma_weights(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&w)[PARTS][2])
+{
+    if constexpr (EXACT) {
+        float t[4];
+        mma_bf16_first(t, a, w[PARTS - 1][0], w[PARTS - 1][1]);
+#pragma unroll
+        for (int q = PARTS - 2; q >= 0; --q) mma_bf16(t, a, w[q][0], w[q][1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] += t[e];
+    } else {
+#pragma unroll
+        for (int q = PARTS - 1; q >= 0; --q) mma_bf16(c, a, w[q][0], w[q][1]);
+    }
+}
+
 // Codes as numbers, without arithmetic: the bits of a small whole number u are the fp16 number u 2^-24 (u < 2048) and the bf16 number
 // u 2^-133 (u < 256), and matrix products take such numbers exactly.  A word of two halves of four codes plus 8 gives, by masks,
 // pairs of codes 0 and 2 and, sixteen times as large, of codes 1 and 3 of the halves.
@@ -114,6 +141,30 @@ __device__ __forceinline__ uint32_t add_bf16(uint32_t x, uint32_t y)
     uint32_t r;
     asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
     return r;
+}
+// fp32 calls: such small numbers have few bits above the matrix product's sums, which align what they add by exponents as written, so codes become
+// numbers of full size, their offsets taken off: 1024 + u, 1024 + 16 u in fp16, 128 + u in bf16, 2^23 + u of bytes on the way to bf16.
+__device__ __forceinline__ uint32_t add_f16(uint32_t x, uint32_t y)
+{
+    uint32_t r;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+constexpr uint32_t AQ_F16_8 = 0xe408e408u, AQ_F16_128 = 0xe480e480u;       // -1032, -1152 in fp16
+__device__ __forceinline__ void nibbles_f16(uint32_t (&r)[4], uint32_t x)       // codes 1 and 3 sixteenfold
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t y = i < 2 ? x : x >> 8;
+        r[i] = add_f16((i & 1 ? y & 0x00f000f0u : y & 0x000f000fu) | 0x64006400u, i & 1 ? AQ_F16_128 : AQ_F16_8);
+    }
+}
+__device__ __forceinline__ uint32_t bytes_f16(uint32_t x, int sel) { return add_f16(__byte_perm(x ^ 0x80808080u, 0x64646464u, sel), AQ_F16_128); }
+__device__ __forceinline__ uint32_t nibble_bf16(uint32_t x, int n) { return add_bf16(((x >> (4 * n)) & 0x000f000fu) | 0x43004300u, 0xc308c308u); }      // -136
+__device__ __forceinline__ uint32_t byte_pair_bf16(uint32_t a, uint32_t b, int n)      // byte n of two words (codes plus 128)
+{
+    const float x = __uint_as_float(__byte_perm(a, 0x4b000000u, 0x7440 + n)), y = __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7440 + n));
+    return pack_bf16(x - 8388736.f, y - 8388736.f);
 }
 // Bytes n and n + 1 (n even) of two words as pairs.
 __device__ __forceinline__ void byte_pairs(uint32_t &lo, uint32_t &hi, uint32_t a, uint32_t b, int n)
@@ -267,6 +318,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
     constexpr int IL = NT <= 2 ? SUB : 1;                 // runs of sixteen keys worked on side by side
     constexpr int PARTS = sizeof(TIN) == 4 ? 2 : 1;       // of a query
     constexpr int WPARTS = sizeof(TIN) == 4 ? 3 : 1;      // of a weight
+    constexpr bool EXACT = sizeof(TIN) == 4;              // codes at their full size
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0) attend_status(p);
@@ -341,7 +393,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
             sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
             qs.off[nt][j][g8] = sum[j] * (BITS == 4 ? -0x1p-21f : -0x1p-17f);       // -8, -128 times 2^-24
         }
-        qs.c[nt][g8] = p.c * 0x1p24f * down;
+        qs.c[nt][g8] = p.c * (EXACT ? 1.f : 0x1p24f) * down;
     }
     __syncthreads();
     float row_c[NT][2];                                   // what makes logits (log2) of a product's rows 8 nt + 2 (lane mod 4) + e
@@ -396,8 +448,14 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
                 float acc[IL][NT][4];
 #pragma unroll
                 for (int sub = 0; sub < IL; ++sub) {
-                    nibbles(n0[sub], __byte_perm(w0[sub][j >> 1], w0[sub][(j >> 1) + KW / 2], sel));
-                    nibbles(n1[sub], __byte_perm(w1[sub][j >> 1], w1[sub][(j >> 1) + KW / 2], sel));
+                    const uint32_t y = __byte_perm(w0[sub][j >> 1], w0[sub][(j >> 1) + KW / 2], sel), z = __byte_perm(w1[sub][j >> 1], w1[sub][(j >> 1) + KW / 2], sel);
+                    if constexpr (EXACT) {
+                        nibbles_f16(n0[sub], y);
+                        nibbles_f16(n1[sub], z);
+                    } else {
+                        nibbles(n0[sub], y);
+                        nibbles(n1[sub], z);
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -420,7 +478,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float f = e < 2 ? k0 : k1, y = acc[sub][nt][e] + qs.off[nt][j][2 * t4 + (e & 1)];
+                            const float f = e < 2 ? k0 : k1, y = EXACT ? acc[sub][nt][e] : acc[sub][nt][e] + qs.off[nt][j][2 * t4 + (e & 1)];
                             s[s0 + sub][nt][e] = j == 0 ? y * f : fmaf(y, f, s[s0 + sub][nt][e]);
                         }
                 }
@@ -440,8 +498,19 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 #pragma unroll
                     for (int sub = 0; sub < IL; ++sub) {
                         const int k = 4 * half + i;
-                        const uint32_t x = w0[sub][i] ^ 0x80808080u, y = w1[sub][i] ^ 0x80808080u;
-                        const uint32_t a[4] = {__byte_perm(x, 0u, 0x4140), __byte_perm(y, 0u, 0x4140), __byte_perm(x, 0u, 0x4342), __byte_perm(y, 0u, 0x4342)};
+                        uint32_t a[4];
+                        if constexpr (EXACT) {
+                            a[0] = bytes_f16(w0[sub][i], 0x4140);
+                            a[1] = bytes_f16(w1[sub][i], 0x4140);
+                            a[2] = bytes_f16(w0[sub][i], 0x4342);
+                            a[3] = bytes_f16(w1[sub][i], 0x4342);
+                        } else {
+                            const uint32_t x = w0[sub][i] ^ 0x80808080u, y = w1[sub][i] ^ 0x80808080u;
+                            a[0] = __byte_perm(x, 0u, 0x4140);
+                            a[1] = __byte_perm(y, 0u, 0x4140);
+                            a[2] = __byte_perm(x, 0u, 0x4342);
+                            a[3] = __byte_perm(y, 0u, 0x4342);
+                        }
 #pragma unroll
                         for (int part_q = PARTS - 1; part_q >= 0; --part_q)
 #pragma unroll
@@ -458,7 +527,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[s0 + sub][nt][e] = (acc[sub][nt][0][e] + acc[sub][nt][1][e] + qs.off[nt][0][2 * t4 + (e & 1)]) * (e < 2 ? k0 : k1);
+                    for (int e = 0; e < 4; ++e) s[s0 + sub][nt][e] = (acc[sub][nt][0][e] + acc[sub][nt][1][e] + (EXACT ? 0.f : qs.off[nt][0][2 * t4 + (e & 1)])) * (e < 2 ? k0 : k1);
             }
         }
         }
@@ -494,7 +563,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
                 for (int sub = 1; sub < SUB; ++sub) top = fmaxf(top, fmaxf(s[sub][nt][e], s[sub][nt][2 + e]));
                 over = fmaxf(over, top - m[nt][e]);
             }
-        if (__any_sync(0xffffffffu, over > AQ_BIAS + AF_RAISE)) {
+        if (__any_sync(0xffffffffu, over > AQ_BIAS<TIN> + AF_RAISE)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -504,7 +573,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
                     for (int sub = 0; sub < SUB; ++sub) mx = fmaxf(mx, fmaxf(s[sub][nt][e], s[sub][nt][2 + e]));
 #pragma unroll
                     for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                    mx = fmaxf(mx - AQ_BIAS, m[nt][e]);
+                    mx = fmaxf(mx - AQ_BIAS<TIN>, m[nt][e]);
                     const float f = ex2(m[nt][e] - mx);
                     m[nt][e] = mx;
                     l[nt][e] *= f;
@@ -550,25 +619,26 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 #pragma unroll
                             for (int q = 0; q < WPARTS; ++q) pf[sub][nt][q][u] = transpose8x8(pw[q]);
                         }
-                    nibbles(ab[sub], __byte_perm(w[sub][0][j >> 1], w[sub][1][j >> 1], sel));
-                    nibbles(cd[sub], __byte_perm(w[sub][2][j >> 1], w[sub][3][j >> 1], sel));
+                    const uint32_t y = __byte_perm(w[sub][0][j >> 1], w[sub][1][j >> 1], sel), z = __byte_perm(w[sub][2][j >> 1], w[sub][3][j >> 1], sel);
+                    if constexpr (!EXACT) {
+                        nibbles(ab[sub], y);
+                        nibbles(cd[sub], z);
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        ab[sub][i] = add_bf16(ab[sub][i], i & 1 ? AQ_MINUS_128 : AQ_MINUS_8);
-                        cd[sub][i] = add_bf16(cd[sub][i], i & 1 ? AQ_MINUS_128 : AQ_MINUS_8);
+                        ab[sub][i] = EXACT ? nibble_bf16(y, i) : add_bf16(ab[sub][i], i & 1 ? AQ_MINUS_128 : AQ_MINUS_8);
+                        cd[sub][i] = EXACT ? nibble_bf16(z, i) : add_bf16(cd[sub][i], i & 1 ? AQ_MINUS_128 : AQ_MINUS_8);
                     }
                 }
 #pragma unroll
                 for (int sub = 0; sub < IL; ++sub)
 #pragma unroll
-                    for (int q = WPARTS - 1; q >= 0; --q)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const uint32_t a[4] = {ab[sub][2 * i], ab[sub][2 * i + 1], cd[sub][2 * i], cd[sub][2 * i + 1]};
-                                mma_bf16(o[nt][2 * j + i], a, pf[sub][nt][q][0], pf[sub][nt][q][1]);
-                            }
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t a[4] = {ab[sub][2 * i], ab[sub][2 * i + 1], cd[sub][2 * i], cd[sub][2 * i + 1]};
+                            mma_weights<EXACT, WPARTS>(o[nt][2 * j + i], a, pf[sub][nt]);
+                        }
             }
             }
         } else {
@@ -595,14 +665,17 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
                     uint32_t a[4];
-                    byte_pairs(a[0], a[1], w[0][i >> 1], w[1][i >> 1], 2 * (i & 1));
-                    byte_pairs(a[2], a[3], w[2][i >> 1], w[3][i >> 1], 2 * (i & 1));
+                    if constexpr (EXACT) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) a[e] = add_bf16(a[e], AQ_MINUS_128);
+                        for (int e = 0; e < 4; ++e) a[e] = byte_pair_bf16(w[e & 2][i >> 1], w[(e & 2) + 1][i >> 1], 2 * (i & 1) + (e & 1));
+                    } else {
+                        byte_pairs(a[0], a[1], w[0][i >> 1], w[1][i >> 1], 2 * (i & 1));
+                        byte_pairs(a[2], a[3], w[2][i >> 1], w[3][i >> 1], 2 * (i & 1));
 #pragma unroll
-                    for (int q = WPARTS - 1; q >= 0; --q)
+                        for (int e = 0; e < 4; ++e) a[e] = add_bf16(a[e], AQ_MINUS_128);
+                    }
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][i], a, pf[nt][q][0], pf[nt][q][1]);
+                    for (int nt = 0; nt < NT; ++nt) mma_weights<EXACT, WPARTS>(o[nt][i], a, pf[nt]);
                 }
             }
         }
@@ -613,7 +686,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 
     // the warps' results: O as [warp][row][D + 4], then references and sums; tile k of O holds channels (lane / 4) D / 8 + 2 k, + 1
     constexpr int LD = D + 4;
-    constexpr float O2 = BITS == 4 ? 0x1p63f : 0x1p67f;
+    constexpr float O0 = EXACT ? 1.f : 0x1p66f, O1 = EXACT ? 1.f : 0x1p67f, O2 = EXACT ? 1.f : BITS == 4 ? 0x1p63f : 0x1p67f;      // out of the codes' unit, in two steps
     float *osm = reinterpret_cast<float *>(aq_sm), *ml = osm + AF_WARPS * ROWS * LD;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -626,7 +699,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
             if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt][e]; ml[(warp * ROWS + row) * 2 + 1] = z; }
 #pragma unroll
             for (int k = 0; k < KS; k += 2)
-                *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e] * 0x1p66f * 0x1p67f, o[nt][k][2 + e] * 0x1p66f * O2, o[nt][k + 1][e] * 0x1p66f * 0x1p67f, o[nt][k + 1][2 + e] * 0x1p66f * O2);
+                *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e] * O0 * O1, o[nt][k][2 + e] * O0 * O2, o[nt][k + 1][e] * O0 * O1, o[nt][k + 1][2 + e] * O0 * O2);
         }
     __syncthreads();
     few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, walk.kr, walk.v0, walk.v1);

@@ -28,6 +28,7 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
     constexpr int W = RB / 32, OT = D / 32, HT = OT / W;  // words of V, tiles of O, tiles of a word
     constexpr int PARTS = sizeof(TIN) == 4 ? 2 : 1;       // of a query
     constexpr int WPARTS = sizeof(TIN) == 4 ? 3 : 1;      // of a weight
+    constexpr bool EXACT = sizeof(TIN) == 4;              // codes at their full size
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0) attend_status(p);
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
 #pragma unroll
             for (int u = 0; u < 2; ++u) q_off[nt][j][u] = __shfl_sync(0xffffffffu, sum[j], 4 * (2 * t4 + u)) * (BITS == 4 ? -0x1p-21f : -0x1p-17f);
         }
-        row_c[nt] = p.c * 0x1p24f * __shfl_sync(0xffffffffu, down, 8 * t4);
+        row_c[nt] = p.c * (EXACT ? 1.f : 0x1p24f) * __shfl_sync(0xffffffffu, down, 8 * t4);
     }
 
     float o[NT][OT][4], m[NT], l[NT];
@@ -153,6 +154,15 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
                                 a[1] = (hh ? z >> 8 : z) & 0x000f000fu;
                                 a[2] = (hh ? y >> 8 : y) & 0x00f000f0u;
                                 a[3] = (hh ? z >> 8 : z) & 0x00f000f0u;
+                                if constexpr (EXACT) {
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) a[e] = add_f16(a[e] | 0x64006400u, e < 2 ? AQ_F16_8 : AQ_F16_128);
+                                }
+                            } else if constexpr (EXACT) {
+                                a[0] = bytes_f16(y, 0x4140);
+                                a[1] = bytes_f16(z, 0x4140);
+                                a[2] = bytes_f16(y, 0x4342);
+                                a[3] = bytes_f16(z, 0x4342);
                             } else {
                                 a[0] = __byte_perm(y ^ 0x80808080u, 0u, 0x4140);
                                 a[1] = __byte_perm(z ^ 0x80808080u, 0u, 0x4140);
@@ -178,7 +188,8 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
                     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                         for (int j = 0; j < PAIRS; ++j) {
-                            const float y = acc[sub][nt][j][2 * u] + q_off[nt][j][0], z = acc[sub][nt][j][2 * u + 1] + q_off[nt][j][1];
+                            const float y = EXACT ? acc[sub][nt][j][2 * u] : acc[sub][nt][j][2 * u] + q_off[nt][j][0];
+                            const float z = EXACT ? acc[sub][nt][j][2 * u + 1] : acc[sub][nt][j][2 * u + 1] + q_off[nt][j][1];
                             if constexpr (BITS == 4) {
                                 s[sub][nt][u] = j == 0 ? y * bf16_lo(f[0]) : fmaf(y, bf16_lo(f[j]), s[sub][nt][u]);
                                 s[sub][nt][u] = fmaf(z, bf16_hi(f[j]), s[sub][nt][u]);
@@ -212,13 +223,13 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
             for (int sub = 1; sub < SUB; ++sub) top[nt] = fmaxf(top[nt], fmaxf(s[sub][nt][0], s[sub][nt][1]));
             over = fmaxf(over, top[nt] - m[nt]);
         }
-        if (__any_sync(0xffffffffu, over > AQ_BIAS + AF_RAISE)) {
+        if (__any_sync(0xffffffffu, over > AQ_BIAS<TIN> + AF_RAISE)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float mx = top[nt];
 #pragma unroll
                 for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                mx = fmaxf(mx - AQ_BIAS, m[nt]);
+                mx = fmaxf(mx - AQ_BIAS<TIN>, m[nt]);
                 const float f = ex2(m[nt] - mx);
                 m[nt] = mx;
                 l[nt] *= f;
@@ -268,7 +279,13 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
 #pragma unroll
                     for (int key = 0; key < 2; ++key) {
                         const uint32_t y = w[key][q];
-                        if constexpr (BITS == 4) {
+                        if constexpr (BITS == 4 && EXACT) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) a[i / 2][2 * key + i % 2] = nibble_bf16(y, i);
+                        } else if constexpr (EXACT) {
+                            a[0][2 * key] = byte_pair_bf16(y ^ 0x80808080u, (y ^ 0x80808080u) >> 8, 0);
+                            a[0][2 * key + 1] = byte_pair_bf16(y ^ 0x80808080u, (y ^ 0x80808080u) >> 8, 2);
+                        } else if constexpr (BITS == 4) {
                             // codes 0 and 2 of the halves alone, with 1 and 3 sixteenfold on top
                             const uint32_t z = __byte_perm(y, 0u, 0x4341);
                             a[0][2 * key] = add_bf16(y & 0x000f000fu, AQ_MINUS_8);
@@ -281,12 +298,9 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
                         }
                     }
 #pragma unroll
-                    for (int part_w = WPARTS - 1; part_w >= 0; --part_w)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int i = 0; i < HT; ++i)
-                                mma_bf16(o[nt][q * HT + i], a[i], pf[nt][BITS == 4 ? q : 0][part_w][0], pf[nt][BITS == 4 ? q : 0][part_w][1]);
+                        for (int i = 0; i < HT; ++i) mma_weights<EXACT, WPARTS>(o[nt][q * HT + i], a[i], pf[nt][BITS == 4 ? q : 0]);
                 }
             }
         slot = slot + 1 == ST ? 0 : slot + 1;
@@ -305,14 +319,14 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
         const int row = 4 * nt + t4;
         if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt]; ml[(warp * ROWS + row) * 2 + 1] = z; }
         float *dst = &osm[(warp * ROWS + row) * LD + g8 * (D / 8)];
-        constexpr float A = 0x1p66f, B = 0x1p67f, B16 = 0x1p63f;       // 2^133, the codes' unit, in two steps
+        constexpr float A = EXACT ? 1.f : 0x1p66f, B = EXACT ? 1.f : 0x1p67f, B16 = EXACT ? 1.f : 0x1p63f;     // out of the codes' unit, in two steps
         if constexpr (BITS == 4) {
 #pragma unroll
             for (int q = 0; q < W; ++q)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float (&lo)[4] = o[nt][2 * q], (&hi)[4] = o[nt][2 * q + 1];
-                    *reinterpret_cast<float4 *>(dst + 8 * q + 4 * e) = make_float4(lo[e] * A * B, (lo[2 + e] - lo[e]) * A * B16, hi[e] * A * B, (hi[2 + e] - hi[e]) * A * B16);
+                    *reinterpret_cast<float4 *>(dst + 8 * q + 4 * e) = make_float4(lo[e] * A * B, (EXACT ? lo[2 + e] : lo[2 + e] - lo[e]) * A * B16, hi[e] * A * B, (EXACT ? hi[2 + e] : hi[2 + e] - hi[e]) * A * B16);
                 }
         } else {
 #pragma unroll
