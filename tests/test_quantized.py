@@ -458,6 +458,31 @@ def test_queries_of_any_size(bits):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n_q", [1, 3, 900])
+def test_values_of_any_size(bits, dtype, n_q):
+    # scales larger and smaller by powers of two give outputs likewise, and another sign of them the other sign
+    gen = torch.Generator().manual_seed(4)
+    cache = _held(gen, 1, 2, 900, 128, bits)
+    q = torch.randn(1, 8, n_q, 128, generator=gen).to(dtype).cuda()
+    want = P.attend_quantized(q, cache)["out"]
+    for f in (2.0 ** -50, 2.0 ** 40, -1.0):
+        got = P.attend_quantized(q, cache._replace(v_scale=cache.v_scale * f))["out"]
+        assert torch.equal(got, want * f)
+
+
+@pytest.mark.gpu
+def test_positions_beyond_any_number_are_not_written():
+    cache = _empty(4, 1, 20, 64, 4)
+    before = [_bytes(t) for t in cache]
+    x = torch.ones(4, 1, 700, 64, dtype=BF16, device="cuda")
+    n = torch.tensor([-(1 << 31), (1 << 31) - 1, 1 << 20, -1], dtype=torch.int32, device="cuda")
+    P.write_quantized(cache, x, x, lens=n)
+    assert all(np.array_equal(a, _bytes(t)) for a, t in zip(before, cache))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("n_q", [1, 12, 50, 800])
 def test_scales_that_are_not_numbers_are_seen(bits, n_q):
     gen = torch.Generator().manual_seed(5)
