@@ -471,8 +471,8 @@ typedef struct {
 /* Enqueues the writing on `stream`; needs no workspace, allocates nothing, never synchronises, can be captured into a graph. */
 obf_status_t obf_quantized_write(const obf_quantized_write_t *args, const obf_quantized_t *cache, void *stream);
 
-/* Reads rows first .. first + rows - 1 back as fp32 or bfloat16 numbers (rounded once), those below lens[b]; what stands behind them in the
-   outputs is left as it was.  As above otherwise. */
+/* Reads rows first .. first + rows - 1 back as fp32 or bfloat16 numbers, those below lens[b]; what stands behind them in the outputs is left as it
+   was.  (Rounded once; values of 8 bits as bfloat16 by way of fp32.)  As above otherwise. */
 typedef struct {
     int32_t batch, kv_heads, head_dim, capacity;
     int32_t first, rows;                /* 0 <= first, 1 <= rows, first + rows <= capacity                       */
@@ -489,9 +489,19 @@ obf_status_t obf_quantized_read(const obf_quantized_read_t *args, const obf_quan
  * v, mass_in and mass_out must be NULL (k_stride and v_stride are not looked at), flags 0 or OBF_FLAG_GENERIC_PATH (the kernel
  * that multiplies codes whatever the number of query rows).
  *
- * Numerics: codes are exact in the products, scales are applied in fp32, queries of a row are scaled by a power of two.  A bf16 call's
- * weights times the values' scales are rounded to bf16 before they multiply the codes.  Scales of keys beyond 2^100, or a value that obf_attend names as
- * too large, may overflow.  A scale that is not a number spoils the queries that see its row, and may spoil those of the same head that do not.
+ * Small numbers of query rows (G n_q) are worked on by the codes themselves.  bf16 calls of many (some hundred, or more) read the rows that they see
+ * back into the workspace first, which then takes 4 bytes per channel, KV head and row of capacity (8 bits: 8 bytes a row more); where that
+ * would be more than 4 GB they stay on the codes.
+ *
+ * Numerics: codes are exact in the products, sums are fp32, scales are applied in fp32; queries of a row are brought to one size by a power of two.  On the way to
+ * the second product weights (bits 8 or codes: times the values' scales) are rounded to bf16 in bf16 calls, to 24 bits in fp32 calls.  Rows in 4 bits
+ * that are read back are bf16 numbers if their scales have at most five significant bits, as the library writes them, and are rounded
+ * to bf16 (half a step, 2^-8) if not.  Where 2^-60 <= |value scale| <= 2^44 (bf16; fp32: 2^100) and |key scale| <= 2^100 nothing overflows or loses bits.
+ * A scale that is not a number spoils the queries that see its row, and may spoil those of the same head that do not; what lies behind a length or
+ * that no query of the sequence sees is not read into any result.  Results do not depend on what else the batch holds except
+ * through its sizes, and are the same in every run.
+ *
+ * Workspace, capture, waits and the status word as for obf_attend (make the first call of a kind before a stream capture).
  */
 obf_status_t obf_attend_quantized_workspace_bytes(const obf_attend_t *args, const obf_quantized_t *cache, size_t *bytes);
 obf_status_t obf_attend_quantized(const obf_attend_t *args, const obf_quantized_t *cache, void *workspace, size_t workspace_bytes, void *stream);

@@ -375,6 +375,7 @@ def _attended(B, kv, G, d, n_q, cap, bits, dtype, lens=None, q_lens=None, window
     dict(B=40, kv=2, G=4, n_q=1, cap=700, lens=[700 - 17 * i for i in range(40)]),
     dict(B=1, kv=1, G=4, n_q=1, cap=9000, window=5000, sinks=4),
     dict(B=1, kv=2, G=5, n_q=1, cap=5001, size=12.0),
+    dict(B=3, kv=2, G=2, n_q=2, cap=65, lens=[65, 0, 64], q_lens=[0, 2, 1], window=3),
 ])
 def test_attention(dtype, bits, d, kw):
     _attended(d=d, bits=bits, dtype=dtype, seed=bits + d + kw["cap"], **kw)
@@ -390,7 +391,7 @@ def test_attention(dtype, bits, d, kw):
     dict(B=3, kv=2, G=8, n_q=13, cap=515, lens=[515, 7, 13], q_lens=[13, 13, 1], window=200, sinks=1),
     dict(B=1, kv=1, G=128, n_q=3, cap=140, scale=0.3), dict(B=1, kv=1, G=100, n_q=1, cap=4097, window=4000),
     dict(B=1, kv=2, G=3, n_q=301, cap=301, size=15.0), dict(B=1, kv=1, G=129, n_q=1, cap=70),
-    dict(B=2, kv=2, G=5, n_q=4, cap=450, lens=[450, 300], token_major=True), dict(B=1, kv=3, G=23, n_q=1, cap=1100, window=700, sinks=2), dict(B=2, kv=1, G=5, n_q=60, cap=2000, window=1, sinks=300),
+    dict(B=3, kv=1, G=4, n_q=30, cap=90, lens=[90, 50, 0], q_lens=[0, 30, 0]), dict(B=2, kv=2, G=5, n_q=4, cap=450, lens=[450, 300], token_major=True), dict(B=1, kv=3, G=23, n_q=1, cap=1100, window=700, sinks=2), dict(B=2, kv=1, G=5, n_q=60, cap=2000, window=1, sinks=300),
 ])
 @pytest.mark.parametrize("dtype,flags", [(BF16, 0), (BF16, binding.OBF_FLAG_GENERIC_PATH), (F32, 0)])
 def test_attention_of_many_queries(bits, d, kw, dtype, flags):
