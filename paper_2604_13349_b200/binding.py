@@ -470,13 +470,23 @@ def _enqueue(name: str, device: int, args, stream) -> None:
         stream = torch._C._cuda_getCurrentRawStream(device)
     elif not isinstance(stream, int):
         stream = stream.cuda_stream
-    if device != torch.cuda.current_device():
+    if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             rc = _packed(name)(*args, stream)
     else:
         rc = _packed(name)(*args, stream)
     if rc != OBF_OK:
         raise ObfError(rc, name)
+
+
+def _try_enqueue(name: str, device: int, args) -> bool:
+    """The call on the device's current stream; whether its workspace was large enough."""
+    if device != torch._C._cuda_getDevice():
+        return False
+    rc = _packed(name)(*args, torch._C._cuda_getCurrentRawStream(device))
+    if rc != OBF_OK and rc != OBF_ERR_WORKSPACE:
+        raise ObfError(rc, name)
+    return rc == OBF_OK
 
 
 def _attend_call(name, args, prefix, q, out, lse_out, mass_out, workspace, want_status, stream):
@@ -671,19 +681,25 @@ def quantized_cache(batch: int, kv_heads: int, capacity: int, head_dim: int, bit
                           *(torch.zeros(scales, dtype=_F32 if bits == 8 else _BF16, device=device) for _ in range(2)))
 
 
+_QUANTIZED_BITS = {torch.int8: 8, torch.uint8: 4}
+
+
 def _quantized_args(cache: QuantizedCache):
     """Checks a cache; gives its struct, shape and device."""
     k, v, ks, vs = cache
     shape, dt, dev = k.shape, k.dtype, k.get_device()
-    bits = 8 if dt is torch.int8 else 4 if dt is torch.uint8 else 0
-    if not bits or dev < 0 or len(shape) != 4:
+    bits = _QUANTIZED_BITS.get(dt)
+    if bits is None or dev < 0 or len(shape) != 4:
         raise ValueError("cache.k: int8 [batch, kv_heads, capacity, head_dim] or uint8 [.., head_dim / 2] on a device expected")
     B, kv, cap, row = shape
-    d = row * 8 // bits
+    if bits == 8:
+        d, scales, sdt = row, (B, kv, cap), _F32
+    else:
+        d, sdt = 2 * row, _BF16
+        scales = (B, kv, cap, row >> 4)
     sk, sv, ss, st = k.stride(), v.stride(), ks.stride(), vs.stride()
-    scales, sdt = ((B, kv, cap), _F32) if bits == 8 else ((B, kv, cap, d // 32), _BF16)
     if not (v.shape == shape and v.dtype is dt and v.get_device() == dev and ks.shape == scales and vs.shape == scales and ks.dtype is sdt and vs.dtype is sdt and
-            ks.get_device() == dev and vs.get_device() == dev and sk[3] == sv[3] == 1 and (bits == 8 or ss[3] == st[3] == 1)):
+            ks.get_device() == dev and vs.get_device() == dev and sk[3] == 1 and sv[3] == 1 and (bits == 8 or (ss[3] == 1 and st[3] == 1))):
         for t, want, type_, name in ((k, shape, dt, "k"), (v, shape, dt, "v"), (ks, scales, sdt, "k_scale"), (vs, scales, sdt, "v_scale")):
             if t.shape != want or t.dtype is not type_ or t.get_device() != dev or (t.dim() == 4 and t.stride(3) != 1):
                 _refuse("cache.%s (contiguous rows)" % name, t, want, type_, k.device)
@@ -716,11 +732,22 @@ def write_quantized(cache: QuantizedCache, k: torch.Tensor, v: torch.Tensor, *, 
             v_values = make(shape, dtype=dt, device=k.device) if v_values is None else v_values
     if (k_values is None) != (v_values is None):
         raise ValueError("k_values, v_values: both or neither expected")
-    sk, sv = _rows(k, shape, dt, dev, "k"), _rows(v, shape, dt, dev, "v")
-    none = (0, 0, 0)
-    s1, s2 = (none, none) if k_values is None else (_rows(k_values, shape, dt, dev, "k_values"), _rows(v_values, shape, dt, dev, "v_values"))
+    sk, sv = k.stride(), v.stride()
+    if not (k.shape == shape and v.shape == shape and v.dtype is dt and k.get_device() == dev and v.get_device() == dev and sk[3] == 1 and sv[3] == 1):
+        for t, name in ((k, "k"), (v, "v")):
+            _rows(t, shape, dt, dev, name)                       # names the one that is wrong
+    if k_values is None:
+        p1 = p2 = 0
+        s1 = s2 = (0, 0, 0)
+    else:
+        p1, p2 = k_values.data_ptr(), v_values.data_ptr()
+        s1, s2 = k_values.stride(), v_values.stride()
+        if not (k_values.shape == shape and v_values.shape == shape and k_values.dtype is dt and v_values.dtype is dt and k_values.get_device() == dev and
+                v_values.get_device() == dev and s1[3] == 1 and s2[3] == 1):
+            for t, name in ((k_values, "k_values"), (v_values, "v_values")):
+                _rows(t, shape, dt, dev, name)
     args = _QUANTIZED_WRITE.pack(
-        B, kv, d, cap, rows, code, k.data_ptr(), v.data_ptr(), 0 if k_values is None else k_values.data_ptr(), 0 if v_values is None else v_values.data_ptr(),
+        B, kv, d, cap, rows, code, k.data_ptr(), v.data_ptr(), p1, p2,
         sk[0], sk[1], sk[2], sv[0], sv[1], sv[2], s1[0], s1[1], s1[2], s2[0], s2[1], s2[2],
         0 if lens is None else _dense(lens, (B,), _I32, dev, "lens"), 0 if new_lens is None else _dense(new_lens, (B,), _I32, dev, "new_lens"))
     _enqueue("obf_quantized_write", dev, (args, packed), stream)
@@ -758,8 +785,14 @@ def _attend_quantized_args(q, shape, device, lens, q_lens, window, sinks, scale,
     shape_q = q.shape
     if code < 0 or len(shape_q) != 4:
         raise ValueError("q: a float32 or bfloat16 device tensor [batch, q_heads, n_q, head_dim] expected")
-    want = (B, shape_q[1], shape_q[2], d)
-    sq, so = _rows(q, want, dt, device, "q"), (0, 0, 0) if out is None else _rows(out, want, dt, device, "out")
+    sq = q.stride()
+    so = (0, 0, 0, 1) if out is None else out.stride()
+    if not (shape_q[0] == B and shape_q[3] == d and q.get_device() == device and sq[3] == 1 and so[3] == 1 and
+            (out is None or (out.shape == shape_q and out.dtype is dt and out.get_device() == device))):
+        want = (B, shape_q[1], shape_q[2], d)
+        for t, name in ((q, "q"), (out, "out")):
+            if t is not None:
+                _rows(t, want, dt, device, name)                 # names the one that is wrong
     return _ATTEND.pack(
         B, kv, shape_q[1], d, shape_q[2], cap, min(window, _MOST), min(sinks, _MOST), code, scale, 1.0, flags,
         q.data_ptr(), 0, 0, 0 if out is None else out.data_ptr(), sq[0], sq[1], sq[2], 0, 0, 0, 0, 0, 0, so[0], so[1], so[2],
@@ -777,6 +810,11 @@ def attend_quantized(q: torch.Tensor, cache: QuantizedCache, *, lens: Optional[t
     packed, shape, dev = _quantized_args(cache)
     out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
     args = _attend_quantized_args(q, shape, dev, lens, q_lens, window, sinks, scale, out, lse_out, flags)
+    if workspace is None and not want_status and stream is None:
+        # a small call needs no more than a status word, and asking how much it needs takes as long as trying
+        word = _status_words.get(dev)
+        if word is not None and _try_enqueue("obf_attend_quantized", dev, (args, packed, word.data_ptr(), _STATUS_ONLY)):
+            return {"out": out} if lse_out is None else {"out": out, "lse": lse_out}
     return _attend_call("obf_attend_quantized", args, packed, q, out, lse_out, None, workspace, want_status, stream)
 
 
