@@ -215,6 +215,24 @@ __device__ __forceinline__ void tops4(uint32_t (&top)[4], const Sixteen<T> &in, 
     }
 }
 
+// Largest magnitude of sixteen channels, as bits.
+template <typename T>
+__device__ __forceinline__ uint32_t top8(const Sixteen<T> &in)
+{
+    uint32_t top = 0u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+            const uint4 w = in.half[i].w[k];
+            if constexpr (sizeof(T) == 2)
+                top = __vmaxu2(top, __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu)));
+            else
+                top = max(top, max(max(w.x & 0x7fffffffu, w.y & 0x7fffffffu), max(w.z & 0x7fffffffu, w.w & 0x7fffffffu)));
+        }
+    return sizeof(T) == 2 ? max(top << 16, top & 0xffff0000u) : top;
+}
+
 // Rows of a thread in flight, and blocks of a multiprocessor (bf16 rows to 4 bits: 4 rows 81 us, 2 rows 84; to 8 bits 88 and 74).
 template <typename T, int BITS>
 constexpr int QW_AHEAD = sizeof(T) == 2 && BITS == 4 ? 4 : 2;
@@ -285,14 +303,7 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
         if constexpr (BITS == 4) {
             tops4<T>(top, in[u], L);
         } else {
-            top[0] = 0u;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float x[8];
-                in[u].half[i].get(x);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) top[0] = max(top[0], __float_as_uint(x[k]) & 0x7fffffffu);
-            }
+            top[0] = top8(in[u]);
 #pragma unroll
             for (int w = 1; w < L; w <<= 1) top[0] = max(top[0], __shfl_xor_sync(0xffffffffu, top[0], w));
         }
@@ -337,25 +348,24 @@ __device__ __forceinline__ void quant_write(const RowsDev &p, const QuantDev &c,
                 }
                 word[half] = w - 0x4b400000u * 0x11111111u;      // (modulo 2^32: what the places of 1.5 * 2^23 add up to)
             } else {
-                float v[8], worst = 0.f;
+                float t[8], worst = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float t = __fmaf_rn(x[i], inv[0], QC_ONES);
-                    v[i] = t - QC_ONES;
-                    worst = fmaxf(worst, fabsf(__fmaf_rn(x[i], inv[0], -v[i])));
+                    t[i] = __fmaf_rn(x[i], inv[0], QC_ONES);
+                    worst = fmaxf(worst, fabsf(__fmaf_rn(x[i], inv[0], QC_ONES - t[i])));
                 }
                 // The code is the whole number nearest to the fp32 quotient, which the product is within 1.2e-5 of (|x / scale| <= 127): only
                 // where one is nearer than that to n + 1/2 the quotients are formed.
                 if (worst > 0.49998f && s[0] > 0.f) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        if (fabsf(__fmaf_rn(x[i], inv[0], -v[i])) > 0.49998f) v[i] = rintf(__fdiv_rn(x[i], s[0]));
+                        if (fabsf(__fmaf_rn(x[i], inv[0], QC_ONES - t[i])) > 0.49998f) t[i] = __fadd_rn(__fdiv_rn(x[i], s[0]), QC_ONES);
                 }
                 uint32_t b[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    b[i] = __float_as_uint(v[i] + QC_ONES);
-                    y[i] = v[i] * s[0];
+                    b[i] = __float_as_uint(t[i]);
+                    y[i] = (t[i] - QC_ONES) * s[0];
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
