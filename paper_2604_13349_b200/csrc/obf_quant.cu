@@ -139,7 +139,7 @@ static obf_status_t quant_read(const obf_quantized_read_t *a, const obf_quantize
     OBF_TRY(validate_words(a->lens, nullptr));
     RowsDev p = {};
     unsigned blocks;
-    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->rows, a->first, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 8) * QR_AHEAD));
+    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->rows, a->first, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 16) * QR_AHEAD));
     p.k_out = a->k_out; p.v_out = a->v_out;
     for (int i = 0; i < 3; ++i) { p.kos[i] = a->k_out_stride[i]; p.vos[i] = a->v_out_stride[i]; }
     const QuantDev d = quant_dev(c);
@@ -303,7 +303,7 @@ static obf_status_t attend_tiles(const QuantLayout &L, const obf_attend_t *a, co
 {
     RowsDev p = {};
     unsigned blocks;
-    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->capacity, 0, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 8) * QR_AHEAD));
+    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->capacity, 0, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 16) * QR_AHEAD));
     obf_attend_t r = *a;
     r.k = p.k_out = ws + L.off_k;
     r.v = p.v_out = ws + L.off_v;

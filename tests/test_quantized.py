@@ -285,6 +285,26 @@ def test_rows_read_back(dtype, bits, d, B, kv, cap, first, rows, lens, token_maj
     assert again["K"].dtype is dtype and torch.equal(again["V"].float().cpu(), qref.values(cache)[1][:, :, first : first + rows].float().to(dtype).float())
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("start,gap", [(1, 0), (0, 1), (1, 1), (1, 2)])
+def test_rows_read_back_to_places_of_16_bytes(dtype, bits, d, start, gap):
+    """Rows that begin on multiples of 16 bytes that are none of 32; what lies between them stays."""
+    cache = _held(torch.Generator().manual_seed(d + bits + start), 2, 2, 37, d, bits)
+    e = 16 // dtype.itemsize
+    step = d + gap * e
+    want = [x.float().to(dtype) for x in qref.values(cache)]
+    w = [torch.full((start * e + 2 * 2 * 37 * step,), -77.0, dtype=dtype, device="cuda") for _ in range(2)]
+    out = [torch.as_strided(x, (2, 2, 37, d), (2 * 37 * step, 37 * step, step, 1), start * e) for x in w]
+    P.read_quantized(cache, k_out=out[0], v_out=out[1])
+    for x, got, y in zip(w, out, want):
+        assert torch.equal(got.cpu(), y)
+        got.fill_(-77.0)
+        assert bool((x == -77.0).all())
+
+
 def _hold(t, want, tol, what):
     off = (t.double().cpu() - want).abs()
     worst = (off / tol.clamp_min(1e-300)).max().item() if off.numel() else 0.0
