@@ -108,8 +108,9 @@ static obf_status_t quant_write(const obf_quantized_write_t *a, const obf_quanti
     OBF_TRY(validate_words(a->lens, a->new_lens));
     RowsDev p = {};
     unsigned blocks;
-    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->rows, 0, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 16) * (a->dtype == OBF_BF16 ? (c->bits == 4 ? QW_AHEAD<__nv_bfloat16, 4> : QW_AHEAD<__nv_bfloat16, 8>)
-                                                                                                  : (c->bits == 4 ? QW_AHEAD<float, 4> : QW_AHEAD<float, 8>))));
+    const int ahead = a->dtype == OBF_BF16 ? (c->bits == 4 ? QW_AHEAD<__nv_bfloat16, 4> : QW_AHEAD<__nv_bfloat16, 8>)
+                                           : (c->bits == 4 ? QW_AHEAD<float, 4> : QW_AHEAD<float, 8>);
+    OBF_TRY(rows_dev(&p, a->batch, a->kv_heads, a->rows, 0, a->capacity, a->lens, &blocks, QC_NT / (a->head_dim / 16) * ahead));
     p.new_lens = a->new_lens;
     p.k = a->k; p.v = a->v; p.k_out = a->k_values; p.v_out = a->v_values;
     for (int i = 0; i < 3; ++i) { p.ks[i] = a->k_stride[i]; p.vs[i] = a->v_stride[i]; p.kos[i] = a->k_values_stride[i]; p.vos[i] = a->v_values_stride[i]; }
