@@ -435,7 +435,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             it.head = im.head;
             it.lo = im.lo;
             it.hi = im.hi;
-            if (FACTORS) { it.b = im.b; it.h = im.h; }
             bool real = im.valid[x] && row_b < im.nb;
             {
                 const int i = im.fi[x] + row_i, b = im.fb[x] + row_b;
@@ -447,15 +446,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_consta
             bool started = false, known = true;           // known: all rows have references
             for (int j = jb; j < je; ++j) {
                 if (!(j < sk || (j >= ja && j < jz))) continue;
-                float4 own_factors;
                 if constexpr (FACTORS) {
-                    // the warp's 64 keys' factors, two keys a lane, under way while the logits are waited for
+                    // the warp's 64 keys' factors, two keys a lane, while the logits are waited for
                     const int v = j * AT_TILE + col0 + 2 * lane;
-                    own_factors = p.factors[(((long long)it.b * p.kv_heads + it.h) * p.factor_stride + (v < it.head ? v : it.lo + v - it.head)) / 2];
+                    factors[lane] = p.factors[(((long long)im.b * p.kv_heads + im.h) * p.factor_stride + (v < it.head ? v : it.lo + v - it.head)) / 2];
                 }
                 const bool late = !tc::mbar_wait(&bar_s[x], ns & 1u, wc);
                 ++ns;
-                if constexpr (FACTORS) factors[lane] = own_factors;
                 __syncwarp();
                 tc::tc_fence_after();
                 const int width = it.width(j);
