@@ -218,7 +218,8 @@ __device__ __forceinline__ uint32_t column_bits(int a, int b)
 }
 
 // FACTORS: keys and values come with a factor each (p.factors), which a key's logits and weights are multiplied by in fp32: two products more for each logit, in the
-// softmax, which is the longer side of a tile's chain already (prompt of 4096, 32 heads of 128 channels over 8: 255 us against 160; 8 x 40 queries over 4136 keys 70 us).
+// softmax, which is the longer side of a tile's chain already (prompt of 4096, 32 heads of 128 channels over 8: 219 us against 160).  What counts there are registers:
+// factors held in them until the logits came, and the sequence's place, were 255 us; logits as matrix fragments, of which a lane needs a quarter of the factors, 247.
 template <int D, bool PREFIX, bool FACTORS>
 __global__ void __launch_bounds__(AT_THREADS, 1) k_attend_tc(const __grid_constant__ AttendDev p, const __grid_constant__ AttendTcMaps tm, const int items,
                                                            const int first)

@@ -179,11 +179,11 @@ struct QuantLayout {
 
 // Query rows of a KV head from which on bf16 calls read the cache's rows back and attend over those on the tensor cores' tiles of 128 rows.
 // (16 sequences of 7000 to 8192 keys of 128 channels, us, on codes and on rows read back: 4 bits, 64 rows 185 and 223, 96 rows 264 and 225; 8 bits, 96 rows
-// 214 and 296, 128 rows 295 and 297.  64 channels: 4 bits, 64 rows 109 and 155; 4 of 4096 keys, 128 rows 36.4 and 34.4.)
-static long long quant_tiles_from(int bits, int head_dim) { return bits == 8 ? 129 : head_dim == 128 ? 81 : 113; }
+// 215 and 275, 112 rows 293 and 275.  64 channels: 4 bits, 64 rows 109 and 155; 4 of 4096 keys, 128 rows 36.4 and 34.4; 8 bits, 96 rows 148 and 197, 128 rows 188 and 197.)
+static long long quant_tiles_from(int bits, int head_dim) { return bits == 8 ? (head_dim == 128 ? 97 : 129) : head_dim == 128 ? 81 : 113; }
 // In small calls the two launches more take longer.  (us on codes and on rows read back: 2 x 40 queries of 32 heads over 1012 keys in 4 bits, 2.6 million rows times
-// keys, 22.4 and 23.2, in 8 bits 18.8 and 26.3; 2 x 64 in 8 bits, 4.1 million, 22.2 and 27.4; a prompt of 128, 0.5 million, 8.4 and 13.4, of 512, 8.4 million,
-// 36.2 and 20.2; 2 x 200, 13 million, 48.6 and 29.0.)
+// keys, 22.4 and 23.2, in 8 bits 18.6 and 25.7; 2 x 64 in 8 bits, 4.1 million, 22.2 and 27.0; a prompt of 128, 0.5 million, in 4 bits 8.4 and 13.4, of 512, 8.4 million,
+// 36.2 and 20.2, in 8 bits 31.5 and 20.7; 2 x 200, 13 million, 56.1 and 33.3.)
 constexpr long long QUANT_TILES_WORK = 6000000;
 // What the rows may take of a workspace.
 constexpr size_t QUANT_ROWS_BYTES = (size_t)4 << 30;
