@@ -595,6 +595,41 @@ def test_captured_steps_on_another_stream_follow_the_lengths(bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("d,B,kv,G,n_q,cap", [(128, 2, 2, 4, 257, 1301), (64, 3, 1, 2, 700, 1500), (128, 2, 2, 4, 6, 1301), (64, 5, 4, 4, 1, 4099)])
+def test_calls_at_the_same_time_and_from_graphs_keep_apart(bits, d, B, kv, G, n_q, cap):
+    """Two calls on two streams, each with its workspace, and two captured ones that are replayed side by side, over rows read back and over codes: what each
+    gives is what it gives alone."""
+    gen = torch.Generator().manual_seed(n_q + bits)
+    caches = [_held(gen, B, kv, cap, d, bits) for _ in range(2)]
+    q = [torch.randn(B, kv * G, n_q, d, generator=gen).to(BF16).cuda() for _ in range(2)]
+    lens = [torch.tensor([cap - 7 * i * (b + 1) for b in range(B)], dtype=torch.int32, device="cuda") for i in range(2)]
+    ws = [P.attend_quantized_workspace(q[0], caches[0], window=600, sinks=3) for _ in range(2)]
+    out = [torch.empty_like(x) for x in q]
+    alone = [P.attend_quantized(q[i], caches[i], lens=lens[i], window=600, sinks=3)["out"] for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    graphs = []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i], stream=streams[i]):
+            P.attend_quantized(q[i], caches[i], lens=lens[i], window=600, sinks=3, out=out[i], workspace=ws[i])
+    for replayed in (False, True):
+        for _ in range(5):
+            for x in out:
+                x.fill_(-77.0)
+            torch.cuda.synchronize()
+            for i in range(2):
+                with torch.cuda.stream(streams[i]):
+                    if replayed:
+                        graphs[i].replay()
+                    else:
+                        P.attend_quantized(q[i], caches[i], lens=lens[i], window=600, sinks=3, out=out[i], workspace=ws[i])
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, alone))
+
+
+@pytest.mark.gpu
 def test_from_the_relay_s_int8_copy_to_a_cache_that_goes_on():
     # compress with an int8 copy; the next agent attends over the copy as it is; its rows go on in a cache with room, in 8 and 4 bits, that grows
     # and is read back, evicted from and compressed again
