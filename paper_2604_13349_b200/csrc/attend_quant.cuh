@@ -29,6 +29,12 @@ constexpr float AQ_NONE = -3e38f;                         // reference of a row 
 // bf16 calls: references lie so far below the maximum at which they were last raised, since what weights multiply is in units of 2^-133.
 template <typename TIN>
 constexpr float AQ_BIAS = sizeof(TIN) == 4 ? 0.f : 75.f;
+// What brings sums of weights, and of weights times codes, out of the bias, the latter out of the codes' unit too: at once, since 2^75 times a value
+// and a number of keys may be beyond fp32's range where their average is not.
+template <typename TIN>
+constexpr float AQ_UNBIASED = sizeof(TIN) == 4 ? 1.f : 0x1p-75f;
+template <typename TIN>
+constexpr float AQ_VALUE = sizeof(TIN) == 4 ? 1.f : 0x1p58f;
 
 template <int BITS, int D>
 struct QuantStage {
@@ -691,7 +697,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 
     // the warps' results: O as [warp][row][D + 4], then references and sums; tile k of O holds channels (lane / 4) D / 8 + 2 k, + 1
     constexpr int LD = D + 4;
-    constexpr float O0 = EXACT ? 1.f : 0x1p66f, O1 = EXACT ? 1.f : 0x1p67f, O2 = EXACT ? 1.f : BITS == 4 ? 0x1p63f : 0x1p67f;      // out of the codes' unit, in two steps
+    constexpr float U = AQ_VALUE<TIN>, U2 = BITS == 4 && !EXACT ? U * 0.0625f : U;         // (4 bits: every second pair is sixteenfold)
     float *osm = reinterpret_cast<float *>(aq_sm), *ml = osm + AF_WARPS * ROWS * LD;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -701,10 +707,10 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) z += __shfl_xor_sync(0xffffffffu, z, w);
             const int row = 8 * nt + 2 * t4 + e;
-            if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt][e]; ml[(warp * ROWS + row) * 2 + 1] = z; }
+            if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt][e] + AQ_BIAS<TIN>; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_UNBIASED<TIN>; }
 #pragma unroll
             for (int k = 0; k < KS; k += 2)
-                *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e] * O0 * O1, o[nt][k][2 + e] * O0 * O2, o[nt][k + 1][e] * O0 * O1, o[nt][k + 1][2 + e] * O0 * O2);
+                *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e] * U, o[nt][k][2 + e] * U2, o[nt][k + 1][e] * U, o[nt][k + 1][2 + e] * U2);
         }
     __syncthreads();
     few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, walk.kr, walk.v0, walk.v1);

@@ -319,21 +319,21 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
 #pragma unroll
         for (int w = 4; w < 32; w <<= 1) z += __shfl_xor_sync(0xffffffffu, z, w);
         const int row = 4 * nt + t4;
-        if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt]; ml[(warp * ROWS + row) * 2 + 1] = z; }
+        if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt] + AQ_BIAS<TIN>; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_UNBIASED<TIN>; }
         float *dst = &osm[(warp * ROWS + row) * LD + g8 * (D / 8)];
-        constexpr float A = EXACT ? 1.f : 0x1p66f, B = EXACT ? 1.f : 0x1p67f, B16 = EXACT ? 1.f : 0x1p63f;     // out of the codes' unit, in two steps
+        constexpr float U = AQ_VALUE<TIN>, U2 = BITS == 4 && !EXACT ? U * 0.0625f : U;
         if constexpr (BITS == 4) {
 #pragma unroll
             for (int q = 0; q < W; ++q)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float (&lo)[4] = o[nt][2 * q], (&hi)[4] = o[nt][2 * q + 1];
-                    *reinterpret_cast<float4 *>(dst + 8 * q + 4 * e) = make_float4(lo[e] * A * B, (EXACT ? lo[2 + e] : lo[2 + e] - lo[e]) * A * B16, hi[e] * A * B, (EXACT ? hi[2 + e] : hi[2 + e] - hi[e]) * A * B16);
+                    *reinterpret_cast<float4 *>(dst + 8 * q + 4 * e) = make_float4(lo[e] * U, (EXACT ? lo[2 + e] : lo[2 + e] - lo[e]) * U2, hi[e] * U, (EXACT ? hi[2 + e] : hi[2 + e] - hi[e]) * U2);
                 }
         } else {
 #pragma unroll
             for (int q = 0; q < W; ++q)
-                *reinterpret_cast<float4 *>(dst + 4 * q) = make_float4(o[nt][q][0] * A * B, o[nt][q][1] * A * B, o[nt][q][2] * A * B, o[nt][q][3] * A * B);
+                *reinterpret_cast<float4 *>(dst + 4 * q) = make_float4(o[nt][q][0] * U, o[nt][q][1] * U, o[nt][q][2] * U, o[nt][q][3] * U);
         }
     }
     __syncthreads();

@@ -1,0 +1,58 @@
+"""A relayed cache held in 8 or 4 bits at the ends of its ranges: sizes of scales and logits, and calls that read rows back."""
+import math
+
+import pytest
+import torch
+
+import paper_2604_13349_b200 as P
+from tests import _attend_ref as ref
+from tests import _quant_ref as qref
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+# rows of queries per KV head that reach every kernel and tile: (G, n_q)
+SHAPES = [(1, 1), (4, 1), (8, 1), (4, 4), (8, 3), (4, 8), (8, 400)]
+
+
+def _cache(B, kv, cap, d, bits, k_codes, v_codes, k_scale, v_scale):
+    """A cache with the given codes [B, kv, cap, d] (whole numbers) and scales, one or one for each row."""
+    def pack(c):
+        c = c.expand(B, kv, cap, d).contiguous()
+        if bits == 8:
+            return c.to(torch.int8).cuda()
+        u = (c + 8).to(torch.uint8)
+        return (u[..., 0::2] | (u[..., 1::2] << 4)).cuda()
+
+    def scale(s):
+        s = torch.as_tensor(s, dtype=F32).expand(B, kv, cap)
+        return s.contiguous().cuda() if bits == 8 else s[..., None].expand(B, kv, cap, d // 32).to(BF16).contiguous().cuda()
+    return P.QuantizedCache(pack(k_codes), pack(v_codes), scale(k_scale), scale(v_scale))
+
+
+def _top(bits):
+    return 127 if bits == 8 else 7
+
+
+def _hold(got, want, tol):
+    off = (got.double().cpu() - want).abs()
+    assert bool((off <= tol).all()), "%.3g of the bound" % (off / tol).nan_to_num(math.inf).max().item()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("G,n_q", SHAPES)
+@pytest.mark.parametrize("same", [True, False])
+def test_values_at_the_ends_of_their_range(dtype, d, bits, G, n_q, same):
+    # the largest and the smallest scales of values, thousands of keys of equal weight: the largest codes, and any
+    gen = torch.Generator().manual_seed(bits + d + n_q)
+    cap, t = 3000, _top(bits)
+    codes = torch.full((1, 2, cap, d), t) if same else torch.randint(-t, t + 1, (1, 2, cap, d), generator=gen)
+    q = torch.zeros(1, 2 * G, n_q, d, dtype=dtype)
+    for size in (44 if dtype is BF16 else 100, -60):
+        cache = _cache(1, 2, cap, d, bits, codes, codes, 1.0, 2.0 ** size)
+        got = P.attend_quantized(q.cuda(), cache, want_lse=True)
+        _, v = qref.values(cache)
+        out, tol, lse, lse_tol, _, _ = ref.attend(q, torch.zeros_like(v), v, [cap], [n_q])
+        _hold(got["out"], out, tol)
+        _hold(got["lse"], lse, lse_tol)
