@@ -26,7 +26,8 @@
 namespace obf {
 
 constexpr float AQ_NONE = -3e38f;                         // reference of a row that has seen no key: any logit raises it
-// bf16 calls: references lie so far below the maximum at which they were last raised, since what weights multiply is in units of 2^-133.
+// bf16 calls: weights are 2^75 times as large, since what they multiply is in units of 2^-133.  Added to a logit behind the subtraction of its reference, not
+// taken off the reference, where it would be lost from logits of 2^31 on.
 template <typename TIN>
 constexpr float AQ_BIAS = sizeof(TIN) == 4 ? 0.f : 75.f;
 // What brings sums of weights, and of weights times codes, out of the bias, the latter out of the codes' unit too: at once, since 2^75 times a value
@@ -35,6 +36,9 @@ template <typename TIN>
 constexpr float AQ_UNBIASED = sizeof(TIN) == 4 ? 1.f : 0x1p-75f;
 template <typename TIN>
 constexpr float AQ_VALUE = sizeof(TIN) == 4 ? 1.f : 0x1p58f;
+
+template <typename TIN>
+__device__ __forceinline__ float aq_weight(float s, float m) { return ex2(AQ_BIAS<TIN> == 0.f ? s - m : __fadd_rn(s - m, AQ_BIAS<TIN>)); }
 
 template <int BITS, int D>
 struct QuantStage {
@@ -574,7 +578,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
                 for (int sub = 1; sub < SUB; ++sub) top = fmaxf(top, fmaxf(s[sub][nt][e], s[sub][nt][2 + e]));
                 over = fmaxf(over, top - m[nt][e]);
             }
-        if (__any_sync(0xffffffffu, over > AQ_BIAS<TIN> + AF_RAISE)) {
+        if (__any_sync(0xffffffffu, over > AF_RAISE)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -584,7 +588,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
                     for (int sub = 0; sub < SUB; ++sub) mx = fmaxf(mx, fmaxf(s[sub][nt][e], s[sub][nt][2 + e]));
 #pragma unroll
                     for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                    mx = fmaxf(mx - AQ_BIAS<TIN>, m[nt][e]);
+                    mx = fmaxf(mx, m[nt][e]);
                     const float f = ex2(m[nt][e] - mx);
                     m[nt][e] = mx;
                     l[nt][e] *= f;
@@ -598,7 +602,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[sub][nt][e] = ex2(s[sub][nt][e] - m[nt][e & 1]);
+                    s[sub][nt][e] = aq_weight<TIN>(s[sub][nt][e], m[nt][e & 1]);
                     l[nt][e & 1] += s[sub][nt][e];
                 }
         // ---- values ----
@@ -707,7 +711,7 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) z += __shfl_xor_sync(0xffffffffu, z, w);
             const int row = 8 * nt + 2 * t4 + e;
-            if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt][e] + AQ_BIAS<TIN>; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_UNBIASED<TIN>; }
+            if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt][e]; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_UNBIASED<TIN>; }
 #pragma unroll
             for (int k = 0; k < KS; k += 2)
                 *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e] * U, o[nt][k][2 + e] * U2, o[nt][k + 1][e] * U, o[nt][k + 1][2 + e] * U2);

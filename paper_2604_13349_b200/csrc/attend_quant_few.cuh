@@ -225,13 +225,13 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
             for (int sub = 1; sub < SUB; ++sub) top[nt] = fmaxf(top[nt], fmaxf(s[sub][nt][0], s[sub][nt][1]));
             over = fmaxf(over, top[nt] - m[nt]);
         }
-        if (__any_sync(0xffffffffu, over > AQ_BIAS<TIN> + AF_RAISE)) {
+        if (__any_sync(0xffffffffu, over > AF_RAISE)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float mx = top[nt];
 #pragma unroll
                 for (int w = 4; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                mx = fmaxf(mx - AQ_BIAS<TIN>, m[nt]);
+                mx = fmaxf(mx, m[nt]);
                 const float f = ex2(m[nt] - mx);
                 m[nt] = mx;
                 l[nt] *= f;
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    s[sub][nt][u] = ex2(s[sub][nt][u] - m[nt]);
+                    s[sub][nt][u] = aq_weight<TIN>(s[sub][nt][u], m[nt]);
                     l[nt] += s[sub][nt][u];
                 }
         // ---- values: columns 2 r + e of O are row r's channels in halves e of the words ----
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
 #pragma unroll
         for (int w = 4; w < 32; w <<= 1) z += __shfl_xor_sync(0xffffffffu, z, w);
         const int row = 4 * nt + t4;
-        if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt] + AQ_BIAS<TIN>; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_UNBIASED<TIN>; }
+        if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt]; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_UNBIASED<TIN>; }
         float *dst = &osm[(warp * ROWS + row) * LD + g8 * (D / 8)];
         constexpr float U = AQ_VALUE<TIN>, U2 = BITS == 4 && !EXACT ? U * 0.0625f : U;
         if constexpr (BITS == 4) {

@@ -56,3 +56,33 @@ def test_values_at_the_ends_of_their_range(dtype, d, bits, G, n_q, same):
         out, tol, lse, lse_tol, _, _ = ref.attend(q, torch.zeros_like(v), v, [cap], [n_q])
         _hold(got["out"], out, tol)
         _hold(got["lse"], lse, lse_tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("G,n_q", SHAPES)
+@pytest.mark.parametrize("size", [24, 34, 60])
+def test_logits_of_any_size(dtype, d, bits, G, n_q, size):
+    # keys with a logit of about 2^size among others whose is zero, all of one value: the output is that value, whatever its scale.  (Not an average of several: where
+    # keys are cut into parts, those are weighed by their fp32 lse, whose last bit is a power of two in the weights from logits of 2^24 on.)
+    gen = torch.Generator().manual_seed(bits + d + n_q + size)
+    cap, t = 3000, _top(bits)
+    hot = torch.rand(1, 2, cap, generator=gen) < 0.02
+    hot[..., cap - n_q] = True                                       # every query sees one
+    k = torch.zeros(1, 2, cap, d)
+    k[..., 0] = hot * t
+    value = torch.randint(-t, t + 1, (1, 2, 1, d), generator=gen)
+    v = torch.where(hot[..., None], value, torch.randint(-t, t + 1, (1, 2, cap, d), generator=gen))
+    q = torch.zeros(1, 2 * G, n_q, d, dtype=dtype)
+    q[..., 0] = 8.0
+    for e in (0, -14, -24, -44):
+        step = 2.0 ** (size - 3 - t.bit_length())                    # of the keys
+        got = P.attend_quantized(q.cuda(), _cache(1, 2, cap, d, bits, k, v, step, 2.0 ** e), scale=1.0, want_lse=True)
+        want = value.double().repeat_interleave(G, 1).expand(1, 2 * G, n_q, d) * 2.0 ** e
+        # a sum of at most 3000 numbers, a bf16 weight and the output's rounding
+        _hold(got["out"], want, (cap * 2.0 ** -24 + 2.0 ** -20 + 2 * ref.STEP[dtype]) * want.abs())
+        # the logit: exact products, scaled with three roundings; the number of keys; the sum's rounding
+        n = (torch.tril(torch.ones(n_q, cap, dtype=torch.float64), cap - n_q) * hot[0, :, None]).sum(-1)
+        x = 8.0 * t * step
+        _hold(got["lse"].reshape(2, G, n_q), x + n.log()[:, None], torch.full((2, 1, n_q), 2.0 ** -21 * x))
