@@ -80,13 +80,13 @@ __device__ __forceinline__ float cluster_load(uint32_t a)
 
 // The end of a block with few rows: its warps' results, in shared memory, are weighed together and stored, or joined with those of
 // the cluster's other blocks first.  osm: O as [warp][row][D + 4], ml: references and sums as [warp][row][2], room for one more
-// result behind them.
+// result behind them; sums are in units of 1 / lse_unit.
 template <int D, int ROWS>
 __host__ __device__ constexpr size_t few_finish_smem() { return ((size_t)AF_WARPS * ROWS * (D + 4 + 2) + ROWS * (D + 4 + 1)) * 4; }
 
 template <typename TIN, int D, int ROWS, bool PREFIX, bool CLUSTER>
 __device__ __forceinline__ void few_finish(const AttendDev &p, const float *osm, float *ml, int tile, int part, int parts, int rows_run, int rows_seq, int h,
-                                           int b_own, int len_own, int ql_own, const KeyRange &kr, int v0, int v1)
+                                           int b_own, int len_own, int ql_own, const KeyRange &kr, int v0, int v1, const float lse_unit = 1.f)
 {
     auto locate_row = [&](int run, int &b, int &r) {
         b = PREFIX ? run / rows_seq : b_own;
@@ -117,7 +117,7 @@ __device__ __forceinline__ void few_finish(const AttendDev &p, const float *osm,
             Z += f * z;
             a.x += f * u.x; a.y += f * u.y; a.z += f * u.z; a.w += f * u.w;
         }
-        const float inv = Z == 0.f ? 0.f : 1.f / Z, lse2 = Z == 0.f ? -INFINITY : M + log2f(Z);
+        const float inv = Z == 0.f ? 0.f : 1.f / Z, lse2 = Z == 0.f ? -INFINITY : M + log2f(Z * lse_unit);
         a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
         if constexpr (CLUSTER) {
             *reinterpret_cast<float4 *>(&cl[row * LD + c]) = a;

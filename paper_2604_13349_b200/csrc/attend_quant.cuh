@@ -26,19 +26,22 @@
 namespace obf {
 
 constexpr float AQ_NONE = -3e38f;                         // reference of a row that has seen no key: any logit raises it
-// bf16 calls: weights are 2^75 times as large, since what they multiply is in units of 2^-133.  Added to a logit behind the subtraction of its reference, not
-// taken off the reference, where it would be lost from logits of 2^31 on.
+// The power of two of weights, added to a logit behind the subtraction of its reference (taken off the reference it would be lost from logits of 2^31 on).
+// bf16 calls: 2^75 times as large, since what they multiply is in units of 2^-133.  fp32 calls: 2^-24 times, so that 2^20 keys that weigh 2^8 times as much
+// as their reference stay within fp32's range with values of 2^107.
 template <typename TIN>
-constexpr float AQ_BIAS = sizeof(TIN) == 4 ? 0.f : 75.f;
-// What brings sums of weights, and of weights times codes, out of the bias, the latter out of the codes' unit too: at once, since 2^75 times a value
-// and a number of keys may be beyond fp32's range where their average is not.
+constexpr float AQ_BIAS = sizeof(TIN) == 4 ? -24.f : 75.f;
+// What brings a warp's sums of weights, and of weights times codes, to where they are joined: in bf16 out of the bias, the latter out of the codes' unit too (at once,
+// since 2^75 times a value and a number of keys may be beyond fp32's range where their average is not); in fp32 nothing, the bias is left to the lse.
 template <typename TIN>
-constexpr float AQ_UNBIASED = sizeof(TIN) == 4 ? 1.f : 0x1p-75f;
+constexpr float AQ_SUM = sizeof(TIN) == 4 ? 1.f : 0x1p-75f;
 template <typename TIN>
 constexpr float AQ_VALUE = sizeof(TIN) == 4 ? 1.f : 0x1p58f;
+template <typename TIN>
+constexpr float AQ_LSE = sizeof(TIN) == 4 ? 0x1p24f : 1.f;
 
 template <typename TIN>
-__device__ __forceinline__ float aq_weight(float s, float m) { return ex2(AQ_BIAS<TIN> == 0.f ? s - m : __fadd_rn(s - m, AQ_BIAS<TIN>)); }
+__device__ __forceinline__ float aq_weight(float s, float m) { return ex2(__fadd_rn(s - m, AQ_BIAS<TIN>)); }
 
 template <int BITS, int D>
 struct QuantStage {
@@ -711,13 +714,13 @@ __global__ void __launch_bounds__(AF_NT, (AQ_BLOCKS<TIN, BITS, D, NT>)) k_attend
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) z += __shfl_xor_sync(0xffffffffu, z, w);
             const int row = 8 * nt + 2 * t4 + e;
-            if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt][e]; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_UNBIASED<TIN>; }
+            if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt][e]; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_SUM<TIN>; }
 #pragma unroll
             for (int k = 0; k < KS; k += 2)
                 *reinterpret_cast<float4 *>(&osm[(warp * ROWS + row) * LD + g8 * (D / 8) + 2 * k]) = make_float4(o[nt][k][e] * U, o[nt][k][2 + e] * U2, o[nt][k + 1][e] * U, o[nt][k + 1][2 + e] * U2);
         }
     __syncthreads();
-    few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, walk.kr, walk.v0, walk.v1);
+    few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, walk.kr, walk.v0, walk.v1, AQ_LSE<TIN>);
 }
 
 }  // namespace obf

@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
 #pragma unroll
         for (int w = 4; w < 32; w <<= 1) z += __shfl_xor_sync(0xffffffffu, z, w);
         const int row = 4 * nt + t4;
-        if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt]; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_UNBIASED<TIN>; }
+        if (lane < 4) { ml[(warp * ROWS + row) * 2] = m[nt]; ml[(warp * ROWS + row) * 2 + 1] = z * AQ_SUM<TIN>; }
         float *dst = &osm[(warp * ROWS + row) * LD + g8 * (D / 8)];
         constexpr float U = AQ_VALUE<TIN>, U2 = BITS == 4 && !EXACT ? U * 0.0625f : U;
         if constexpr (BITS == 4) {
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(AF_NT, (AQF_BLOCKS<TIN, NT>)) k_attend_quant_f
         }
     }
     __syncthreads();
-    few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, walk.kr, walk.v0, walk.v1);
+    few_finish<TIN, D, ROWS, false, CLUSTER>(p, osm, ml, tile, part, parts, rows_seq, rows_seq, h, b, len, ql, walk.kr, walk.v0, walk.v1, AQ_LSE<TIN>);
 }
 
 }  // namespace obf

@@ -59,6 +59,21 @@ def test_values_at_the_ends_of_their_range(dtype, d, bits, G, n_q, same):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_values_of_many_keys_that_barely_leave_their_reference(d):
+    # fp32: all keys but the first weigh 2^7.9 times as much, too little for their reference to be raised
+    cap, G, n_q = 1 << 16, 8, 1 << 13
+    k = torch.zeros(1, 1, cap, d)
+    k[:, :, 128:, 0] = 100
+    cache = _cache(1, 1, cap, d, 8, k, torch.full((1, 1, 1, d), 127), 1.0, 2.0 ** 100)
+    q = torch.zeros(1, G, n_q, d)
+    q[..., 0] = 1.0
+    out = P.attend_quantized(q.cuda(), cache, scale=7.9 * math.log(2) / 100)["out"]
+    # an average of equal numbers: 2^16 sums in fp32, a division
+    assert bool(((out / 2.0 ** 100 - 127).abs() <= 127 * (2.0 ** 16 * 2.0 ** -24 + 2.0 ** -20)).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("G,n_q", SHAPES)
