@@ -684,9 +684,11 @@ def quantized_cache(batch: int, kv_heads: int, capacity: int, head_dim: int, bit
 _QUANTIZED_BITS = {torch.int8: 8, torch.uint8: 4}
 
 
-def _quantized_args(cache: QuantizedCache):
-    """Checks a cache; gives its struct, shape and device."""
+def _quantized_args(cache: QuantizedCache, call: Optional[str] = None):
+    """Checks a cache; gives its struct, shape and device.  `call`: the entry point that reads or writes it."""
     k, v, ks, vs = cache
+    if call is not None and torch.is_grad_enabled() and (ks.requires_grad or vs.requires_grad):
+        _refuse_graph(call)
     shape, dt, dev = k.shape, k.dtype, k.get_device()
     bits = _QUANTIZED_BITS.get(dt)
     if bits is None or dev < 0 or len(shape) != 4:
@@ -714,11 +716,11 @@ def write_quantized(cache: QuantizedCache, k: torch.Tensor, v: torch.Tensor, *, 
 
     The first ``new_lens[b]`` rows (int32 device tensor, None: all) go to the last rows of a cache that then holds ``lens[b]`` (None:
     ``new_lens``), as ``attend_quantized`` takes them for its queries.  ``k_values, v_values``, or ``want_values``: the rows as the cache holds them,
-    in the type of ``k``, returned as ``K, V``.  Gradients do not pass: where autograd records, tensors that require one are refused.
+    in the type of ``k``, returned as ``K, V``.  Gradients do not pass: where autograd records, rows and scales that require one are refused.
     """
     if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad):
         _refuse_graph("write_quantized")
-    packed, (B, kv, cap, d), dev = _quantized_args(cache)
+    packed, (B, kv, cap, d), dev = _quantized_args(cache, "write_quantized")
     dt = k.dtype
     code = OBF_BF16 if dt is _BF16 else OBF_F32 if dt is _F32 else -1
     if code < 0 or k.dim() != 4:
@@ -757,8 +759,9 @@ def write_quantized(cache: QuantizedCache, k: torch.Tensor, v: torch.Tensor, *, 
 def read_quantized(cache: QuantizedCache, *, dtype: Optional[torch.dtype] = None, lens: Optional[torch.Tensor] = None, first: int = 0, rows: Optional[int] = None,
                    k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
     """Reads rows ``first .. first + rows - 1`` (None: the rest) of a cache back (``obf_quantized_read``), those of sequence b below ``lens[b]``,
-    as ``dtype`` (that of ``k_out``, else bfloat16).  Returns ``K, V [batch, kv_heads, rows, d]``."""
-    packed, (B, kv, cap, d), dev = _quantized_args(cache)
+    as ``dtype`` (that of ``k_out``, else bfloat16).  Returns ``K, V [batch, kv_heads, rows, d]``.  Where autograd records, scales that require a
+    gradient are refused."""
+    packed, (B, kv, cap, d), dev = _quantized_args(cache, "read_quantized")
     rows = cap - first if rows is None else rows
     given = k_out if k_out is not None else v_out
     dt = dtype if dtype is not None else _BF16 if given is None else given.dtype
@@ -804,10 +807,11 @@ def attend_quantized(q: torch.Tensor, cache: QuantizedCache, *, lens: Optional[t
                      window: int = 0, sinks: int = 0, scale: float = 0.0, out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
                      want_lse: bool = False, flags: int = 0, workspace: Optional[torch.Tensor] = None, want_status: bool = False,
                      stream=None) -> Dict[str, torch.Tensor]:
-    """``attend`` over a cache held in 8 or 4 bits (``obf_attend_quantized``): the same masks, lengths, strides, outputs and errors; no masses."""
+    """``attend`` over a cache held in 8 or 4 bits (``obf_attend_quantized``): the same masks, lengths, strides, outputs and errors; no
+    masses.  Where autograd records, queries and scales that require a gradient are refused."""
     if torch.is_grad_enabled() and q.requires_grad:
         _refuse_graph("attend_quantized")
-    packed, shape, dev = _quantized_args(cache)
+    packed, shape, dev = _quantized_args(cache, "attend_quantized")
     out, lse_out = _attend_outputs(q, q_lens, out, lse_out, want_lse, stream)
     args = _attend_quantized_args(q, shape, dev, lens, q_lens, window, sinks, scale, out, lse_out, flags)
     if workspace is None and not want_status and stream is None:
