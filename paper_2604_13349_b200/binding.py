@@ -790,8 +790,8 @@ def _attend_quantized_args(q, shape, device, lens, q_lens, window, sinks, scale,
         raise ValueError("q: a float32 or bfloat16 device tensor [batch, q_heads, n_q, head_dim] expected")
     sq = q.stride()
     so = (0, 0, 0, 1) if out is None else out.stride()
-    if not (shape_q[0] == B and shape_q[3] == d and q.get_device() == device and sq[3] == 1 and so[3] == 1 and
-            (out is None or (out.shape == shape_q and out.dtype is dt and out.get_device() == device))):
+    if not (shape_q[0] == B and shape_q[3] == d and q.get_device() == device and sq[3] == 1 and
+            (out is None or (out.shape == shape_q and so[3] == 1 and out.dtype is dt and out.get_device() == device))):
         want = (B, shape_q[1], shape_q[2], d)
         for t, name in ((q, "q"), (out, "out")):
             if t is not None:
