@@ -49,7 +49,7 @@ struct QuantStage {
     static constexpr int KEYS = Row::BYTES == 128 ? 16 : 32;
     static constexpr int CODES = KEYS * Row::BYTES, SCALES = KEYS * Row::SCALE_BYTES;
     static constexpr int BYTES = 2 * CODES + 2 * SCALES;               // K's codes, V's codes, K's scales, V's scales
-    static constexpr int STAGES = BYTES > 4400 ? 2 : BYTES > 4000 ? 2 : 3;
+    static constexpr int STAGES = BYTES > 4000 ? 2 : 3;
 };
 
 // Shared memory of a block: the rings, `more` behind them, over all of it at the end the warps' results.
