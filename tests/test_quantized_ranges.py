@@ -101,3 +101,31 @@ def test_logits_of_any_size(dtype, d, bits, G, n_q, size):
         n = (torch.tril(torch.ones(n_q, cap, dtype=torch.float64), cap - n_q) * hot[0, :, None]).sum(-1)
         x = 8.0 * t * step
         _hold(got["lse"].reshape(2, G, n_q), x + n.log()[:, None], torch.full((2, 1, n_q), 2.0 ** -21 * x))
+
+
+def _held(gen, kv, cap, d, bits, k_size):
+    t = _top(bits)
+    codes = [torch.randint(-t, t + 1, (1, kv, cap, d), generator=gen) for _ in range(2)]
+    scale = [torch.randint(16, 32, (1, kv, cap), generator=gen) * 2.0 ** -4 * x for x in (k_size, 2.0 ** -4)]
+    return _cache(1, kv, cap, d, bits, *codes, *scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("G,n_q", SHAPES)
+def test_queries_of_any_size_over_keys_of_any_size(dtype, d, bits, G, n_q):
+    # powers of two moved from the keys' scales to the queries change nothing; and queries of up to 2^112 against 64 bits
+    gen = torch.Generator().manual_seed(bits + d + n_q)
+    cap = 3000
+    cache = _held(gen, 2, cap, d, bits, 2.0 ** -3 / _top(bits))
+    q = torch.randn(1, 2 * G, n_q, d, generator=gen).clamp(-4, 4).to(dtype)
+    want = P.attend_quantized(q.cuda(), cache, want_lse=True)
+    for e in (100, 30, -60):
+        got = P.attend_quantized((q * 2.0 ** e).cuda(), cache._replace(k_scale=cache.k_scale * 2.0 ** -e), want_lse=True)
+        assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
+    k, v = qref.values(cache)
+    out, tol, lse, lse_tol, _, _ = ref.attend(q, k, v, [cap], [n_q])
+    got = P.attend_quantized((q * 2.0 ** 110).cuda(), cache._replace(k_scale=cache.k_scale * 2.0 ** -110), want_lse=True)
+    _hold(got["out"], out, tol)
+    _hold(got["lse"], lse, lse_tol)
