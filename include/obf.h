@@ -437,7 +437,8 @@ obf_status_t obf_evict_by_mass(const obf_evict_t *args, void *stream);
  *            values are bfloat16 numbers.  (Other scales, and the code -8, are read as they stand.)
  *
  * A row (8 bits) or group (4 bits) that holds a number which is not finite gets a scale that is not a number; one whose magnitudes are all
- * below 2^-110 is held as zeros.
+ * below 2^-110 is held as zeros.  Rows read from a cache in 4 bits and written again get the same codes and scales (but for groups whose largest magnitude was
+ * within 2^-5 of 2^-110, which may become zeros).
  * ---------------------------------------------------------------------------------------------------------------- */
 typedef struct {
     int32_t bits;                       /* 8 or 4                                                                */
@@ -452,7 +453,8 @@ typedef struct {
 /*
  * Quantises rows of K and V as they are written.  The first new_lens[b] of sequence b's `rows` rows go, in order, to rows
  * lens[b] - new_lens[b] .. lens[b] - 1 of its cache (the tokens that obf_attend takes for the last queries, with the same two arrays);
- * rows that would stand outside 0 .. capacity - 1 are not written.  What else the cache holds is left as it was.  k_values and
+ * rows that would stand outside 0 .. capacity - 1 are not written, which nothing reports here (attention with such a length in `lens` does, in its
+ * status word).  What else the cache holds is left as it was.  k_values and
  * v_values receive the rows as the cache holds them, rounded to the rows' type (a bfloat16 or fp32 cache that a prompt's own attention can
  * run over and see what later tokens will see); rows that are not written are left alone there too.  Inputs must not overlap
  * outputs.  Two calls that write rows of one cache may overlap if the rows differ.
@@ -491,15 +493,16 @@ obf_status_t obf_quantized_read(const obf_quantized_read_t *args, const obf_quan
  *
  * Small numbers of query rows (G n_q) are worked on by the codes themselves.  bf16 calls of many (some hundred, or more) read the rows that they see
  * back into the workspace first, which then takes 4 bytes per channel, KV head and row of capacity (8 bits: 8 bytes a row more); where that
- * would be more than 4 GB they stay on the codes.
+ * would be more than 4 GB they stay on the codes, which takes a large prompt some four times as long.
  *
- * Numerics: codes are exact in the products, sums are fp32, scales are applied in fp32; queries of a row are brought to one size by a power of two.  On the way to
- * the second product weights (bits 8 or codes: times the values' scales) are rounded to bf16 in bf16 calls, to 24 bits in fp32 calls.  Rows in 4 bits
- * that are read back are bf16 numbers if their scales have at most five significant bits, as the library writes them, and are rounded
- * to bf16 (half a step, 2^-8) if not.  Where 2^-60 <= |value scale| <= 2^44 (bf16; fp32: 2^100) and |key scale| <= 2^100 nothing overflows or loses bits.
- * A scale that is not a number spoils the queries that see its row, and may spoil those of the same head that do not; what lies behind a length or
- * that no query of the sequence sees is not read into any result.  Results do not depend on what else the batch holds except
- * through its sizes, and are the same in every run.
+ * Numerics: codes are exact in the products, sums are fp32, scales are applied in fp32; on the codes the queries of a row are brought to one size by a power of
+ * two first.  On the way to the second product weights (bits 8 or codes: times the values' scales) are rounded to bf16 in bf16 calls, to 24 bits in fp32
+ * calls.  Where keys are cut into parts, these are weighed by their fp32 lse.  Rows in 4 bits that are read back are bf16 numbers if their scales have at
+ * most five significant bits, as the library writes them, and are rounded to bf16 (half a step, 2^-8) if not.
+ * Nothing overflows or loses bits where 2^-60 <= |value scale| <= 2^44 (fp32: 2^100), 2^-117 <= |key scale| <= 2^100 (times `scale`, too), a query's largest
+ * number is 2^-100 to 2^112, zeros aside, and products of queries and keys are within fp32's range.  A scale that is not finite spoils the queries that see its
+ * row, and may spoil those of the same head that do not; what lies behind a length or that no query of the sequence sees is not read into any
+ * result.  Results do not depend on what else the batch holds except through its sizes, and are the same in every run.
  *
  * Workspace, capture, waits and the status word as for obf_attend (make the first call of a kind before a stream capture).
  */

@@ -13,9 +13,10 @@
 // operands agree, so a lane takes whole words of a row and never moves a code to another lane.  A product's eight columns are eight query rows; their
 // fragments stand in shared memory for all four warps, which leaves the registers to the output.
 //
-// Bound by instructions and their latencies in tiles of 16 rows and more: the matrix pipe is busy for 25 % (16 rows in bf16) and 38 % (fp32, 24 rows), issue slots for 53 %,
-// with two or three blocks of four warps a multiprocessor.  16 sequences of 7000 to 8192 keys in 4 bits, us from a graph: 16, 20 and 64 query rows a KV head 65, 91 and 185;
-// fp32, 64 channels, 20 rows 78, where three weights' parts, two queries' and their sums of sixteen keys make 60 products of 8 cycles for sixteen keys.
+// Bound by instructions and their latencies in tiles of 16 rows and more: the matrix pipe is busy for 32 % (tiles of 16 rows in bf16) and 37 % (fp32, 24 rows), issue slots
+// for 59 % and 54 %, with two blocks of four warps a multiprocessor, which wait most for their own last results.  16 sequences in 4 bits, us from a graph: 16, 20 and 64
+// query rows a KV head 66, 90 and 190; fp32, 64 channels, 20 rows 80, where three weights' parts, two queries' and their sums of sixteen keys make 60 products of 8 cycles
+// for sixteen keys.
 #pragma once
 
 #include <cuda_fp16.h>

@@ -4,10 +4,11 @@
 // row r's numbers in the places of halves e and zeros in the others.  A word of a key then goes into both products as it is, whatever
 // groups its halves belong to, where the other kernel first brings halves of one group, and of two keys, together; and four rows, the group
 // that most models have, take half the exponentials, transposes and registers.
-// Bound by the integer pipe that takes codes apart in 4 bits (124 of its instructions, of 290 in all, for sixteen keys of 128 channels, two cycles each; fp32
-// arithmetic and matrix products partly wait for the same ports): 4 tokens over 100001 to 131072 keys 111 us, 4.8 TB/s; one of 8192 keys for 16 and for 32
-// sequences 35.8 and 61.9 us from a graph.  Bound by HBM in 8 bits: DRAM 77 % busy, 16 tokens over 4096 of 8192 keys 28 us.  fp32 takes twice the matrix products for
-// logits and three times those for outputs: 60 us against 36.
+// Bound by arithmetic in 4 bits: taking codes apart is 124 of the 290 instructions for sixteen keys of 128 channels, on the integer pipe at two cycles each, and
+// products and fp32 arithmetic partly wait for the same ports.  32 sequences of 8192 keys: issue slots 70 % busy, the integer pipe 59 %, DRAM 59 %, and what warps
+// wait for most is a pipe.  4 tokens over 100001 to 131072 keys 104 us from a graph, 5.1 TB/s; one of 8192 keys for 16 and for 32 sequences 36 and
+// 62 us.  Bound by HBM in 8 bits: DRAM 77 % busy, 16 tokens over 4096 of 8192 keys 27 us.  fp32 takes twice the matrix products for logits and
+// three times those for outputs: 60 us against 36.
 #pragma once
 
 #include "attend_quant.cuh"

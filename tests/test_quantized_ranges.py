@@ -115,13 +115,13 @@ def _held(gen, kv, cap, d, bits, k_size):
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("G,n_q", SHAPES)
 def test_queries_of_any_size_over_keys_of_any_size(dtype, d, bits, G, n_q):
-    # powers of two moved from the keys' scales to the queries change nothing; and queries of up to 2^112 against 64 bits
+    # powers of two moved between the keys' scales and the queries change nothing; and queries of up to 2^112 against 64 bits
     gen = torch.Generator().manual_seed(bits + d + n_q)
     cap = 3000
     cache = _held(gen, 2, cap, d, bits, 2.0 ** -3 / _top(bits))
     q = torch.randn(1, 2 * G, n_q, d, generator=gen).clamp(-4, 4).to(dtype)
     want = P.attend_quantized(q.cuda(), cache, want_lse=True)
-    for e in (100, 30, -60):
+    for e in (100, 30, -60, -97):
         got = P.attend_quantized((q * 2.0 ** e).cuda(), cache._replace(k_scale=cache.k_scale * 2.0 ** -e), want_lse=True)
         assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
     k, v = qref.values(cache)
