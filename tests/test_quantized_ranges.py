@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2604_13349_b200 as P
+from paper_2604_13349_b200 import binding
 from tests import _attend_ref as ref
 from tests import _quant_ref as qref
 
@@ -60,17 +61,19 @@ def test_values_at_the_ends_of_their_range(dtype, d, bits, G, n_q, same):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
-def test_the_largest_values_of_many_keys_that_barely_leave_their_reference(d):
-    # fp32: all keys but the first weigh 2^7.9 times as much, too little for their reference to be raised
-    cap, G, n_q = 1 << 16, 8, 1 << 13
+@pytest.mark.parametrize("dtype,flags", [(F32, 0), (BF16, 0), (BF16, binding.OBF_FLAG_GENERIC_PATH)])
+def test_the_largest_values_of_many_keys_that_barely_leave_their_reference(d, dtype, flags):
+    # all keys but the first weigh 2^7.9 times as much, too little for their reference to be raised
+    cap, G, n_q, size = 1 << 16, 8, 1 << 13, 2.0 ** (100 if dtype is F32 else 44)
     k = torch.zeros(1, 1, cap, d)
     k[:, :, 128:, 0] = 100
-    cache = _cache(1, 1, cap, d, 8, k, torch.full((1, 1, 1, d), 127), 1.0, 2.0 ** 100)
-    q = torch.zeros(1, G, n_q, d)
+    cache = _cache(1, 1, cap, d, 8, k, torch.full((1, 1, 1, d), 127), 1.0, size)
+    q = torch.zeros(1, G, n_q, d, dtype=dtype)
     q[..., 0] = 1.0
-    out = P.attend_quantized(q.cuda(), cache, scale=7.9 * math.log(2) / 100)["out"]
-    # an average of equal numbers: 2^16 sums in fp32, a division
-    assert bool(((out / 2.0 ** 100 - 127).abs() <= 127 * (2.0 ** 16 * 2.0 ** -24 + 2.0 ** -20)).all())
+    for rows in (n_q, 1):
+        out = P.attend_quantized(q[:, :, :rows].contiguous().cuda(), cache, scale=7.9 * math.log(2) / 100, flags=flags)["out"].float()
+        # an average of equal numbers: 2^16 sums in fp32, a division; a bf16 weight and output
+        assert bool(((out / size - 127).abs() <= 127 * (2.0 ** 16 * 2.0 ** -24 + 2.0 ** -20 + (2 * 2.0 ** -8 if dtype is BF16 else 0.0))).all())
 
 
 @pytest.mark.gpu
